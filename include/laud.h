@@ -58,7 +58,9 @@ typedef enum {
                                  library's fixed LAUD_NOALLOC_SCRATCH_BYTES; use laud_dyn_bottleneck */
 } laud_status;
 
-typedef enum { LAUD_F32 = 0, LAUD_BF16 = 1 } laud_dtype;
+/* LAUD_E4M3 (OCP 8-bit floating point, 1-4-3 bits, largest value 448) is a type of the token operators' operands only; feature
+ * maps and the blocks above them are float32 or bf16. */
+typedef enum { LAUD_F32 = 0, LAUD_BF16 = 1, LAUD_E4M3 = 2 } laud_dtype;
 
 typedef enum {
   LAUD_OP_MASK_GEN = 0,
@@ -352,6 +354,104 @@ size_t laud_channel_masker_workspace(laud_fmap fx);
 int laud_channel_masker(const void* x, laud_fmap fx, const float* wa, const float* ba, int hidden,
                         const float* wb, const float* bb, int D, uint8_t* cmask, float* logits2,
                         void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * ---- Token operators ------------------------------------------------------------------------------------------------------
+ * What surrounds a dynamic block when the map is a list of tokens (Sec. 3.1: the block carries over to transformers, which skip
+ * tokens and layers): norms with gate and residual, products of 8-bit operands, and a feed-forward layer that is itself
+ * conditional (a router picks a few experts per token).  A token list is a feature map of N = rows, H = W = 1: laud_mask_gen
+ * with S = 1 scores it, and its mask is the `keep` argument below.
+ *   - Rows may be further apart than they are long: an `ld` argument is the distance of two rows in elements, at least the
+ *     row length and, like it, a multiple of 8 (of 16 for LAUD_E4M3 operands of a product).  Bases are 16-byte aligned.
+ *   - No row (rows, M or T = 0): LAUD_OK, nothing is launched.
+ *   - Sizes of one tensor are limited by memory only: rows are addressed with 64 bits.
+ *   - Sums, statistics and accumulators are float32; each result is rounded once, to nearest even.
+ */
+
+/* 8-bit blocks: an E4M3 tensor [rows][cols] comes with one float32 scale for each block of block_rows x 128 elements, row-major
+ * [ceil(rows/block_rows)][ceil(cols/128)]; the last blocks of a row or column may be shorter.  Element = code * scale. */
+
+/*
+ * Quantises x [rows][cols] (dtype, cols a multiple of 8): scale = max(max|x| / 448, 2^-126) over the block, q = e4m3(x / scale), the
+ * quotient in float32, ties to even.  A NaN or an infinity makes its block's codes NaN.  block_rows: 1 (activations) or 128
+ * (weights).
+ */
+int laud_quantize_e4m3(const void* x, int64_t ldx, int rows, int cols, int dtype, int block_rows, void* q, int64_t ldq,
+                       float* scale, void* stream);
+
+typedef enum { LAUD_NORM_RMS = 0, LAUD_NORM_LAYER = 1 } laud_norm_kind;
+
+/* The norm after a block and the norm before the next one.  Weights and biases are float32 [C], device. */
+typedef struct {
+  int32_t C;            /* channels: a multiple of 8, at most 32768 */
+  int32_t dtype;        /* LAUD_F32 or LAUD_BF16: x, y and out */
+  int32_t kind;         /* laud_norm_kind of both norms */
+  float eps;
+  const float* post_w;  /* NULL: y as it is */
+  const float* post_b;  /* NULL: none */
+  const float* pre_w;   /* may be NULL where z is NULL */
+  const float* pre_b;   /* NULL: none */
+  float alpha, beta;    /* scales of the residual and of the branch */
+} laud_norm_block;
+
+/*
+ * The seam between two residual blocks, in one pass over the rows:
+ *   p = y, or norm(y; post_w, post_b);   r = x + branch on the rows a block ran on:  r = alpha * x + beta * gate * p  if keep, else x;
+ *   out = r;   z = norm(r; pre_w, pre_b), taken from r before its rounding.
+ * norm(v) = v / sqrt(mean(v^2) + eps) * w + b (RMS) or (v - mean(v)) / sqrt(var(v) + eps) * w + b (LAYER).
+ *   x     [rows][C]   residual stream
+ *   y     [rows][C]   the block's result, or NULL: r = x (only the norm before a block; keep, gate must be NULL)
+ *   keep  [rows] bytes or NULL (all kept): a row with 0 passes x on bit for bit; its y is not read
+ *   gate  [ceil(rows/rows_per_gate)][C] float32 or NULL: row t uses gate row t / rows_per_gate (1: a gate per token, rows
+ *         of a sample: a gate per sample, rows: one per channel)
+ *   out   [rows][C] or NULL; may be x or y
+ *   z     [rows][C] of z_dtype, or NULL (not both NULL): p->dtype, or LAUD_E4M3 with z_scale [rows][ceil(C/128)] as
+ *         laud_quantize_e4m3 defines them (the operand of laud_matmul_e4m3); may be x or y where it has their type and ld
+ */
+int laud_norm_residual(const laud_norm_block* p, int rows, const void* x, int64_t ldx, const void* y, int64_t ldy,
+                       const uint8_t* keep, const float* gate, int rows_per_gate, void* out, int64_t ldo, void* z, int64_t ldz,
+                       int z_dtype, float* z_scale, void* stream);
+
+/*
+ * out[m][n] = sum_k a[m][k] * sa[m][k/128] * b[n][k] * sb[n/128][k/128]: products of 8-bit operands are added in float32 over a
+ * block of 128, the block's sum takes its two scales.  a [M][K], b [N][K] E4M3, K a multiple of 16, N of 8; sa [M][ceil(K/128)],
+ * sb [ceil(N/128)][ceil(K/128)] (laud_quantize_e4m3 with block_rows 1 and 128); out [M][N] of out_dtype (LAUD_F32 or
+ * LAUD_BF16), no alias of an input.  Workspace: laud_matmul_e4m3_workspace(M, N, K) bytes, 0 for most shapes (then ws may
+ * be NULL).
+ */
+size_t laud_matmul_e4m3_workspace(int M, int N, int K);
+int laud_matmul_e4m3(const void* a, int64_t lda, const float* sa, const void* b, int64_t ldb, const float* sb, int M, int N,
+                     int K, void* out, int64_t ldo, int out_dtype, void* ws, size_t ws_bytes, void* stream);
+
+/* One mixture-of-experts layer.  Device pointers; matrices are dense. */
+typedef struct {
+  int32_t C, F;         /* token width and hidden width of an expert: multiples of 8 (of 16 with E4M3 weights) */
+  int32_t E, top_k;     /* experts (at most 1024), experts a token goes to (1 .. min(E, 32)) */
+  int32_t dtype;        /* LAUD_F32 or LAUD_BF16: x, router and out */
+  int32_t w_dtype;      /* experts' weights: dtype, or LAUD_E4M3 where dtype is LAUD_BF16 */
+  const void* router;   /* [E][C] */
+  const void* up;       /* [E][2][F][C]: gate projection, up projection */
+  const void* down;     /* [E][C][F] */
+  const float* s_up;    /* E4M3: [E][2][ceil(F/128)][ceil(C/128)], else unused */
+  const float* s_down;  /* E4M3: [E][ceil(C/128)][ceil(F/128)] */
+  int32_t renormalise;  /* non-zero: a token's weights are divided by their sum */
+  float scale;          /* factor on all weights */
+} laud_moe_layer;
+
+/*
+ * A whole mixture-of-experts layer for a few tokens: l = router * x; the top_k experts by l (of equal ones the lower index; a NaN
+ * comes last); weight = softmax(l over all experts) of the chosen ones, renormalised if asked for, times scale;
+ *   out = sum over the chosen e of weight_e * down_e * (silu(gate_e * x) * (up_e * x)).
+ * The hidden values stay float32.  A token with keep 0 is not routed: out row 0, experts -1, weights 0.
+ *   x [T][C], out [T][C] dtype (out may be x); keep [T] bytes or NULL
+ *   experts [T][top_k] int32 (ascending) and weights [T][top_k] float32: outputs, each may be NULL
+ * T is at most LAUD_MOE_MAX_TOKENS (LAUD_ERR_UNSUPPORTED beyond): every expert's weights are read once per 64 tokens.
+ * Workspace: laud_moe_workspace(p, T) bytes.
+ */
+#define LAUD_MOE_MAX_TOKENS 1024
+size_t laud_moe_workspace(const laud_moe_layer* p, int T);
+int laud_moe(const laud_moe_layer* p, int T, const void* x, int64_t ldx, const uint8_t* keep, void* out, int64_t ldo,
+             int32_t* experts, float* weights, void* ws, size_t ws_bytes, void* stream);
 
 /*
  * Instrumentation (host side; not part of the paper's method): per-stage GPU time of the

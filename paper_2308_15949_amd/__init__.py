@@ -11,4 +11,6 @@ from .binding import (  # noqa: F401
     dyn_projection_workspace, GroupSE, laud_dyn_group_se_bottleneck, laud_dyn_group_se_projection_bottleneck, make_group_se,
     laud_stage_timing_enable, laud_stage_timing_read, load, laud_init, laud_dyn_bottleneck_noalloc, laud_probe_mfma, laud_probe_copy, laud_probe_read, laud_pack_weights, packed_weights_size,
     make_bottleneck, status_string, workspace_size,
+    E4M3, MoeLayer, NormBlock, laud_matmul_e4m3, laud_moe, laud_norm_residual, laud_quantize_e4m3, make_moe, make_norm_block,
+    matmul_e4m3_workspace, moe_workspace,
 )

@@ -13,7 +13,9 @@ import os
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "liblaud.so")
 
-F32, BF16 = 0, 1
+F32, BF16, E4M3 = 0, 1, 2
+NORM_RMS, NORM_LAYER = 0, 1
+MOE_MAX_TOKENS = 1024
 OP_MASK_GEN, OP_COMPACT, OP_GATHER, OP_DYN_BOTTLENECK, OP_CHANNEL_SKIP = range(5)
 OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_WORKSPACE, ERR_HIP, ERR_SCRATCH_LIMIT = 0, -1, -2, -3, -4, -5
 NOALLOC_SCRATCH_BYTES = 16 << 20
@@ -25,7 +27,9 @@ EXPORTS = ["laud_status_string", "laud_abi_version", "laud_workspace_size", "lau
            "laud_stem", "laud_stem3x3", "laud_stem_workspace", "laud_dyn_projection_bottleneck", "laud_dyn_projection_workspace",
            "laud_dyn_group_se_bottleneck", "laud_dyn_group_se_projection_bottleneck", "laud_stage_timing_enable", "laud_stage_timing_read", "laud_stage_name",
            "laud_init", "laud_dyn_bottleneck_noalloc", "laud_probe_mfma", "laud_probe_copy", "laud_probe_read",
-           "laud_packed_weights_size", "laud_pack_weights"]
+           "laud_packed_weights_size", "laud_pack_weights",
+           "laud_norm_residual", "laud_quantize_e4m3", "laud_matmul_e4m3_workspace", "laud_matmul_e4m3", "laud_moe_workspace",
+           "laud_moe"]
 STAGE_COUNT = 13
 
 
@@ -43,6 +47,17 @@ class Bottleneck(C.Structure):
 class GroupSE(C.Structure):
     _fields_ = [("group_width", C.c_int32), ("se_width", C.c_int32), ("w_se1", C.c_void_p), ("b_se1", C.c_void_p),
                 ("w_se2", C.c_void_p), ("b_se2", C.c_void_p)]
+
+
+class NormBlock(C.Structure):
+    _fields_ = [("C", C.c_int32), ("dtype", C.c_int32), ("kind", C.c_int32), ("eps", C.c_float), ("post_w", C.c_void_p),
+                ("post_b", C.c_void_p), ("pre_w", C.c_void_p), ("pre_b", C.c_void_p), ("alpha", C.c_float), ("beta", C.c_float)]
+
+
+class MoeLayer(C.Structure):
+    _fields_ = [("C", C.c_int32), ("F", C.c_int32), ("E", C.c_int32), ("top_k", C.c_int32), ("dtype", C.c_int32),
+                ("w_dtype", C.c_int32), ("router", C.c_void_p), ("up", C.c_void_p), ("down", C.c_void_p), ("s_up", C.c_void_p),
+                ("s_down", C.c_void_p), ("renormalise", C.c_int32), ("scale", C.c_float)]
 
 
 class LaudError(RuntimeError):
@@ -126,6 +141,19 @@ def load() -> C.CDLL:
     lib.laud_channel_masker_workspace.argtypes = [Fmap]
     lib.laud_channel_masker.restype = i32
     lib.laud_channel_masker.argtypes = [vp, Fmap, vp, vp, i32, vp, vp, i32, vp, vp, vp, sz, vp]
+    i64 = C.c_int64
+    lib.laud_norm_residual.restype = i32
+    lib.laud_norm_residual.argtypes = [C.POINTER(NormBlock), i32, vp, i64, vp, i64, vp, vp, i32, vp, i64, vp, i64, i32, vp, vp]
+    lib.laud_quantize_e4m3.restype = i32
+    lib.laud_quantize_e4m3.argtypes = [vp, i64, i32, i32, i32, i32, vp, i64, vp, vp]
+    lib.laud_matmul_e4m3_workspace.restype = sz
+    lib.laud_matmul_e4m3_workspace.argtypes = [i32, i32, i32]
+    lib.laud_matmul_e4m3.restype = i32
+    lib.laud_matmul_e4m3.argtypes = [vp, i64, vp, vp, i64, vp, i32, i32, i32, vp, i64, i32, vp, sz, vp]
+    lib.laud_moe_workspace.restype = sz
+    lib.laud_moe_workspace.argtypes = [C.POINTER(MoeLayer), i32]
+    lib.laud_moe.restype = i32
+    lib.laud_moe.argtypes = [C.POINTER(MoeLayer), i32, vp, i64, vp, vp, i64, vp, vp, vp, sz, vp]
     lib.laud_stage_timing_enable.restype = i32
     lib.laud_stage_timing_enable.argtypes = [i32]
     lib.laud_stage_timing_read.restype = i32
@@ -364,6 +392,163 @@ def laud_channel_masker(x, fx: Fmap, wa, ba, hidden: int, wb, bb, D: int, cmask,
     wp, wb_ = _ws_args(ws)
     _check(load().laud_channel_masker(_ptr(x), fx, _ptr(wa), _ptr(ba), int(hidden), _ptr(wb), _ptr(bb), int(D),
                                       _ptr(cmask), _ptr(logits2), wp, wb_, _stream()), "laud_channel_masker")
+
+
+# ----- token operators --------------------------------------------------------------------------------------------------------
+# (Their tensors come with strides and in three types, so the binding checks what a pointer no longer tells: device, type, shape.
+# A tensor that does not fit raises LaudError like an argument the library refuses.)
+_dtypes = None
+
+
+def _dtype_of(t) -> int:
+    """laud_dtype of a tensor, -1 for other types."""
+    global _dtypes
+    if _dtypes is None:
+        import torch
+        _dtypes = {torch.float32: F32, torch.bfloat16: BF16, torch.float8_e4m3fn: E4M3}
+    return _dtypes.get(t.dtype, -1)
+
+
+def _need(ok: bool, where: str) -> None:
+    if not ok:
+        raise LaudError(ERR_INVALID_ARG, where)
+
+
+def _rows(t, where: str, cols: int | None = None, rows: int | None = None):
+    """(pointer, elements from row to row) of a device tensor [rows][cols] whose rows are contiguous."""
+    _need(t.is_cuda and t.dim() == 2, where)
+    (n, c), (ld, step) = t.shape, t.stride()
+    _need((step == 1 or c == 1) and (cols is None or c == cols) and (rows is None or n == rows), where)
+    return t.data_ptr(), (ld if n > 1 else c)
+
+
+def _dense(t, shape, dtype: int, where: str):
+    """Pointer of a contiguous device tensor of that shape and type; None -> None."""
+    if t is None:
+        return None
+    _need(t.is_cuda and tuple(t.shape) == tuple(shape) and _dtype_of(t) == dtype and t.is_contiguous(), where)
+    return t.data_ptr()
+
+
+def _bytes(t, n: int, where: str):
+    """Pointer of a byte (or truth value) per row; None -> None."""
+    if t is None:
+        return None
+    _need(t.is_cuda and t.element_size() == 1 and not t.is_floating_point() and t.numel() == n and t.is_contiguous(), where)
+    return t.data_ptr()
+
+
+def _blocks(n: int) -> int:
+    return -(-n // 128)
+
+
+def make_norm_block(c: int, dtype, kind: str, eps: float, post_w=None, post_b=None, pre_w=None, pre_b=None, alpha: float = 1.0,
+                    beta: float = 1.0) -> NormBlock:
+    """Descriptor of the norms after a block and before the next one over float32 device vectors [c]; dtype: torch's type of the
+    rows, kind "rms" or "layer".  The caller keeps the tensors alive."""
+    import torch
+    where = "make_norm_block"
+    _need(kind in ("rms", "layer") and dtype in (torch.float32, torch.bfloat16), where)
+    v = [_dense(t, (c,), F32, where) for t in (post_w, post_b, pre_w, pre_b)]
+    return NormBlock(int(c), BF16 if dtype == torch.bfloat16 else F32, NORM_LAYER if kind == "layer" else NORM_RMS, float(eps), *v,
+                     float(alpha), float(beta))
+
+
+def laud_norm_residual(p: NormBlock, x, y=None, keep=None, gate=None, rows_per_gate: int = 0, out=None, z=None, z_scale=None) -> None:
+    """x, y, out, z [rows][C]; keep [rows] bytes; gate [ceil(rows / rows_per_gate)][C] float32; z float8_e4m3fn with
+    z_scale [rows][ceil(C / 128)], or of x's type."""
+    where = "laud_norm_residual"
+    n, c = x.shape if x.dim() == 2 else (-1, -1)
+    _need(c == p.C and _dtype_of(x) == p.dtype, where)
+    xp, ldx = _rows(x, where)
+    yp = op = zp = gp = None
+    ldy = ldo = ldz = 0
+    z_dtype = p.dtype
+    if y is not None:
+        _need(_dtype_of(y) == p.dtype, where)
+        yp, ldy = _rows(y, where, c, n)
+    if out is not None:
+        _need(_dtype_of(out) == p.dtype, where)
+        op, ldo = _rows(out, where, c, n)
+    if z is not None:
+        z_dtype = _dtype_of(z)
+        _need(z_dtype == E4M3 or z_dtype == p.dtype, where)
+        zp, ldz = _rows(z, where, c, n)
+    if gate is not None:
+        _need(rows_per_gate > 0, where)
+        gp = _dense(gate, (-(-n // rows_per_gate), c), F32, where)
+    zs = _dense(z_scale, (n, _blocks(c)), F32, where) if z_dtype == E4M3 and z is not None else None
+    _check(load().laud_norm_residual(C.byref(p), n, xp, ldx, yp, ldy, _bytes(keep, n, where), gp, int(rows_per_gate), op, ldo, zp, ldz,
+                                     z_dtype, zs, _stream()), where)
+
+
+def laud_quantize_e4m3(x, q, scale, block_rows: int = 1) -> None:
+    """x [rows][cols] float32 or bf16 -> q [rows][cols] float8_e4m3fn and scale [ceil(rows / block_rows)][ceil(cols / 128)]."""
+    where = "laud_quantize_e4m3"
+    xp, ldx = _rows(x, where)
+    n, c = x.shape
+    _need(_dtype_of(q) == E4M3 and _dtype_of(x) in (F32, BF16) and block_rows in (1, 128), where)
+    qp, ldq = _rows(q, where, c, n)
+    _check(load().laud_quantize_e4m3(xp, ldx, n, c, _dtype_of(x), int(block_rows), qp, ldq,
+                                     _dense(scale, (-(-n // block_rows), _blocks(c)), F32, where), _stream()), where)
+
+
+def matmul_e4m3_workspace(m: int, n: int, k: int) -> int:
+    return int(load().laud_matmul_e4m3_workspace(int(m), int(n), int(k)))
+
+
+def laud_matmul_e4m3(a, sa, b, sb, out, ws=None) -> None:
+    """out [M][N] (float32 or bf16) = a [M][K] times b [N][K] transposed, both float8_e4m3fn with scales sa [M][ceil(K / 128)] and
+    sb [ceil(N / 128)][ceil(K / 128)]."""
+    where = "laud_matmul_e4m3"
+    ap, lda = _rows(a, where)
+    m, k = a.shape
+    bp, ldb = _rows(b, where, k)
+    n = b.shape[0]
+    op, ldo = _rows(out, where, n, m)
+    _need(_dtype_of(a) == E4M3 and _dtype_of(b) == E4M3, where)
+    wp, wb = _ws_args(ws)
+    _check(load().laud_matmul_e4m3(ap, lda, _dense(sa, (m, _blocks(k)), F32, where), bp, ldb,
+                                   _dense(sb, (_blocks(n), _blocks(k)), F32, where), m, n, k, op, ldo, _dtype_of(out), wp, wb,
+                                   _stream()), where)
+
+
+def make_moe(router, up, down, s_up=None, s_down=None, top_k: int = 1, renormalise: bool = False, scale: float = 1.0) -> MoeLayer:
+    """Descriptor of a mixture-of-experts layer over device tensors router [E][C], up [E][2][F][C] (gate, up) and down [E][C][F];
+    float8_e4m3fn weights come with s_up [E][2][ceil(F/128)][ceil(C/128)] and s_down [E][ceil(C/128)][ceil(F/128)].  The caller
+    keeps the tensors alive."""
+    where = "make_moe"
+    _need(router.dim() == 2 and up.dim() == 4 and up.shape[1] == 2, where)
+    (e, c), f = router.shape, up.shape[2]
+    wd = _dtype_of(up)
+    v = [_dense(router, (e, c), _dtype_of(router), where), _dense(up, (e, 2, f, c), wd, where), _dense(down, (e, c, f), wd, where)]
+    s = [None, None]
+    if wd == E4M3:
+        _need(s_up is not None and s_down is not None, where)
+        s = [_dense(s_up, (e, 2, _blocks(f), _blocks(c)), F32, where), _dense(s_down, (e, _blocks(c), _blocks(f)), F32, where)]
+    return MoeLayer(int(c), int(f), int(e), int(top_k), _dtype_of(router), wd, *v, *s, 1 if renormalise else 0, float(scale))
+
+
+def moe_workspace(p: MoeLayer, t: int) -> int:
+    return int(load().laud_moe_workspace(C.byref(p), int(t)))
+
+
+def laud_moe(p: MoeLayer, x, keep, out, experts, weights, ws) -> None:
+    """x, out [T][C] of the router's type; keep [T] bytes or None; experts [T][top_k] int32 and weights [T][top_k] float32 receive
+    the routing, each may be None."""
+    where = "laud_moe"
+    xp, ldx = _rows(x, where, p.C)
+    n = x.shape[0]
+    op, ldo = _rows(out, where, p.C, n)
+    _need(_dtype_of(x) == p.dtype and _dtype_of(out) == p.dtype, where)
+    ep = None
+    if experts is not None:
+        _need(experts.is_cuda and tuple(experts.shape) == (n, p.top_k) and experts.element_size() == 4 and
+              not experts.is_floating_point() and experts.is_contiguous(), where)
+        ep = experts.data_ptr()
+    wp, wb = _ws_args(ws)
+    _check(load().laud_moe(C.byref(p), n, xp, ldx, _bytes(keep, n, where), op, ldo, ep, _dense(weights, (n, p.top_k), F32, where),
+                           wp, wb, _stream()), where)
 
 
 def laud_stage_timing_enable(on: bool) -> None:
