@@ -315,6 +315,7 @@ struct TailArgs {
 };
 
 bool tail_supported(int dtype, int c_mid, int c_out);
+int matmul8_init_device();
 int tail_init_device();
 size_t tail_packed_bytes(int c_mid, int c_out);
 // re-orders w2 [c_mid][3][3][c_mid] and w3 [c_out][c_mid] into the order the fused kernel streams them

@@ -1597,6 +1597,7 @@ extern "C" int laud_init(void) {
   if ((rc = first_init_device()) != LAUD_OK) return rc;
   if ((rc = stem_init_device(nullptr)) != LAUD_OK) return rc;
   if ((rc = tail_init_device()) != LAUD_OK) return rc;
+  if ((rc = matmul8_init_device()) != LAUD_OK) return rc;
   return head_init_device();
 }
 

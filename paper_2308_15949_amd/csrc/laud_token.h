@@ -2,7 +2,7 @@
 // elements, 8-bit floating point (e4m3) in blocks of 128.
 #pragma once
 
-#include "laud_common.h"
+#include "laud_tile_util.h"
 
 namespace laud {
 
@@ -119,10 +119,6 @@ __device__ __forceinline__ tok_u2 codes8(const float (&f)[8], float s) {
   }
   return q;
 }
-
-typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
-typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
-typedef __attribute__((ext_vector_type(2))) float f32x2;
 
 __device__ __forceinline__ bf16x8 widen8(unsigned lo, unsigned hi) {  // eight e4m3 codes, exact in bf16
   union { bf16x2 h[4]; bf16x8 v; } u;
