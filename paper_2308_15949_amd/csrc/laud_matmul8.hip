@@ -162,6 +162,10 @@ __global__ __launch_bounds__(BM / WM * (BN / WN) * kWave) void k_mm8_tile(Mm8Arg
   for (int i = 0; i < kNT; ++i)
 #pragma unroll
     for (int j = 0; j < kMT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  f32x4 p[kNT];
+  float f = 0.f;
+#pragma unroll
+  for (int i = 0; i < kNT; ++i) p[i] = f32x4{0.f, 0.f, 0.f, 0.f};
   request(0);
   for (int kb = 0; kb < g.kb; ++kb) {
     vm_wait<0>();
@@ -169,28 +173,43 @@ __global__ __launch_bounds__(BM / WM * (BN / WN) * kWave) void k_mm8_tile(Mm8Arg
     if (kb + 1 < g.kb) request(kb + 1);
     const uint8_t* stage = lds + (kb & 1) * L::kStage;
     const uint8_t *fb = stage + L::kB + wn * kScaleBlock, *fa = stage + L::kA + wm * kScaleBlock;
+    const float* sa = reinterpret_cast<const float*>(stage + L::kSa) + wm + r16;
     const float sb = *reinterpret_cast<const float*>(stage + L::kSb + wn / kScaleBlock * 4);
-    tok_u4 nf[kNT][2];
+    tok_u4 nf[kNT][2], mf[2][2];
+    float s[2];
+    auto read_m = [&](int j) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) mf[j & 1][h] = *reinterpret_cast<const tok_u4*>(fa + j * 2048 + (frag ^ (h * 64)));
+      s[j & 1] = sa[j * 16];
+    };
+    read_m(0);
 #pragma unroll
     for (int i = 0; i < kNT; ++i)
 #pragma unroll
       for (int h = 0; h < 2; ++h) nf[i][h] = *reinterpret_cast<const tok_u4*>(fb + i * 2048 + (frag ^ (h * 64)));
+    // A product's scaling stands behind the matrix instruction of the next row tile (in the last of a block: of the next block's
+    // first), in this order and no other: an instruction's result is there long before it is asked for.
 #pragma unroll
     for (int j = 0; j < kMT; ++j) {
-      tok_u4 mf[2];
-#pragma unroll
-      for (int h = 0; h < 2; ++h) mf[h] = *reinterpret_cast<const tok_u4*>(fa + j * 2048 + (frag ^ (h * 64)));
-      const float f = sb * *reinterpret_cast<const float*>(stage + L::kSa + (wm + j * 16 + r16) * 4);
+      const float f_old = f;
+      f = sb * s[j & 1];
+      if (j + 1 < kMT) read_m(j + 1);
 #pragma unroll
       for (int i = 0; i < kNT; ++i) {
-        f32x4 p;
-        if constexpr (sizeof(OT) == 2) p = mma_block8(nf[i], mf);
-        else p = mma_block(nf[i], mf);
+        const f32x4 old = p[i];
+        if constexpr (sizeof(OT) == 2) p[i] = mma_block8(nf[i], mf[j & 1]);
+        else p[i] = mma_block(nf[i], mf[j & 1]);
+        f32x4& c = acc[i][(j + kMT - 1) % kMT];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) acc[i][j][e] = fmaf(p[e], f, acc[i][j][e]);
+        for (int e = 0; e < 4; ++e) c[e] = fmaf(old[e], f_old, c[e]);
+        __builtin_amdgcn_sched_barrier(0);
       }
     }
   }
+#pragma unroll
+  for (int i = 0; i < kNT; ++i)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) acc[i][kMT - 1][e] = fmaf(p[i][e], f, acc[i][kMT - 1][e]);
   // Lane (row r16 of a, quarter) holds columns 4 * quarter .. +3 of every 16: after a swap of neighbouring quarters between two
   // column tiles it holds eight in a row, and four lanes 64 bytes of a row of bf16 results.
 #pragma unroll
