@@ -20,12 +20,15 @@ constexpr int64_t kMaxLd = 1 << 22;    // elements from row to row: 256 rows of 
 // row l % 16 of the second.  The codes are widened to bf16, which holds them exactly: the 8-bit matrix instructions add groups of
 // eight products with 14 bits below the group's largest (2^16 + 2^2 in one group is 2^16; measured 1.5e-5 of a result's
 // norm, against 3e-7 here).
-__device__ __forceinline__ f32x4 mma_block(const tok_u4 (&a)[2], const tok_u4 (&b)[2]) {
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+__device__ __forceinline__ i32x8 join(const tok_u4& a, const tok_u4& b) {
+  return __builtin_bit_cast(i32x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+__device__ __forceinline__ f32x4 mma_block(const i32x8& a, const i32x8& b) {
   f32x4 c = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-  for (int h = 0; h < 2; ++h)
-#pragma unroll
-    for (int u = 0; u < 2; ++u) c = mma_bf16_16(widen8(a[h][2 * u], a[h][2 * u + 1]), widen8(b[h][2 * u], b[h][2 * u + 1]), c);
+  for (int h = 0; h < 8; h += 2)
+    c = mma_bf16_16(widen8((unsigned)a[h], (unsigned)a[h + 1]), widen8((unsigned)b[h], (unsigned)b[h + 1]), c);
   return c;
 }
 
@@ -71,7 +74,7 @@ __global__ __launch_bounds__(kSplit * kWave) void k_mm8_split(Mm8Args g, int nti
 #pragma unroll
         for (int h = 0; h < 2; ++h) x[h] = load16(ra, (int)k[h] < g.K ? off_a[t] + k[h] : kOutside);
         const float f = s * sa[t][kb];
-        const f32x4 p = mma_block(w, x);
+        const f32x4 p = mma_block(join(w[0], w[1]), join(x[0], x[1]));
 #pragma unroll
         for (int i = 0; i < 4; ++i) acc[t][i] = fmaf(p[i], f, acc[t][i]);
       }
@@ -96,16 +99,12 @@ __global__ __launch_bounds__(kSplit * kWave) void k_mm8_split(Mm8Args g, int nti
 // two stages that take turns: one barrier a block, the next block's loads are under way while this one is multiplied.  A row's
 // eight 16-byte chunks lie XOR-swizzled (chunk ^ row % 8; the swizzle is applied to the global side).  The first operand of the
 // matrix instructions is b: a lane's results are consecutive columns, its row of a - and that row's scale - is one for all of them.
-typedef int i32x8 __attribute__((ext_vector_type(8)));
-
 // The block's products in 8-bit instructions: twice the rate of the bf16 ones.  They add groups of eight products with 14 bits below
 // the group's largest, an error of 1.5e-5 of the result's norm: a hundredth of what a bf16 result's rounding adds, and taken for
 // bf16 results only.
-__device__ __forceinline__ f32x4 mma_block8(const tok_u4 (&a)[2], const tok_u4 (&b)[2]) {
-  const i32x8 p = {(int)a[0][0], (int)a[0][1], (int)a[0][2], (int)a[0][3], (int)a[1][0], (int)a[1][1], (int)a[1][2], (int)a[1][3]};
-  const i32x8 q = {(int)b[0][0], (int)b[0][1], (int)b[0][2], (int)b[0][3], (int)b[1][0], (int)b[1][1], (int)b[1][2], (int)b[1][3]};
+__device__ __forceinline__ f32x4 mma_block8(const i32x8& a, const i32x8& b) {
   const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
-  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(p, q, zero, 0, 0, 0, 0, 0, 0);
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, zero, 0, 0, 0, 0, 0, 0);
 }
 
 template <int BM, int BN> struct TileLds {
@@ -118,7 +117,7 @@ __global__ __launch_bounds__(BM / WM * (BN / WN) * kWave) void k_mm8_tile(Mm8Arg
   typedef TileLds<BM, BN> L;
   constexpr int kWaves = BM / WM * (BN / WN), kMT = WM / 16, kNT = WN / 16;
   constexpr int kLoadsB = BN / 8 / kWaves, kLoadsA = BM / 8 / kWaves;
-  static_assert(kLoadsB * 8 * kWaves == BN && kLoadsA * 8 * kWaves == BM && BM <= kWaves * kWave, "rows shared evenly");
+  static_assert(kLoadsB * 8 * kWaves == BN && kLoadsA * 8 * kWaves == BM && BM < kWaves * kWave && BM % kWave == 0 && kMT % 2 == 0, "rows shared evenly");
   extern __shared__ __align__(1024) uint8_t lds[];
   const unsigned lds0 = (unsigned)(size_t)(__attribute__((address_space(3))) uint8_t*)lds;
   const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), r16 = lane % 16, quarter = lane / 16;
@@ -138,74 +137,99 @@ __global__ __launch_bounds__(BM / WM * (BN / WN) * kWave) void k_mm8_tile(Mm8Arg
   for (int i = 0; i < kLoadsB; ++i) vb[i] = (unsigned)(min((wave * kLoadsB + i) * 8 + lane / 8, nrows - 1) * g.ldb) + chunk * 16;
 #pragma unroll
   for (int i = 0; i < kLoadsA; ++i) va[i] = (unsigned)(min((wave * kLoadsA + i) * 8 + lane / 8, mrows - 1) * g.lda) + chunk * 16;
-  const unsigned vsa = wave * kWave < BM ? (unsigned)(min(wave * kWave + lane, mrows - 1) * (long long)g.kb * 4) : kOutside;
-  const unsigned vsb = lane < (nrows - 1) / kScaleBlock + 1 ? (unsigned)(lane * g.kb * 4) : kOutside;
+  // the first waves bring the rows' scales, 64 each, the others the one or two of the columns (all to the same place)
+  const bool rows_scales = wave < BM / kWave;
+  const unsigned vs = rows_scales ? (unsigned)(min(wave * kWave + lane, mrows - 1) * (long long)g.kb * 4)
+                                  : lane < (nrows - 1) / kScaleBlock + 1 ? (unsigned)(lane * g.kb * 4) : kOutside;
+  const unsigned to_s = rows_scales ? L::kSa + wave * 256 : L::kSb;
   const uint8_t *pa = g.a + m0 * g.lda, *pb = g.b + (long long)n0 * g.ldb;
-  const float *psa = g.sa + m0 * g.kb, *psb = g.sb + (long long)(n0 / kScaleBlock) * g.kb;
+  const float* ps = rows_scales ? g.sa + m0 * g.kb : g.sb + (long long)(n0 / kScaleBlock) * g.kb;
 
-  auto request = [&](int kb) {
+  // The loads of block kb, kPer of them behind each row tile's matrix instructions.  Behind the last block they fetch nothing: the loop
+  // over the blocks has no branch, across which the compiler would gather the scalings.
+  constexpr int kLoads = kLoadsB + kLoadsA + 1, kPer = (kLoads - 1) / (kMT - 1) + 1;
+  static_assert(kPer * kMT >= kLoads, "all of a block's loads before its last row tile");
+  auto request = [&](int kb, int from, int to) {
     const unsigned stage = lds0 + (kb & 1) * L::kStage;
     const bool in = kb * kScaleBlock + chunk * 16 < g.K;
-    const __amdgpu_buffer_rsrc_t rb = bytes_of(pb + kb * kScaleBlock, 0x7fffffff), ra = bytes_of(pa + kb * kScaleBlock, 0x7fffffff);
 #pragma unroll
-    for (int i = 0; i < kLoadsB; ++i) dma16(rb, in ? vb[i] : kOutside, 0, stage + L::kB + (wave * kLoadsB + i) * 1024);
-#pragma unroll
-    for (int i = 0; i < kLoadsA; ++i) dma16(ra, in ? va[i] : kOutside, 0, stage + L::kA + (wave * kLoadsA + i) * 1024);
-    if (wave * kWave < BM) dma4(bytes_of(psa + kb, 0x7fffffff), vsa, 0, stage + L::kSa + wave * 256);
-    if (wave == kWaves - 1) dma4(bytes_of(psb + kb, 0x7fffffff), vsb, 0, stage + L::kSb);
+    for (int i = from; i < to; ++i) {
+      if (i == 0) dma4(bytes_of(ps + kb, 0x7fffffff), kb < g.kb ? vs : kOutside, 0, stage + to_s);
+      else if (i <= kLoadsB) dma16(bytes_of(pb + kb * kScaleBlock, 0x7fffffff), in ? vb[i - 1] : kOutside, 0, stage + L::kB + (wave * kLoadsB + i - 1) * 1024);
+      else if (i < kLoads) dma16(bytes_of(pa + kb * kScaleBlock, 0x7fffffff), in ? va[i - 1 - kLoadsB] : kOutside, 0, stage + L::kA + (wave * kLoadsA + i - 1 - kLoadsB) * 1024);
+    }
   };
 
   const int wm = wave % (BM / WM) * WM, wn = wave / (BM / WM) * WN;
   const unsigned frag = (unsigned)(r16 * kScaleBlock + ((quarter ^ (lane & 7)) << 4));
-  f32x4 acc[kNT][kMT];
-#pragma unroll
-  for (int i = 0; i < kNT; ++i)
-#pragma unroll
-    for (int j = 0; j < kMT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  float acc[kNT][kMT][4];  // (plain floats: as vectors the compiler moves them about in fours)
   f32x4 p[kNT];
-  float f = 0.f;
+  i32x8 nf[kNT], mf[2];
+  float s[2], sb, f = 0.f;
+  auto read_m = [&](int kb, int j) {
+    const uint8_t* at = lds + (kb & 1) * L::kStage;
+    s[j & 1] = *reinterpret_cast<const float*>(at + L::kSa + (wm + j * 16 + r16) * 4);
+    at += L::kA + (wm + j * 16) * kScaleBlock;
+    mf[j & 1] = join(*reinterpret_cast<const tok_u4*>(at + frag), *reinterpret_cast<const tok_u4*>(at + (frag ^ 64)));
+  };
+  auto read_n = [&](int kb, int i) {
+    const uint8_t* at = lds + (kb & 1) * L::kStage + L::kB + (wn + i * 16) * kScaleBlock;
+    nf[i] = join(*reinterpret_cast<const tok_u4*>(at + frag), *reinterpret_cast<const tok_u4*>(at + (frag ^ 64)));
+  };
+  auto read_sb = [&](int kb) { sb = *reinterpret_cast<const float*>(lds + (kb & 1) * L::kStage + L::kSb + wn / kScaleBlock * 4); };
 #pragma unroll
-  for (int i = 0; i < kNT; ++i) p[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-  request(0);
+  for (int i = 0; i < kNT; ++i) {
+#pragma unroll
+    for (int j = 0; j < kMT; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[i][j][e] = 0.f;
+    p[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  request(0, 0, kLoads);
+  vm_wait<0>();
+  __syncthreads();
+  request(1, 0, kPer);
+  read_m(0, 0);
+  read_sb(0);
+#pragma unroll
+  for (int i = 0; i < kNT; ++i) read_n(0, i);
+  // A product's scaling stands behind the matrix instruction of the next row tile (in the last of a block: of the next block's
+  // first), in this order and no other: an instruction's result is there long before it is asked for.  The barrier stands in front
+  // of a block's last row tile, whose operands are in registers by then: behind it the next block's first ones come from LDS, and
+  // the loads of the block after that may overwrite this one's stage.  (Behind the last block it reads what is there, unused.)
   for (int kb = 0; kb < g.kb; ++kb) {
-    vm_wait<0>();
-    __syncthreads();
-    if (kb + 1 < g.kb) request(kb + 1);
-    const uint8_t* stage = lds + (kb & 1) * L::kStage;
-    const uint8_t *fb = stage + L::kB + wn * kScaleBlock, *fa = stage + L::kA + wm * kScaleBlock;
-    const float* sa = reinterpret_cast<const float*>(stage + L::kSa) + wm + r16;
-    const float sb = *reinterpret_cast<const float*>(stage + L::kSb + wn / kScaleBlock * 4);
-    tok_u4 nf[kNT][2], mf[2][2];
-    float s[2];
-    auto read_m = [&](int j) {
-#pragma unroll
-      for (int h = 0; h < 2; ++h) mf[j & 1][h] = *reinterpret_cast<const tok_u4*>(fa + j * 2048 + (frag ^ (h * 64)));
-      s[j & 1] = sa[j * 16];
-    };
-    read_m(0);
-#pragma unroll
-    for (int i = 0; i < kNT; ++i)
-#pragma unroll
-      for (int h = 0; h < 2; ++h) nf[i][h] = *reinterpret_cast<const tok_u4*>(fb + i * 2048 + (frag ^ (h * 64)));
-    // A product's scaling stands behind the matrix instruction of the next row tile (in the last of a block: of the next block's
-    // first), in this order and no other: an instruction's result is there long before it is asked for.
 #pragma unroll
     for (int j = 0; j < kMT; ++j) {
       const float f_old = f;
       f = sb * s[j & 1];
-      if (j + 1 < kMT) read_m(j + 1);
+      if (j == kMT - 1) {
+        lds_wait();
+        vm_wait<0>();
+        __syncthreads();
+        read_m(kb + 1, 0);
+        read_sb(kb + 1);
+        request(kb + 2, 0, kPer);
+      } else {
+        request(kb + 1, (j + 1) * kPer, (j + 2) * kPer);
+        read_m(kb, j + 1);
+      }
 #pragma unroll
       for (int i = 0; i < kNT; ++i) {
         const f32x4 old = p[i];
         if constexpr (sizeof(OT) == 2) p[i] = mma_block8(nf[i], mf[j & 1]);
         else p[i] = mma_block(nf[i], mf[j & 1]);
-        f32x4& c = acc[i][(j + kMT - 1) % kMT];
+        __builtin_amdgcn_sched_barrier(0);
+        float(&c)[4] = acc[i][(j + kMT - 1) % kMT];
 #pragma unroll
         for (int e = 0; e < 4; ++e) c[e] = fmaf(old[e], f_old, c[e]);
         __builtin_amdgcn_sched_barrier(0);
+        if (j == kMT - 1) read_n(kb + 1, i);
+        if (i == 0) __builtin_amdgcn_s_setprio(1);  // (a wave amid its products goes ahead of one that loads)
+        if (i == kNT - 1) __builtin_amdgcn_s_setprio(0);
       }
     }
   }
+  vm_wait<0>();  // (no load into LDS is left behind)
 #pragma unroll
   for (int i = 0; i < kNT; ++i)
 #pragma unroll
@@ -218,17 +242,16 @@ __global__ __launch_bounds__(BM / WM * (BN / WN) * kWave) void k_mm8_tile(Mm8Arg
     OT* out = reinterpret_cast<OT*>(g.out) + (m0 + m) * g.ldo + n0;
 #pragma unroll
     for (int i = 0; i < kNT; i += 2) {
-      f32x4 lo = acc[i][j], hi = acc[i + 1][j];
+      float v[8];
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(lo[e]), __float_as_uint(hi[e]), false, false);
-        lo[e] = __uint_as_float(r[0]);
-        hi[e] = __uint_as_float(r[1]);
+        auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(acc[i][j][e]), __float_as_uint(acc[i + 1][j][e]), false, false);
+        v[e] = __uint_as_float(r[0]);
+        v[4 + e] = __uint_as_float(r[1]);
       }
       const int n = wn + (i + quarter % 2) * 16 + quarter / 2 * 8;
       if (m < mrows && n < nrows) {
         piece8<OT> q;
-        const float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
         q.put(v);
         q.store(out + n, 0);
       }
