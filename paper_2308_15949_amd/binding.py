@@ -396,37 +396,43 @@ def laud_channel_masker(x, fx: Fmap, wa, ba, hidden: int, wb, bb, D: int, cmask,
 
 # ----- token operators --------------------------------------------------------------------------------------------------------
 # (Their tensors come with strides and in three types, so the binding checks what a pointer no longer tells: device, type, shape.
-# A tensor that does not fit raises LaudError like an argument the library refuses.)
-_dtypes = None
+# A tensor that does not fit raises LaudError like an argument the library refuses.  A call on a few rows is a launch of a few
+# microseconds, so the checks are written out for speed: attributes read once, shapes compared whole.)
+_CODES: dict = {}  # torch's types -> laud_dtype
+
+
+def _codes() -> dict:
+    if not _CODES:
+        import torch
+        _CODES.update({torch.float32: F32, torch.bfloat16: BF16, torch.float8_e4m3fn: E4M3})
+    return _CODES
 
 
 def _dtype_of(t) -> int:
     """laud_dtype of a tensor, -1 for other types."""
-    global _dtypes
-    if _dtypes is None:
-        import torch
-        _dtypes = {torch.float32: F32, torch.bfloat16: BF16, torch.float8_e4m3fn: E4M3}
-    return _dtypes.get(t.dtype, -1)
+    return (_CODES or _codes()).get(t.dtype, -1)
 
 
-def _need(ok: bool, where: str) -> None:
-    if not ok:
-        raise LaudError(ERR_INVALID_ARG, where)
+def _bad(where: str):
+    raise LaudError(ERR_INVALID_ARG, where)
 
 
-def _rows(t, where: str, cols: int | None = None, rows: int | None = None):
-    """(pointer, elements from row to row) of a device tensor [rows][cols] whose rows are contiguous."""
-    _need(t.is_cuda and t.dim() == 2, where)
-    (n, c), (ld, step) = t.shape, t.stride()
-    _need((step == 1 or c == 1) and (cols is None or c == cols) and (rows is None or n == rows), where)
-    return t.data_ptr(), (ld if n > 1 else c)
+def _rows(t, shape, dtype, where: str):
+    """(pointer, elements from row to row) of a device tensor [rows][cols] of that shape and torch type whose rows are contiguous."""
+    if not (t.is_cuda and t.dtype == dtype and t.shape == shape):
+        _bad(where)
+    ld, step = t.stride()
+    if step != 1 and shape[1] != 1:
+        _bad(where)
+    return t.data_ptr(), (ld if shape[0] > 1 else shape[1])
 
 
-def _dense(t, shape, dtype: int, where: str):
+def _dense(t, shape, code: int, where: str):
     """Pointer of a contiguous device tensor of that shape and type; None -> None."""
     if t is None:
         return None
-    _need(t.is_cuda and tuple(t.shape) == tuple(shape) and _dtype_of(t) == dtype and t.is_contiguous(), where)
+    if not (t.is_cuda and t.shape == shape and _dtype_of(t) == code and t.is_contiguous()):
+        _bad(where)
     return t.data_ptr()
 
 
@@ -434,7 +440,8 @@ def _bytes(t, n: int, where: str):
     """Pointer of a byte (or truth value) per row; None -> None."""
     if t is None:
         return None
-    _need(t.is_cuda and t.element_size() == 1 and not t.is_floating_point() and t.numel() == n and t.is_contiguous(), where)
+    if not (t.is_cuda and t.numel() == n and t.element_size() == 1 and not t.is_floating_point() and t.is_contiguous()):
+        _bad(where)
     return t.data_ptr()
 
 
@@ -448,7 +455,8 @@ def make_norm_block(c: int, dtype, kind: str, eps: float, post_w=None, post_b=No
     rows, kind "rms" or "layer".  The caller keeps the tensors alive."""
     import torch
     where = "make_norm_block"
-    _need(kind in ("rms", "layer") and dtype in (torch.float32, torch.bfloat16), where)
+    if kind not in ("rms", "layer") or dtype not in (torch.float32, torch.bfloat16):
+        _bad(where)
     v = [_dense(t, (c,), F32, where) for t in (post_w, post_b, pre_w, pre_b)]
     return NormBlock(int(c), BF16 if dtype == torch.bfloat16 else F32, NORM_LAYER if kind == "layer" else NORM_RMS, float(eps), *v,
                      float(alpha), float(beta))
@@ -458,39 +466,44 @@ def laud_norm_residual(p: NormBlock, x, y=None, keep=None, gate=None, rows_per_g
     """x, y, out, z [rows][C]; keep [rows] bytes; gate [ceil(rows / rows_per_gate)][C] float32; z float8_e4m3fn with
     z_scale [rows][ceil(C / 128)], or of x's type."""
     where = "laud_norm_residual"
-    n, c = x.shape if x.dim() == 2 else (-1, -1)
-    _need(c == p.C and _dtype_of(x) == p.dtype, where)
-    xp, ldx = _rows(x, where)
-    yp = op = zp = gp = None
+    shape, dtype = x.shape, x.dtype
+    if len(shape) != 2 or shape[1] != p.C or (_CODES or _codes()).get(dtype) != p.dtype:
+        _bad(where)
+    n, c = shape
+    xp, ldx = _rows(x, shape, dtype, where)
+    yp = op = zp = gp = zs = None
     ldy = ldo = ldz = 0
     z_dtype = p.dtype
     if y is not None:
-        _need(_dtype_of(y) == p.dtype, where)
-        yp, ldy = _rows(y, where, c, n)
+        yp, ldy = _rows(y, shape, dtype, where)
     if out is not None:
-        _need(_dtype_of(out) == p.dtype, where)
-        op, ldo = _rows(out, where, c, n)
+        op, ldo = _rows(out, shape, dtype, where)
     if z is not None:
-        z_dtype = _dtype_of(z)
-        _need(z_dtype == E4M3 or z_dtype == p.dtype, where)
-        zp, ldz = _rows(z, where, c, n)
+        if z_scale is not None:
+            z_dtype = E4M3
+            zs = _dense(z_scale, (n, _blocks(c)), F32, where)
+        zp, ldz = _rows(z, shape, z.dtype, where)
+        if _CODES.get(z.dtype) != z_dtype:
+            _bad(where)
     if gate is not None:
-        _need(rows_per_gate > 0, where)
+        if rows_per_gate <= 0:
+            _bad(where)
         gp = _dense(gate, (-(-n // rows_per_gate), c), F32, where)
-    zs = _dense(z_scale, (n, _blocks(c)), F32, where) if z_dtype == E4M3 and z is not None else None
-    _check(load().laud_norm_residual(C.byref(p), n, xp, ldx, yp, ldy, _bytes(keep, n, where), gp, int(rows_per_gate), op, ldo, zp, ldz,
-                                     z_dtype, zs, _stream()), where)
+    _check(load().laud_norm_residual(C.byref(p), n, xp, ldx, yp, ldy, None if keep is None else _bytes(keep, n, where), gp,
+                                     rows_per_gate, op, ldo, zp, ldz, z_dtype, zs, _stream()), where)
 
 
 def laud_quantize_e4m3(x, q, scale, block_rows: int = 1) -> None:
     """x [rows][cols] float32 or bf16 -> q [rows][cols] float8_e4m3fn and scale [ceil(rows / block_rows)][ceil(cols / 128)]."""
     where = "laud_quantize_e4m3"
-    xp, ldx = _rows(x, where)
-    n, c = x.shape
-    _need(_dtype_of(q) == E4M3 and _dtype_of(x) in (F32, BF16) and block_rows in (1, 128), where)
-    qp, ldq = _rows(q, where, c, n)
-    _check(load().laud_quantize_e4m3(xp, ldx, n, c, _dtype_of(x), int(block_rows), qp, ldq,
-                                     _dense(scale, (-(-n // block_rows), _blocks(c)), F32, where), _stream()), where)
+    shape, code = x.shape, _dtype_of(x)
+    if len(shape) != 2 or _dtype_of(q) != E4M3 or code not in (F32, BF16) or block_rows not in (1, 128):
+        _bad(where)
+    n, c = shape
+    xp, ldx = _rows(x, shape, x.dtype, where)
+    qp, ldq = _rows(q, shape, q.dtype, where)
+    _check(load().laud_quantize_e4m3(xp, ldx, n, c, code, block_rows, qp, ldq,
+                                     _dense(scale, (n if block_rows == 1 else _blocks(n), _blocks(c)), F32, where), _stream()), where)
 
 
 def matmul_e4m3_workspace(m: int, n: int, k: int) -> int:
@@ -501,16 +514,17 @@ def laud_matmul_e4m3(a, sa, b, sb, out, ws=None) -> None:
     """out [M][N] (float32 or bf16) = a [M][K] times b [N][K] transposed, both float8_e4m3fn with scales sa [M][ceil(K / 128)] and
     sb [ceil(N / 128)][ceil(K / 128)]."""
     where = "laud_matmul_e4m3"
-    ap, lda = _rows(a, where)
-    m, k = a.shape
-    bp, ldb = _rows(b, where, k)
-    n = b.shape[0]
-    op, ldo = _rows(out, where, n, m)
-    _need(_dtype_of(a) == E4M3 and _dtype_of(b) == E4M3, where)
+    shape_a, shape_b, dtype = a.shape, b.shape, a.dtype
+    if len(shape_a) != 2 or len(shape_b) != 2 or shape_a[1] != shape_b[1] or (_CODES or _codes()).get(dtype) != E4M3:
+        _bad(where)
+    m, k = shape_a
+    n, kb = shape_b[0], -(-k // 128)
+    ap, lda = _rows(a, shape_a, dtype, where)
+    bp, ldb = _rows(b, shape_b, dtype, where)
+    op, ldo = _rows(out, (m, n), out.dtype, where)
     wp, wb = _ws_args(ws)
-    _check(load().laud_matmul_e4m3(ap, lda, _dense(sa, (m, _blocks(k)), F32, where), bp, ldb,
-                                   _dense(sb, (_blocks(n), _blocks(k)), F32, where), m, n, k, op, ldo, _dtype_of(out), wp, wb,
-                                   _stream()), where)
+    _check(load().laud_matmul_e4m3(ap, lda, _dense(sa, (m, kb), F32, where), bp, ldb, _dense(sb, (-(-n // 128), kb), F32, where), m, n, k,
+                                   op, ldo, _CODES.get(out.dtype, -1), wp, wb, _stream()), where)
 
 
 def make_moe(router, up, down, s_up=None, s_down=None, top_k: int = 1, renormalise: bool = False, scale: float = 1.0) -> MoeLayer:
@@ -518,13 +532,15 @@ def make_moe(router, up, down, s_up=None, s_down=None, top_k: int = 1, renormali
     float8_e4m3fn weights come with s_up [E][2][ceil(F/128)][ceil(C/128)] and s_down [E][ceil(C/128)][ceil(F/128)].  The caller
     keeps the tensors alive."""
     where = "make_moe"
-    _need(router.dim() == 2 and up.dim() == 4 and up.shape[1] == 2, where)
+    if router.dim() != 2 or up.dim() != 4 or up.shape[1] != 2:
+        _bad(where)
     (e, c), f = router.shape, up.shape[2]
     wd = _dtype_of(up)
     v = [_dense(router, (e, c), _dtype_of(router), where), _dense(up, (e, 2, f, c), wd, where), _dense(down, (e, c, f), wd, where)]
     s = [None, None]
     if wd == E4M3:
-        _need(s_up is not None and s_down is not None, where)
+        if s_up is None or s_down is None:
+            _bad(where)
         s = [_dense(s_up, (e, 2, _blocks(f), _blocks(c)), F32, where), _dense(s_down, (e, _blocks(c), _blocks(f)), F32, where)]
     return MoeLayer(int(c), int(f), int(e), int(top_k), _dtype_of(router), wd, *v, *s, 1 if renormalise else 0, float(scale))
 
@@ -537,18 +553,21 @@ def laud_moe(p: MoeLayer, x, keep, out, experts, weights, ws) -> None:
     """x, out [T][C] of the router's type; keep [T] bytes or None; experts [T][top_k] int32 and weights [T][top_k] float32 receive
     the routing, each may be None."""
     where = "laud_moe"
-    xp, ldx = _rows(x, where, p.C)
-    n = x.shape[0]
-    op, ldo = _rows(out, where, p.C, n)
-    _need(_dtype_of(x) == p.dtype and _dtype_of(out) == p.dtype, where)
+    shape, dtype = x.shape, x.dtype
+    if len(shape) != 2 or shape[1] != p.C or (_CODES or _codes()).get(dtype) != p.dtype:
+        _bad(where)
+    n = shape[0]
+    xp, ldx = _rows(x, shape, dtype, where)
+    op, ldo = _rows(out, shape, dtype, where)
     ep = None
     if experts is not None:
-        _need(experts.is_cuda and tuple(experts.shape) == (n, p.top_k) and experts.element_size() == 4 and
-              not experts.is_floating_point() and experts.is_contiguous(), where)
+        if not (experts.is_cuda and experts.shape == (n, p.top_k) and experts.element_size() == 4 and
+                not experts.is_floating_point() and experts.is_contiguous()):
+            _bad(where)
         ep = experts.data_ptr()
     wp, wb = _ws_args(ws)
-    _check(load().laud_moe(C.byref(p), n, xp, ldx, _bytes(keep, n, where), op, ldo, ep, _dense(weights, (n, p.top_k), F32, where),
-                           wp, wb, _stream()), where)
+    _check(load().laud_moe(C.byref(p), n, xp, ldx, None if keep is None else _bytes(keep, n, where), op, ldo, ep,
+                           _dense(weights, (n, p.top_k), F32, where), wp, wb, _stream()), where)
 
 
 def laud_stage_timing_enable(on: bool) -> None:
