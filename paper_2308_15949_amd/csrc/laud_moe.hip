@@ -5,7 +5,6 @@ namespace laud {
 namespace {
 
 constexpr int kMaxExperts = 1024, kMaxTopK = 32;
-constexpr int kTokenBlock = 64;             // tokens the last product takes at a time
 
 struct MoeArgs {
   int T, C, F, E, top_k, renormalise;
@@ -19,7 +18,12 @@ struct MoeArgs {
   int32_t* experts;     // [T][top_k], the caller's or the workspace's
   float* weights;       // [T][top_k]
   float* h;             // [T * top_k][Fp]
+  float* y;             // [T * top_k][C]: an entry's weighted result
+  unsigned* arrived;    // [column tiles of the last product]: workgroups that are done, 0 behind the routing
 };
+
+constexpr int kColumns = 32;  // output channels of a workgroup of the last product
+__host__ __device__ inline int column_tiles(int C) { return (C - 1) / kColumns + 1; }
 
 // ---- routing ----------------------------------------------------------------------------------------------------------------
 // Floats as unsigned integers in their order; a NaN lies below all.
@@ -75,6 +79,8 @@ template <typename ET>
 __global__ __launch_bounds__(kRouteThreads) void k_moe_route(MoeArgs a) {
   __shared__ float logits[kMaxExperts];
   const int t = blockIdx.x, lane = lane_id(), wave = threadIdx.x / kWave;
+  if (t == 0)
+    for (int i = threadIdx.x; i < column_tiles(a.C); i += kRouteThreads) a.arrived[i] = 0;
   int32_t* experts = a.experts + (long long)t * a.top_k;
   float* weights = a.weights + (long long)t * a.top_k;
   if (a.keep && a.keep[t] == 0) {
@@ -82,21 +88,29 @@ __global__ __launch_bounds__(kRouteThreads) void k_moe_route(MoeArgs a) {
     return;
   }
   const ET* x = reinterpret_cast<const ET*>(a.x) + t * a.ldx;
-  for (int e = wave; e < a.E; e += kRouteThreads / kWave) {
-    const ET* w = reinterpret_cast<const ET*>(a.router) + (long long)e * a.C;
-    float s = 0.f;
+  constexpr int kAtOnce = 4;  // experts a wave takes at a time, so that their loads are under way together
+  for (int e0 = wave * kAtOnce; e0 < a.E; e0 += kRouteThreads / kWave * kAtOnce) {
+    float s[kAtOnce] = {};
+#pragma unroll 2
     for (int c = lane; c < a.C / 8; c += kWave) {
-      piece8<ET> p, q;
+      piece8<ET> p, q[kAtOnce];
       float f[8], g[8];
       p.load(x, c);
-      q.load(w, c);
-      p.get(f);
-      q.get(g);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) s = fmaf(f[i], g[i], s);
+      for (int i = 0; i < kAtOnce; ++i) q[i].load(reinterpret_cast<const ET*>(a.router) + (long long)min(e0 + i, a.E - 1) * a.C, c);
+      p.get(f);
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i) {
+        q[i].get(g);
+#pragma unroll
+        for (int u = 0; u < 8; ++u) s[i] = fmaf(f[u], g[u], s[i]);
+      }
     }
-    s = lanes64_sum(s);
-    if (lane == 0) logits[e] = s;
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i) {
+      s[i] = lanes64_sum(s[i]);
+      if (lane == 0 && e0 + i < a.E) logits[e0 + i] = s[i];
+    }
   }
   __syncthreads();
   if (wave == 0) choose_experts(logits, a.E, a.top_k, a.renormalise != 0, a.scale, experts, weights);
@@ -155,48 +169,53 @@ __device__ __forceinline__ f32x4 mma_wide(const tok_u4& w, const f32x4* v, f32x4
   return c;
 }
 
-// The n-th expert that some entry chose, in ascending order, or -1; called by a whole workgroup.  flags: kMaxExperts bytes.
-__device__ __forceinline__ int nth_expert(const int32_t* experts, int entries, int E, int n, uint8_t* flags) {
-  for (int e = threadIdx.x; e < kMaxExperts; e += blockDim.x) flags[e] = 0;
+// The products run for (tile of channels, slot): a slot is an expert, or, where the entries (token, choice) are fewer than the
+// experts, an entry, whose workgroups take its expert if no earlier entry has the same.  Returns the expert and in `list` its
+// entries (in any order: no entry's value depends on it), or no entries.  Called by a whole workgroup.
+constexpr int kSplit = 8;  // waves of a workgroup, which share the reduction by blocks of 128
+__device__ __forceinline__ int slot_entries(const int32_t* experts, int entries, int E, int slot, int* list, int* counts, int& len) {
+  const bool by_entry = entries < E;
+  if (threadIdx.x < 2) counts[threadIdx.x] = 0;
+  const int e = by_entry ? experts[slot] : slot;
   __syncthreads();
-  for (int i = threadIdx.x; i < entries; i += blockDim.x) {
-    const int e = experts[i];
-    if (e >= 0) flags[e] = 1;
-  }
-  __syncthreads();
-  int before = 0;
-  for (int e0 = 0; e0 < E; e0 += kWave) {
-    const unsigned long long b = __ballot(flags[e0 + lane_id()] != 0);
-    const int c = __popcll(b);
-    if (n < before + c) {
-      const unsigned long long hit = __ballot((b >> lane_id() & 1ull) && ballot_prefix(b) == n - before);
-      return e0 + __ffsll((long long)hit) - 1;
+  if (e >= 0) {
+    for (int i = threadIdx.x; i < entries; i += kSplit * kWave) {
+      if (experts[i] != e) continue;
+      if (by_entry && i < slot) counts[1] = 1;
+      list[atomicAdd(&counts[0], 1)] = i;
     }
-    before += c;
   }
-  return -1;
+  __syncthreads();
+  len = counts[1] ? 0 : counts[0];
+  return e;
 }
 
-// h of one expert's entries for 16 hidden channels: workgroup (expert, channel tile), reduction split over the waves by blocks
-// of 128.
-constexpr int kSplit = 8;
+// Sums of the waves' parts of two row tiles, in the waves' order, for the first wave.
+__device__ __forceinline__ void join_waves(f32x4 (&v)[2], f32x4 (*part)[2][kWave], int wave, int lane) {
+  part[wave][0][lane] = v[0];
+  part[wave][1][lane] = v[1];
+  __syncthreads();
+  if (wave == 0) {
+#pragma unroll
+    for (int w = 1; w < kSplit; ++w) {
+      v[0] += part[w][0][lane];
+      v[1] += part[w][1][lane];
+    }
+  }
+  __syncthreads();
+}
+
+// h of one expert's entries for 16 hidden channels.
 template <int W>
 __global__ __launch_bounds__(kSplit * kWave) void k_moe_up(MoeArgs a) {
   typedef Weights<W> WT;
   constexpr int kXP = W == W_E4M3 ? 2 : 1;
-  __shared__ uint8_t flags[kMaxExperts];
-  __shared__ int list[LAUD_MOE_MAX_TOKENS];
-  __shared__ int list_len;
+  __shared__ int list[LAUD_MOE_MAX_TOKENS], counts[2];
   __shared__ f32x4 part[kSplit][2][kWave];
   const int lane = lane_id(), wave = threadIdx.x / kWave, r16 = lane % 16, quarter = lane / 16;
-  const int entries = a.T * a.top_k;
-  if (threadIdx.x == 0) list_len = 0;
-  const int e = nth_expert(a.experts, entries, a.E, blockIdx.y, flags);
-  if (e < 0) return;
-  for (int i = threadIdx.x; i < entries; i += kSplit * kWave)
-    if (a.experts[i] == e) list[atomicAdd(&list_len, 1)] = i;  // (their order changes no entry's value)
-  __syncthreads();
-  const int len = list_len;
+  int len;
+  const int e = slot_entries(a.experts, a.T * a.top_k, a.E, blockIdx.y, list, counts, len);
+  if (len == 0) return;
   const int f0 = blockIdx.x * 16, rows = min(16, a.F - f0);  // (from F to the end of its block of 128 h is 0: rows may be none)
   const int kb_all = scale_blocks(a.C);
   const long long row_bytes = (long long)a.C * WT::kBytes;
@@ -214,7 +233,7 @@ __global__ __launch_bounds__(kSplit * kWave) void k_moe_up(MoeArgs a) {
   for (int l0 = 0; l0 < len; l0 += 16) {
     const int entry = list[min(l0 + r16, len - 1)];
     const unsigned xoff = (unsigned)(entry / a.top_k * a.ldx * xb);
-    f32x4 g = {0.f, 0.f, 0.f, 0.f}, u = g;
+    f32x4 v[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
     for (int kb = wave; kb < kb_all; kb += kSplit) {
       f32x4 pg = {0.f, 0.f, 0.f, 0.f}, pu = pg;
 #pragma unroll
@@ -232,114 +251,120 @@ __global__ __launch_bounds__(kSplit * kWave) void k_moe_up(MoeArgs a) {
       const float fg = sg ? sg[kb] : 1.f, fu = su ? su[kb] : 1.f;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        g[i] = fmaf(pg[i], fg, g[i]);
-        u[i] = fmaf(pu[i], fu, u[i]);
+        v[0][i] = fmaf(pg[i], fg, v[0][i]);
+        v[1][i] = fmaf(pu[i], fu, v[1][i]);
       }
     }
-    part[wave][0][lane] = g;
-    part[wave][1][lane] = u;
-    __syncthreads();
+    join_waves(v, part, wave, lane);
     if (wave == 0 && l0 + r16 < len) {
-#pragma unroll
-      for (int w = 1; w < kSplit; ++w) {
-        g += part[w][0][lane];
-        u += part[w][1][lane];
-      }
       f32x4 h;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) h[i] = quarter * 4 < rows ? g[i] / (1.f + expf(-g[i])) * u[i] : 0.f;
+      for (int i = 0; i < 4; ++i) h[i] = quarter * 4 < rows ? v[0][i] / (1.f + expf(-v[0][i])) * v[1][i] : 0.f;
       *reinterpret_cast<f32x4*>(a.h + (long long)entry * a.Fp + f0 + quarter * 4) = h;
     }
-    __syncthreads();
   }
 }
 
-// Sixteen output channels of up to 64 tokens: the waves take the block's experts in turn and add into sums of their own, which
-// are added in the waves' order.
+// Values that workgroups on different XCDs hand over within a launch go past the XCDs' caches, which do not see each other (a
+// release and an acquire by every workgroup instead, which write back and drop a whole cache, made the launch three times as long).
+__device__ __forceinline__ void shared_store(float* p, float v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+__device__ __forceinline__ float shared_load(const float* p) {
+  return __hip_atomic_load(const_cast<float*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+// One expert's entries for 32 output channels, weighted; the last workgroup of a tile of channels to get here adds each token's
+// entries up, in the order of its experts.
 template <int W, typename OT>
 __global__ __launch_bounds__(kSplit * kWave) void k_moe_down(MoeArgs a) {
   typedef Weights<W> WT;
-  __shared__ uint8_t flags[kMaxExperts];
-  __shared__ f32x4 sums[kSplit][kTokenBlock][4];
-  __shared__ short list[kSplit][kTokenBlock];
+  __shared__ int list[LAUD_MOE_MAX_TOKENS], counts[2];
+  __shared__ f32x4 part[kSplit][2][kWave];
+  __shared__ unsigned place;
   const int lane = lane_id(), wave = threadIdx.x / kWave, r16 = lane % 16, quarter = lane / 16;
-  const int t0 = blockIdx.y * kTokenBlock, nt = min(kTokenBlock, a.T - t0), entries = nt * a.top_k;
-  const int32_t* experts = a.experts + (long long)t0 * a.top_k;
-  const int c0 = blockIdx.x * 16, rows = min(16, a.C - c0);
-  for (int e = threadIdx.x; e < kMaxExperts; e += kSplit * kWave) flags[e] = 0;
-  for (int i = threadIdx.x; i < kSplit * kTokenBlock * 4; i += kSplit * kWave) (&sums[0][0][0])[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-  __syncthreads();
-  for (int i = threadIdx.x; i < entries; i += kSplit * kWave) {
-    const int e = experts[i];
-    if (e >= 0) flags[e] = 1;
-  }
-  __syncthreads();
-  const int kb_all = scale_blocks(a.F);
-  const long long row_bytes = (long long)a.F * WT::kBytes;
-  int turn = 0;
-  for (int e = 0; e < a.E; ++e) {
-    if (!flags[e]) continue;
-    if (turn++ % kSplit != wave) continue;
-    int len = 0;
-    for (int i0 = 0; i0 < entries; i0 += kWave) {  // a token holds an expert once: at most 64
-      const bool hit = i0 + lane < entries && experts[i0 + lane] == e;
-      const unsigned long long b = __ballot(hit);
-      if (hit) list[wave][len + ballot_prefix(b)] = (short)(i0 + lane);
-      len += __popcll(b);
-    }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  int len;
+  const int e = slot_entries(a.experts, a.T * a.top_k, a.E, blockIdx.y, list, counts, len);
+  const int c0 = blockIdx.x * kColumns, rows = min(kColumns, a.C - c0);
+  if (len > 0) {
+    const int kb_all = scale_blocks(a.F);
+    const long long row_bytes = (long long)a.F * WT::kBytes;
     const __amdgpu_buffer_rsrc_t rw =
         bytes_of(reinterpret_cast<const uint8_t*>(a.down) + ((long long)e * a.C + c0) * row_bytes, rows * row_bytes);
     const float* sw = W == W_E4M3 ? a.s_down + ((long long)e * scale_blocks(a.C) + c0 / kScaleBlock) * kb_all : nullptr;
     for (int l0 = 0; l0 < len; l0 += 16) {
-      const int entry = list[wave][min(l0 + r16, len - 1)];
-      const long long at = (long long)t0 * a.top_k + entry;
-      const float* h = a.h + at * a.Fp;
-      f32x4 y = {0.f, 0.f, 0.f, 0.f};
-      for (int kb = 0; kb < kb_all; ++kb) {
-        f32x4 py = {0.f, 0.f, 0.f, 0.f};
+      const int entry = list[min(l0 + r16, len - 1)];
+      const float* h = a.h + (long long)entry * a.Fp;
+      f32x4 v[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+      for (int kb = wave; kb < kb_all; kb += kSplit) {
+        f32x4 p0 = {0.f, 0.f, 0.f, 0.f}, p1 = p0;
 #pragma unroll
         for (int p = 0; p < WT::kPieces; ++p) {
           const int k = kb * kScaleBlock + WT::first(p, quarter);
-          const tok_u4 w = load16(rw, k < a.F && r16 < rows ? (unsigned)(r16 * row_bytes) + (unsigned)k * WT::kBytes : kOutside);
-          f32x4 v[WT::kElems / 4];
+          const unsigned off = (unsigned)(r16 * row_bytes) + (unsigned)k * WT::kBytes;
+          const tok_u4 w0 = load16(rw, k < a.F && r16 < rows ? off : kOutside);
+          const tok_u4 w1 = load16(rw, k < a.F && 16 + r16 < rows ? off + (unsigned)(16 * row_bytes) : kOutside);
+          f32x4 x[WT::kElems / 4];
 #pragma unroll
-          for (int i = 0; i < WT::kElems / 4; ++i) v[i] = *reinterpret_cast<const f32x4*>(h + k + 4 * i);
-          py = mma_wide<W>(w, v, py);
+          for (int i = 0; i < WT::kElems / 4; ++i) x[i] = *reinterpret_cast<const f32x4*>(h + k + 4 * i);
+          p0 = mma_wide<W>(w0, x, p0);
+          p1 = mma_wide<W>(w1, x, p1);
         }
         const float f = sw ? sw[kb] : 1.f;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) y[i] = fmaf(py[i], f, y[i]);
+        for (int i = 0; i < 4; ++i) {
+          v[0][i] = fmaf(p0[i], f, v[0][i]);
+          v[1][i] = fmaf(p1[i], f, v[1][i]);
+        }
       }
-      if (l0 + r16 < len) sums[wave][entry / a.top_k][quarter] += y * a.weights[at];
+      join_waves(v, part, wave, lane);
+      if (wave == 0 && l0 + r16 < len) {
+        const float w = a.weights[entry];
+        float* y = a.y + (long long)entry * a.C + c0;
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+          if (i * 16 + quarter * 4 < rows)
+#pragma unroll
+            for (int n = 0; n < 4; ++n) shared_store(y + i * 16 + quarter * 4 + n, v[i][n] * w);
+      }
     }
   }
+  vm_wait<0>();  // (the stores have arrived before the workgroup counts as done)
   __syncthreads();
-  for (int i = threadIdx.x; i < nt * 4; i += kSplit * kWave) {
-    const int t = i / 4, n = c0 + i % 4 * 4;
-    if (n >= a.C) continue;
-    f32x4 v = sums[0][t][i % 4];
+  if (threadIdx.x == 0)
+    place = __hip_atomic_fetch_add(a.arrived + blockIdx.x, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  __syncthreads();
+  if (place + 1 != gridDim.y) return;
+  for (int i = threadIdx.x; i < a.T * (kColumns / 4); i += kSplit * kWave) {
+    const int t = i / (kColumns / 4), c = i % (kColumns / 4) * 4;
+    if (c >= rows) continue;
+    f32x4 s = {0.f, 0.f, 0.f, 0.f};
+    if (!a.keep || a.keep[t] != 0) {
+      const float* y = a.y + (long long)t * a.top_k * a.C + c0 + c;
+      for (int j = 0; j < a.top_k; ++j)
 #pragma unroll
-    for (int w = 1; w < kSplit; ++w) v += sums[w][t][i % 4];
-    store4(reinterpret_cast<OT*>(a.out) + (t0 + t) * a.ldo + n, v);
+        for (int n = 0; n < 4; ++n) s[n] += shared_load(y + (long long)j * a.C + n);
+    }
+    store4(reinterpret_cast<OT*>(a.out) + t * a.ldo + c0 + c, s);
   }
 }
 
 template <int W, typename ET>
 void launch_moe(const MoeArgs& a, hipStream_t st) {
   hipLaunchKernelGGL((k_moe_route<ET>), dim3(a.T), dim3(kRouteThreads), 0, st, a);
-  hipLaunchKernelGGL((k_moe_up<W>), dim3(a.Fp / 16, min((long long)a.E, (long long)a.T * a.top_k)), dim3(kSplit * kWave), 0, st, a);
-  hipLaunchKernelGGL((k_moe_down<W, ET>), dim3((a.C - 1) / 16 + 1, (a.T - 1) / kTokenBlock + 1), dim3(kSplit * kWave), 0, st, a);
+  const unsigned slots = (unsigned)min((long long)a.E, (long long)a.T * a.top_k);
+  hipLaunchKernelGGL((k_moe_up<W>), dim3(a.Fp / 16, slots), dim3(kSplit * kWave), 0, st, a);
+  hipLaunchKernelGGL((k_moe_down<W, ET>), dim3(column_tiles(a.C), slots), dim3(kSplit * kWave), 0, st, a);
 }
 
-struct MoeWs { size_t experts, weights, h, bytes; };
+struct MoeWs { size_t experts, weights, h, y, arrived, bytes; };
 MoeWs moe_ws(const laud_moe_layer* p, int T) {
   MoeWs w;
   const size_t n = (size_t)T * p->top_k;
   w.experts = 0;
   w.weights = align_up(n * 4, 256);
   w.h = w.weights + align_up(n * 4, 256);
-  w.bytes = w.h + n * (size_t)scale_blocks(p->F) * kScaleBlock * 4;
+  w.y = align_up(w.h + n * (size_t)scale_blocks(p->F) * kScaleBlock * 4, 256);
+  w.arrived = align_up(w.y + n * (size_t)p->C * 4, 256);
+  w.bytes = w.arrived + (size_t)column_tiles(p->C) * 4;
   return w;
 }
 
@@ -386,6 +411,8 @@ extern "C" int laud_moe(const laud_moe_layer* p, int T, const void* x, int64_t l
   a.experts = experts ? experts : (int32_t*)((char*)ws + w.experts);
   a.weights = weights ? weights : (float*)((char*)ws + w.weights);
   a.h = (float*)((char*)ws + w.h);
+  a.y = (float*)((char*)ws + w.y);
+  a.arrived = (unsigned*)((char*)ws + w.arrived);
   clear_stale_error();
   hipStream_t st = (hipStream_t)stream;
   if (p->w_dtype == LAUD_E4M3) launch_moe<W_E4M3, bf16_t>(a, st);
