@@ -17,7 +17,7 @@ struct MoeArgs {
   int64_t ldx, ldo;
   int32_t* experts;     // [T][top_k], the caller's or the workspace's
   float* weights;       // [T][top_k]
-  float* h;             // [T * top_k][Fp]
+  void* h;              // [T * top_k][Fp] float32, or two planes of it in bf16
   float* y;             // [T * top_k][C]: an entry's weighted result
   unsigned* arrived;    // [column tiles of the last product]: workgroups that are done, 0 behind the routing
 };
@@ -32,37 +32,42 @@ __device__ __forceinline__ unsigned order_key(float f) {
   return f != f ? 0u : (u & 0x80000000u) ? ~u : u | 0x80000000u;
 }
 
-// The choice of one token by one wave from logits [E] in LDS.
-__device__ __forceinline__ void choose_experts(const float* logits, int E, int top_k, bool renormalise, float scale, int32_t* experts,
-                                               float* weights) {
+constexpr int kRouteThreads = 1024;
+
+// The choice of one token by its workgroup from logits [E] in LDS: an expert is chosen if fewer than top_k come before it, and
+// sixteen lanes count those of one expert.
+__device__ __forceinline__ void choose_experts(const float* logits, uint8_t* chosen, int E, int top_k, bool renormalise, float scale,
+                                               int32_t* experts, float* weights) {
   const int lane = lane_id();
-  unsigned chosen = 0;  // bit j: expert 64 j + lane
+  for (int e0 = 0; e0 < E; e0 += kRouteThreads / 16) {
+    const int e = e0 + (int)threadIdx.x / 16;
+    if (e >= E) continue;  // (sixteen lanes at a time)
+    const unsigned key = order_key(logits[e]);
+    int before = 0;
+    for (int j = (int)threadIdx.x % 16; j < E; j += 16) {
+      const unsigned k = order_key(logits[j]);
+      before += k > key || (k == key && j < e);
+    }
+    const float n = lanes16_sum((float)before);
+    if (threadIdx.x % 16 == 0) chosen[e] = n < (float)top_k;
+  }
+  __syncthreads();
+  if ((int)threadIdx.x >= kWave) return;
   float top = -INFINITY;
   for (int e = lane; e < E; e += kWave) top = fmaxf(top, logits[e]);
   {
     const unsigned k = lanes64_max(order_key(top));
     top = __uint_as_float((k & 0x80000000u) ? k & 0x7fffffffu : ~k);
   }
-  for (int n = 0; n < top_k; ++n) {
-    unsigned key = 0, id = 0;  // id: bits of 2^31 - 1 - expert, so that the lower expert is the larger one
-    for (int e = lane, j = 0; e < E; e += kWave, ++j) {
-      if (chosen >> j & 1u) continue;
-      const unsigned k = order_key(logits[e]);
-      if (k > key || id == 0) { key = k; id = 0x7fffffffu - (unsigned)e; }
-    }
-    const unsigned best = lanes64_max(key);
-    const unsigned e = 0x7fffffffu - lanes64_max(key == best ? id : 0u);
-    if ((e & 63u) == (unsigned)lane) chosen |= 1u << (e >> 6);
-  }
   float sum = 0.f;
-  for (int e = lane, j = 0; e < E; e += kWave, ++j) {
+  for (int e = lane; e < E; e += kWave) {
     const float p = expf(logits[e] - top);
-    if (!renormalise || (chosen >> j & 1u) || p != p) sum += p;  // (a NaN anywhere is in every softmax value)
+    if (!renormalise || chosen[e] || p != p) sum += p;  // (a NaN anywhere is in every softmax value)
   }
   sum = lanes64_sum(sum);
   int before = 0;
-  for (int e0 = 0, j = 0; e0 < E; e0 += kWave, ++j) {
-    const bool mine = chosen >> j & 1u;
+  for (int e0 = 0; e0 < E; e0 += kWave) {
+    const bool mine = e0 + lane < E && chosen[e0 + lane];
     const unsigned long long b = __ballot(mine);
     if (mine) {
       const int at = before + ballot_prefix(b);
@@ -73,11 +78,11 @@ __device__ __forceinline__ void choose_experts(const float* logits, int E, int t
   }
 }
 
-// One workgroup a token: the waves take the experts' logits in turn, the first one chooses.
-constexpr int kRouteThreads = 1024;
+// One workgroup a token.
 template <typename ET>
 __global__ __launch_bounds__(kRouteThreads) void k_moe_route(MoeArgs a) {
   __shared__ float logits[kMaxExperts];
+  __shared__ uint8_t chosen[kMaxExperts];
   const int t = blockIdx.x, lane = lane_id(), wave = threadIdx.x / kWave;
   if (t == 0)
     for (int i = threadIdx.x; i < column_tiles(a.C); i += kRouteThreads) a.arrived[i] = 0;
@@ -91,7 +96,7 @@ __global__ __launch_bounds__(kRouteThreads) void k_moe_route(MoeArgs a) {
   constexpr int kAtOnce = 4;  // experts a wave takes at a time, so that their loads are under way together
   for (int e0 = wave * kAtOnce; e0 < a.E; e0 += kRouteThreads / kWave * kAtOnce) {
     float s[kAtOnce] = {};
-#pragma unroll 2
+#pragma unroll 4
     for (int c = lane; c < a.C / 8; c += kWave) {
       piece8<ET> p, q[kAtOnce];
       float f[8], g[8];
@@ -113,7 +118,7 @@ __global__ __launch_bounds__(kRouteThreads) void k_moe_route(MoeArgs a) {
     }
   }
   __syncthreads();
-  if (wave == 0) choose_experts(logits, a.E, a.top_k, a.renormalise != 0, a.scale, experts, weights);
+  choose_experts(logits, chosen, a.E, a.top_k, a.renormalise != 0, a.scale, experts, weights);
 }
 
 // ---- products -----------------------------------------------------------------------------------------------------------------
@@ -143,61 +148,52 @@ __device__ __forceinline__ f32x4 mma_stored(const tok_u4& w, const tok_u4 (&x)[W
     return mma_bf16_16(widen8(w[2], w[3]), __builtin_bit_cast(bf16x8, x[1]), c);
   }
 }
-// ... or float32 values, which go through bf16 instructions as a sum of two: the part bf16 holds and its remainder, 16 bits
-// together (a hidden value rounded to bf16 alone would add an error as large as the result's own rounding).
-template <int W>
-__device__ __forceinline__ f32x4 mma_wide(const tok_u4& w, const f32x4* v, f32x4 c) {
-  if constexpr (W == W_F32) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(w[i]), v[0][i], c, 0, 0, 0);
-  } else {
-#pragma unroll
-    for (int u = 0; u < (W == W_E4M3 ? 2 : 1); ++u) {
-      union { bf16x2 p[4]; bf16x8 v; } hi, lo;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const f32x2 f = {v[2 * u + i / 2][i % 2 * 2], v[2 * u + i / 2][i % 2 * 2 + 1]};
-        hi.p[i] = __builtin_convertvector(f, bf16x2);
-        const f32x2 rest = {f[0] - (float)hi.p[i][0], f[1] - (float)hi.p[i][1]};
-        lo.p[i] = __builtin_convertvector(rest, bf16x2);
-      }
-      const bf16x8 a = W == W_E4M3 ? widen8(w[2 * u], w[2 * u + 1]) : __builtin_bit_cast(bf16x8, w);
-      c = mma_bf16_16(a, hi.v, c);
-      c = mma_bf16_16(a, lo.v, c);
-    }
-  }
-  return c;
-}
+// Hidden values are float32.  Through bf16 instructions they go as a sum of two, the part bf16 holds and its remainder, 16 bits
+// together (rounded to bf16 alone they would add an error as large as the result's own rounding): the first product leaves them in
+// two planes [entries][Fp], bf16 each, or, for float32 weights, in one of float32.
+template <int W> constexpr int kHiddenPlanes = W == W_F32 ? 1 : 2;
 
 // The products run for (tile of channels, slot): a slot is an expert, or, where the entries (token, choice) are fewer than the
-// experts, an entry, whose workgroups take its expert if no earlier entry has the same.  Returns the expert and in `list` its
-// entries (in any order: no entry's value depends on it), or no entries.  Called by a whole workgroup.
-constexpr int kSplit = 8;  // waves of a workgroup, which share the reduction by blocks of 128
-__device__ __forceinline__ int slot_entries(const int32_t* experts, int entries, int E, int slot, int* list, int* counts, int& len) {
-  const bool by_entry = entries < E;
+// experts, an entry, whose workgroups take its expert if no earlier entry has the same.
+struct Slot {
+  int expert, entries;
+  bool by_entry, early;
+};
+// early: the expert is all but sure to have entries (at least four a slot on average), so that its weights are requested before
+// its entries are looked for.
+__device__ __forceinline__ Slot slot_of(const MoeArgs& a) {
+  Slot s;
+  s.entries = a.T * a.top_k;
+  s.by_entry = s.entries < a.E;
+  s.expert = s.by_entry ? a.experts[blockIdx.y] : (int)blockIdx.y;
+  s.early = s.expert >= 0 && (s.by_entry || s.entries >= 4 * a.E);
+  return s;
+}
+// The slot's entries in `list` (in any order: no entry's value depends on it) and their number, 0 if it has none or an earlier slot
+// has its expert.  Called by a whole workgroup.
+__device__ __forceinline__ int find_entries(const MoeArgs& a, const Slot& s, int* list, int* counts) {
   if (threadIdx.x < 2) counts[threadIdx.x] = 0;
-  const int e = by_entry ? experts[slot] : slot;
   __syncthreads();
-  if (e >= 0) {
-    for (int i = threadIdx.x; i < entries; i += kSplit * kWave) {
-      if (experts[i] != e) continue;
-      if (by_entry && i < slot) counts[1] = 1;
+  if (s.expert >= 0) {
+    for (int i = threadIdx.x; i < s.entries; i += blockDim.x) {
+      if (a.experts[i] != s.expert) continue;
+      if (s.by_entry && i < (int)blockIdx.y) counts[1] = 1;
       list[atomicAdd(&counts[0], 1)] = i;
     }
   }
   __syncthreads();
-  len = counts[1] ? 0 : counts[0];
-  return e;
+  return counts[1] ? 0 : counts[0];
 }
 
-// Sums of the waves' parts of two row tiles, in the waves' order, for the first wave.
+// Sums of the S waves' parts of two row tiles, in the waves' order, for the first wave.
+template <int S>
 __device__ __forceinline__ void join_waves(f32x4 (&v)[2], f32x4 (*part)[2][kWave], int wave, int lane) {
   part[wave][0][lane] = v[0];
   part[wave][1][lane] = v[1];
   __syncthreads();
   if (wave == 0) {
 #pragma unroll
-    for (int w = 1; w < kSplit; ++w) {
+    for (int w = 1; w < S; ++w) {
       v[0] += part[w][0][lane];
       v[1] += part[w][1][lane];
     }
@@ -205,69 +201,94 @@ __device__ __forceinline__ void join_waves(f32x4 (&v)[2], f32x4 (*part)[2][kWave
   __syncthreads();
 }
 
+// Waves of a workgroup, which share the reduction by blocks of 128: half as many where a block is half the bytes (16 tokens, 64
+// experts of 2048 x 1424 in 8 bits, four / eight waves: 116 / 129 us; of 2048 x 1024 in bf16 on 64 tokens 220 / 208).
+template <int W> constexpr int kSplit = W == W_E4M3 ? 4 : 8;
+// Whether a wave requests its first weights ahead of the search for the slot's entries: in 8 bits 116 -> 108 us; the larger blocks of
+// the other types need the registers that this takes for a third workgroup on a compute unit (208 -> 219).
+template <int W> constexpr bool kEarly = W == W_E4M3;
+
 // h of one expert's entries for 16 hidden channels.
 template <int W>
-__global__ __launch_bounds__(kSplit * kWave) void k_moe_up(MoeArgs a) {
+__global__ __launch_bounds__(kSplit<W> * kWave) void k_moe_up(MoeArgs a) {
   typedef Weights<W> WT;
-  constexpr int kXP = W == W_E4M3 ? 2 : 1;
+  constexpr int S = kSplit<W>, kXP = W == W_E4M3 ? 2 : 1, xb = W == W_F32 ? 4 : 2;
   __shared__ int list[LAUD_MOE_MAX_TOKENS], counts[2];
-  __shared__ f32x4 part[kSplit][2][kWave];
-  const int lane = lane_id(), wave = threadIdx.x / kWave, r16 = lane % 16, quarter = lane / 16;
-  int len;
-  const int e = slot_entries(a.experts, a.T * a.top_k, a.E, blockIdx.y, list, counts, len);
-  if (len == 0) return;
+  __shared__ f32x4 part[S][2][kWave];
+  const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), r16 = lane % 16, quarter = lane / 16;
+  const Slot slot = slot_of(a);
   const int f0 = blockIdx.x * 16, rows = min(16, a.F - f0);  // (from F to the end of its block of 128 h is 0: rows may be none)
   const int kb_all = scale_blocks(a.C);
   const long long row_bytes = (long long)a.C * WT::kBytes;
-  const uint8_t* base = reinterpret_cast<const uint8_t*>(a.up) + ((long long)e * 2 * a.F + f0) * row_bytes;
+  const uint8_t* base = reinterpret_cast<const uint8_t*>(a.up) + ((long long)max(slot.expert, 0) * 2 * a.F + f0) * row_bytes;
   const __amdgpu_buffer_rsrc_t rg = bytes_of(base, max(rows, 0) * row_bytes);
   const __amdgpu_buffer_rsrc_t ru = bytes_of(base + a.F * row_bytes, max(rows, 0) * row_bytes);
-  const int xb = W == W_F32 ? 4 : 2;
+  tok_u4 wg[WT::kPieces], wu[WT::kPieces];
+  auto request = [&](int kb) {
+#pragma unroll
+    for (int p = 0; p < WT::kPieces; ++p) {
+      const int k = kb * kScaleBlock + WT::first(p, quarter);
+      const unsigned off = k < a.C && r16 < rows ? (unsigned)(r16 * row_bytes) + (unsigned)k * WT::kBytes : kOutside;
+      wg[p] = load16(rg, off);
+      wu[p] = load16(ru, off);
+    }
+  };
+  if (kEarly<W> && slot.early) request(wave);
+  const int len = find_entries(a, slot, list, counts);
+  if (len == 0) return;
+  if (kEarly<W> && !slot.early) request(wave);
   const __amdgpu_buffer_rsrc_t rx = bytes_of(a.x, ((a.T - 1) * a.ldx + a.C) * xb);
-  const float *sg = nullptr, *su = nullptr;
-  if (W == W_E4M3 && rows > 0) {
-    const int fb = scale_blocks(a.F);
-    sg = a.s_up + ((long long)e * 2 * fb + f0 / kScaleBlock) * kb_all;
-    su = sg + (long long)fb * kb_all;
-  }
+  const int fb = scale_blocks(a.F);
+  const float* s = W == W_E4M3 && rows > 0 ? a.s_up + ((long long)slot.expert * 2 * fb + f0 / kScaleBlock) * kb_all : nullptr;
   for (int l0 = 0; l0 < len; l0 += 16) {
     const int entry = list[min(l0 + r16, len - 1)];
+    const bool real = l0 + r16 < len;  // (of the other rows nothing is fetched)
     const unsigned xoff = (unsigned)(entry / a.top_k * a.ldx * xb);
     f32x4 v[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
-    for (int kb = wave; kb < kb_all; kb += kSplit) {
+    for (int kb = wave; kb < kb_all; kb += S) {
+      if (!kEarly<W> || kb != wave || l0 != 0) request(kb);
+      const float fg = s ? s[kb] : 1.f, fu = s ? s[fb * kb_all + kb] : 1.f;
       f32x4 pg = {0.f, 0.f, 0.f, 0.f}, pu = pg;
 #pragma unroll
       for (int p = 0; p < WT::kPieces; ++p) {
         const int k = kb * kScaleBlock + WT::first(p, quarter);
-        const bool in = k < a.C;
-        const unsigned woff = in && r16 < rows ? (unsigned)(r16 * row_bytes) + (unsigned)k * WT::kBytes : kOutside;
-        const tok_u4 wg = load16(rg, woff), wu = load16(ru, woff);
         tok_u4 x[kXP];
 #pragma unroll
-        for (int i = 0; i < kXP; ++i) x[i] = load16(rx, in ? xoff + (unsigned)(k + 8 * i) * xb : kOutside);
-        pg = mma_stored<W>(wg, x, pg);
-        pu = mma_stored<W>(wu, x, pu);
+        for (int i = 0; i < kXP; ++i) x[i] = load16(rx, k < a.C && real ? xoff + (unsigned)(k + 8 * i) * xb : kOutside);
+        pg = mma_stored<W>(wg[p], x, pg);
+        pu = mma_stored<W>(wu[p], x, pu);
       }
-      const float fg = sg ? sg[kb] : 1.f, fu = su ? su[kb] : 1.f;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         v[0][i] = fmaf(pg[i], fg, v[0][i]);
         v[1][i] = fmaf(pu[i], fu, v[1][i]);
       }
     }
-    join_waves(v, part, wave, lane);
-    if (wave == 0 && l0 + r16 < len) {
+    join_waves<S>(v, part, wave, lane);
+    if (wave == 0 && real) {
       f32x4 h;
 #pragma unroll
       for (int i = 0; i < 4; ++i) h[i] = quarter * 4 < rows ? v[0][i] / (1.f + expf(-v[0][i])) * v[1][i] : 0.f;
-      *reinterpret_cast<f32x4*>(a.h + (long long)entry * a.Fp + f0 + quarter * 4) = h;
+      const long long at = (long long)entry * a.Fp + f0 + quarter * 4;
+      if constexpr (kHiddenPlanes<W> == 1) {
+        *reinterpret_cast<f32x4*>(reinterpret_cast<float*>(a.h) + at) = h;
+      } else {
+        typedef __attribute__((ext_vector_type(4))) __bf16 b4;
+        const b4 hi = __builtin_convertvector(h, b4);
+        const b4 lo = __builtin_convertvector(h - __builtin_convertvector(hi, f32x4), b4);
+        bf16_t* plane = reinterpret_cast<bf16_t*>(a.h) + at;
+        *reinterpret_cast<tok_u2*>(plane) = __builtin_bit_cast(tok_u2, hi);
+        *reinterpret_cast<tok_u2*>(plane + (long long)a.T * a.top_k * a.Fp) = __builtin_bit_cast(tok_u2, lo);
+      }
     }
   }
 }
 
 // Values that workgroups on different XCDs hand over within a launch go past the XCDs' caches, which do not see each other (a
 // release and an acquire by every workgroup instead, which write back and drop a whole cache, made the launch three times as long).
-__device__ __forceinline__ void shared_store(float* p, float v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+__device__ __forceinline__ void shared_store(float* p, const f32x4& v) {
+  asm volatile("global_store_dwordx4 %0, %1, off sc1" ::"v"(p), "v"(v) : "memory");
+}
 __device__ __forceinline__ float shared_load(const float* p) {
   return __hip_atomic_load(const_cast<float*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
@@ -275,75 +296,92 @@ __device__ __forceinline__ float shared_load(const float* p) {
 // One expert's entries for 32 output channels, weighted; the last workgroup of a tile of channels to get here adds each token's
 // entries up, in the order of its experts.
 template <int W, typename OT>
-__global__ __launch_bounds__(kSplit * kWave) void k_moe_down(MoeArgs a) {
+__global__ __launch_bounds__(kSplit<W> * kWave) void k_moe_down(MoeArgs a) {
   typedef Weights<W> WT;
+  constexpr int S = kSplit<W>;
+  constexpr unsigned kHb = W == W_F32 ? 4 : 2;  // bytes of a hidden value in a plane
   __shared__ int list[LAUD_MOE_MAX_TOKENS], counts[2];
-  __shared__ f32x4 part[kSplit][2][kWave];
+  __shared__ f32x4 part[S][2][kWave];
   __shared__ unsigned place;
-  const int lane = lane_id(), wave = threadIdx.x / kWave, r16 = lane % 16, quarter = lane / 16;
-  int len;
-  const int e = slot_entries(a.experts, a.T * a.top_k, a.E, blockIdx.y, list, counts, len);
+  const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), r16 = lane % 16, quarter = lane / 16;
+  const Slot slot = slot_of(a);
   const int c0 = blockIdx.x * kColumns, rows = min(kColumns, a.C - c0);
+  const int kb_all = scale_blocks(a.F);
+  const long long row_bytes = (long long)a.F * WT::kBytes;
+  const __amdgpu_buffer_rsrc_t rw =
+      bytes_of(reinterpret_cast<const uint8_t*>(a.down) + ((long long)max(slot.expert, 0) * a.C + c0) * row_bytes, rows * row_bytes);
+  tok_u4 w0[WT::kPieces], w1[WT::kPieces];
+  auto request = [&](int kb) {
+#pragma unroll
+    for (int p = 0; p < WT::kPieces; ++p) {
+      const int k = kb * kScaleBlock + WT::first(p, quarter);
+      const unsigned off = (unsigned)(r16 * row_bytes) + (unsigned)k * WT::kBytes;
+      w0[p] = load16(rw, k < a.F && r16 < rows ? off : kOutside);
+      w1[p] = load16(rw, k < a.F && 16 + r16 < rows ? off + (unsigned)(16 * row_bytes) : kOutside);
+    }
+  };
+  if (kEarly<W> && slot.early) request(wave);
+  const int len = find_entries(a, slot, list, counts);
   if (len > 0) {
-    const int kb_all = scale_blocks(a.F);
-    const long long row_bytes = (long long)a.F * WT::kBytes;
-    const __amdgpu_buffer_rsrc_t rw =
-        bytes_of(reinterpret_cast<const uint8_t*>(a.down) + ((long long)e * a.C + c0) * row_bytes, rows * row_bytes);
-    const float* sw = W == W_E4M3 ? a.s_down + ((long long)e * scale_blocks(a.C) + c0 / kScaleBlock) * kb_all : nullptr;
+    if (kEarly<W> && !slot.early) request(wave);
+    const __amdgpu_buffer_rsrc_t rh = bytes_of(a.h, (long long)a.T * a.top_k * a.Fp * 4);
+    const unsigned plane = (unsigned)(a.T * a.top_k) * (unsigned)a.Fp * kHb;
+    const float* s = W == W_E4M3 ? a.s_down + ((long long)slot.expert * scale_blocks(a.C) + c0 / kScaleBlock) * kb_all : nullptr;
     for (int l0 = 0; l0 < len; l0 += 16) {
       const int entry = list[min(l0 + r16, len - 1)];
-      const float* h = a.h + (long long)entry * a.Fp;
+      const bool real = l0 + r16 < len;
+      const unsigned at = (unsigned)entry * (unsigned)a.Fp * kHb;
+      const float share = a.weights[entry];
       f32x4 v[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
-      for (int kb = wave; kb < kb_all; kb += kSplit) {
+      for (int kb = wave; kb < kb_all; kb += S) {
+        if (!kEarly<W> || kb != wave || l0 != 0) request(kb);
+        const float f = s ? s[kb] : 1.f;
         f32x4 p0 = {0.f, 0.f, 0.f, 0.f}, p1 = p0;
 #pragma unroll
         for (int p = 0; p < WT::kPieces; ++p) {
           const int k = kb * kScaleBlock + WT::first(p, quarter);
-          const unsigned off = (unsigned)(r16 * row_bytes) + (unsigned)k * WT::kBytes;
-          const tok_u4 w0 = load16(rw, k < a.F && r16 < rows ? off : kOutside);
-          const tok_u4 w1 = load16(rw, k < a.F && 16 + r16 < rows ? off + (unsigned)(16 * row_bytes) : kOutside);
-          f32x4 x[WT::kElems / 4];
+          constexpr int kXP = W == W_E4M3 ? 2 : 1;
 #pragma unroll
-          for (int i = 0; i < WT::kElems / 4; ++i) x[i] = *reinterpret_cast<const f32x4*>(h + k + 4 * i);
-          p0 = mma_wide<W>(w0, x, p0);
-          p1 = mma_wide<W>(w1, x, p1);
+          for (int i = 0; i < kHiddenPlanes<W>; ++i) {
+            tok_u4 x[kXP];
+#pragma unroll
+            for (int u = 0; u < kXP; ++u) x[u] = load16(rh, real ? i * plane + at + (unsigned)(k + 8 * u) * kHb : kOutside);
+            p0 = mma_stored<W>(w0[p], x, p0);
+            p1 = mma_stored<W>(w1[p], x, p1);
+          }
         }
-        const float f = sw ? sw[kb] : 1.f;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           v[0][i] = fmaf(p0[i], f, v[0][i]);
           v[1][i] = fmaf(p1[i], f, v[1][i]);
         }
       }
-      join_waves(v, part, wave, lane);
-      if (wave == 0 && l0 + r16 < len) {
-        const float w = a.weights[entry];
+      join_waves<S>(v, part, wave, lane);
+      if (wave == 0 && real) {
         float* y = a.y + (long long)entry * a.C + c0;
 #pragma unroll
         for (int i = 0; i < 2; ++i)
-          if (i * 16 + quarter * 4 < rows)
-#pragma unroll
-            for (int n = 0; n < 4; ++n) shared_store(y + i * 16 + quarter * 4 + n, v[i][n] * w);
+          if (i * 16 + quarter * 4 < rows) shared_store(y + i * 16 + quarter * 4, v[i] * share);
       }
     }
   }
-  vm_wait<0>();  // (the stores have arrived before the workgroup counts as done)
-  __syncthreads();
-  if (threadIdx.x == 0)
-    place = __hip_atomic_fetch_add(a.arrived + blockIdx.x, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  if (wave == 0) {
+    vm_wait<0>();  // (the stores, all of them this wave's, have arrived before the workgroup counts as done)
+    if (lane == 0) place = __hip_atomic_fetch_add(a.arrived + blockIdx.x, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }
   __syncthreads();
   if (place + 1 != gridDim.y) return;
-  for (int i = threadIdx.x; i < a.T * (kColumns / 4); i += kSplit * kWave) {
+  for (int i = threadIdx.x; i < a.T * (kColumns / 4); i += S * kWave) {
     const int t = i / (kColumns / 4), c = i % (kColumns / 4) * 4;
     if (c >= rows) continue;
-    f32x4 s = {0.f, 0.f, 0.f, 0.f};
+    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
     if (!a.keep || a.keep[t] != 0) {
       const float* y = a.y + (long long)t * a.top_k * a.C + c0 + c;
       for (int j = 0; j < a.top_k; ++j)
 #pragma unroll
-        for (int n = 0; n < 4; ++n) s[n] += shared_load(y + (long long)j * a.C + n);
+        for (int n = 0; n < 4; ++n) sum[n] += shared_load(y + (long long)j * a.C + n);
     }
-    store4(reinterpret_cast<OT*>(a.out) + t * a.ldo + c0 + c, s);
+    store4(reinterpret_cast<OT*>(a.out) + t * a.ldo + c0 + c, sum);
   }
 }
 
@@ -351,8 +389,8 @@ template <int W, typename ET>
 void launch_moe(const MoeArgs& a, hipStream_t st) {
   hipLaunchKernelGGL((k_moe_route<ET>), dim3(a.T), dim3(kRouteThreads), 0, st, a);
   const unsigned slots = (unsigned)min((long long)a.E, (long long)a.T * a.top_k);
-  hipLaunchKernelGGL((k_moe_up<W>), dim3(a.Fp / 16, slots), dim3(kSplit * kWave), 0, st, a);
-  hipLaunchKernelGGL((k_moe_down<W, ET>), dim3(column_tiles(a.C), slots), dim3(kSplit * kWave), 0, st, a);
+  hipLaunchKernelGGL((k_moe_up<W>), dim3(a.Fp / 16, slots), dim3(kSplit<W> * kWave), 0, st, a);
+  hipLaunchKernelGGL((k_moe_down<W, ET>), dim3(column_tiles(a.C), slots), dim3(kSplit<W> * kWave), 0, st, a);
 }
 
 struct MoeWs { size_t experts, weights, h, y, arrived, bytes; };
@@ -375,7 +413,7 @@ int validate_moe(const laud_moe_layer* p, int T) {
   if (p->w_dtype == LAUD_E4M3 && p->dtype != LAUD_BF16) return LAUD_ERR_UNSUPPORTED;
   const int step = p->w_dtype == LAUD_E4M3 ? 16 : 8;
   if (p->C % step || p->F % step || p->C > (1 << 20) || p->F > (1 << 20) || p->E > kMaxExperts || p->top_k > kMaxTopK ||
-      T > LAUD_MOE_MAX_TOKENS)
+      T > LAUD_MOE_MAX_TOKENS || (long long)T * p->top_k * (scale_blocks(p->F) * kScaleBlock) * 4 > 0x7fffffffll)
     return LAUD_ERR_UNSUPPORTED;
   return LAUD_OK;
 }
@@ -410,7 +448,7 @@ extern "C" int laud_moe(const laud_moe_layer* p, int T, const void* x, int64_t l
   a.keep = keep; a.out = out; a.ldx = ldx; a.ldo = ldo;
   a.experts = experts ? experts : (int32_t*)((char*)ws + w.experts);
   a.weights = weights ? weights : (float*)((char*)ws + w.weights);
-  a.h = (float*)((char*)ws + w.h);
+  a.h = (char*)ws + w.h;
   a.y = (float*)((char*)ws + w.y);
   a.arrived = (unsigned*)((char*)ws + w.arrived);
   clear_stale_error();
