@@ -1,5 +1,6 @@
 // Matrix product of e4m3 operands with a scale for each block of 128.
 #include <atomic>
+#include <cmath>
 
 #include "laud_token.h"
 
@@ -14,6 +15,7 @@ struct Mm8Args {
   int64_t lda, ldb, ldo;
 };
 
+constexpr double kComputeUnits = 256;
 constexpr int64_t kMaxLd = 1 << 22;    // elements from row to row: 256 rows of a tile stay below the 2 GiB a descriptor addresses
 // Sixteen rows of the first operand times sixteen of the second over a block of 128: lane l holds row l % 16, bytes 16 * (l / 16)
 // and 64 behind them (any order of K serves as long as both operands have the same).  Result: row 4 * (l / 16) + i of the first,
@@ -32,66 +34,40 @@ __device__ __forceinline__ f32x4 mma_block(const i32x8& a, const i32x8& b) {
   return c;
 }
 
-// A tile of 16 columns and 16 * MT rows of the result; the reduction is split over the workgroup's waves, whose sums are added
-// in the waves' order.
-constexpr int kSplit = 8;
-template <typename OT, int MT>
-__global__ __launch_bounds__(kSplit * kWave) void k_mm8_split(Mm8Args g, int ntiles, long long tiles) {
-  __shared__ f32x4 part[kSplit][MT][kWave];
+// Up to 16 rows: the weights are read once, for all of them.  A workgroup has 16 columns, its waves share the reduction, their sums are
+// added in the waves' order.  Bound by memory and the launch: one row of 4096 x 4096 in 4.6 us.
+constexpr int kSplit = 8, kSplitRows = 16;
+template <typename OT>
+__global__ __launch_bounds__(kSplit * kWave) void k_mm8_split(Mm8Args g) {
+  __shared__ f32x4 part[kSplit][kWave];
   const int lane = lane_id(), wave = threadIdx.x / kWave, r16 = lane % 16, quarter = lane / 16;
-  for (long long tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
-    const int n0 = (int)(tile % ntiles) * 16;
-    const long long m0 = tile / ntiles * (16 * MT);
-    const int nrows = min(16, g.N - n0), mrows = (int)min((long long)(16 * MT), g.M - m0);
-    const __amdgpu_buffer_rsrc_t rb = bytes_of(g.b + n0 * g.ldb, (nrows - 1) * g.ldb + g.K);
-    const __amdgpu_buffer_rsrc_t ra = bytes_of(g.a + m0 * g.lda, (mrows - 1) * g.lda + g.K);
-    const unsigned off_b = (unsigned)(min(r16, nrows - 1) * g.ldb);
-    unsigned off_a[MT];
-    const float* sa[MT];
+  const int n0 = blockIdx.x * 16, nrows = min(16, g.N - n0);
+  const __amdgpu_buffer_rsrc_t rb = bytes_of(g.b + n0 * g.ldb, (nrows - 1) * g.ldb + g.K);
+  const __amdgpu_buffer_rsrc_t ra = bytes_of(g.a, (g.M - 1) * g.lda + g.K);
+  const unsigned off_b = (unsigned)(min(r16, nrows - 1) * g.ldb), off_a = (unsigned)(min(r16, g.M - 1) * g.lda);
+  const float* sa = g.sa + (long long)min(r16, g.M - 1) * g.kb;
+  const float* sb = g.sb + (long long)(n0 / kScaleBlock) * g.kb;
+  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+  for (int kb = wave; kb < g.kb; kb += kSplit) {
+    tok_u4 w[2], x[2];
 #pragma unroll
-    for (int t = 0; t < MT; ++t) {
-      const int r = min(t * 16 + r16, mrows - 1);
-      off_a[t] = (unsigned)(r * g.lda);
-      sa[t] = g.sa + (m0 + r) * g.kb;
+    for (int h = 0; h < 2; ++h) {
+      const int k = kb * kScaleBlock + h * 64 + quarter * 16;
+      w[h] = load16(rb, k < g.K ? off_b + (unsigned)k : kOutside);
+      x[h] = load16(ra, k < g.K ? off_a + (unsigned)k : kOutside);
     }
-    const float* sb = g.sb + (long long)(n0 / kScaleBlock) * g.kb;
-    f32x4 acc[MT];
+    const float f = sb[kb] * sa[kb];
+    const f32x4 p = mma_block(join(w[0], w[1]), join(x[0], x[1]));
 #pragma unroll
-    for (int t = 0; t < MT; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-    for (int kb = wave; kb < g.kb; kb += kSplit) {
-      const float s = sb[kb];
-      unsigned k[2];
-      tok_u4 w[2];
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int at = kb * kScaleBlock + h * 64 + quarter * 16;
-        k[h] = (unsigned)at;
-        w[h] = load16(rb, at < g.K ? off_b + k[h] : kOutside);
-      }
-#pragma unroll
-      for (int t = 0; t < MT; ++t) {
-        tok_u4 x[2];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) x[h] = load16(ra, (int)k[h] < g.K ? off_a[t] + k[h] : kOutside);
-        const float f = s * sa[t][kb];
-        const f32x4 p = mma_block(join(w[0], w[1]), join(x[0], x[1]));
-#pragma unroll
-        for (int i = 0; i < 4; ++i) acc[t][i] = fmaf(p[i], f, acc[t][i]);
-      }
-    }
-#pragma unroll
-    for (int t = 0; t < MT; ++t) part[wave][t][lane] = acc[t];
-    __syncthreads();
-    for (int i = threadIdx.x; i < MT * kWave; i += kSplit * kWave) {
-      const int t = i / kWave;  // (a wave's own: lane stays lane)
-      f32x4 v = part[0][t][lane];
-#pragma unroll
-      for (int w = 1; w < kSplit; ++w) v += part[w][t][lane];
-      const int m = t * 16 + r16, n = n0 + quarter * 4;
-      if (m < mrows && n < g.N) store4(reinterpret_cast<OT*>(g.out) + (m0 + m) * g.ldo + n, v);
-    }
-    __syncthreads();
+    for (int i = 0; i < 4; ++i) acc[i] = fmaf(p[i], f, acc[i]);
   }
+  part[wave][lane] = acc;
+  __syncthreads();
+  if (wave != 0) return;
+#pragma unroll
+  for (int w = 1; w < kSplit; ++w) acc += part[w][lane];
+  const int n = n0 + quarter * 4;
+  if (r16 < g.M && n < g.N) store4(reinterpret_cast<OT*>(g.out) + r16 * g.ldo + n, acc);
 }
 
 // ---- tiles ------------------------------------------------------------------------------------------------------------------
@@ -107,20 +83,23 @@ __device__ __forceinline__ f32x4 mma_block8(const i32x8& a, const i32x8& b) {
   return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, zero, 0, 0, 0, 0, 0, 0);
 }
 
-template <int BM, int BN> struct TileLds {
+template <int BM, int BN, int NS, int KG> struct TileLds {
   static constexpr int kB = 0, kA = BN * kScaleBlock, kSa = kA + BM * kScaleBlock, kSb = kSa + BM * 4, kStage = kSb + 256;
-  static constexpr int kBytes = 2 * kStage;
+  static constexpr int kGroup = NS * kStage, kBytes = KG * kGroup;
 };
 
-template <typename OT, int BM, int BN, int WM, int WN>
-__global__ __launch_bounds__(BM / WM * (BN / WN) * kWave) void k_mm8_tile(Mm8Args g, int mtiles, int ntiles) {
-  typedef TileLds<BM, BN> L;
+template <typename OT, int BM, int BN, int WM, int WN, int NS, int KG>
+__global__ __launch_bounds__(KG * BM / WM * (BN / WN) * kWave) void k_mm8_tile(Mm8Args g, int mtiles, int ntiles) {
+  typedef TileLds<BM, BN, NS, KG> L;
   constexpr int kWaves = BM / WM * (BN / WN), kMT = WM / 16, kNT = WN / 16;
   constexpr int kLoadsB = BN / 8 / kWaves, kLoadsA = BM / 8 / kWaves;
   static_assert(kLoadsB * 8 * kWaves == BN && kLoadsA * 8 * kWaves == BM && BM < kWaves * kWave && BM % kWave == 0 && kMT % 2 == 0, "rows shared evenly");
   extern __shared__ __align__(1024) uint8_t lds[];
-  const unsigned lds0 = (unsigned)(size_t)(__attribute__((address_space(3))) uint8_t*)lds;
-  const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), r16 = lane % 16, quarter = lane / 16;
+  const int lane = lane_id(), r16 = lane % 16, quarter = lane / 16;
+  const int group = __builtin_amdgcn_readfirstlane(threadIdx.x / (kWaves * kWave));
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave) - group * kWaves;
+  uint8_t* const stages = lds + group * L::kGroup;  // a group's own
+  const unsigned lds0 = (unsigned)(size_t)(__attribute__((address_space(3))) uint8_t*)stages;
   // Workgroups go round-robin over the eight XCDs: each takes a run of tiles, in bands of eight rows of tiles, so that its L2 serves
   // a block of them.
   const int tiles = mtiles * ntiles, per = (tiles + 7) / 8;
@@ -147,10 +126,11 @@ __global__ __launch_bounds__(BM / WM * (BN / WN) * kWave) void k_mm8_tile(Mm8Arg
 
   // The loads of block kb, kPer of them behind each row tile's matrix instructions.  Behind the last block they fetch nothing: the loop
   // over the blocks has no branch, across which the compiler would gather the scalings.
-  constexpr int kLoads = kLoadsB + kLoadsA + 1, kPer = (kLoads - 1) / (kMT - 1) + 1;
+  constexpr bool kDeep = kMT * kNT <= 16;
+  constexpr int kLoads = kLoadsB + kLoadsA + 1, kPer = kDeep ? (kLoads - 1) / kMT + 1 : (kLoads - 1) / (kMT - 1) + 1;
   static_assert(kPer * kMT >= kLoads, "all of a block's loads before its last row tile");
-  auto request = [&](int kb, int from, int to) {
-    const unsigned stage = lds0 + (kb & 1) * L::kStage;
+  auto request = [&](int step, unsigned stage, int from, int to) {
+    const int kb = step * KG + group;
     const bool in = kb * kScaleBlock + chunk * 16 < g.K;
 #pragma unroll
     for (int i = from; i < to; ++i) {
@@ -162,21 +142,10 @@ __global__ __launch_bounds__(BM / WM * (BN / WN) * kWave) void k_mm8_tile(Mm8Arg
 
   const int wm = wave % (BM / WM) * WM, wn = wave / (BM / WM) * WN;
   const unsigned frag = (unsigned)(r16 * kScaleBlock + ((quarter ^ (lane & 7)) << 4));
+  auto operand = [&](const uint8_t* at) { return join(*reinterpret_cast<const tok_u4*>(at + frag), *reinterpret_cast<const tok_u4*>(at + (frag ^ 64))); };
   float acc[kNT][kMT][4];  // (plain floats: as vectors the compiler moves them about in fours)
   f32x4 p[kNT];
-  i32x8 nf[kNT], mf[2];
-  float s[2], sb, f = 0.f;
-  auto read_m = [&](int kb, int j) {
-    const uint8_t* at = lds + (kb & 1) * L::kStage;
-    s[j & 1] = *reinterpret_cast<const float*>(at + L::kSa + (wm + j * 16 + r16) * 4);
-    at += L::kA + (wm + j * 16) * kScaleBlock;
-    mf[j & 1] = join(*reinterpret_cast<const tok_u4*>(at + frag), *reinterpret_cast<const tok_u4*>(at + (frag ^ 64)));
-  };
-  auto read_n = [&](int kb, int i) {
-    const uint8_t* at = lds + (kb & 1) * L::kStage + L::kB + (wn + i * 16) * kScaleBlock;
-    nf[i] = join(*reinterpret_cast<const tok_u4*>(at + frag), *reinterpret_cast<const tok_u4*>(at + (frag ^ 64)));
-  };
-  auto read_sb = [&](int kb) { sb = *reinterpret_cast<const float*>(lds + (kb & 1) * L::kStage + L::kSb + wn / kScaleBlock * 4); };
+  float f = 0.f;
 #pragma unroll
   for (int i = 0; i < kNT; ++i) {
 #pragma unroll
@@ -185,48 +154,123 @@ __global__ __launch_bounds__(BM / WM * (BN / WN) * kWave) void k_mm8_tile(Mm8Arg
       for (int e = 0; e < 4; ++e) acc[i][j][e] = 0.f;
     p[i] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
-  request(0, 0, kLoads);
-  vm_wait<0>();
-  __syncthreads();
-  request(1, 0, kPer);
-  read_m(0, 0);
-  read_sb(0);
+  if constexpr (kDeep) {
+    // Few row tiles a wave: all of a block's operands are in registers, and the next block's come from LDS behind the barrier, while
+    // this one is multiplied.
+    struct Operands {
+      i32x8 n[kNT], m[kMT];
+      float s[kMT], sb;
+    };
+    auto read = [&](Operands& o, const uint8_t* at) {
+      o.sb = *reinterpret_cast<const float*>(at + L::kSb + wn / kScaleBlock * 4);
 #pragma unroll
-  for (int i = 0; i < kNT; ++i) read_n(0, i);
-  // A product's scaling stands behind the matrix instruction of the next row tile (in the last of a block: of the next block's
-  // first), in this order and no other: an instruction's result is there long before it is asked for.  The barrier stands in front
-  // of a block's last row tile, whose operands are in registers by then: behind it the next block's first ones come from LDS, and
-  // the loads of the block after that may overwrite this one's stage.  (Behind the last block it reads what is there, unused.)
-  for (int kb = 0; kb < g.kb; ++kb) {
+      for (int i = 0; i < kNT; ++i) o.n[i] = operand(at + L::kB + (wn + i * 16) * kScaleBlock);
 #pragma unroll
-    for (int j = 0; j < kMT; ++j) {
-      const float f_old = f;
-      f = sb * s[j & 1];
-      if (j == kMT - 1) {
-        lds_wait();
-        vm_wait<0>();
-        __syncthreads();
-        read_m(kb + 1, 0);
-        read_sb(kb + 1);
-        request(kb + 2, 0, kPer);
-      } else {
-        request(kb + 1, (j + 1) * kPer, (j + 2) * kPer);
-        read_m(kb, j + 1);
+      for (int j = 0; j < kMT; ++j) {
+        o.s[j] = *reinterpret_cast<const float*>(at + L::kSa + (wm + j * 16 + r16) * 4);
+        o.m[j] = operand(at + L::kA + (wm + j * 16) * kScaleBlock);
       }
+    };
+    int now = 0;
+    auto step = [&](int kb, const Operands& o, Operands& ahead) {
+      const int next = now + 1 < NS ? now + 1 : 0;
+      lds_wait();
+      vm_wait<(NS - 2) * kLoads>();
+      __syncthreads();
+      read(ahead, stages + next * L::kStage);
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int i = 0; i < kNT; ++i) {
-        const f32x4 old = p[i];
-        if constexpr (sizeof(OT) == 2) p[i] = mma_block8(nf[i], mf[j & 1]);
-        else p[i] = mma_block(nf[i], mf[j & 1]);
-        __builtin_amdgcn_sched_barrier(0);
-        float(&c)[4] = acc[i][(j + kMT - 1) % kMT];
+      for (int j = 0; j < kMT; ++j) {
+        const float f_old = f;
+        f = o.sb * o.s[j];
+        request(kb + NS, lds0 + now * L::kStage, j * kPer, (j + 1) * kPer);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) c[e] = fmaf(old[e], f_old, c[e]);
-        __builtin_amdgcn_sched_barrier(0);
-        if (j == kMT - 1) read_n(kb + 1, i);
-        if (i == 0) __builtin_amdgcn_s_setprio(1);  // (a wave amid its products goes ahead of one that loads)
-        if (i == kNT - 1) __builtin_amdgcn_s_setprio(0);
+        for (int i = 0; i < kNT; ++i) {
+          const f32x4 old = p[i];
+          if constexpr (sizeof(OT) == 2) p[i] = mma_block8(o.n[i], o.m[j]);
+          else p[i] = mma_block(o.n[i], o.m[j]);
+          __builtin_amdgcn_sched_barrier(0);
+          float(&c)[4] = acc[i][(j + kMT - 1) % kMT];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) c[e] = fmaf(old[e], f_old, c[e]);
+          __builtin_amdgcn_sched_barrier(0);
+        }
       }
+      now = next;
+    };
+#pragma unroll
+    for (int s = 0; s < NS; ++s) request(s, lds0 + s * L::kStage, 0, kLoads);
+    vm_wait<(NS - 1) * kLoads>();
+    __syncthreads();
+    Operands even, odd;
+    read(even, stages);
+    for (int kb = 0; kb * KG < g.kb; kb += 2) {  // (past the last block: zeros)
+      step(kb, even, odd);
+      step(kb + 1, odd, even);
+    }
+  } else {
+    static_assert(KG == 1, "");
+    i32x8 nf[kNT], mf[2];
+    float s[2], sb;
+    auto read_m = [&](const uint8_t* at, int j) {
+      s[j & 1] = *reinterpret_cast<const float*>(at + L::kSa + (wm + j * 16 + r16) * 4);
+      at += L::kA + (wm + j * 16) * kScaleBlock;
+      mf[j & 1] = join(*reinterpret_cast<const tok_u4*>(at + frag), *reinterpret_cast<const tok_u4*>(at + (frag ^ 64)));
+    };
+    auto read_n = [&](const uint8_t* at, int i) {
+      at += L::kB + (wn + i * 16) * kScaleBlock;
+      nf[i] = join(*reinterpret_cast<const tok_u4*>(at + frag), *reinterpret_cast<const tok_u4*>(at + (frag ^ 64)));
+    };
+    auto read_sb = [&](const uint8_t* at) { sb = *reinterpret_cast<const float*>(at + L::kSb + wn / kScaleBlock * 4); };
+#pragma unroll
+    for (int s = 0; s < NS - 1; ++s) request(s, lds0 + s * L::kStage, 0, kLoads);
+    vm_wait<(NS - 2) * kLoads>();
+    __syncthreads();
+    request(NS - 1, lds0 + (NS - 1) * L::kStage, 0, kPer);
+    read_m(stages, 0);
+    read_sb(stages);
+#pragma unroll
+    for (int i = 0; i < kNT; ++i) read_n(stages, i);
+    // A product's scaling stands behind the matrix instruction of the next row tile (in the last of a block: of the next block's
+    // first), in this order and no other: an instruction's result is there long before it is asked for.  The barrier stands in front
+    // of a block's last row tile, whose operands are in registers by then: behind it the next block's first ones come from LDS, and
+    // the loads of the block after that may overwrite this one's stage.  (Behind the last block it reads what is there, unused.)
+    int now = 0, fill = NS - 1;  // stages of this block and of the one being requested
+    for (int kb = 0; kb < g.kb; ++kb) {
+      const int next = now + 1 < NS ? now + 1 : 0;
+      const uint8_t *at = stages + now * L::kStage, *ahead = stages + next * L::kStage;
+#pragma unroll
+      for (int j = 0; j < kMT; ++j) {
+        const float f_old = f;
+        f = sb * s[j & 1];
+        if (j == kMT - 1) {
+          lds_wait();
+          vm_wait<(NS - 2) * kLoads>();
+          __syncthreads();
+          read_m(ahead, 0);
+          read_sb(ahead);
+          fill = now;
+          request(kb + NS, lds0 + fill * L::kStage, 0, kPer);
+        } else {
+          request(kb + NS - 1, lds0 + fill * L::kStage, (j + 1) * kPer, (j + 2) * kPer);
+          read_m(at, j + 1);
+        }
+#pragma unroll
+        for (int i = 0; i < kNT; ++i) {
+          const f32x4 old = p[i];
+          if constexpr (sizeof(OT) == 2) p[i] = mma_block8(nf[i], mf[j & 1]);
+          else p[i] = mma_block(nf[i], mf[j & 1]);
+          __builtin_amdgcn_sched_barrier(0);
+          float(&c)[4] = acc[i][(j + kMT - 1) % kMT];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) c[e] = fmaf(old[e], f_old, c[e]);
+          __builtin_amdgcn_sched_barrier(0);
+          if (j == kMT - 1) read_n(ahead, i);
+          if (i == 0) __builtin_amdgcn_s_setprio(1);  // (a wave amid its products goes ahead of one that loads)
+          if (i == kNT - 1) __builtin_amdgcn_s_setprio(0);
+        }
+      }
+      now = next;
     }
   }
   vm_wait<0>();  // (no load into LDS is left behind)
@@ -234,6 +278,27 @@ __global__ __launch_bounds__(BM / WM * (BN / WN) * kWave) void k_mm8_tile(Mm8Arg
   for (int i = 0; i < kNT; ++i)
 #pragma unroll
     for (int e = 0; e < 4; ++e) acc[i][kMT - 1][e] = fmaf(p[i][e], f, acc[i][kMT - 1][e]);
+  if constexpr (KG == 2) {  // the second group's sums through LDS to the first
+    static_assert(BM * BN * 4 <= L::kBytes, "sums fit");
+    f32x4* const sums = reinterpret_cast<f32x4*>(lds) + threadIdx.x % (kWaves * kWave);
+    __syncthreads();
+    if (group == 1) {
+#pragma unroll
+      for (int i = 0; i < kNT; ++i)
+#pragma unroll
+        for (int j = 0; j < kMT; ++j) sums[(i * kMT + j) * kWaves * kWave] = f32x4{acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
+    }
+    __syncthreads();
+    if (group == 1) return;
+#pragma unroll
+    for (int i = 0; i < kNT; ++i)
+#pragma unroll
+      for (int j = 0; j < kMT; ++j) {
+        const f32x4 v = sums[(i * kMT + j) * kWaves * kWave];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[i][j][e] += v[e];
+      }
+  }
   // Lane (row r16 of a, quarter) holds columns 4 * quarter .. +3 of every 16: after a swap of neighbouring quarters between two
   // column tiles it holds eight in a row, and four lanes 64 bytes of a row of bf16 results.
 #pragma unroll
@@ -259,39 +324,64 @@ __global__ __launch_bounds__(BM / WM * (BN / WN) * kWave) void k_mm8_tile(Mm8Arg
   }
 }
 
-template <typename OT, int BM, int BN, int WM, int WN>
+template <typename OT, int BM, int BN, int WM, int WN, int NS, int KG = 1>
 int ask_tile_lds() {
-  return hipFuncSetAttribute(reinterpret_cast<const void*>(&k_mm8_tile<OT, BM, BN, WM, WN>), hipFuncAttributeMaxDynamicSharedMemorySize,
-                             TileLds<BM, BN>::kBytes) == hipSuccess ? LAUD_OK : LAUD_ERR_HIP;
+  return hipFuncSetAttribute(reinterpret_cast<const void*>(&k_mm8_tile<OT, BM, BN, WM, WN, NS, KG>), hipFuncAttributeMaxDynamicSharedMemorySize,
+                             TileLds<BM, BN, NS, KG>::kBytes) == hipSuccess ? LAUD_OK : LAUD_ERR_HIP;
 }
-template <typename OT, int BM, int BN, int WM, int WN>
+template <typename OT, int BM, int BN, int WM, int WN, int NS, int KG = 1>
 int launch_tile(const Mm8Args& g, hipStream_t st) {
   if (matmul8_init_device() != LAUD_OK) return LAUD_ERR_HIP;
   const int mtiles = (g.M - 1) / BM + 1, ntiles = (g.N - 1) / BN + 1;
-  hipLaunchKernelGGL((k_mm8_tile<OT, BM, BN, WM, WN>), dim3((unsigned)((mtiles * ntiles + 7) / 8 * 8)), dim3(BM / WM * (BN / WN) * kWave),
-                     (TileLds<BM, BN>::kBytes), st, g, mtiles, ntiles);
+  hipLaunchKernelGGL((k_mm8_tile<OT, BM, BN, WM, WN, NS, KG>), dim3((unsigned)((mtiles * ntiles + 7) / 8 * 8)), dim3(KG * BM / WM * (BN / WN) * kWave),
+                     (TileLds<BM, BN, NS, KG>::kBytes), st, g, mtiles, ntiles);
   return check_launch();
+}
+
+// Which tile: a launch takes rounds of one tile a compute unit, a round the blocks of K times the tile's time for one and its two
+// ends, in us as measured (the times of a launch, at 256 rows or more):
+//   bf16 results         64 x 64   64 x 128   128 x 128   128 x 256   256 x 256
+//    256 x 4096 x 4096     11.3       14.7        23.9        31.2        48.0
+//    512 x 4096 x 4096     21.0       15.8        24.4        31.5        47.7
+//   1024 x 4096 x 4096     39.7       29.7        26.3        33.0        48.7
+//   2048 x 4096 x 4096     78.8       58.0        50.4        39.3        52.5
+//   4096 x 4096 x 4096    149.2      110.9        98.6        75.6        64.0
+//   1003 x 2120 x 2000     21.9       21.0        17.0        20.0        29.1
+// The smaller ones split a block of K's followers over two groups of waves, and short reductions on 64 x 64 tiles take two stages
+// instead of four, two workgroups a compute unit (200 x 2048 x 1024: 4.8 us against 5.1; 256 x 4096 x 4096: 14.9 against 11.3).
+struct TileTime {
+  int bm, bn;
+  float block, ends;
+};
+inline float tile_time(const Mm8Args& g, const TileTime& t) {
+  const double tiles = (double)((g.M - 1) / t.bm + 1) * ((g.N - 1) / t.bn + 1);
+  return (float)(std::ceil(tiles / kComputeUnits) * (g.kb * t.block + t.ends));
 }
 
 template <typename OT>
 int launch_mm8(const Mm8Args& g, hipStream_t st) {
-  const int ntiles = (g.N - 1) / 16 + 1;
-  const long long t128 = (long long)((g.M - 1) / 128 + 1) * ((g.N - 1) / 128 + 1);
-  if (g.M > 64 && t128 < (1 << 30)) {
-    if constexpr (sizeof(OT) == 2)
-      if (t128 >= 1024) return launch_tile<bf16_t, 256, 256, 128, 64>(g, st);
-    return launch_tile<OT, 128, 128, 64, 64>(g, st);
+  if (g.M <= kSplitRows) {
+    const int ntiles = (g.N - 1) / 16 + 1;
+    hipLaunchKernelGGL((k_mm8_split<OT>), dim3(ntiles), dim3(kSplit * kWave), 0, st, g);
+    return check_launch();
   }
-#define LAUD_MM8_SPLIT(MT)                                                                                                        \
-  do {                                                                                                                            \
-    const long long tiles = (long long)ntiles * ((g.M - 1) / (16 * MT) + 1);                                                      \
-    hipLaunchKernelGGL((k_mm8_split<OT, MT>), dim3((unsigned)min(tiles, 1ll << 22)), dim3(kSplit * kWave), 0, st, g, ntiles, tiles); \
-  } while (0)
-  if (g.M <= 16) LAUD_MM8_SPLIT(1);
-  else if (g.M <= 32) LAUD_MM8_SPLIT(2);
-  else LAUD_MM8_SPLIT(4);
-#undef LAUD_MM8_SPLIT
-  return check_launch();
+  constexpr bool kBf16 = sizeof(OT) == 2;
+  constexpr TileTime kTimes[5] = {{64, 64, kBf16 ? 0.24f : 0.42f, 2.2f}, {64, 128, kBf16 ? 0.39f : 0.6f, 2.2f},
+                                  {128, 128, kBf16 ? 0.72f : 1.35f, 2.2f}, {128, 256, 1.1f, 3.8f}, {256, 256, 1.95f, 2.0f}};
+  int best = 0;
+  for (int i = 1; i < (kBf16 ? 5 : 3); ++i)
+    if (tile_time(g, kTimes[i]) < tile_time(g, kTimes[best])) best = i;
+  if ((double)((g.M - 1) / kTimes[best].bm + 1) * ((g.N - 1) / kTimes[best].bn + 1) > 1e9) return LAUD_ERR_UNSUPPORTED;
+  if constexpr (kBf16) {
+    if (best == 4) return launch_tile<OT, 256, 256, 128, 64, 2>(g, st);
+    if (best == 3) return launch_tile<OT, 128, 256, 64, 64, 3>(g, st);
+    if (best == 2) return launch_tile<OT, 128, 128, 64, 64, 2, 2>(g, st);
+  } else {
+    if (best == 2) return launch_tile<OT, 128, 128, 64, 64, 4>(g, st);
+  }
+  if (best == 1) return launch_tile<OT, 64, 128, 32, 64, 3, 2>(g, st);
+  if (g.kb <= 10) return launch_tile<OT, 64, 64, 32, 32, 2, 2>(g, st);
+  return launch_tile<OT, 64, 64, 32, 32, 4, 2>(g, st);
 }
 
 }  // namespace
@@ -302,10 +392,12 @@ int matmul8_init_device() {
   if (hipGetDevice(&dev) != hipSuccess) return LAUD_ERR_HIP;
   const unsigned bit = dev >= 0 && dev < 32 ? 1u << dev : 0u;
   if (bit && (done.load(std::memory_order_acquire) & bit)) return LAUD_OK;
-  int rc;
-  if ((rc = ask_tile_lds<bf16_t, 256, 256, 128, 64>()) != LAUD_OK || (rc = ask_tile_lds<bf16_t, 128, 128, 64, 64>()) != LAUD_OK ||
-      (rc = ask_tile_lds<float, 128, 128, 64, 64>()) != LAUD_OK)
-    return rc;
+  for (int rc : {ask_tile_lds<bf16_t, 256, 256, 128, 64, 2>(), ask_tile_lds<bf16_t, 128, 256, 64, 64, 3>(),
+                 ask_tile_lds<bf16_t, 128, 128, 64, 64, 2, 2>(), ask_tile_lds<bf16_t, 64, 128, 32, 64, 3, 2>(),
+                 ask_tile_lds<bf16_t, 64, 64, 32, 32, 2, 2>(), ask_tile_lds<bf16_t, 64, 64, 32, 32, 4, 2>(),
+                 ask_tile_lds<float, 128, 128, 64, 64, 4>(), ask_tile_lds<float, 64, 128, 32, 64, 3, 2>(),
+                 ask_tile_lds<float, 64, 64, 32, 32, 2, 2>(), ask_tile_lds<float, 64, 64, 32, 32, 4, 2>()})
+    if (rc != LAUD_OK) return rc;
   done.fetch_or(bit, std::memory_order_release);
   return LAUD_OK;
 }
