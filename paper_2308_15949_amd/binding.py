@@ -1,4 +1,4 @@
-"""Thin ctypes binding of liblaud.so: argument marshalling only.
+"""Thin binding of liblaud.so (ctypes; the token operators' calls through a small extension): argument marshalling only.
 
 Every function below has the name and the meaning of the C entry point declared in
 include/laud.h; tensors are torch CUDA tensors used purely as device memory, the
@@ -198,8 +198,8 @@ def _stream():
 
 
 def _forget_raw_stream():
-    global _raw_stream
-    _raw_stream = None
+    global _raw_stream, _calls
+    _raw_stream = _calls = None
 
 
 # a forked child goes through torch once more, which refuses a device state that was initialised in the parent
@@ -395,36 +395,38 @@ def laud_channel_masker(x, fx: Fmap, wa, ba, hidden: int, wb, bb, D: int, cmask,
 
 
 # ----- token operators --------------------------------------------------------------------------------------------------------
-# (Their tensors come with strides and in three types, so the binding checks what a pointer no longer tells: device, type, shape.
-# A tensor that does not fit raises LaudError like an argument the library refuses.  A call on a few rows is a launch of a few
-# microseconds, so the checks are written out for speed: attributes read once, shapes compared whole.)
-_CODES: dict = {}  # torch's types -> laud_dtype
+# (Their tensors come with strides and in three types, so their calls check device, type and shape: a tensor that does not fit raises
+# LaudError like an argument the library refuses.  The calls go through _laud_torch.so, an extension that reads the tensors in C++:
+# a call on a few rows is a launch of two or three microseconds, the same reading in Python and ctypes took five.)
+FAST_PATH = os.path.join(HERE, "_laud_torch.so")
+_calls = None
 
 
-def _codes() -> dict:
-    if not _CODES:
-        import torch
-        _CODES.update({torch.float32: F32, torch.bfloat16: BF16, torch.float8_e4m3fn: E4M3})
-    return _CODES
+def _token_calls():
+    """The extension, bound to the loaded library's entry points.  Raises if it has not been built: there is no other path."""
+    global _calls
+    lib = load()
+    if not os.path.exists(FAST_PATH):
+        raise RuntimeError(f"{FAST_PATH} is missing: build it with `python -m paper_2308_15949_amd.build`")
+    import torch  # (loads the libraries that the extension is linked against)
 
-
-def _dtype_of(t) -> int:
-    """laud_dtype of a tensor, -1 for other types."""
-    return (_CODES or _codes()).get(t.dtype, -1)
+    from . import _laud_torch
+    if torch.cuda.is_available():
+        torch.cuda.current_stream()  # initialises torch's device state, which the extension takes for granted
+    _laud_torch.bind(*(C.cast(f, C.c_void_p).value for f in (lib.laud_norm_residual, lib.laud_quantize_e4m3, lib.laud_matmul_e4m3,
+                                                              lib.laud_moe)))
+    _calls = _laud_torch
+    return _calls
 
 
 def _bad(where: str):
     raise LaudError(ERR_INVALID_ARG, where)
 
 
-def _rows(t, shape, dtype, where: str):
-    """(pointer, elements from row to row) of a device tensor [rows][cols] of that shape and torch type whose rows are contiguous."""
-    if not (t.is_cuda and t.dtype == dtype and t.shape == shape):
-        _bad(where)
-    ld, step = t.stride()
-    if step != 1 and shape[1] != 1:
-        _bad(where)
-    return t.data_ptr(), (ld if shape[0] > 1 else shape[1])
+def _dtype_of(t) -> int:
+    """laud_dtype of a tensor, -1 for other types."""
+    import torch
+    return {torch.float32: F32, torch.bfloat16: BF16, torch.float8_e4m3fn: E4M3}.get(t.dtype, -1)
 
 
 def _dense(t, shape, code: int, where: str):
@@ -432,15 +434,6 @@ def _dense(t, shape, code: int, where: str):
     if t is None:
         return None
     if not (t.is_cuda and t.shape == shape and _dtype_of(t) == code and t.is_contiguous()):
-        _bad(where)
-    return t.data_ptr()
-
-
-def _bytes(t, n: int, where: str):
-    """Pointer of a byte (or truth value) per row; None -> None."""
-    if t is None:
-        return None
-    if not (t.is_cuda and t.numel() == n and t.element_size() == 1 and not t.is_floating_point() and t.is_contiguous()):
         _bad(where)
     return t.data_ptr()
 
@@ -465,45 +458,16 @@ def make_norm_block(c: int, dtype, kind: str, eps: float, post_w=None, post_b=No
 def laud_norm_residual(p: NormBlock, x, y=None, keep=None, gate=None, rows_per_gate: int = 0, out=None, z=None, z_scale=None) -> None:
     """x, y, out, z [rows][C]; keep [rows] bytes; gate [ceil(rows / rows_per_gate)][C] float32; z float8_e4m3fn with
     z_scale [rows][ceil(C / 128)], or of x's type."""
-    where = "laud_norm_residual"
-    shape, dtype = x.shape, x.dtype
-    if len(shape) != 2 or shape[1] != p.C or (_CODES or _codes()).get(dtype) != p.dtype:
-        _bad(where)
-    n, c = shape
-    xp, ldx = _rows(x, shape, dtype, where)
-    yp = op = zp = gp = zs = None
-    ldy = ldo = ldz = 0
-    z_dtype = p.dtype
-    if y is not None:
-        yp, ldy = _rows(y, shape, dtype, where)
-    if out is not None:
-        op, ldo = _rows(out, shape, dtype, where)
-    if z is not None:
-        if z_scale is not None:
-            z_dtype = E4M3
-            zs = _dense(z_scale, (n, _blocks(c)), F32, where)
-        zp, ldz = _rows(z, shape, z.dtype, where)
-        if _CODES.get(z.dtype) != z_dtype:
-            _bad(where)
-    if gate is not None:
-        if rows_per_gate <= 0:
-            _bad(where)
-        gp = _dense(gate, (-(-n // rows_per_gate), c), F32, where)
-    _check(load().laud_norm_residual(C.byref(p), n, xp, ldx, yp, ldy, None if keep is None else _bytes(keep, n, where), gp,
-                                     rows_per_gate, op, ldo, zp, ldz, z_dtype, zs, _stream()), where)
+    s = (_calls or _token_calls()).norm_residual(p, x, y, keep, gate, rows_per_gate, out, z, z_scale)
+    if s:
+        raise LaudError(s, "laud_norm_residual")
 
 
 def laud_quantize_e4m3(x, q, scale, block_rows: int = 1) -> None:
     """x [rows][cols] float32 or bf16 -> q [rows][cols] float8_e4m3fn and scale [ceil(rows / block_rows)][ceil(cols / 128)]."""
-    where = "laud_quantize_e4m3"
-    shape, code = x.shape, _dtype_of(x)
-    if len(shape) != 2 or _dtype_of(q) != E4M3 or code not in (F32, BF16) or block_rows not in (1, 128):
-        _bad(where)
-    n, c = shape
-    xp, ldx = _rows(x, shape, x.dtype, where)
-    qp, ldq = _rows(q, shape, q.dtype, where)
-    _check(load().laud_quantize_e4m3(xp, ldx, n, c, code, block_rows, qp, ldq,
-                                     _dense(scale, (n if block_rows == 1 else _blocks(n), _blocks(c)), F32, where), _stream()), where)
+    s = (_calls or _token_calls()).quantize(x, q, scale, block_rows)
+    if s:
+        raise LaudError(s, "laud_quantize_e4m3")
 
 
 def matmul_e4m3_workspace(m: int, n: int, k: int) -> int:
@@ -513,18 +477,9 @@ def matmul_e4m3_workspace(m: int, n: int, k: int) -> int:
 def laud_matmul_e4m3(a, sa, b, sb, out, ws=None) -> None:
     """out [M][N] (float32 or bf16) = a [M][K] times b [N][K] transposed, both float8_e4m3fn with scales sa [M][ceil(K / 128)] and
     sb [ceil(N / 128)][ceil(K / 128)]."""
-    where = "laud_matmul_e4m3"
-    shape_a, shape_b, dtype = a.shape, b.shape, a.dtype
-    if len(shape_a) != 2 or len(shape_b) != 2 or shape_a[1] != shape_b[1] or (_CODES or _codes()).get(dtype) != E4M3:
-        _bad(where)
-    m, k = shape_a
-    n, kb = shape_b[0], -(-k // 128)
-    ap, lda = _rows(a, shape_a, dtype, where)
-    bp, ldb = _rows(b, shape_b, dtype, where)
-    op, ldo = _rows(out, (m, n), out.dtype, where)
-    wp, wb = _ws_args(ws)
-    _check(load().laud_matmul_e4m3(ap, lda, _dense(sa, (m, kb), F32, where), bp, ldb, _dense(sb, (-(-n // 128), kb), F32, where), m, n, k,
-                                   op, ldo, _CODES.get(out.dtype, -1), wp, wb, _stream()), where)
+    s = (_calls or _token_calls()).matmul(a, sa, b, sb, out, ws)
+    if s:
+        raise LaudError(s, "laud_matmul_e4m3")
 
 
 def make_moe(router, up, down, s_up=None, s_down=None, top_k: int = 1, renormalise: bool = False, scale: float = 1.0) -> MoeLayer:
@@ -552,22 +507,9 @@ def moe_workspace(p: MoeLayer, t: int) -> int:
 def laud_moe(p: MoeLayer, x, keep, out, experts, weights, ws) -> None:
     """x, out [T][C] of the router's type; keep [T] bytes or None; experts [T][top_k] int32 and weights [T][top_k] float32 receive
     the routing, each may be None."""
-    where = "laud_moe"
-    shape, dtype = x.shape, x.dtype
-    if len(shape) != 2 or shape[1] != p.C or (_CODES or _codes()).get(dtype) != p.dtype:
-        _bad(where)
-    n = shape[0]
-    xp, ldx = _rows(x, shape, dtype, where)
-    op, ldo = _rows(out, shape, dtype, where)
-    ep = None
-    if experts is not None:
-        if not (experts.is_cuda and experts.shape == (n, p.top_k) and experts.element_size() == 4 and
-                not experts.is_floating_point() and experts.is_contiguous()):
-            _bad(where)
-        ep = experts.data_ptr()
-    wp, wb = _ws_args(ws)
-    _check(load().laud_moe(C.byref(p), n, xp, ldx, None if keep is None else _bytes(keep, n, where), op, ldo, ep,
-                           _dense(weights, (n, p.top_k), F32, where), wp, wb, _stream()), where)
+    s = (_calls or _token_calls()).moe(p, x, keep, out, experts, weights, ws)
+    if s:
+        raise LaudError(s, "laud_moe")
 
 
 def laud_stage_timing_enable(on: bool) -> None:

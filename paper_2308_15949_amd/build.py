@@ -1,4 +1,5 @@
-"""Builds liblaud.so (gfx950 HIP kernels + C ABI) in-tree with hipcc.
+"""Builds liblaud.so (gfx950 HIP kernels + C ABI) in-tree with hipcc, and _laud_torch.so, the extension that calls the token
+operators from torch tensors, with the host compiler.
 
     python -m paper_2308_15949_amd.build
 
@@ -17,6 +18,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(CSRC, "_build")
 LIB = os.path.join(HERE, "liblaud.so")
+EXTENSION = os.path.join(HERE, "_laud_torch.so")
 SOURCES = ["laud_api.hip", "laud_mask.hip", "laud_chanmask.hip", "laud_static.hip", "laud_se.hip", "laud_gemm.hip", "laud_pipe_a.hip", "laud_pipe_b.hip", "laud_pipe_c.hip", "laud_group.hip", "laud_group_fused.hip", "laud_skinny.hip", "laud_narrow.hip", "laud_first.hip",
            "laud_probe.hip", "laud_tail.hip", "laud_head.hip", "laud_norm.hip", "laud_matmul8.hip", "laud_moe.hip"]
 # packed-fp32 code generation is switched off for device code (the host pass warns that it
@@ -33,9 +35,22 @@ def _run(cmd, verbose):
     err = "\n".join(l for l in res.stderr.splitlines() if "is not a recognized feature" not in l)
     if res.returncode != 0:
         sys.stderr.write(err + "\n")
-        raise RuntimeError("hipcc failed: " + " ".join(cmd[-3:]))
+        raise RuntimeError(os.path.basename(cmd[0]) + " failed: " + " ".join(cmd[-3:]))
     if verbose and err.strip():
         print(err)
+
+
+def extension_command() -> list[str]:
+    """The host compiler's command for _laud_torch.so (host code only: Python, torch and HIP runtime headers)."""
+    import sysconfig
+
+    import torch
+    home = os.path.dirname(torch.__file__)
+    include = [os.path.join(home, "include"), os.path.join(home, "include", "torch", "csrc", "api", "include"), "/opt/rocm/include"]
+    return [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-shared", "-fPIC", "-D__HIP_PLATFORM_AMD__=1", "-DUSE_ROCM=1",
+            "-I", os.path.join(ROOT, "include"), "-I", sysconfig.get_paths()["include"],
+            *(a for d in include for a in ("-isystem", d)), os.path.join(CSRC, "laud_torch.cpp"), "-o", EXTENSION,
+            "-L", os.path.join(home, "lib"), "-lc10", "-lc10_hip", "-ltorch_cpu", "-ltorch_python"]
 
 
 def build(verbose: bool = True) -> str:
@@ -43,6 +58,7 @@ def build(verbose: bool = True) -> str:
     os.makedirs(OBJ, exist_ok=True)
     objs = [os.path.join(OBJ, s.replace(".hip", ".o")) for s in SOURCES]
     jobs = [[hipcc, *FLAGS, "-c", os.path.join(CSRC, s), "-o", o] for s, o in zip(SOURCES, objs)]
+    jobs.append(extension_command())
     with ThreadPoolExecutor(max_workers=min(8, len(jobs))) as ex:
         list(ex.map(lambda c: _run(c, verbose), jobs))
     _run([hipcc, "--offload-arch=gfx950", "-shared", "-fPIC", *objs, "-o", LIB], verbose)
