@@ -22,8 +22,8 @@ struct MoeArgs {
   unsigned* arrived;    // [column tiles of the last product]: workgroups that are done, 0 behind the routing
 };
 
-// A workgroup of the last product has 16 * NC output channels.
-__host__ __device__ inline int column_tiles(int C, int nc) { return (C - 1) / (16 * nc) + 1; }
+constexpr int kColumns = 32;  // output channels of a workgroup of the last product
+__host__ __device__ inline int column_tiles(int C) { return (C - 1) / kColumns + 1; }
 
 // ---- routing ----------------------------------------------------------------------------------------------------------------
 // Floats as unsigned integers in their order; a NaN lies below all.
@@ -85,7 +85,7 @@ __global__ __launch_bounds__(kRouteThreads) void k_moe_route(MoeArgs a) {
   __shared__ uint8_t chosen[kMaxExperts];
   const int t = blockIdx.x, lane = lane_id(), wave = threadIdx.x / kWave;
   if (t == 0)
-    for (int i = threadIdx.x; i < column_tiles(a.C, 2); i += kRouteThreads) a.arrived[i] = 0;
+    for (int i = threadIdx.x; i < column_tiles(a.C); i += kRouteThreads) a.arrived[i] = 0;
   int32_t* experts = a.experts + (long long)t * a.top_k;
   float* weights = a.weights + (long long)t * a.top_k;
   if (a.keep && a.keep[t] == 0) {
@@ -185,17 +185,20 @@ __device__ __forceinline__ int find_entries(const MoeArgs& a, const Slot& s, int
   return counts[1] ? 0 : counts[0];
 }
 
-// Sums of the S waves' parts of N row tiles, in the waves' order: tile i's for wave i.
-template <int S, int N>
-__device__ __forceinline__ void join_waves(f32x4 (&v)[N], f32x4 (*part)[N][kWave], int wave, int lane) {
-#pragma unroll
-  for (int i = 0; i < N; ++i) part[wave][i][lane] = v[i];
+// Sums of the S waves' parts of two row tiles, in the waves' order, for the first wave.
+template <int S>
+__device__ __forceinline__ void join_waves(f32x4 (&v)[2], f32x4 (*part)[2][kWave], int wave, int lane) {
+  part[wave][0][lane] = v[0];
+  part[wave][1][lane] = v[1];
   __syncthreads();
-  if (wave < N) {
-    v[0] = part[0][wave][lane];
+  if (wave == 0) {
 #pragma unroll
-    for (int w = 1; w < S; ++w) v[0] += part[w][wave][lane];
+    for (int w = 1; w < S; ++w) {
+      v[0] += part[w][0][lane];
+      v[1] += part[w][1][lane];
+    }
   }
+  __syncthreads();
 }
 
 // Waves of a workgroup, which share the reduction by blocks of 128: half as many where a block is half the bytes (16 tokens, 64
@@ -261,13 +264,7 @@ __global__ __launch_bounds__(kSplit<W> * kWave) void k_moe_up(MoeArgs a) {
         v[1][i] = fmaf(pu[i], fu, v[1][i]);
       }
     }
-    join_waves<S, 2>(v, part, wave, lane);
-    if (wave == 0) {
-      v[1] = part[0][1][lane];
-#pragma unroll
-      for (int w = 1; w < S; ++w) v[1] += part[w][1][lane];
-    }
-    __syncthreads();
+    join_waves<S>(v, part, wave, lane);
     if (wave == 0 && real) {
       f32x4 h;
 #pragma unroll
@@ -296,16 +293,15 @@ __device__ __forceinline__ float shared_load(const float* p) {
   return __hip_atomic_load(const_cast<float*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
-// One expert's entries for 16 * NC output channels, weighted; the last workgroup of a tile of channels to get here adds each token's
+// One expert's entries for 32 output channels, weighted; the last workgroup of a tile of channels to get here adds each token's
 // entries up, in the order of its experts.
-template <int W, typename OT, int NC>
+template <int W, typename OT>
 __global__ __launch_bounds__(kSplit<W> * kWave) void k_moe_down(MoeArgs a) {
   typedef Weights<W> WT;
-  constexpr int S = kSplit<W>, kColumns = 16 * NC, kXP = W == W_E4M3 ? 2 : 1;
+  constexpr int S = kSplit<W>;
   constexpr unsigned kHb = W == W_F32 ? 4 : 2;  // bytes of a hidden value in a plane
-  static_assert(NC <= S && kScaleBlock % kColumns == 0, "a wave a row tile of the sums, one scale a tile");
   __shared__ int list[LAUD_MOE_MAX_TOKENS], counts[2];
-  __shared__ f32x4 part[S][NC][kWave];
+  __shared__ f32x4 part[S][2][kWave];
   __shared__ unsigned place;
   const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), r16 = lane % 16, quarter = lane / 16;
   const Slot slot = slot_of(a);
@@ -314,14 +310,14 @@ __global__ __launch_bounds__(kSplit<W> * kWave) void k_moe_down(MoeArgs a) {
   const long long row_bytes = (long long)a.F * WT::kBytes;
   const __amdgpu_buffer_rsrc_t rw =
       bytes_of(reinterpret_cast<const uint8_t*>(a.down) + ((long long)max(slot.expert, 0) * a.C + c0) * row_bytes, rows * row_bytes);
-  tok_u4 w[NC][WT::kPieces];
+  tok_u4 w0[WT::kPieces], w1[WT::kPieces];
   auto request = [&](int kb) {
 #pragma unroll
     for (int p = 0; p < WT::kPieces; ++p) {
       const int k = kb * kScaleBlock + WT::first(p, quarter);
-#pragma unroll
-      for (int n = 0; n < NC; ++n)
-        w[n][p] = load16(rw, k < a.F && n * 16 + r16 < rows ? (unsigned)((n * 16 + r16) * row_bytes) + (unsigned)k * WT::kBytes : kOutside);
+      const unsigned off = (unsigned)(r16 * row_bytes) + (unsigned)k * WT::kBytes;
+      w0[p] = load16(rw, k < a.F && r16 < rows ? off : kOutside);
+      w1[p] = load16(rw, k < a.F && 16 + r16 < rows ? off + (unsigned)(16 * row_bytes) : kOutside);
     }
   };
   if (kEarly<W> && slot.early) request(wave);
@@ -336,37 +332,43 @@ __global__ __launch_bounds__(kSplit<W> * kWave) void k_moe_down(MoeArgs a) {
       const bool real = l0 + r16 < len;
       const unsigned at = (unsigned)entry * (unsigned)a.Fp * kHb;
       const float share = a.weights[entry];
-      f32x4 v[NC] = {};
+      f32x4 v[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
       for (int kb = wave; kb < kb_all; kb += S) {
         if (!kEarly<W> || kb != wave || l0 != 0) request(kb);
         const float f = s ? s[kb] : 1.f;
-        f32x4 q[NC] = {};
+        f32x4 p0 = {0.f, 0.f, 0.f, 0.f}, p1 = p0;
 #pragma unroll
         for (int p = 0; p < WT::kPieces; ++p) {
           const int k = kb * kScaleBlock + WT::first(p, quarter);
+          constexpr int kXP = W == W_E4M3 ? 2 : 1;
 #pragma unroll
           for (int i = 0; i < kHiddenPlanes<W>; ++i) {
             tok_u4 x[kXP];
 #pragma unroll
             for (int u = 0; u < kXP; ++u) x[u] = load16(rh, real ? i * plane + at + (unsigned)(k + 8 * u) * kHb : kOutside);
-#pragma unroll
-            for (int n = 0; n < NC; ++n) q[n] = mma_stored<W>(w[n][p], x, q[n]);
+            p0 = mma_stored<W>(w0[p], x, p0);
+            p1 = mma_stored<W>(w1[p], x, p1);
           }
         }
 #pragma unroll
-        for (int n = 0; n < NC; ++n)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) v[n][i] = fmaf(q[n][i], f, v[n][i]);
+        for (int i = 0; i < 4; ++i) {
+          v[0][i] = fmaf(p0[i], f, v[0][i]);
+          v[1][i] = fmaf(p1[i], f, v[1][i]);
+        }
       }
-      join_waves<S, NC>(v, part, wave, lane);
-      if (wave < NC && real && wave * 16 + quarter * 4 < rows)
-        shared_store(a.y + (long long)entry * a.C + c0 + wave * 16 + quarter * 4, v[0] * share);
-      __syncthreads();
+      join_waves<S>(v, part, wave, lane);
+      if (wave == 0 && real) {
+        float* y = a.y + (long long)entry * a.C + c0;
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+          if (i * 16 + quarter * 4 < rows) shared_store(y + i * 16 + quarter * 4, v[i] * share);
+      }
     }
   }
-  vm_wait<0>();  // (the stores have arrived before the workgroup counts as done)
-  __syncthreads();
-  if (threadIdx.x == 0) place = __hip_atomic_fetch_add(a.arrived + blockIdx.x, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  if (wave == 0) {
+    vm_wait<0>();  // (the stores, all of them this wave's, have arrived before the workgroup counts as done)
+    if (lane == 0) place = __hip_atomic_fetch_add(a.arrived + blockIdx.x, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }
   __syncthreads();
   if (place + 1 != gridDim.y) return;
   for (int i = threadIdx.x; i < a.T * (kColumns / 4); i += S * kWave) {
@@ -388,15 +390,7 @@ void launch_moe(const MoeArgs& a, hipStream_t st) {
   hipLaunchKernelGGL((k_moe_route<ET>), dim3(a.T), dim3(kRouteThreads), 0, st, a);
   const unsigned slots = (unsigned)min((long long)a.E, (long long)a.T * a.top_k);
   hipLaunchKernelGGL((k_moe_up<W>), dim3(a.Fp / 16, slots), dim3(kSplit<W> * kWave), 0, st, a);
-  // 64 channels a workgroup where those of 8-bit weights fill the chip four times over: h is read half as often (16 tokens, 64 experts
-  // of 2048 x 1424: the launch 55 -> 45 us; 64 tokens, 2048 x 1024 in bf16: 79 -> 82, its waves have twice the registers).
-  if constexpr (W == W_E4M3) {
-    if ((long long)slots * column_tiles(a.C, 4) >= 1024) {
-      hipLaunchKernelGGL((k_moe_down<W, ET, 4>), dim3(column_tiles(a.C, 4), slots), dim3(kSplit<W> * kWave), 0, st, a);
-      return;
-    }
-  }
-  hipLaunchKernelGGL((k_moe_down<W, ET, 2>), dim3(column_tiles(a.C, 2), slots), dim3(kSplit<W> * kWave), 0, st, a);
+  hipLaunchKernelGGL((k_moe_down<W, ET>), dim3(column_tiles(a.C), slots), dim3(kSplit<W> * kWave), 0, st, a);
 }
 
 struct MoeWs { size_t experts, weights, h, y, arrived, bytes; };
@@ -408,7 +402,7 @@ MoeWs moe_ws(const laud_moe_layer* p, int T) {
   w.h = w.weights + align_up(n * 4, 256);
   w.y = align_up(w.h + n * (size_t)scale_blocks(p->F) * kScaleBlock * 4, 256);
   w.arrived = align_up(w.y + n * (size_t)p->C * 4, 256);
-  w.bytes = w.arrived + (size_t)column_tiles(p->C, 2) * 4;
+  w.bytes = w.arrived + (size_t)column_tiles(p->C) * 4;
   return w;
 }
 
