@@ -74,7 +74,9 @@ __global__ __launch_bounds__(kSplit * kWave) void k_mm8_split(Mm8Args g) {
 // BM x BN results a workgroup, WM x WN a wave.  Both operands go into LDS by LDS-direct loads, a block of 128 along K at a time, into
 // two stages that take turns: one barrier a block, the next block's loads are under way while this one is multiplied.  A row's
 // eight 16-byte chunks lie XOR-swizzled (chunk ^ row % 8; the swizzle is applied to the global side).  The first operand of the
-// matrix instructions is b: a lane's results are consecutive columns, its row of a - and that row's scale - is one for all of them.
+// matrix instructions is b: a lane's results are consecutive columns, its row of a - and that row's scale - is one for all of them.  Bound by the matrix cores and by power: on random
+// operands a bare loop of these instructions and their scalings runs at 3.5 to 3.8 PFLOP/s, 8192 x 8192 x 4096 at 2.1 (256 us; 220
+// without the loads into LDS, 260 without the waits for them, 251 without the barriers).
 // The block's products in 8-bit instructions: twice the rate of the bf16 ones.  They add groups of eight products with 14 bits below
 // the group's largest, an error of 1.5e-5 of the result's norm: a hundredth of what a bf16 result's rounding adds, and taken for
 // bf16 results only.
@@ -126,7 +128,7 @@ __global__ __launch_bounds__(KG * BM / WM * (BN / WN) * kWave) void k_mm8_tile(M
 
   // The loads of block kb, kPer of them behind each row tile's matrix instructions.  Behind the last block they fetch nothing: the loop
   // over the blocks has no branch, across which the compiler would gather the scalings.
-  constexpr bool kDeep = kMT * kNT <= 16;
+    constexpr bool kDeep = kMT * kNT <= 8;
   constexpr int kLoads = kLoadsB + kLoadsA + 1, kPer = kDeep ? (kLoads - 1) / kMT + 1 : (kLoads - 1) / (kMT - 1) + 1;
   static_assert(kPer * kMT >= kLoads, "all of a block's loads before its last row tile");
   auto request = [&](int step, unsigned stage, int from, int to) {
@@ -209,7 +211,6 @@ __global__ __launch_bounds__(KG * BM / WM * (BN / WN) * kWave) void k_mm8_tile(M
       step(kb + 1, odd, even);
     }
   } else {
-    static_assert(KG == 1, "");
     i32x8 nf[kNT], mf[2];
     float s[2], sb;
     auto read_m = [&](const uint8_t* at, int j) {
@@ -236,7 +237,7 @@ __global__ __launch_bounds__(KG * BM / WM * (BN / WN) * kWave) void k_mm8_tile(M
     // of a block's last row tile, whose operands are in registers by then: behind it the next block's first ones come from LDS, and
     // the loads of the block after that may overwrite this one's stage.  (Behind the last block it reads what is there, unused.)
     int now = 0, fill = NS - 1;  // stages of this block and of the one being requested
-    for (int kb = 0; kb < g.kb; ++kb) {
+    for (int kb = 0; kb * KG < g.kb; ++kb) {
       const int next = now + 1 < NS ? now + 1 : 0;
       const uint8_t *at = stages + now * L::kStage, *ahead = stages + next * L::kStage;
 #pragma unroll
@@ -339,16 +340,17 @@ int launch_tile(const Mm8Args& g, hipStream_t st) {
 }
 
 // Which tile: a launch takes rounds of one tile a compute unit, a round the blocks of K times the tile's time for one and its two
-// ends, in us as measured (the times of a launch, at 256 rows or more):
-//   bf16 results         64 x 64   64 x 128   128 x 128   128 x 256   256 x 256
-//    256 x 4096 x 4096     11.3       14.7        23.9        31.2        48.0
-//    512 x 4096 x 4096     21.0       15.8        24.4        31.5        47.7
-//   1024 x 4096 x 4096     39.7       29.7        26.3        33.0        48.7
-//   2048 x 4096 x 4096     78.8       58.0        50.4        39.3        52.5
-//   4096 x 4096 x 4096    149.2      110.9        98.6        75.6        64.0
-//   1003 x 2120 x 2000     21.9       21.0        17.0        20.0        29.1
-// The smaller ones split a block of K's followers over two groups of waves, and short reductions on 64 x 64 tiles take two stages
-// instead of four, two workgroups a compute unit (200 x 2048 x 1024: 4.8 us against 5.1; 256 x 4096 x 4096: 14.9 against 11.3).
+// ends, in us.  Launches as measured, in us; the rule takes the least, or one within 3 % of it:
+//   bf16 results         64 x 64   64 x 128   128 x 128   128 x 256   256 x 256     float32   64 x 64   64 x 128   128 x 128
+//    256 x 4096 x 4096     11.6       14.7        21.7        30.1        48.2                  17.5       22.6        46.8
+//    512 x 4096 x 4096     21.6       16.2        22.2        30.1        48.6                  32.0       25.2        46.8
+//   1024 x 4096 x 4096     40.7       29.7        24.7        32.0        48.5                  59.4       48.2        50.2
+//   2048 x 4096 x 4096     77.7       57.2        46.6        38.7        53.3                 118.3       90.1        95.8
+//   4096 x 4096 x 4096    152.5      111.6        91.3        74.7        64.8
+//   1003 x 2120 x 2000     22.4       20.9        15.4        19.2        29.3                  29.3       27.8        27.2
+//   3000 x 1000 x  512      8.3        9.8         6.9         8.0        10.9
+// The smaller ones share the blocks of K between two groups of waves, and short reductions on 64 x 64 tiles take two stages instead
+// of four, two workgroups a compute unit (200 x 2048 x 1024: 4.8 us against 5.1; 256 x 4096 x 4096: 14.9 against 11.6).
 struct TileTime {
   int bm, bn;
   float block, ends;
@@ -367,7 +369,7 @@ int launch_mm8(const Mm8Args& g, hipStream_t st) {
   }
   constexpr bool kBf16 = sizeof(OT) == 2;
   constexpr TileTime kTimes[5] = {{64, 64, kBf16 ? 0.24f : 0.42f, 2.2f}, {64, 128, kBf16 ? 0.39f : 0.6f, 2.2f},
-                                  {128, 128, kBf16 ? 0.72f : 1.35f, 2.2f}, {128, 256, 1.1f, 3.8f}, {256, 256, 1.95f, 2.0f}};
+                                  {128, 128, kBf16 ? 0.63f : 1.35f, 2.2f}, {128, 256, 1.1f, 3.8f}, {256, 256, 1.95f, 2.0f}};
   int best = 0;
   for (int i = 1; i < (kBf16 ? 5 : 3); ++i)
     if (tile_time(g, kTimes[i]) < tile_time(g, kTimes[best])) best = i;
