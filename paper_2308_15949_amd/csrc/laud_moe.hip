@@ -273,12 +273,14 @@ __global__ __launch_bounds__(kSplit<W> * kWave) void k_moe_up(MoeArgs a) {
       if constexpr (kHiddenPlanes<W> == 1) {
         *reinterpret_cast<f32x4*>(reinterpret_cast<float*>(a.h) + at) = h;
       } else {
-        typedef __attribute__((ext_vector_type(4))) __bf16 b4;
-        const b4 hi = __builtin_convertvector(h, b4);
-        const b4 lo = __builtin_convertvector(h - __builtin_convertvector(hi, f32x4), b4);
+        const tok_u2 hi = {pack_bf16(h[0], h[1]), pack_bf16(h[2], h[3])};
+        f32x4 rest;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) rest[i] = h[i] - __uint_as_float(i % 2 ? hi[i / 2] & 0xffff0000u : hi[i / 2] << 16);
+        const tok_u2 lo = {pack_bf16(rest[0], rest[1]), pack_bf16(rest[2], rest[3])};
         bf16_t* plane = reinterpret_cast<bf16_t*>(a.h) + at;
-        *reinterpret_cast<tok_u2*>(plane) = __builtin_bit_cast(tok_u2, hi);
-        *reinterpret_cast<tok_u2*>(plane + (long long)a.T * a.top_k * a.Fp) = __builtin_bit_cast(tok_u2, lo);
+        *reinterpret_cast<tok_u2*>(plane) = hi;
+        *reinterpret_cast<tok_u2*>(plane + (long long)a.T * a.top_k * a.Fp) = lo;
       }
     }
   }
@@ -287,7 +289,10 @@ __global__ __launch_bounds__(kSplit<W> * kWave) void k_moe_up(MoeArgs a) {
 // Values that workgroups on different XCDs hand over within a launch go past the XCDs' caches, which do not see each other (a
 // release and an acquire by every workgroup instead, which write back and drop a whole cache, made the launch three times as long).
 __device__ __forceinline__ void shared_store(float* p, const f32x4& v) {
-  asm volatile("global_store_dwordx4 %0, %1, off sc1" ::"v"(p), "v"(v) : "memory");
+  typedef unsigned long long u64;
+  const tok_u2 lo = {__float_as_uint(v[0]), __float_as_uint(v[1])}, hi = {__float_as_uint(v[2]), __float_as_uint(v[3])};
+  __hip_atomic_store(reinterpret_cast<u64*>(p), __builtin_bit_cast(u64, lo), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  __hip_atomic_store(reinterpret_cast<u64*>(p) + 1, __builtin_bit_cast(u64, hi), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 __device__ __forceinline__ float shared_load(const float* p) {
   return __hip_atomic_load(const_cast<float*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);

@@ -300,8 +300,8 @@ void launch_quant(const void* x, int64_t ldx, int rows, int cols, int block_rows
   const int kb = scale_blocks(cols);
   if (block_rows == 1) {
     const long long blocks = (long long)rows * kb;
-    hipLaunchKernelGGL((k_quant_rows<ET>), dim3((unsigned)min((blocks + 15) / 16, (long long)kMostGroups)), dim3(256), 0, st, (const ET*)x, ldx, blocks, kb, cols,
-                       (uint8_t*)q, ldq, scale);
+    hipLaunchKernelGGL((k_quant_rows<ET>), dim3((unsigned)min((blocks + 15) / 16, (long long)kMostGroups)), dim3(256), 0, st, (const ET*)x, ldx,
+                       blocks, kb, cols, (uint8_t*)q, ldq, scale);
   } else {
     const int rbs = scale_blocks(rows), per = min(rbs, 32768);
     hipLaunchKernelGGL((k_quant_square<ET>), dim3((unsigned)kb, (unsigned)per, (unsigned)((rbs + per - 1) / per)), dim3(256), 0, st,

@@ -65,13 +65,8 @@ template <> struct piece8<bf16_t> {
     }
   }
   __device__ __forceinline__ void put(const float (&f)[8]) {
-    typedef __attribute__((ext_vector_type(2))) __bf16 b2;
-    typedef __attribute__((ext_vector_type(2))) float f2;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const f2 w = {f[2 * e], f[2 * e + 1]};
-      v[e] = __builtin_bit_cast(unsigned, __builtin_convertvector(w, b2));  // nearest even
-    }
+    for (int e = 0; e < 4; ++e) v[e] = pack_bf16(f[2 * e], f[2 * e + 1]);  // nearest even
   }
 };
 template <> struct piece8<float> {
@@ -150,8 +145,7 @@ __device__ __forceinline__ void store4(OT* out, const f32x4& v) {
   if constexpr (sizeof(OT) == 4) {
     *reinterpret_cast<f32x4*>(out) = v;
   } else {
-    typedef __attribute__((ext_vector_type(4))) __bf16 b4;
-    *reinterpret_cast<tok_u2*>(out) = __builtin_bit_cast(tok_u2, __builtin_convertvector(v, b4));
+    *reinterpret_cast<tok_u2*>(out) = tok_u2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
   }
 }
 

@@ -80,6 +80,15 @@ struct Pair {
   unsigned v[2];
   unsigned operator[](int i) const { return v[i]; }
 };
+struct Zero {  // whatever a conversion instruction returns
+  template <typename T>
+  operator T() const { return T{}; }
+};
+// the lane that a data-parallel move inside a row of sixteen lanes reads
+static inline int moved_lane(int control) {
+  const int l = current->lane;
+  return control == 0xB1 ? l ^ 1 : control == 0x4E ? l ^ 2 : control == 0x141 ? l ^ 7 : control == 0x140 ? l ^ 15 : l;
+}
 static inline int lanes_below(unsigned mask, int first) {  // set bits of 32 lanes from `first` on, below the calling lane
   const int n = std::min(std::max(current->lane - first, 0), 32);
   return __builtin_popcount(n < 32 ? mask & ((1u << n) - 1) : mask);
@@ -108,6 +117,16 @@ static inline int lanes_below(unsigned mask, int first) {  // set bits of 32 lan
 #define __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, x, y, z) (c)
 #define __builtin_amdgcn_mfma_f32_32x32x2f32(a, b, c, x, y, z) (c)
 #define __builtin_amdgcn_permlane32_swap(a, b, c, d) (host::Pair{{a, b}})
+#define __builtin_amdgcn_permlane16_swap(a, b, c, d) (host::Pair{{a, b}})
+#define __builtin_amdgcn_update_dpp(o, v, c, r, b, z) host::shuffle(host::FROM, v, host::moved_lane(c))
+#define __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, x, y, z, u, v, w) (c)
+#define __builtin_amdgcn_cvt_pk_fp8_f32(a, b, old, hi) (old)
+#define __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, s, hi) host::Zero()
+#define __HIP_MEMORY_SCOPE_AGENT 0
+#define __hip_atomic_store(p, v, order, scope) (*(p) = (v))
+#define __hip_atomic_load(p, order, scope) (*(p))
+#define __hip_atomic_fetch_add(p, v, order, scope) __atomic_fetch_add(p, v, __ATOMIC_RELAXED)
+#define atomicAdd(p, v) __atomic_fetch_add(p, v, __ATOMIC_RELAXED)
 #define __builtin_amdgcn_readfirstlane(x) (x)
 #define __builtin_amdgcn_sched_barrier(x)
 #define __builtin_amdgcn_s_setprio(x)
