@@ -456,7 +456,7 @@ def make_norm_block(c: int, dtype, kind: str, eps: float, post_w=None, post_b=No
 
 
 def laud_norm_residual(p: NormBlock, x, y=None, keep=None, gate=None, rows_per_gate: int = 0, out=None, z=None, z_scale=None) -> None:
-    """x, y, out, z [rows][C]; keep [rows] bytes; gate [ceil(rows / rows_per_gate)][C] float32; z float8_e4m3fn with
+    """x, y, out, z [rows][C]; keep [rows] bytes; gate [ceil(rows / rows_per_gate) or more][C] float32; z float8_e4m3fn with
     z_scale [rows][ceil(C / 128)], or of x's type."""
     s = (_calls or _token_calls()).norm_residual(p, x, y, keep, gate, rows_per_gate, out, z, z_scale)
     if s:

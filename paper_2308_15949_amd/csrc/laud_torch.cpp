@@ -57,11 +57,13 @@ Rows rows(PyObject* o, int64_t n, int64_t c) {
   if (r.n != n || r.c != c) throw Refused{};
   return r;
 }
-// A dense float32 matrix; None: null.
-float* floats(PyObject* o, int64_t n, int64_t c) {
+// A dense float32 matrix, of n rows or, with `more`, of at least as many; None: null.
+float* floats(PyObject* o, int64_t n, int64_t c, bool more = false) {
   if (o == Py_None) return nullptr;
   const at::Tensor& t = tensor(o);
-  if (t.scalar_type() != at::kFloat || t.dim() != 2 || t.size(0) != n || t.size(1) != c || !t.is_contiguous()) throw Refused{};
+  if (t.scalar_type() != at::kFloat || t.dim() != 2 || t.size(0) < n || (!more && t.size(0) != n) || t.size(1) != c ||
+      !t.is_contiguous())
+    throw Refused{};
   return static_cast<float*>(t.data_ptr());
 }
 // A byte (or truth value) per row; None: null.
@@ -139,7 +141,7 @@ PyObject* norm_residual(PyObject*, PyObject* const* a, Py_ssize_t n) {
     float* gate = nullptr;
     if (a[4] != Py_None) {
       if (per <= 0) throw Refused{};
-      gate = floats(a[4], (x.n + per - 1) / per, x.c);
+      gate = floats(a[4], (x.n + per - 1) / per, x.c, true);
     }
     float* zs = z_dtype == LAUD_E4M3 ? floats(a[8], x.n, blocks(x.c)) : nullptr;
     return p_norm(&p, (int)x.n, x.p, x.ld, y.p, y.ld, bytes(a[3], x.n), gate, (int)per, out.p, out.ld, z.p, z.ld, z_dtype, zs, stream());

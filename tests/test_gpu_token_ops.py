@@ -109,6 +109,19 @@ def test_norm_rows_strides_and_masks(rows):
     norm_case(rows, 640, torch.float32, "rms", rows, post=False, keep=np.ones(rows), z=None, inplace=True)
 
 
+@pytest.mark.parametrize("rows,per,gates", [(16, 3, 7), (5, 2, 3), (3, 4, 9)])
+def test_norm_gates_that_no_row_has(rows, per, gates):
+    g = gen(rows)
+    x, y, gate, w = rand(g, rows, 264), rand(g, rows, 264), rand(g, gates, 264), torch.ones(264, device="cuda")
+    p = L.make_norm_block(264, torch.float32, "rms", 1e-5, w)
+    few, more = (torch.zeros(rows, 264, device="cuda") for _ in range(2))
+    L.laud_norm_residual(p, x.cuda(), y.cuda(), None, gate[: -(-rows // per)].cuda(), per, few)
+    L.laud_norm_residual(p, x.cuda(), y.cuda(), None, gate.cuda(), per, more)
+    assert torch.equal(few, more) and not torch.equal(few.cpu(), x)
+    with pytest.raises(L.LaudError):
+        L.laud_norm_residual(p, x.cuda(), y.cuda(), None, gate[: -(-rows // per) - 1].cuda(), per, more)
+
+
 def test_norm_alone_and_no_rows():
     x = rand(gen(1), 6, 520).cuda()
     w = torch.linspace(0.5, 1.5, 520).cuda()
