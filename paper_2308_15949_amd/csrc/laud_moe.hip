@@ -19,6 +19,7 @@ struct MoeArgs {
   float* weights;       // [T][top_k]
   void* h;              // [T * top_k][Fp] float32, or two planes of it in bf16
   float* y;             // [T * top_k][C]: an entry's weighted result
+  float* logits;        // [E], of a single token
   unsigned* arrived;    // [column tiles of the last product]: workgroups that are done, 0 behind the routing
 };
 
@@ -32,14 +33,41 @@ __device__ __forceinline__ unsigned order_key(float f) {
   return f != f ? 0u : (u & 0x80000000u) ? ~u : u | 0x80000000u;
 }
 
-constexpr int kRouteThreads = 1024;
+constexpr int kRouteThreads = 1024, kLogitWaves = 4;
 
-// The choice of one token by its workgroup from logits [E] in LDS: an expert is chosen if fewer than top_k come before it, and
-// sixteen lanes count those of one expert.
-__device__ __forceinline__ void choose_experts(const float* logits, uint8_t* chosen, int E, int top_k, bool renormalise, float scale,
-                                               int32_t* experts, float* weights) {
+// The logits of N experts from e0 on, by one wave.
+template <typename ET, int N>
+__device__ __forceinline__ void router_logits(const MoeArgs& a, const ET* x, int e0, float* logits) {
   const int lane = lane_id();
-  for (int e0 = 0; e0 < E; e0 += kRouteThreads / 16) {
+  float s[N] = {};
+#pragma unroll 4
+  for (int c = lane; c < a.C / 8; c += kWave) {
+    piece8<ET> p, q[N];
+    float f[8], g[8];
+    p.load(x, c);
+#pragma unroll
+    for (int i = 0; i < N; ++i) q[i].load(reinterpret_cast<const ET*>(a.router) + (long long)min(e0 + i, a.E - 1) * a.C, c);
+    p.get(f);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      q[i].get(g);
+#pragma unroll
+      for (int u = 0; u < 8; ++u) s[i] = fmaf(f[u], g[u], s[i]);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    s[i] = lanes64_sum(s[i]);
+    if (lane == 0 && e0 + i < a.E) logits[e0 + i] = s[i];
+  }
+}
+
+// The choice of one token by a workgroup of THREADS from logits [E] in LDS, and its weights: an expert is chosen if fewer than top_k
+// come before it, and sixteen lanes count those of one expert.  The first wave writes both.
+template <int THREADS>
+__device__ __forceinline__ void choose_experts(const MoeArgs& a, const float* logits, uint8_t* chosen, int32_t* experts, float* weights) {
+  const int lane = lane_id(), E = a.E;
+  for (int e0 = 0; e0 < E; e0 += THREADS / 16) {
     const int e = e0 + (int)threadIdx.x / 16;
     if (e >= E) continue;  // (sixteen lanes at a time)
     const unsigned key = order_key(logits[e]);
@@ -49,7 +77,7 @@ __device__ __forceinline__ void choose_experts(const float* logits, uint8_t* cho
       before += k > key || (k == key && j < e);
     }
     const float n = lanes16_sum((float)before);
-    if (threadIdx.x % 16 == 0) chosen[e] = n < (float)top_k;
+    if (threadIdx.x % 16 == 0) chosen[e] = n < (float)a.top_k;
   }
   __syncthreads();
   if ((int)threadIdx.x >= kWave) return;
@@ -62,7 +90,7 @@ __device__ __forceinline__ void choose_experts(const float* logits, uint8_t* cho
   float sum = 0.f;
   for (int e = lane; e < E; e += kWave) {
     const float p = expf(logits[e] - top);
-    if (!renormalise || chosen[e] || p != p) sum += p;  // (a NaN anywhere is in every softmax value)
+    if (!a.renormalise || chosen[e] || p != p) sum += p;  // (a NaN anywhere is in every softmax value)
   }
   sum = lanes64_sum(sum);
   int before = 0;
@@ -72,7 +100,7 @@ __device__ __forceinline__ void choose_experts(const float* logits, uint8_t* cho
     if (mine) {
       const int at = before + ballot_prefix(b);
       experts[at] = e0 + lane;
-      weights[at] = expf(logits[e0 + lane] - top) / sum * scale;
+      weights[at] = expf(logits[e0 + lane] - top) / sum * a.scale;
     }
     before += __popcll(b);
   }
@@ -83,7 +111,7 @@ template <typename ET>
 __global__ __launch_bounds__(kRouteThreads) void k_moe_route(MoeArgs a) {
   __shared__ float logits[kMaxExperts];
   __shared__ uint8_t chosen[kMaxExperts];
-  const int t = blockIdx.x, lane = lane_id(), wave = threadIdx.x / kWave;
+  const int t = blockIdx.x, wave = threadIdx.x / kWave;
   if (t == 0)
     for (int i = threadIdx.x; i < column_tiles(a.C); i += kRouteThreads) a.arrived[i] = 0;
   int32_t* experts = a.experts + (long long)t * a.top_k;
@@ -92,33 +120,19 @@ __global__ __launch_bounds__(kRouteThreads) void k_moe_route(MoeArgs a) {
     if ((int)threadIdx.x < a.top_k) { experts[threadIdx.x] = -1; weights[threadIdx.x] = 0.f; }
     return;
   }
-  const ET* x = reinterpret_cast<const ET*>(a.x) + t * a.ldx;
   constexpr int kAtOnce = 4;  // experts a wave takes at a time, so that their loads are under way together
-  for (int e0 = wave * kAtOnce; e0 < a.E; e0 += kRouteThreads / kWave * kAtOnce) {
-    float s[kAtOnce] = {};
-#pragma unroll 4
-    for (int c = lane; c < a.C / 8; c += kWave) {
-      piece8<ET> p, q[kAtOnce];
-      float f[8], g[8];
-      p.load(x, c);
-#pragma unroll
-      for (int i = 0; i < kAtOnce; ++i) q[i].load(reinterpret_cast<const ET*>(a.router) + (long long)min(e0 + i, a.E - 1) * a.C, c);
-      p.get(f);
-#pragma unroll
-      for (int i = 0; i < kAtOnce; ++i) {
-        q[i].get(g);
-#pragma unroll
-        for (int u = 0; u < 8; ++u) s[i] = fmaf(f[u], g[u], s[i]);
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < kAtOnce; ++i) {
-      s[i] = lanes64_sum(s[i]);
-      if (lane == 0 && e0 + i < a.E) logits[e0 + i] = s[i];
-    }
-  }
+  for (int e0 = wave * kAtOnce; e0 < a.E; e0 += kRouteThreads / kWave * kAtOnce)
+    router_logits<ET, kAtOnce>(a, reinterpret_cast<const ET*>(a.x) + t * a.ldx, e0, logits);
   __syncthreads();
-  choose_experts(logits, chosen, a.E, a.top_k, a.renormalise != 0, a.scale, experts, weights);
+  choose_experts<kRouteThreads>(a, logits, chosen, experts, weights);
+}
+
+// A single token's logits, an expert a wave over many workgroups, where one workgroup would wait for its share of the memory's rate;
+// the workgroups of the first product then choose, each for itself.  (One token, 8 of 64 experts of 2048 x 1024, bf16: 32.0 -> 30.9 us.)
+template <typename ET>
+__global__ __launch_bounds__(kLogitWaves * kWave) void k_moe_logits(MoeArgs a) {
+  const int e = blockIdx.x * kLogitWaves + (int)threadIdx.x / kWave;
+  if (e < a.E && !(a.keep && a.keep[0] == 0)) router_logits<ET, 1>(a, reinterpret_cast<const ET*>(a.x), e, a.logits);
 }
 
 // ---- products -----------------------------------------------------------------------------------------------------------------
@@ -208,15 +222,35 @@ template <int W> constexpr int kSplit = W == W_E4M3 ? 4 : 8;
 // the other types need the registers that this takes for a third workgroup on a compute unit (208 -> 219).
 template <int W> constexpr bool kEarly = W == W_E4M3;
 
-// h of one expert's entries for 16 hidden channels.
-template <int W>
+// h of one expert's entries for 16 hidden channels; ONE: of one entry of the single token.
+template <int W, bool ONE>
 __global__ __launch_bounds__(kSplit<W> * kWave) void k_moe_up(MoeArgs a) {
   typedef Weights<W> WT;
   constexpr int S = kSplit<W>, kXP = W == W_E4M3 ? 2 : 1, xb = W == W_F32 ? 4 : 2;
   __shared__ int list[LAUD_MOE_MAX_TOKENS], counts[2];
   __shared__ f32x4 part[S][2][kWave];
   const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), r16 = lane % 16, quarter = lane / 16;
-  const Slot slot = slot_of(a);
+  Slot slot;
+  if constexpr (ONE) {
+    __shared__ float logits[kMaxExperts], weights[kMaxTopK];
+    __shared__ uint8_t chosen[kMaxExperts];
+    const bool dropped = a.keep && a.keep[0] == 0;
+    if (!dropped) {
+      for (int e = threadIdx.x; e < a.E; e += S * kWave) logits[e] = a.logits[e];
+      __syncthreads();
+      choose_experts<S * kWave>(a, logits, chosen, list, weights);
+      __syncthreads();
+    }
+    if (blockIdx.x == 0 && blockIdx.y == 0 && (int)threadIdx.x < a.top_k) {
+      a.experts[threadIdx.x] = dropped ? -1 : list[threadIdx.x];
+      a.weights[threadIdx.x] = dropped ? 0.f : weights[threadIdx.x];
+    }
+    if (dropped) return;
+    slot.expert = __builtin_amdgcn_readfirstlane(list[blockIdx.y]);
+    slot.early = true;
+  } else {
+    slot = slot_of(a);
+  }
   const int f0 = blockIdx.x * 16, rows = min(16, a.F - f0);  // (from F to the end of its block of 128 h is 0: rows may be none)
   const int kb_all = scale_blocks(a.C);
   const long long row_bytes = (long long)a.C * WT::kBytes;
@@ -234,14 +268,14 @@ __global__ __launch_bounds__(kSplit<W> * kWave) void k_moe_up(MoeArgs a) {
     }
   };
   if (kEarly<W> && slot.early) request(wave);
-  const int len = find_entries(a, slot, list, counts);
+  const int len = ONE ? 1 : find_entries(a, slot, list, counts);
   if (len == 0) return;
   if (kEarly<W> && !slot.early) request(wave);
   const __amdgpu_buffer_rsrc_t rx = bytes_of(a.x, ((a.T - 1) * a.ldx + a.C) * xb);
   const int fb = scale_blocks(a.F);
   const float* s = W == W_E4M3 && rows > 0 ? a.s_up + ((long long)slot.expert * 2 * fb + f0 / kScaleBlock) * kb_all : nullptr;
   for (int l0 = 0; l0 < len; l0 += 16) {
-    const int entry = list[min(l0 + r16, len - 1)];
+    const int entry = ONE ? (int)blockIdx.y : list[min(l0 + r16, len - 1)];
     const bool real = l0 + r16 < len;  // (of the other rows nothing is fetched)
     const unsigned xoff = (unsigned)(entry / a.top_k * a.ldx * xb);
     f32x4 v[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
@@ -390,15 +424,114 @@ __global__ __launch_bounds__(kSplit<W> * kWave) void k_moe_down(MoeArgs a) {
   }
 }
 
-template <int W, typename ET>
-void launch_moe(const MoeArgs& a, hipStream_t st) {
-  hipLaunchKernelGGL((k_moe_route<ET>), dim3(a.T), dim3(kRouteThreads), 0, st, a);
-  const unsigned slots = (unsigned)min((long long)a.E, (long long)a.T * a.top_k);
-  hipLaunchKernelGGL((k_moe_up<W>), dim3(a.Fp / 16, slots), dim3(kSplit<W> * kWave), 0, st, a);
-  hipLaunchKernelGGL((k_moe_down<W, ET>), dim3(column_tiles(a.C), slots), dim3(kSplit<W> * kWave), 0, st, a);
+// One token's entries for 8 output channels, weighted and added up by one workgroup: where the entries are no more than the experts, so
+// that tokens seldom share one, nothing is gained by joining theirs and nothing has to be handed from workgroup to workgroup.  All
+// of a wave's loads are under way together.  The waves share the entries' blocks of the reduction, two at a time, as the two halves
+// of a matrix instruction's sixteen rows of weights; of the token side, column 0 is the even block and column 1 the odd one, columns
+// 2 and 3 the remainders of both; a half's results stand in its columns.  Sums are added in the waves' order.
+// The layer, with k_moe_down / with this kernel, in us:
+//   8 of 64 experts of 2048 x 1024, bf16    1 token 35.6 / 32.0    4 tokens 89.3 / 83.2    8 tokens 129.5 / 127.6    16 tokens 162.6 / 188.5
+//   6 of 64 experts of 2048 x 1424, e4m3            29.4 / 24.7             65.4 / 58.7              90.9 /  87.3             116.0 / 123.6
+//   2 of  8 experts of 4096 x 2048, bf16            37.3 / 33.5             76.7 / 75.3              96.0 / 106.9
+// (Two pairs of blocks at a time take 78 registers in bf16, four take 140 and leave room for one workgroup of 8 waves a compute unit
+// instead of two: 54.6 against 62.5 us for two tokens of the last one.)
+constexpr int kFewColumns = 8;
+template <int W> constexpr int kPairs = W == W_F32 ? 1 : 2;  // pairs whose loads a wave has under way together
+template <int W, typename OT, int S>
+__global__ __launch_bounds__(S * kWave) void k_moe_down_few(MoeArgs a) {
+  typedef Weights<W> WT;
+  constexpr unsigned kHb = W == W_F32 ? 4 : 2;
+  constexpr int kXP = W == W_E4M3 ? 2 : 1, P = kHiddenPlanes<W>, kAtOnce = kPairs<W>;
+  __shared__ f32x4 part[S][4][P];
+  const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), r16 = lane % 16, quarter = lane / 16;
+  const int t = blockIdx.y, c0 = blockIdx.x * kFewColumns;
+  const int kb_all = scale_blocks(a.F), pairs = (kb_all + 1) / 2, items = a.keep && a.keep[t] == 0 ? 0 : a.top_k * pairs;
+  const long long row_bytes = (long long)a.F * WT::kBytes;
+  const __amdgpu_buffer_rsrc_t rh = bytes_of(a.h, (long long)a.T * a.top_k * a.Fp * 4);
+  const unsigned plane = (unsigned)(a.T * a.top_k) * (unsigned)a.Fp * kHb;
+  f32x4 v = {0.f, 0.f, 0.f, 0.f};
+  for (int i0 = wave; i0 < items; i0 += S * kAtOnce) {
+    tok_u4 w[kAtOnce][WT::kPieces], x[kAtOnce][WT::kPieces][kXP];
+    int expert[kAtOnce], entry[kAtOnce], kb[kAtOnce];
+    float f[kAtOnce];
+    auto live = [&](int n) { return i0 + n * S < items; };  // (behind the last pair: zeros)
+#pragma unroll
+    for (int n = 0; n < kAtOnce; ++n) {
+      const int i = min(i0 + n * S, items - 1);
+      entry[n] = t * a.top_k + i / pairs;
+      kb[n] = i % pairs * 2;
+      expert[n] = a.experts[entry[n]];
+    }
+#pragma unroll
+    for (int n = 0; n < kAtOnce; ++n) {
+      const int e = __builtin_amdgcn_readfirstlane(expert[n]);
+      const __amdgpu_buffer_rsrc_t rw =
+          bytes_of(reinterpret_cast<const uint8_t*>(a.down) + ((long long)e * a.C + c0) * row_bytes, kFewColumns * row_bytes);
+#pragma unroll
+      for (int p = 0; p < WT::kPieces; ++p) {
+        const int k = (kb[n] + r16 / 8) * kScaleBlock + WT::first(p, quarter);
+        w[n][p] = load16(rw, k < a.F && live(n) ? (unsigned)(r16 % 8 * row_bytes) + (unsigned)k * WT::kBytes : kOutside);
+      }
+      f[n] = live(n) ? a.weights[entry[n]] : 0.f;
+      if constexpr (W == W_E4M3) {
+        const bool in = live(n) && kb[n] + quarter / 2 < kb_all;
+        f[n] *= in ? a.s_down[((long long)e * scale_blocks(a.C) + c0 / kScaleBlock) * kb_all + kb[n] + quarter / 2] : 0.f;
+      }
+    }
+#pragma unroll
+    for (int n = 0; n < kAtOnce; ++n)
+#pragma unroll
+      for (int p = 0; p < WT::kPieces; ++p) {
+        const unsigned k = (unsigned)((kb[n] + r16 % 2) * kScaleBlock + WT::first(p, quarter));
+        const unsigned at = r16 / 2 * plane + ((unsigned)entry[n] * (unsigned)a.Fp + k) * kHb;
+#pragma unroll
+        for (int u = 0; u < kXP; ++u) x[n][p][u] = load16(rh, r16 < 2 * P && (int)k < a.Fp && live(n) ? at + 8 * u * kHb : kOutside);
+      }
+    __builtin_amdgcn_sched_barrier(0);  // (the loads stay in front of the products)
+#pragma unroll
+    for (int n = 0; n < kAtOnce; ++n) {
+      f32x4 r = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int p = 0; p < WT::kPieces; ++p) r = mma_stored<W>(w[n][p], x[n][p], r);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) v[q] = fmaf(r[q], f[n], v[q]);
+    }
+  }
+  if (r16 < 2 * P && r16 % 2 == quarter / 2) part[wave][quarter][r16 / 2] = v;
+  __syncthreads();
+  if ((int)threadIdx.x >= kFewColumns / 4) return;
+  f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int n = 0; n < S; ++n)
+#pragma unroll
+    for (int p = 0; p < P; ++p) sum += part[n][threadIdx.x][p] + part[n][threadIdx.x + 2][p];
+  store4(reinterpret_cast<OT*>(a.out) + t * a.ldo + c0 + threadIdx.x * 4, sum);
 }
 
-struct MoeWs { size_t experts, weights, h, y, arrived, bytes; };
+template <int W, typename ET>
+void launch_moe(const MoeArgs& a, hipStream_t st) {
+  const long long entries = (long long)a.T * a.top_k;
+  const dim3 up(a.Fp / 16, (unsigned)min((long long)a.E, entries));
+  if (a.T == 1) {
+    hipLaunchKernelGGL((k_moe_logits<ET>), dim3((a.E - 1) / kLogitWaves + 1), dim3(kLogitWaves * kWave), 0, st, a);
+    hipLaunchKernelGGL((k_moe_up<W, true>), up, dim3(kSplit<W> * kWave), 0, st, a);
+  } else {
+    hipLaunchKernelGGL((k_moe_route<ET>), dim3(a.T), dim3(kRouteThreads), 0, st, a);
+    hipLaunchKernelGGL((k_moe_up<W, false>), up, dim3(kSplit<W> * kWave), 0, st, a);
+  }
+  if (entries > a.E) {
+    hipLaunchKernelGGL((k_moe_down<W, ET>), dim3(column_tiles(a.C), a.E), dim3(kSplit<W> * kWave), 0, st, a);
+  } else {
+    const dim3 down(a.C / kFewColumns, a.T);
+    // Eight waves where four would take more than two rounds: one token of the layers above with 32 and 36 pairs, four waves / eight,
+    // 33.1 / 32.0 and 25.8 / 24.7 us; 4 of 30 experts of 1024 x 512, e4m3, 8 pairs, 8 tokens 19.2 / 20.8.
+    if (a.top_k * ((scale_blocks(a.F) + 1) / 2) > 2 * 4 * kPairs<W>)
+      hipLaunchKernelGGL((k_moe_down_few<W, ET, 8>), down, dim3(8 * kWave), 0, st, a);
+    else hipLaunchKernelGGL((k_moe_down_few<W, ET, 4>), down, dim3(4 * kWave), 0, st, a);
+  }
+}
+
+struct MoeWs { size_t experts, weights, h, y, logits, arrived, bytes; };
 MoeWs moe_ws(const laud_moe_layer* p, int T) {
   MoeWs w;
   const size_t n = (size_t)T * p->top_k;
@@ -406,7 +539,8 @@ MoeWs moe_ws(const laud_moe_layer* p, int T) {
   w.weights = align_up(n * 4, 256);
   w.h = w.weights + align_up(n * 4, 256);
   w.y = align_up(w.h + n * (size_t)scale_blocks(p->F) * kScaleBlock * 4, 256);
-  w.arrived = align_up(w.y + n * (size_t)p->C * 4, 256);
+  w.logits = align_up(w.y + n * (size_t)p->C * 4, 256);
+  w.arrived = w.logits + align_up((size_t)p->E * 4, 256);
   w.bytes = w.arrived + (size_t)column_tiles(p->C) * 4;
   return w;
 }
@@ -455,6 +589,7 @@ extern "C" int laud_moe(const laud_moe_layer* p, int T, const void* x, int64_t l
   a.weights = weights ? weights : (float*)((char*)ws + w.weights);
   a.h = (char*)ws + w.h;
   a.y = (float*)((char*)ws + w.y);
+  a.logits = (float*)((char*)ws + w.logits);
   a.arrived = (unsigned*)((char*)ws + w.arrived);
   clear_stale_error();
   hipStream_t st = (hipStream_t)stream;

@@ -112,6 +112,10 @@ CASES = {
     "moe_f32": (moe, 3, 136, 24, 20, 3, B.F32, B.F32, 8, True, False),
     "moe_e4m3": (moe, 7, 272, 144, 6, 2, B.BF16, B.E4M3, 8, True, True),
     "moe_one_token_e4m3": (moe, 1, 16, 16, 3, 1, B.BF16, B.E4M3, 0, False, True),
+    "moe_one_token": (moe, 1, 40, 264, 5, 3, B.BF16, B.BF16, 8, False, True),
+    "moe_one_token_f32": (moe, 1, 24, 1160, 5, 4, B.F32, B.F32, 0, False, False),
+    "moe_one_token_long_e4m3": (moe, 1, 144, 2064, 9, 8, B.BF16, B.E4M3, 8, False, True),
+    "moe_one_token_dropped": (moe, 1, 24, 8, 5, 4, B.F32, B.F32, 0, True, True),
     "moe_one_expert": (moe, 37, 40, 8, 1, 1, B.BF16, B.BF16, 8, False, True),
     "moe_many_experts": (moe, 2, 24, 8, 1024, 32, B.F32, B.F32, 0, False, True),
     "moe_two_rounds": (moe, 70, 72, 40, 3, 2, B.BF16, B.BF16, 8, True, True),
