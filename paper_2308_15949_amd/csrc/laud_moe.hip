@@ -171,16 +171,13 @@ template <int W> constexpr int kHiddenPlanes = W == W_F32 ? 1 : 2;
 // experts, an entry, whose workgroups take its expert if no earlier entry has the same.
 struct Slot {
   int expert, entries;
-  bool by_entry, early;
+  bool by_entry;
 };
-// early: the expert is all but sure to have entries (at least four a slot on average), so that its weights are requested before
-// its entries are looked for.
 __device__ __forceinline__ Slot slot_of(const MoeArgs& a) {
   Slot s;
   s.entries = a.T * a.top_k;
   s.by_entry = s.entries < a.E;
   s.expert = s.by_entry ? a.experts[blockIdx.y] : (int)blockIdx.y;
-  s.early = s.expert >= 0 && (s.by_entry || s.entries >= 4 * a.E);
   return s;
 }
 // The slot's entries in `list` (in any order: no entry's value depends on it) and their number, 0 if it has none or an earlier slot
@@ -215,18 +212,19 @@ __device__ __forceinline__ void join_waves(f32x4 (&v)[2], f32x4 (*part)[2][kWave
   __syncthreads();
 }
 
-// Waves of a workgroup, which share the reduction by blocks of 128: half as many where a block is half the bytes (16 tokens, 64
-// experts of 2048 x 1424 in 8 bits, four / eight waves: 116 / 129 us; of 2048 x 1024 in bf16 on 64 tokens 220 / 208).
-template <int W> constexpr int kSplit = W == W_E4M3 ? 4 : 8;
-// Whether a wave requests its first weights ahead of the search for the slot's entries: in 8 bits 116 -> 108 us; the larger blocks of
-// the other types need the registers that this takes for a third workgroup on a compute unit (208 -> 219).
-template <int W> constexpr bool kEarly = W == W_E4M3;
+// Waves of a workgroup, which share the reduction by blocks of 128.  Few waves leave room for more workgroups, which wait for their
+// entries, their weights and each other at different times (16 / 64 tokens, 8 of 64 experts of 2048 x 1024, bf16, eight / four / two
+// waves: 162 / 149 / 159 and 191 / 184 / 194 us; 16 tokens, 6 of 64 of 2048 x 1424, 8 bits, 125 / 102 / 105); float32 blocks need the
+// registers of the longer ones (32 tokens, 2 of 16 experts of 1024 x 1024, eight / four: 58.0 / 60.5).  A single token's workgroups,
+// one or two a compute unit, have eight (30.6 against 31.9 us).
+template <int W> constexpr int kSplit = W == W_F32 ? 8 : 4;
+constexpr int kSplitOne = 8;
 
 // h of one expert's entries for 16 hidden channels; ONE: of one entry of the single token.
 template <int W, bool ONE>
-__global__ __launch_bounds__(kSplit<W> * kWave) void k_moe_up(MoeArgs a) {
+__global__ __launch_bounds__((ONE ? kSplitOne : kSplit<W>) * kWave) void k_moe_up(MoeArgs a) {
   typedef Weights<W> WT;
-  constexpr int S = kSplit<W>, kXP = W == W_E4M3 ? 2 : 1, xb = W == W_F32 ? 4 : 2;
+  constexpr int S = ONE ? kSplitOne : kSplit<W>, kXP = W == W_E4M3 ? 2 : 1, xb = W == W_F32 ? 4 : 2;
   __shared__ int list[LAUD_MOE_MAX_TOKENS], counts[2];
   __shared__ f32x4 part[S][2][kWave];
   const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), r16 = lane % 16, quarter = lane / 16;
@@ -247,7 +245,6 @@ __global__ __launch_bounds__(kSplit<W> * kWave) void k_moe_up(MoeArgs a) {
     }
     if (dropped) return;
     slot.expert = __builtin_amdgcn_readfirstlane(list[blockIdx.y]);
-    slot.early = true;
   } else {
     slot = slot_of(a);
   }
@@ -267,10 +264,8 @@ __global__ __launch_bounds__(kSplit<W> * kWave) void k_moe_up(MoeArgs a) {
       wu[p] = load16(ru, off);
     }
   };
-  if (kEarly<W> && slot.early) request(wave);
   const int len = ONE ? 1 : find_entries(a, slot, list, counts);
   if (len == 0) return;
-  if (kEarly<W> && !slot.early) request(wave);
   const __amdgpu_buffer_rsrc_t rx = bytes_of(a.x, ((a.T - 1) * a.ldx + a.C) * xb);
   const int fb = scale_blocks(a.F);
   const float* s = W == W_E4M3 && rows > 0 ? a.s_up + ((long long)slot.expert * 2 * fb + f0 / kScaleBlock) * kb_all : nullptr;
@@ -280,17 +275,21 @@ __global__ __launch_bounds__(kSplit<W> * kWave) void k_moe_up(MoeArgs a) {
     const unsigned xoff = (unsigned)(entry / a.top_k * a.ldx * xb);
     f32x4 v[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
     for (int kb = wave; kb < kb_all; kb += S) {
-      if (!kEarly<W> || kb != wave || l0 != 0) request(kb);
+      request(kb);
       const float fg = s ? s[kb] : 1.f, fu = s ? s[fb * kb_all + kb] : 1.f;
-      f32x4 pg = {0.f, 0.f, 0.f, 0.f}, pu = pg;
+      tok_u4 x[WT::kPieces][kXP];
 #pragma unroll
       for (int p = 0; p < WT::kPieces; ++p) {
         const int k = kb * kScaleBlock + WT::first(p, quarter);
-        tok_u4 x[kXP];
 #pragma unroll
-        for (int i = 0; i < kXP; ++i) x[i] = load16(rx, k < a.C && real ? xoff + (unsigned)(k + 8 * i) * xb : kOutside);
-        pg = mma_stored<W>(wg[p], x, pg);
-        pu = mma_stored<W>(wu[p], x, pu);
+        for (int i = 0; i < kXP; ++i) x[p][i] = load16(rx, k < a.C && real ? xoff + (unsigned)(k + 8 * i) * xb : kOutside);
+      }
+      __builtin_amdgcn_sched_barrier(0);  // (all loads are under way before the first product waits for one)
+      f32x4 pg = {0.f, 0.f, 0.f, 0.f}, pu = pg;
+#pragma unroll
+      for (int p = 0; p < WT::kPieces; ++p) {
+        pg = mma_stored<W>(wg[p], x[p], pg);
+        pu = mma_stored<W>(wu[p], x[p], pu);
       }
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -337,7 +336,7 @@ __device__ __forceinline__ float shared_load(const float* p) {
 template <int W, typename OT>
 __global__ __launch_bounds__(kSplit<W> * kWave) void k_moe_down(MoeArgs a) {
   typedef Weights<W> WT;
-  constexpr int S = kSplit<W>;
+  constexpr int S = kSplit<W>, kXP = W == W_E4M3 ? 2 : 1;
   constexpr unsigned kHb = W == W_F32 ? 4 : 2;  // bytes of a hidden value in a plane
   __shared__ int list[LAUD_MOE_MAX_TOKENS], counts[2];
   __shared__ f32x4 part[S][2][kWave];
@@ -359,11 +358,9 @@ __global__ __launch_bounds__(kSplit<W> * kWave) void k_moe_down(MoeArgs a) {
       w1[p] = load16(rw, k < a.F && 16 + r16 < rows ? off + (unsigned)(16 * row_bytes) : kOutside);
     }
   };
-  if (kEarly<W> && slot.early) request(wave);
   const int len = find_entries(a, slot, list, counts);
   if (len > 0) {
-    if (kEarly<W> && !slot.early) request(wave);
-    const __amdgpu_buffer_rsrc_t rh = bytes_of(a.h, (long long)a.T * a.top_k * a.Fp * 4);
+      const __amdgpu_buffer_rsrc_t rh = bytes_of(a.h, (long long)a.T * a.top_k * a.Fp * 4);
     const unsigned plane = (unsigned)(a.T * a.top_k) * (unsigned)a.Fp * kHb;
     const float* s = W == W_E4M3 ? a.s_down + ((long long)slot.expert * scale_blocks(a.C) + c0 / kScaleBlock) * kb_all : nullptr;
     for (int l0 = 0; l0 < len; l0 += 16) {
@@ -373,22 +370,26 @@ __global__ __launch_bounds__(kSplit<W> * kWave) void k_moe_down(MoeArgs a) {
       const float share = a.weights[entry];
       f32x4 v[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
       for (int kb = wave; kb < kb_all; kb += S) {
-        if (!kEarly<W> || kb != wave || l0 != 0) request(kb);
+        request(kb);
         const float f = s ? s[kb] : 1.f;
-        f32x4 p0 = {0.f, 0.f, 0.f, 0.f}, p1 = p0;
+        tok_u4 x[WT::kPieces][kHiddenPlanes<W>][kXP];
 #pragma unroll
         for (int p = 0; p < WT::kPieces; ++p) {
           const int k = kb * kScaleBlock + WT::first(p, quarter);
-          constexpr int kXP = W == W_E4M3 ? 2 : 1;
+#pragma unroll
+          for (int i = 0; i < kHiddenPlanes<W>; ++i)
+#pragma unroll
+            for (int u = 0; u < kXP; ++u) x[p][i][u] = load16(rh, real ? i * plane + at + (unsigned)(k + 8 * u) * kHb : kOutside);
+        }
+        __builtin_amdgcn_sched_barrier(0);  // (as above)
+        f32x4 p0 = {0.f, 0.f, 0.f, 0.f}, p1 = p0;
+#pragma unroll
+        for (int p = 0; p < WT::kPieces; ++p)
 #pragma unroll
           for (int i = 0; i < kHiddenPlanes<W>; ++i) {
-            tok_u4 x[kXP];
-#pragma unroll
-            for (int u = 0; u < kXP; ++u) x[u] = load16(rh, real ? i * plane + at + (unsigned)(k + 8 * u) * kHb : kOutside);
-            p0 = mma_stored<W>(w0[p], x, p0);
-            p1 = mma_stored<W>(w1[p], x, p1);
+            p0 = mma_stored<W>(w0[p], x[p][i], p0);
+            p1 = mma_stored<W>(w1[p], x[p][i], p1);
           }
-        }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           v[0][i] = fmaf(p0[i], f, v[0][i]);
@@ -514,7 +515,7 @@ void launch_moe(const MoeArgs& a, hipStream_t st) {
   const dim3 up(a.Fp / 16, (unsigned)min((long long)a.E, entries));
   if (a.T == 1) {
     hipLaunchKernelGGL((k_moe_logits<ET>), dim3((a.E - 1) / kLogitWaves + 1), dim3(kLogitWaves * kWave), 0, st, a);
-    hipLaunchKernelGGL((k_moe_up<W, true>), up, dim3(kSplit<W> * kWave), 0, st, a);
+    hipLaunchKernelGGL((k_moe_up<W, true>), up, dim3(kSplitOne * kWave), 0, st, a);
   } else {
     hipLaunchKernelGGL((k_moe_route<ET>), dim3(a.T), dim3(kRouteThreads), 0, st, a);
     hipLaunchKernelGGL((k_moe_up<W, false>), up, dim3(kSplit<W> * kWave), 0, st, a);
