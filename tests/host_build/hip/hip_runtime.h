@@ -122,10 +122,6 @@ static inline int lanes_below(unsigned mask, int first) {  // set bits of 32 lan
 #define __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, x, y, z, u, v, w) (c)
 #define __builtin_amdgcn_cvt_pk_fp8_f32(a, b, old, hi) (old)
 #define __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, s, hi) host::Zero()
-#define __HIP_MEMORY_SCOPE_AGENT 0
-#define __hip_atomic_store(p, v, order, scope) (*(p) = (v))
-#define __hip_atomic_load(p, order, scope) (*(p))
-#define __hip_atomic_fetch_add(p, v, order, scope) __atomic_fetch_add(p, v, __ATOMIC_RELAXED)
 #define atomicAdd(p, v) __atomic_fetch_add(p, v, __ATOMIC_RELAXED)
 #define __builtin_amdgcn_readfirstlane(x) (x)
 #define __builtin_amdgcn_sched_barrier(x)
