@@ -447,7 +447,8 @@ typedef struct {
  * The hidden values stay float32.  A token with keep 0 is not routed: out row 0, experts -1, weights 0.
  *   x [T][C], out [T][C] dtype (out may be x); keep [T] bytes or NULL
  *   experts [T][top_k] int32 (ascending) and weights [T][top_k] float32: outputs, each may be NULL
- * T is at most LAUD_MOE_MAX_TOKENS (LAUD_ERR_UNSUPPORTED beyond): every expert's weights are read once per 64 tokens.
+ * T is at most LAUD_MOE_MAX_TOKENS (LAUD_ERR_UNSUPPORTED beyond).  An expert's weights are fetched once for every sixteen of its tokens;
+ * where T * top_k <= E the down projection's once for each.  A result depends, in its last bits, on which of the two T makes it.
  * Workspace: laud_moe_workspace(p, T) bytes.
  */
 #define LAUD_MOE_MAX_TOKENS 1024
@@ -462,7 +463,8 @@ int laud_moe(const laud_moe_layer* p, int T, const void* x, int64_t ldx, const u
  * later ones are dropped).  laud_stage_timing_enable(1) clears what was collected and starts,
  * (0) stops.  laud_stage_timing_read() waits for the recorded events, adds up the elapsed
  * milliseconds and launch counts per stage into two HOST arrays of LAUD_STAGE_COUNT entries,
- * and clears the collection.  Not thread-safe against concurrent entry-point calls.
+ * and clears the collection.  Not thread-safe against concurrent entry-point calls.  The token operators are not
+ * collected: they are one launch each (laud_moe three or four).
  */
 typedef enum {
   LAUD_STAGE_MASK_LOGITS = 0, /* pooled masker + threshold */
