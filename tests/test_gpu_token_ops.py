@@ -394,6 +394,41 @@ def test_moe_special_values_stay_with_their_token():
         assert torch.equal(out[rows], clean[rows]) and torch.equal(ids[rows], cid[rows]) and bool(out[4].isnan().all())
 
 
+@pytest.mark.parametrize("w", ["bf16", "f32", "e4m3"])
+@pytest.mark.parametrize("E,k,C,F", [(1, 1, 16, 16), (7, 1, 2064, 112), (64, 8, 1024, 784), (30, 4, 144, 400), (1000, 32, 64, 48), (6, 6, 272, 2064)])
+def test_moe_single_token(E, k, C, F, w):
+    moe_check(1, E, C, F, w, k, E, renorm=False, scale=0.5)
+    moe_check(1, E, C, F, w, k, E + 1, keep=torch.ones(1, dtype=torch.uint8))
+    moe_check(1, E, C, F, w, k, E + 2, keep=torch.zeros(1, dtype=torch.uint8))
+    moe_check(E // k, E, C, F, w, k, E + 3, extra=16)  # as many entries as experts
+
+
+def test_moe_single_token_ties_and_nan():
+    x, router, up, down, su, sd = moe_inputs(1, 130, 64, 32, "f32", 9)
+    router[:] = router[0]
+    _, ids, wt = moe_run(x, router, up, down, su, sd, 5, False, 1.0)
+    assert ids.tolist() == [[0, 1, 2, 3, 4]] and bool(((wt - 1 / 130).abs() < 1e-8).all())
+    router = rand(gen(1), 130, 64)
+    router[3] = float("nan")
+    out, ids, wt = moe_run(x, router, up, down, su, sd, 5, True, 1.0)
+    assert 3 not in ids[0].tolist() and ids[0].tolist() == sorted(set(ids[0].tolist()))
+    assert bool(wt.isnan().all()) and bool(out.isnan().all())
+    x[:] = float("nan")
+    _, ids, _ = moe_run(x, router, up, down, su, sd, 5, True, 1.0)
+    assert ids.tolist() == [[0, 1, 2, 3, 4]]
+
+
+def test_moe_special_values_stay_with_their_token_among_many_experts():
+    for w in ("bf16", "f32", "e4m3"):
+        t = list(moe_inputs(4, 16, 144, 400, w, 7))
+        clean, cid, _ = moe_run(*t, 3, True, 1.0)
+        t[0] = t[0].clone()
+        t[0][2, 3] = float("nan")
+        out, ids, _ = moe_run(*t, 3, True, 1.0)
+        rows = torch.arange(4) != 2
+        assert torch.equal(out[rows], clean[rows]) and torch.equal(ids[rows], cid[rows]) and bool(out[2].isnan().all())
+
+
 def test_moe_in_place():
     t = moe_inputs(20, 8, 64, 48, "bf16", 3)
     ref, _, _ = moe_run(*t, 2, True, 1.0)
