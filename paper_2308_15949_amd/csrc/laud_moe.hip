@@ -306,7 +306,10 @@ __global__ __launch_bounds__((ONE ? kSplitOne : kSplit<W>) * kWave) void k_moe_u
         const tok_u2 hi = {pack_bf16(h[0], h[1]), pack_bf16(h[2], h[3])};
         f32x4 rest;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) rest[i] = h[i] - __uint_as_float(i % 2 ? hi[i / 2] & 0xffff0000u : hi[i / 2] << 16);
+        for (int i = 0; i < 4; ++i) {
+          const float top = __uint_as_float(i % 2 ? hi[i / 2] & 0xffff0000u : hi[i / 2] << 16);
+          rest[i] = fabsf(top) == INFINITY ? 0.f : h[i] - top;  // (an infinity has no remainder)
+        }
         const tok_u2 lo = {pack_bf16(rest[0], rest[1]), pack_bf16(rest[2], rest[3])};
         bf16_t* plane = reinterpret_cast<bf16_t*>(a.h) + at;
         *reinterpret_cast<tok_u2*>(plane) = hi;

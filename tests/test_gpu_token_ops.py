@@ -429,6 +429,24 @@ def test_moe_special_values_stay_with_their_token_among_many_experts():
         assert torch.equal(out[rows], clean[rows]) and torch.equal(ids[rows], cid[rows]) and bool(out[2].isnan().all())
 
 
+@pytest.mark.parametrize("w", ["bf16", "f32", "e4m3"])
+@pytest.mark.parametrize("T", [1, 3, 7])
+def test_moe_infinite_hidden_values(T, w):
+    """One hidden value beyond float32, every other one 0: the result is an infinity of the last product's sign."""
+    x, router, up, down, su, sd = moe_inputs(T, 4, 16, 16, w, 1)
+    x[:], router[:], up[:], down[:] = 0, 0, 0, 1
+    x[:, 0], router[1, 0] = 1e30, 1e-30
+    if su is None:
+        up[1, 0, 3, 0], up[1, 1, 3, 0] = 1e9, 1e-29
+    else:
+        up[1, :, 3, 0] = 1
+        su[:, 0], su[:, 1], sd[:] = 1e9, 1e-29, 1
+    down[1, ::2, 3] = -1
+    out, ids, wt = moe_run(x, router, up, down, su, sd, 1, True, 1.0)
+    assert bool((ids == 1).all()) and bool((wt == 1).all())
+    assert bool((out[:, ::2] == -math.inf).all()) and bool((out[:, 1::2] == math.inf).all())
+
+
 def test_moe_in_place():
     t = moe_inputs(20, 8, 64, 48, "bf16", 3)
     ref, _, _ = moe_run(*t, 2, True, 1.0)
