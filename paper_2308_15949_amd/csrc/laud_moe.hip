@@ -192,18 +192,17 @@ __device__ __forceinline__ int find_entries(const MoeArgs& a, const Slot& s, int
   return counts[1] ? 0 : counts[0];
 }
 
-// Sums of the S waves' parts of two row tiles, in the waves' order, for the first wave.
-template <int S>
-__device__ __forceinline__ void join_waves(f32x4 (&v)[2], f32x4 (*part)[2][kWave], int wave, int lane) {
-  part[wave][0][lane] = v[0];
-  part[wave][1][lane] = v[1];
+// Sums of the S waves' parts of N row tiles, in the waves' order, for the first wave.
+template <int S, int N>
+__device__ __forceinline__ void join_waves(f32x4 (&v)[N], f32x4 (*part)[N][kWave], int wave, int lane) {
+#pragma unroll
+  for (int n = 0; n < N; ++n) part[wave][n][lane] = v[n];
   __syncthreads();
   if (wave == 0) {
 #pragma unroll
-    for (int w = 1; w < S; ++w) {
-      v[0] += part[w][0][lane];
-      v[1] += part[w][1][lane];
-    }
+    for (int w = 1; w < S; ++w)
+#pragma unroll
+      for (int n = 0; n < N; ++n) v[n] += part[w][n][lane];
   }
   __syncthreads();
 }
@@ -324,10 +323,10 @@ __global__ __launch_bounds__((ONE ? kSplitOne : kSplit<W>) * kWave) void k_moe_u
 template <int W>
 __global__ __launch_bounds__(kSplit<W> * kWave) void k_moe_down(MoeArgs a) {
   typedef Weights<W> WT;
-  constexpr int S = kSplit<W>, kXP = W == W_E4M3 ? 2 : 1;
+  constexpr int N = kColumns / 16, S = kSplit<W>, kXP = W == W_E4M3 ? 2 : 1;
   constexpr unsigned kHb = W == W_F32 ? 4 : 2;  // bytes of a hidden value in a plane
   __shared__ int list[LAUD_MOE_MAX_TOKENS], counts[2];
-  __shared__ f32x4 part[S][2][kWave];
+  __shared__ f32x4 part[S][N][kWave];
   const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), r16 = lane % 16, quarter = lane / 16;
   const Slot slot = slot_of(a);
   const int c0 = blockIdx.x * kColumns, rows = min(kColumns, a.C - c0);
@@ -335,14 +334,16 @@ __global__ __launch_bounds__(kSplit<W> * kWave) void k_moe_down(MoeArgs a) {
   const long long row_bytes = (long long)a.F * WT::kBytes;
   const __amdgpu_buffer_rsrc_t rw =
       bytes_of(reinterpret_cast<const uint8_t*>(a.down) + ((long long)max(slot.expert, 0) * a.C + c0) * row_bytes, rows * row_bytes);
-  tok_u4 w0[WT::kPieces], w1[WT::kPieces];
+  tok_u4 w[N][WT::kPieces];
   auto request = [&](int kb) {
 #pragma unroll
     for (int p = 0; p < WT::kPieces; ++p) {
       const int k = kb * kScaleBlock + WT::first(p, quarter);
-      const unsigned off = (unsigned)(r16 * row_bytes) + (unsigned)k * WT::kBytes;
-      w0[p] = load16(rw, k < a.F && r16 < rows ? off : kOutside);
-      w1[p] = load16(rw, k < a.F && 16 + r16 < rows ? off + (unsigned)(16 * row_bytes) : kOutside);
+#pragma unroll
+      for (int n = 0; n < N; ++n) {
+        const int row = n * 16 + r16;
+        w[n][p] = load16(rw, k < a.F && row < rows ? (unsigned)(row * row_bytes) + (unsigned)k * WT::kBytes : kOutside);
+      }
     }
   };
   const int len = find_entries(a, slot, list, counts);
@@ -355,7 +356,7 @@ __global__ __launch_bounds__(kSplit<W> * kWave) void k_moe_down(MoeArgs a) {
     const bool real = l0 + r16 < len;
     const unsigned at = (unsigned)entry * (unsigned)a.Fp * kHb;
     const float share = a.weights[entry];
-    f32x4 v[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+    f32x4 v[N] = {};
     for (int kb = wave; kb < kb_all; kb += S) {
       request(kb);
       const float f = s ? s[kb] : 1.f;
@@ -369,25 +370,22 @@ __global__ __launch_bounds__(kSplit<W> * kWave) void k_moe_down(MoeArgs a) {
           for (int u = 0; u < kXP; ++u) x[p][i][u] = load16(rh, real ? i * plane + at + (unsigned)(k + 8 * u) * kHb : kOutside);
       }
       __builtin_amdgcn_sched_barrier(0);  // (as above)
-      f32x4 p0 = {0.f, 0.f, 0.f, 0.f}, p1 = p0;
 #pragma unroll
-      for (int p = 0; p < WT::kPieces; ++p)
+      for (int n = 0; n < N; ++n) {
+        f32x4 r = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int i = 0; i < kHiddenPlanes<W>; ++i) {
-          p0 = mma_stored<W>(w0[p], x[p][i], p0);
-          p1 = mma_stored<W>(w1[p], x[p][i], p1);
-        }
+        for (int p = 0; p < WT::kPieces; ++p)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        v[0][i] = fmaf(p0[i], f, v[0][i]);
-        v[1][i] = fmaf(p1[i], f, v[1][i]);
+          for (int i = 0; i < kHiddenPlanes<W>; ++i) r = mma_stored<W>(w[n][p], x[p][i], r);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[n][i] = fmaf(r[i], f, v[n][i]);
       }
     }
     join_waves<S>(v, part, wave, lane);
     if (wave == 0 && real) {
       float* y = a.y + (long long)entry * a.C + c0;
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
+      for (int i = 0; i < N; ++i)
         if (i * 16 + quarter * 4 < rows) *reinterpret_cast<f32x4*>(y + i * 16 + quarter * 4) = v[i] * share;
     }
   }
