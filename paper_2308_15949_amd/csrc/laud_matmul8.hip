@@ -286,26 +286,30 @@ __global__ __launch_bounds__(KG * BM / WM * (BN / WN) * kWave) void k_mm8_tile(M
   for (int i = 0; i < kNT; ++i)
 #pragma unroll
     for (int e = 0; e < 4; ++e) acc[i][kMT - 1][e] = fmaf(p[i][e], f, acc[i][kMT - 1][e]);
-  if constexpr (KG == 2) {  // the second group's sums through LDS to the first
-    static_assert(BM * BN * 4 <= L::kBytes, "sums fit");
+  if constexpr (KG > 1) {  // the other groups' sums through LDS to the first, in their order
+    static_assert((KG - 1) * BM * BN * 4 <= L::kBytes, "sums fit");
+    constexpr int kTile = BM * BN / 4;  // in f32x4
     f32x4* const sums = reinterpret_cast<f32x4*>(lds) + threadIdx.x % (kWaves * kWave);
     __syncthreads();
-    if (group == 1) {
+    if (group != 0) {
 #pragma unroll
       for (int i = 0; i < kNT; ++i)
 #pragma unroll
-        for (int j = 0; j < kMT; ++j) sums[(i * kMT + j) * kWaves * kWave] = f32x4{acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
+        for (int j = 0; j < kMT; ++j)
+          sums[(group - 1) * kTile + (i * kMT + j) * kWaves * kWave] = f32x4{acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
     }
     __syncthreads();
-    if (group == 1) return;
+    if (group != 0) return;
 #pragma unroll
-    for (int i = 0; i < kNT; ++i)
+    for (int o = 0; o < KG - 1; ++o)
 #pragma unroll
-      for (int j = 0; j < kMT; ++j) {
-        const f32x4 v = sums[(i * kMT + j) * kWaves * kWave];
+      for (int i = 0; i < kNT; ++i)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) acc[i][j][e] += v[e];
-      }
+        for (int j = 0; j < kMT; ++j) {
+          const f32x4 v = sums[o * kTile + (i * kMT + j) * kWaves * kWave];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[i][j][e] += v[e];
+        }
   }
   // Lane (row r16 of a, quarter) holds columns 4 * quarter .. +3 of every 16: after a swap of neighbouring quarters between two
   // column tiles it holds eight in a row, and four lanes 64 bytes of a row of bf16 results.
@@ -358,13 +362,18 @@ int launch_tile(const Mm8Args& g, hipStream_t st) {
 //   3000 x 1000 x  512      8.3        9.8         6.9         8.0        10.9
 // The smaller ones share the blocks of K between two groups of waves, and short reductions on 64 x 64 tiles take two stages instead
 // of four, two workgroups a compute unit (200 x 2048 x 1024: 4.8 us against 5.1; 256 x 4096 x 4096: 14.9 against 11.6).
+// Where there is a compute unit for each, tiles are 64 x 32: two groups of waves and two stages up to 12 blocks of K, four and three
+// beyond.  bf16 / float32 results, 64 x 64 and these two:
+//   64 x 4096 x  512     3.8, 3.3,  4.6 /  4.7,  3.9,  5.2         197 x 2048 x 1024     4.8, 4.3, 4.7 / 6.1, 5.0, 5.4
+//   64 x 4096 x 2048     6.5, 5.8,  5.7 /  9.5,  7.1,  6.9          64 x 4096 x 8192    17.7, 22.3, 14.3 / 26.9, 25.2, 17.0
+// and with two tiles a compute unit, 128 x 8192 x 2048, 7.7, 9.1, 11.5 / 10.7, 11.1, 14.0.
 struct TileTime {
   int bm, bn;
   float block, ends;
 };
+inline double tile_count(const Mm8Args& g, int bm, int bn) { return (double)((g.M - 1) / bm + 1) * ((g.N - 1) / bn + 1); }
 inline float tile_time(const Mm8Args& g, const TileTime& t) {
-  const double tiles = (double)((g.M - 1) / t.bm + 1) * ((g.N - 1) / t.bn + 1);
-  return (float)(std::ceil(tiles / kComputeUnits) * (g.kb * t.block + t.ends));
+  return (float)(std::ceil(tile_count(g, t.bm, t.bn) / kComputeUnits) * (g.kb * t.block + t.ends));
 }
 
 template <typename OT>
@@ -380,7 +389,7 @@ int launch_mm8(const Mm8Args& g, hipStream_t st) {
   int best = 0;
   for (int i = 1; i < (kBf16 ? 5 : 3); ++i)
     if (tile_time(g, kTimes[i]) < tile_time(g, kTimes[best])) best = i;
-  if ((double)((g.M - 1) / kTimes[best].bm + 1) * ((g.N - 1) / kTimes[best].bn + 1) > 1e9) return LAUD_ERR_UNSUPPORTED;
+  if (tile_count(g, kTimes[best].bm, kTimes[best].bn) > 1e9) return LAUD_ERR_UNSUPPORTED;
   if constexpr (kBf16) {
     if (best == 4) return launch_tile<OT, 256, 256, 128, 64, 2>(g, st);
     if (best == 3) return launch_tile<OT, 128, 256, 64, 64, 3>(g, st);
@@ -389,6 +398,10 @@ int launch_mm8(const Mm8Args& g, hipStream_t st) {
     if (best == 2) return launch_tile<OT, 128, 128, 64, 64, 4>(g, st);
   }
   if (best == 1) return launch_tile<OT, 64, 128, 32, 64, 3, 2>(g, st);
+  if (tile_count(g, 64, 32) <= kComputeUnits) {
+    if (g.kb <= 12) return launch_tile<OT, 64, 32, 32, 32, 2, 2>(g, st);
+    return launch_tile<OT, 64, 32, 32, 32, 3, 4>(g, st);
+  }
   if (g.kb <= 10) return launch_tile<OT, 64, 64, 32, 32, 2, 2>(g, st);
   return launch_tile<OT, 64, 64, 32, 32, 4, 2>(g, st);
 }
@@ -402,6 +415,8 @@ int matmul8_init_device() {
   for (int rc : {ask_tile_lds<bf16_t, 256, 256, 128, 64, 2>(), ask_tile_lds<bf16_t, 128, 256, 64, 64, 3>(),
                  ask_tile_lds<bf16_t, 128, 128, 64, 64, 2, 2>(), ask_tile_lds<bf16_t, 64, 128, 32, 64, 3, 2>(),
                  ask_tile_lds<bf16_t, 64, 64, 32, 32, 2, 2>(), ask_tile_lds<bf16_t, 64, 64, 32, 32, 4, 2>(),
+                 ask_tile_lds<bf16_t, 64, 32, 32, 32, 2, 2>(), ask_tile_lds<bf16_t, 64, 32, 32, 32, 3, 4>(),
+                 ask_tile_lds<float, 64, 32, 32, 32, 2, 2>(), ask_tile_lds<float, 64, 32, 32, 32, 3, 4>(),
                  ask_tile_lds<float, 128, 128, 64, 64, 4>(), ask_tile_lds<float, 64, 128, 32, 64, 3, 2>(),
                  ask_tile_lds<float, 64, 64, 32, 32, 2, 2>(), ask_tile_lds<float, 64, 64, 32, 32, 4, 2>()})
     if (rc != LAUD_OK) return rc;

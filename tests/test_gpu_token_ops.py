@@ -234,6 +234,12 @@ def test_matmul_columns_and_reductions(N, K):
         mm_check(M, N, K, torch.float32, N + K + M, extra=8)
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("M,N,K", [(70, 1000, 1536), (129, 504, 1552), (129, 504, 1664), (64, 4096, 2064), (17, 8, 8208), (260, 1640, 272), (512, 1032, 1424)])
+def test_matmul_small_tiles(M, N, K, dtype):
+    mm_check(M, N, K, dtype, M + K, extra=16)
+
+
 def test_matmul_large_and_strided():
     mm_check(1100, 1096, 1040, torch.bfloat16, 1, extra=16)
     mm_check(2048, 2048, 1024, torch.bfloat16, 2)

@@ -97,10 +97,15 @@ CASES = {
     # every tile; sizes that end inside it, reductions of one block and less, of odd and even numbers of them
     "matmul_few_rows": (matmul, 13, 40, 1168, B.BF16, 16),
     "matmul_one": (matmul, 1, 8, 16, B.F32, 0),
-    "matmul_64x64": (matmul, 70, 72, 16, B.BF16, 16),
-    "matmul_64x64_long": (matmul, 17, 136, 1424, B.BF16, 32),
-    "matmul_64x64_f32": (matmul, 65, 8, 272, B.F32, 16),
-    "matmul_64x64_long_f32": (matmul, 17, 136, 1424, B.F32, 32),
+    "matmul_64x32": (matmul, 70, 72, 16, B.BF16, 16),
+    "matmul_64x32_blocks": (matmul, 129, 40, 1456, B.F32, 16),
+    "matmul_64x32_long": (matmul, 17, 136, 1680, B.BF16, 32),
+    "matmul_64x32_f32": (matmul, 65, 8, 272, B.F32, 16),
+    "matmul_64x32_long_f32": (matmul, 17, 136, 2064, B.F32, 32),
+    "matmul_64x64": (matmul, 1000, 600, 144, B.BF16, 16),
+    "matmul_64x64_long": (matmul, 1000, 600, 1424, B.BF16, 32),
+    "matmul_64x64_f32": (matmul, 1000, 600, 272, B.F32, 16),
+    "matmul_64x64_long_f32": (matmul, 1000, 600, 1296, B.F32, 32),
     "matmul_64x128": (matmul, 1000, 1496, 400, B.BF16, 16),
     "matmul_64x128_f32": (matmul, 1000, 1496, 400, B.F32, 16),
     "matmul_128x128": (matmul, 1800, 2040, 272, B.BF16, 16),
@@ -123,6 +128,8 @@ CASES = {
 # The tiles that a case is there for: rows x columns of a workgroup and the stages in LDS.
 REACHES = {
     "matmul_few_rows": "k_mm8_split<unsigned short>", "matmul_one": "k_mm8_split<float>",
+    "matmul_64x32": "k_mm8_tile<unsigned short, 64, 32, 32, 32, 2, 2>", "matmul_64x32_long": "k_mm8_tile<unsigned short, 64, 32, 32, 32, 3, 4>",
+    "matmul_64x32_f32": "k_mm8_tile<float, 64, 32, 32, 32, 2, 2>", "matmul_64x32_long_f32": "k_mm8_tile<float, 64, 32, 32, 32, 3, 4>",
     "matmul_64x64": "k_mm8_tile<unsigned short, 64, 64, 32, 32, 2, 2>", "matmul_64x64_long": "k_mm8_tile<unsigned short, 64, 64, 32, 32, 4, 2>",
     "matmul_64x64_f32": "k_mm8_tile<float, 64, 64, 32, 32, 2, 2>", "matmul_64x64_long_f32": "k_mm8_tile<float, 64, 64, 32, 32, 4, 2>",
     "matmul_64x128": "k_mm8_tile<unsigned short, 64, 128, 32, 64, 3, 2>", "matmul_64x128_f32": "k_mm8_tile<float, 64, 128, 32, 64, 3, 2>",
