@@ -165,7 +165,8 @@ inline bool rows_meet(const void* a, int64_t lda, size_t ea, const void* b, int6
   const size_t pitch = (size_t)lda * ea;
   if (pitch != (size_t)ldb * eb) return true;
   const size_t d = (size_t)((uintptr_t)a < (uintptr_t)b ? (uintptr_t)b - (uintptr_t)a : (uintptr_t)a - (uintptr_t)b) % pitch;
-  const size_t lower = (size_t)cols * ((uintptr_t)a < (uintptr_t)b ? ea : eb), upper = (size_t)cols * ((uintptr_t)a < (uintptr_t)b ? eb : ea);
+  const bool a_first = (uintptr_t)a < (uintptr_t)b;
+  const size_t lower = (size_t)cols * (a_first ? ea : eb), upper = (size_t)cols * (a_first ? eb : ea);
   return d < lower || d + upper > pitch;
 }
 // ... or are the same array (base, type and distance of rows) or apart
