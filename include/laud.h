@@ -416,9 +416,9 @@ int laud_norm_residual(const laud_norm_block* p, int rows, const void* x, int64_
  * out[m][n] = sum_k a[m][k] * sa[m][k/128] * b[n][k] * sb[n/128][k/128]: products of 8-bit operands are added over a block of
  * 128, the block's sum takes its two scales, blocks are added in float32.  a [M][K], b [N][K] E4M3, K a multiple of 16, N of 8,
  * rows at most 2^22 elements apart; sa [M][ceil(K/128)], sb [ceil(N/128)][ceil(K/128)] (laud_quantize_e4m3 with block_rows 1 and
- * 128); out [M][N] of out_dtype (LAUD_F32 or LAUD_BF16), no alias of an input.  Inside a block the sums are float32 for
- * float32 results and for up to 16 rows; for bf16 results of more rows the 8-bit matrix instructions take them, which add every
- * eight products with 14 bits below the largest of them (1.5e-5 of the result's norm, a hundredth of its rounding to bf16).
+ * 128); out [M][N] of out_dtype (LAUD_F32 or LAUD_BF16), no alias of an input.  Codes are widened
+ * to bf16, which holds them exactly; products and sums are float32 for every shape and both types of result, so that the number of
+ * rows changes a row's result by the order of its sums only.
  * Workspace: laud_matmul_e4m3_workspace(M, N, K) bytes; no shape needs any at present (then ws may be NULL).
  */
 size_t laud_matmul_e4m3_workspace(int M, int N, int K);

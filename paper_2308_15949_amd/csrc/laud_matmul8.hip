@@ -18,9 +18,9 @@ constexpr double kComputeUnits = 256;
 constexpr int64_t kMaxLd = 1 << 22;    // elements from row to row: 256 rows of a tile stay below the 2 GiB a descriptor addresses
 // Sixteen rows of the first operand times sixteen of the second over a block of 128: lane l holds row l % 16, bytes 16 * (l / 16)
 // and 64 behind them (any order of K serves as long as both operands have the same).  Result: row 4 * (l / 16) + i of the first,
-// row l % 16 of the second.  The codes are widened to bf16, which holds them exactly: the 8-bit matrix instructions add groups of
-// eight products with 14 bits below the group's largest (2^16 + 2^2 in one group is 2^16; measured 1.5e-5 of a result's
-// norm, against 3e-7 here).
+// row l % 16 of the second.  The codes are widened to bf16, which holds them exactly, for every result: the 8-bit matrix
+// instructions take half the time, but they add groups of eight products with 14 bits below the group's largest (2^16 + 2^2 in one
+// group is 2^16, and 2^16 - 2^16 + 2^2 nothing; measured 1.5e-5 of a result's norm, against 3e-7 here).
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 __device__ __forceinline__ i32x8 join(const tok_u4& a, const tok_u4& b) {
   return __builtin_bit_cast(i32x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
@@ -76,17 +76,8 @@ __global__ __launch_bounds__(kSplit * kWave) void k_mm8_split(Mm8Args g) {
 // loads, a block of 128 along K at a time, into NS stages that take turns: one barrier a block, the next blocks' loads are under way
 // while this one is multiplied.  A row's eight 16-byte chunks lie XOR-swizzled (chunk ^ row % 8; the swizzle is applied to the global
 // side).  The first operand of the matrix instructions is b: a lane's results are consecutive columns, its row of a - and that row's
-// scale - is one for all of them.  Bound by the matrix cores and by power: on random operands a bare loop of these instructions and
-// their scalings runs at 3.5 to 3.8 PFLOP/s, 8192 x 8192 x 4096 at 2.1 (256 us).
-//
-// The block's products in 8-bit instructions: twice the rate of the bf16 ones.  They add groups of eight products with 14 bits below
-// the group's largest, an error of 1.5e-5 of the result's norm: a hundredth of what a bf16 result's rounding adds, and taken for
-// bf16 results only.
-__device__ __forceinline__ f32x4 mma_block8(const i32x8& a, const i32x8& b) {
-  const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
-  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, zero, 0, 0, 0, 0, 0, 0);
-}
-
+// scale - is one for all of them.  Bound by the matrix cores at their bf16 rate: 8192 x 8192 x 4096 in 421 to 444 us, 1.2 to 1.3 PFLOP/s, where a
+// large bf16 product of the vendor's library reaches 1.1.
 template <int BM, int BN, int NS, int KG> struct TileLds {
   static constexpr int kB = 0, kA = BN * kScaleBlock, kSa = kA + BM * kScaleBlock, kSb = kSa + BM * 4, kStage = kSb + 256;
   static constexpr int kGroup = NS * kStage, kBytes = KG * kGroup;
@@ -197,8 +188,7 @@ __global__ __launch_bounds__(KG * BM / WM * (BN / WN) * kWave) void k_mm8_tile(M
 #pragma unroll
         for (int i = 0; i < kNT; ++i) {
           const f32x4 old = p[i];
-          if constexpr (sizeof(OT) == 2) p[i] = mma_block8(o.n[i], o.m[j]);
-          else p[i] = mma_block(o.n[i], o.m[j]);
+          p[i] = mma_block(o.n[i], o.m[j]);
           __builtin_amdgcn_sched_barrier(0);
           float(&c)[4] = acc[i][(j + kMT - 1) % kMT];
 #pragma unroll
@@ -219,31 +209,34 @@ __global__ __launch_bounds__(KG * BM / WM * (BN / WN) * kWave) void k_mm8_tile(M
       step(kb + 1, odd, even);
     }
   } else {
-    i32x8 nf[kNT], mf[2];
+    i32x8 nf[kNT];
+    tok_u4 mf[2];  // the two halves of a row tile's operand
+    bf16x8 n8[kNT][4];
     float s[2], sb;
-    auto read_m = [&](const uint8_t* at, int j) {
-      s[j & 1] = *reinterpret_cast<const float*>(at + L::kSa + (wm + j * 16 + r16) * 4);
-      at += L::kA + (wm + j * 16) * kScaleBlock;
-      mf[j & 1] = join(*reinterpret_cast<const tok_u4*>(at + frag), *reinterpret_cast<const tok_u4*>(at + (frag ^ 64)));
+    auto read_s = [&](const uint8_t* at, int j) { s[j & 1] = *reinterpret_cast<const float*>(at + L::kSa + (wm + j * 16 + r16) * 4); };
+    auto read_m = [&](const uint8_t* at, int j, int half) {
+      mf[half] = *reinterpret_cast<const tok_u4*>(at + L::kA + (wm + j * 16) * kScaleBlock + (half ? frag ^ 64 : frag));
     };
-    auto read_n = [&](const uint8_t* at, int i) {
-      at += L::kB + (wn + i * 16) * kScaleBlock;
-      nf[i] = join(*reinterpret_cast<const tok_u4*>(at + frag), *reinterpret_cast<const tok_u4*>(at + (frag ^ 64)));
-    };
+    auto read_n = [&](const uint8_t* at, int i) { nf[i] = operand(at + L::kB + (wn + i * 16) * kScaleBlock); };
     auto read_sb = [&](const uint8_t* at) { sb = *reinterpret_cast<const float*>(at + L::kSb + wn / kScaleBlock * 4); };
 #pragma unroll
     for (int s = 0; s < NS - 1; ++s) request(s, lds0 + s * L::kStage, 0, kLoads);
     vm_wait<(NS - 2) * kLoads>();
     __syncthreads();
     request(NS - 1, lds0 + (NS - 1) * L::kStage, 0, kPer);
-    read_m(stages, 0);
+    read_m(stages, 0, 0);
+    read_m(stages, 0, 1);
+    read_s(stages, 0);
     read_sb(stages);
 #pragma unroll
     for (int i = 0; i < kNT; ++i) read_n(stages, i);
-    // A product's scaling stands behind the matrix instruction of the next row tile (in the last of a block: of the next block's
-    // first), in this order and no other: an instruction's result is there long before it is asked for.  The barrier stands in front
-    // of a block's last row tile, whose operands are in registers by then: behind it the next block's first ones come from LDS, and
-    // the loads of the block after that may overwrite this one's stage.  (Behind the last block it reads what is there, unused.)
+    // The column tiles' operands stay in registers, widened, for the block; a row tile's is widened a quarter at a time, each time
+    // for all column tiles (with a tile's four instructions one behind the other both were held whole: 23 registers in memory at
+    // 256 x 256, 4096 x 4096 x 4096 149 us against 104).  A product's scaling stands behind the matrix instructions of the next row
+    // tile (in the last of a block: of the next block's first), in this order and no other: a result is there long before it is
+    // asked for.  The barrier stands in front of a block's last row tile, whose operands have been read by then: behind it the next
+    // block's first ones come from LDS, and the loads of the block after that may overwrite this one's stage.  (Behind the last block
+    // it reads what is there, unused.)
     int now = 0, fill = NS - 1;  // stages of this block and of the one being requested
     for (int kb = 0; kb * KG < g.kb; ++kb) {
       const int next = now + 1 < NS ? now + 1 : 0;
@@ -256,27 +249,37 @@ __global__ __launch_bounds__(KG * BM / WM * (BN / WN) * kWave) void k_mm8_tile(M
           lds_wait();
           vm_wait<(NS - 2) * kLoads>();
           __syncthreads();
-          read_m(ahead, 0);
+          read_s(ahead, 0);
           read_sb(ahead);
           fill = now;
           request(kb + NS, lds0 + fill * L::kStage, 0, kPer);
         } else {
           request(kb + NS - 1, lds0 + fill * L::kStage, (j + 1) * kPer, (j + 2) * kPer);
-          read_m(at, j + 1);
+          read_s(at, j + 1);
         }
 #pragma unroll
-        for (int i = 0; i < kNT; ++i) {
-          const f32x4 old = p[i];
-          if constexpr (sizeof(OT) == 2) p[i] = mma_block8(nf[i], mf[j & 1]);
-          else p[i] = mma_block(nf[i], mf[j & 1]);
-          __builtin_amdgcn_sched_barrier(0);
-          float(&c)[4] = acc[i][(j + kMT - 1) % kMT];
+        for (int h = 0; h < 4; ++h) {
+          const bf16x8 m8 = widen8(mf[h / 2][h % 2 * 2], mf[h / 2][h % 2 * 2 + 1]);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) c[e] = fmaf(old[e], f_old, c[e]);
-          __builtin_amdgcn_sched_barrier(0);
-          if (j == kMT - 1) read_n(ahead, i);
-          if (i == 0) __builtin_amdgcn_s_setprio(1);  // (a wave amid its products goes ahead of one that loads)
-          if (i == kNT - 1) __builtin_amdgcn_s_setprio(0);
+          for (int i = 0; i < kNT; ++i) {
+            if (j == 0) n8[i][h] = widen8((unsigned)nf[i][2 * h], (unsigned)nf[i][2 * h + 1]);
+            if (h == 0) {
+              float(&c)[4] = acc[i][(j + kMT - 1) % kMT];
+#pragma unroll
+              for (int e = 0; e < 4; ++e) c[e] = fmaf(p[i][e], f_old, c[e]);
+              p[i] = mma_bf16_16(n8[i][h], m8, f32x4{0.f, 0.f, 0.f, 0.f});
+            } else {
+              p[i] = mma_bf16_16(n8[i][h], m8, p[i]);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            if (i == 0 && h % 2 == 1) {
+              if (j == kMT - 1) read_m(ahead, 0, h / 2);
+              else read_m(at, j + 1, h / 2);
+            }
+            if (j == kMT - 1 && h == 3) read_n(ahead, i);
+            if (h == 0 && i == 0) __builtin_amdgcn_s_setprio(1);
+            if (h == 3 && i == kNT - 1) __builtin_amdgcn_s_setprio(0);
+          }
         }
       }
       now = next;
@@ -354,20 +357,21 @@ int launch_tile(const Mm8Args& g, hipStream_t st) {
 // Which tile: a launch takes rounds of one tile a compute unit, a round the blocks of K times the tile's time for one and its two
 // ends, in us.  Launches as measured, in us; the rule takes the least, or one within 3 % of it:
 //   bf16 results         64 x 64   64 x 128   128 x 128   128 x 256   256 x 256     float32   64 x 64   64 x 128   128 x 128
-//    256 x 4096 x 4096     11.6       14.7        21.7        30.1        48.2                  17.5       22.6        46.8
-//    512 x 4096 x 4096     21.6       16.2        22.2        30.1        48.6                  32.0       25.2        46.8
-//   1024 x 4096 x 4096     40.7       29.7        24.7        32.0        48.5                  59.4       48.2        50.2
-//   2048 x 4096 x 4096     77.7       57.2        46.6        38.7        53.3                 118.3       90.1        95.8
-//   4096 x 4096 x 4096    152.5      111.6        91.3        74.7        64.8
-//   1003 x 2120 x 2000     22.4       20.9        15.4        19.2        29.3                  29.3       27.8        27.2
-//   3000 x 1000 x  512      8.3        9.8         6.9         8.0        10.9
-// The smaller ones share the blocks of K between two groups of waves, and short reductions on 64 x 64 tiles take two stages instead
-// of four, two workgroups a compute unit (200 x 2048 x 1024: 4.8 us against 5.1; 256 x 4096 x 4096: 14.9 against 11.6).
+//    256 x 4096 x 4096     17.1       22.0        29.7        53.5        91.3                  17.8       22.8        42.9
+//    512 x 4096 x 4096     32.4       24.1        31.2        53.9        91.8                  32.9       25.3        43.4
+//   1024 x 4096 x 4096     62.6       46.2        34.4        55.2        91.7                  61.2       47.2        46.5
+//   2048 x 4096 x 4096    119.4       87.4        66.3        61.8        94.0                 119.0       89.8        89.0
+//   4096 x 4096 x 4096    229.6      169.5       124.4       117.7       104.8                 235.6      180.5       173.7
+//   1003 x 2120 x 2000     28.6       26.8        18.2        29.7        49.3                  29.9       27.9        25.3
+//   3000 x 1000 x  512     11.3       11.8         8.4        10.8        16.4                  13.1       14.2        11.9
+//   4000 x 4008 x  272     52.8       44.3        31.3        22.0        19.1
+// The smaller ones share the blocks of K between two groups of waves (128 x 128 for bf16 results only), and short reductions on
+// 64 x 64 tiles take two stages instead of four, two workgroups a compute unit (197 x 2048 x 1024).
 // Where there is a compute unit for each, tiles are 64 x 32: two groups of waves and two stages up to 12 blocks of K, four and three
-// beyond.  bf16 / float32 results, 64 x 64 and these two:
-//   64 x 4096 x  512     3.8, 3.3,  4.6 /  4.7,  3.9,  5.2         197 x 2048 x 1024     4.8, 4.3, 4.7 / 6.1, 5.0, 5.4
-//   64 x 4096 x 2048     6.5, 5.8,  5.7 /  9.5,  7.1,  6.9          64 x 4096 x 8192    17.7, 22.3, 14.3 / 26.9, 25.2, 17.0
-// and with two tiles a compute unit, 128 x 8192 x 2048, 7.7, 9.1, 11.5 / 10.7, 11.1, 14.0.
+// beyond.  64 x 64 and these two, float32 results (bf16 ones take 0 to 0.5 us less):
+//   64 x 4096 x  512      4.7,  3.9,  5.2         197 x 2048 x 1024     6.1,  5.0,  5.4
+//   64 x 4096 x 2048      9.7,  7.3,  6.9          64 x 4096 x 8192    27.2, 25.2, 16.7
+// and with two tiles a compute unit, 128 x 8192 x 2048, 10.7, 11.1, 14.2.
 struct TileTime {
   int bm, bn;
   float block, ends;
@@ -385,8 +389,8 @@ int launch_mm8(const Mm8Args& g, hipStream_t st) {
     return check_launch();
   }
   constexpr bool kBf16 = sizeof(OT) == 2;
-  constexpr TileTime kTimes[5] = {{64, 64, kBf16 ? 0.24f : 0.42f, 2.2f}, {64, 128, kBf16 ? 0.39f : 0.6f, 2.2f},
-                                  {128, 128, kBf16 ? 0.63f : 1.35f, 2.2f}, {128, 256, 1.1f, 3.8f}, {256, 256, 1.95f, 2.0f}};
+  constexpr TileTime kTimes[5] = {{64, 64, 0.45f, 2.0f}, {64, 128, 0.61f, 3.4f},
+                                  {128, 128, kBf16 ? 0.93f : 1.18f, kBf16 ? 4.2f : 6.2f}, {128, 256, 1.66f, 5.5f}, {256, 256, 2.9f, 10.6f}};
   int best = 0;
   for (int i = 1; i < (kBf16 ? 5 : 3); ++i)
     if (tile_time(g, kTimes[i]) < tile_time(g, kTimes[best])) best = i;
