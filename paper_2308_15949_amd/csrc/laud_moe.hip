@@ -17,7 +17,8 @@ struct MoeArgs {
   int64_t ldx, ldo;
   int32_t* experts;     // [T][top_k], the caller's or the workspace's
   float* weights;       // [T][top_k]
-  void* h;              // [T * top_k][Fp] float32, or two planes of it in bf16
+  void* h;              // [T * top_k][Fp] float32, or three planes of it in bf16 (by_token)
+  int by_token;         // the last product is k_moe_down_few's
   float* y;             // [T * top_k][C]: an entry's weighted result
   float* logits;        // [E], of a single token
 };
@@ -172,10 +173,40 @@ __device__ __forceinline__ f32x4 mma_stored(const tok_u4& w, const tok_u4 (&x)[W
     return mma_bf16_16(widen8(w[2], w[3]), __builtin_bit_cast(bf16x8, x[1]), c);
   }
 }
-// Hidden values are float32.  Through bf16 instructions they go as a sum of two, the part bf16 holds and its remainder, 16 bits
-// together (rounded to bf16 alone they would add an error as large as the result's own rounding): the first product leaves them in
-// two planes [entries][Fp], bf16 each, or, for float32 weights, in one of float32.
-template <int W> constexpr int kHiddenPlanes = W == W_F32 ? 1 : 2;
+// Hidden values are float32.  Through bf16 instructions they go as a sum of three: the eight leading bits (not rounded: a finite value
+// stays finite), the eight behind them and the rest, which hold all 24 (rounded to bf16 alone they would add an error as large as
+// the result's own rounding, in two parts one of 2^-17 of theirs).  k_moe_down splits them in registers, beside its loads of weights;
+// k_moe_down_few, whose lanes hold a part each, finds them split in three planes (split there: one token 34.9 us against 29.5).  Where
+// the leading parts' sum is infinite or NaN it is the result: an infinite weight times a part that is zero, or the parts behind an
+// infinity, are none of the formula's.
+__device__ __forceinline__ unsigned leading(float a, float b) {  // of two values, as two bf16
+  return (__float_as_uint(a) >> 16) | (__float_as_uint(b) & 0xffff0000u);
+}
+__device__ __forceinline__ float behind(float a) { return a - __uint_as_float(__float_as_uint(a) & 0xffff0000u); }
+__device__ __forceinline__ void split8(const tok_u4& x, const tok_u4& y, bf16x8 (&part)[3]) {
+  float f[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) f[e] = __uint_as_float(e < 4 ? x[e] : y[e - 4]);
+#pragma unroll
+  for (int n = 0; n < 3; ++n) {
+    tok_u4 v;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      v[e] = leading(f[2 * e], f[2 * e + 1]);
+      f[2 * e] = behind(f[2 * e]);
+      f[2 * e + 1] = behind(f[2 * e + 1]);
+    }
+    part[n] = __builtin_bit_cast(bf16x8, v);
+  }
+}
+__device__ __forceinline__ float joined(float lead, float rest) { return fabsf(lead) < INFINITY ? lead + rest : lead; }
+template <int W> constexpr int kHiddenParts = W == W_F32 ? 1 : 3;
+// Eight codes of a piece of weights (of bf16 ones: all of it).
+template <int W>
+__device__ __forceinline__ bf16x8 eight(const tok_u4& w, int g) {
+  if constexpr (W == W_E4M3) return widen8(w[2 * g], w[2 * g + 1]);
+  else return __builtin_bit_cast(bf16x8, w);
+}
 
 // The products run for (tile of channels, slot): a slot is an expert, or, where the entries (token, choice) are fewer than the
 // experts, an entry, whose workgroups take its expert if no earlier entry has the same.
@@ -313,20 +344,16 @@ __global__ __launch_bounds__((ONE ? kSplitOne : kSplit<W>) * kWave) void k_moe_u
 #pragma unroll
       for (int i = 0; i < 4; ++i) h[i] = quarter * 4 < rows ? v[0][i] / (1.f + expf(-v[0][i])) * v[1][i] : 0.f;
       const long long at = (long long)entry * a.Fp + f0 + quarter * 4;
-      if constexpr (kHiddenPlanes<W> == 1) {
+      if (W == W_F32 || !a.by_token) {
         *reinterpret_cast<f32x4*>(reinterpret_cast<float*>(a.h) + at) = h;
       } else {
-        const tok_u2 hi = {pack_bf16(h[0], h[1]), pack_bf16(h[2], h[3])};
-        f32x4 rest;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float top = __uint_as_float(i % 2 ? hi[i / 2] & 0xffff0000u : hi[i / 2] << 16);
-          rest[i] = fabsf(top) == INFINITY ? 0.f : h[i] - top;  // (an infinity has no remainder)
-        }
-        const tok_u2 lo = {pack_bf16(rest[0], rest[1]), pack_bf16(rest[2], rest[3])};
         bf16_t* plane = reinterpret_cast<bf16_t*>(a.h) + at;
-        *reinterpret_cast<tok_u2*>(plane) = hi;
-        *reinterpret_cast<tok_u2*>(plane + (long long)a.T * a.top_k * a.Fp) = lo;
+#pragma unroll
+        for (int n = 0; n < 3; ++n, plane += (long long)a.T * a.top_k * a.Fp) {
+          *reinterpret_cast<tok_u2*>(plane) = tok_u2{leading(h[0], h[1]), leading(h[2], h[3])};
+#pragma unroll
+          for (int i = 0; i < 4; ++i) h[i] = behind(h[i]);
+        }
       }
     }
   }
@@ -337,8 +364,7 @@ __global__ __launch_bounds__((ONE ? kSplitOne : kSplit<W>) * kWave) void k_moe_u
 template <int W>
 __global__ __launch_bounds__(kSplit<W> * kWave) void k_moe_down(MoeArgs a) {
   typedef Weights<W> WT;
-  constexpr int N = kColumns / 16, S = kSplit<W>, kXP = W == W_E4M3 ? 2 : 1;
-  constexpr unsigned kHb = W == W_F32 ? 4 : 2;  // bytes of a hidden value in a plane
+  constexpr int N = kColumns / 16, S = kSplit<W>, kXP = WT::kElems / 4;
   __shared__ int list[LAUD_MOE_MAX_TOKENS], counts[2];
   __shared__ f32x4 part[S][N][kWave];
   const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), r16 = lane % 16, quarter = lane / 16;
@@ -363,37 +389,49 @@ __global__ __launch_bounds__(kSplit<W> * kWave) void k_moe_down(MoeArgs a) {
   const int len = find_entries(a, slot, list, counts);
   if (len == 0) return;
   const __amdgpu_buffer_rsrc_t rh = bytes_of(a.h, (long long)a.T * a.top_k * a.Fp * 4);
-  const unsigned plane = (unsigned)(a.T * a.top_k) * (unsigned)a.Fp * kHb;
   const float* s = W == W_E4M3 ? a.s_down + ((long long)slot.expert * scale_blocks(a.C) + c0 / kScaleBlock) * kb_all : nullptr;
   for (int l0 = 0; l0 < len; l0 += 16) {
     const int entry = list[min(l0 + r16, len - 1)];
     const bool real = l0 + r16 < len;
-    const unsigned at = (unsigned)entry * (unsigned)a.Fp * kHb;
+    const unsigned at = (unsigned)entry * (unsigned)a.Fp * 4;
     const float share = a.weights[entry];
     f32x4 v[N] = {};
     for (int kb = wave; kb < kb_all; kb += S) {
       request(kb);
       const float f = s ? s[kb] : 1.f;
-      tok_u4 x[WT::kPieces][kHiddenPlanes<W>][kXP];
+      tok_u4 x[WT::kPieces][kXP];
 #pragma unroll
       for (int p = 0; p < WT::kPieces; ++p) {
         const int k = kb * kScaleBlock + WT::first(p, quarter);
 #pragma unroll
-        for (int i = 0; i < kHiddenPlanes<W>; ++i)
-#pragma unroll
-          for (int u = 0; u < kXP; ++u) x[p][i][u] = load16(rh, real ? i * plane + at + (unsigned)(k + 8 * u) * kHb : kOutside);
+        for (int u = 0; u < kXP; ++u) x[p][u] = load16(rh, real ? at + (unsigned)(k + 4 * u) * 4 : kOutside);
       }
       __builtin_amdgcn_sched_barrier(0);  // (as above)
+      f32x4 lead[N] = {}, rest[N] = {};
 #pragma unroll
-      for (int n = 0; n < N; ++n) {
-        f32x4 r = {0.f, 0.f, 0.f, 0.f};
+      for (int p = 0; p < WT::kPieces; ++p) {
+        if constexpr (W == W_F32) {
 #pragma unroll
-        for (int p = 0; p < WT::kPieces; ++p)
+          for (int n = 0; n < N; ++n) lead[n] = mma_stored<W>(w[n][p], x[p], lead[n]);
+        } else {
 #pragma unroll
-          for (int i = 0; i < kHiddenPlanes<W>; ++i) r = mma_stored<W>(w[n][p], x[p][i], r);
+          for (int g = 0; g < kXP / 2; ++g) {
+            bf16x8 h[3];
+            split8(x[p][2 * g], x[p][2 * g + 1], h);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[n][i] = fmaf(r[i], f, v[n][i]);
+            for (int n = 0; n < N; ++n) {
+              const bf16x8 wv = eight<W>(w[n][p], g);
+              lead[n] = mma_bf16_16(wv, h[0], lead[n]);
+              rest[n] = mma_bf16_16(wv, h[1], rest[n]);
+              rest[n] = mma_bf16_16(wv, h[2], rest[n]);
+            }
+          }
+        }
       }
+#pragma unroll
+      for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[n][i] = fmaf(joined(lead[n][i], rest[n][i]), f, v[n][i]);
     }
     join_waves<S>(v, part, wave, lane);
     if (wave == 0 && real) {
@@ -424,7 +462,7 @@ __global__ __launch_bounds__(256) void k_moe_sum(MoeArgs a) {
 // that tokens seldom share one, nothing is gained by joining theirs and nothing has to be handed from workgroup to workgroup.  All
 // of a wave's loads are under way together.  The waves share the entries' blocks of the reduction, two at a time, as the two halves
 // of a matrix instruction's sixteen rows of weights; of the token side, column 0 is the even block and column 1 the odd one, columns
-// 2 and 3 the remainders of both; a half's results stand in its columns.  Sums are added in the waves' order.
+// 2 to 5 the parts behind the leading ones of both; a half's results stand in its columns.  Sums are added in the waves' order.
 // The layer, with k_moe_down / with this kernel, in us:
 //   8 of 64 experts of 2048 x 1024, bf16    1 token 35.6 / 32.0    4 tokens 89.3 / 83.2    8 tokens 129.5 / 127.6    16 tokens 162.6 / 188.5
 //   6 of 64 experts of 2048 x 1424, e4m3            29.4 / 24.7             65.4 / 58.7              90.9 /  87.3             116.0 / 123.6
@@ -436,15 +474,15 @@ template <int W> constexpr int kPairs = W == W_F32 ? 1 : 2;  // pairs whose load
 template <int W, typename OT, int S>
 __global__ __launch_bounds__(S * kWave) void k_moe_down_few(MoeArgs a) {
   typedef Weights<W> WT;
-  constexpr unsigned kHb = W == W_F32 ? 4 : 2;
-  constexpr int kXP = W == W_E4M3 ? 2 : 1, P = kHiddenPlanes<W>, kAtOnce = kPairs<W>;
+  constexpr unsigned kHb = W == W_F32 ? 4 : 2;  // bytes of a hidden value in a plane
+  constexpr int kXP = W == W_E4M3 ? 2 : 1, P = kHiddenParts<W>, kAtOnce = kPairs<W>;
   __shared__ f32x4 part[S][4][P];
   const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), r16 = lane % 16, quarter = lane / 16;
   const int t = blockIdx.y, c0 = blockIdx.x * kFewColumns;
   const int kb_all = scale_blocks(a.F), pairs = (kb_all + 1) / 2, items = a.keep && a.keep[t] == 0 ? 0 : a.top_k * pairs;
   const long long row_bytes = (long long)a.F * WT::kBytes;
-  const __amdgpu_buffer_rsrc_t rh = bytes_of(a.h, (long long)a.T * a.top_k * a.Fp * 4);
-  const unsigned plane = (unsigned)(a.T * a.top_k) * (unsigned)a.Fp * kHb;
+  const unsigned plane = (unsigned)(a.T * a.top_k) * (unsigned)a.Fp * kHb;  // (three of them: below 2^32)
+  const __amdgpu_buffer_rsrc_t rh = bytes_of(a.h, (long long)P * plane);
   f32x4 v = {0.f, 0.f, 0.f, 0.f};
   for (int i0 = wave; i0 < items; i0 += S * kAtOnce) {
     tok_u4 w[kAtOnce][WT::kPieces], x[kAtOnce][WT::kPieces][kXP];
@@ -496,17 +534,22 @@ __global__ __launch_bounds__(S * kWave) void k_moe_down_few(MoeArgs a) {
   if (r16 < 2 * P && r16 % 2 == quarter / 2) part[wave][quarter][r16 / 2] = v;
   __syncthreads();
   if ((int)threadIdx.x >= kFewColumns / 4) return;
-  f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+  f32x4 sum = {0.f, 0.f, 0.f, 0.f}, rest = sum;
 #pragma unroll
-  for (int n = 0; n < S; ++n)
+  for (int n = 0; n < S; ++n) {
+    sum += part[n][threadIdx.x][0] + part[n][threadIdx.x + 2][0];
 #pragma unroll
-    for (int p = 0; p < P; ++p) sum += part[n][threadIdx.x][p] + part[n][threadIdx.x + 2][p];
+    for (int p = 1; p < P; ++p) rest += part[n][threadIdx.x][p] + part[n][threadIdx.x + 2][p];
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) sum[i] = joined(sum[i], rest[i]);
   store4(reinterpret_cast<OT*>(a.out) + t * a.ldo + c0 + threadIdx.x * 4, sum);
 }
 
 template <int W, typename ET>
-void launch_moe(const MoeArgs& a, hipStream_t st) {
+void launch_moe(MoeArgs& a, hipStream_t st) {
   const long long entries = (long long)a.T * a.top_k;
+  a.by_token = entries <= a.E;
   const dim3 up(a.Fp / 16, (unsigned)min((long long)a.E, entries));
   if (a.T == 1) {
     hipLaunchKernelGGL((k_moe_logits<ET>), dim3((a.E - 1) / kLogitWaves + 1), dim3(kLogitWaves * kWave), 0, st, a);
@@ -515,7 +558,7 @@ void launch_moe(const MoeArgs& a, hipStream_t st) {
     hipLaunchKernelGGL((k_moe_route<ET>), dim3(a.T), dim3(kRouteThreads), 0, st, a);
     hipLaunchKernelGGL((k_moe_up<W, false>), up, dim3(kSplit<W> * kWave), 0, st, a);
   }
-  if (entries > a.E) {
+  if (!a.by_token) {
     hipLaunchKernelGGL((k_moe_down<W>), dim3((a.C - 1) / kColumns + 1, a.E), dim3(kSplit<W> * kWave), 0, st, a);
     hipLaunchKernelGGL((k_moe_sum<ET>), dim3((a.C - 1) / 1024 + 1, a.T), dim3(256), 0, st, a);
   } else {
@@ -535,7 +578,8 @@ MoeWs moe_ws(const laud_moe_layer* p, int T) {
   w.experts = 0;
   w.weights = align_up(n * 4, 256);
   w.h = w.weights + align_up(n * 4, 256);
-  w.y = align_up(w.h + n * (size_t)scale_blocks(p->F) * kScaleBlock * 4, 256);
+  // three planes of bf16, or one of float32
+  w.y = align_up(w.h + n * (size_t)scale_blocks(p->F) * kScaleBlock * 6, 256);
   w.logits = align_up(w.y + n * (size_t)p->C * 4, 256);
   w.bytes = w.logits + (size_t)p->E * 4;
   return w;

@@ -134,7 +134,7 @@ __device__ __forceinline__ f32x4 mma_bf16_16(bf16x8 a, bf16x8 b, f32x4 c) { retu
 // ---- memory through descriptors ---------------------------------------------------------------------------------------------
 constexpr unsigned kOutside = 0xfffffff0u;  // an offset past every descriptor: reads zeros
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t bytes_of(const void* base, long long bytes) {
-  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, (int)min(bytes, 0x7fffffffll), 0x00020000);
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, (int)(unsigned)min(bytes, 0xffffffe0ll), 0x00020000);
 }
 __device__ __forceinline__ tok_u4 load16(__amdgpu_buffer_rsrc_t r, unsigned off) {
   return __builtin_bit_cast(tok_u4, __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, 0));
