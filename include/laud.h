@@ -364,7 +364,8 @@ int laud_channel_masker(const void* x, laud_fmap fx, const float* wa, const floa
  *   - Rows may be further apart than they are long: an `ld` argument is the distance of two rows in elements, at least the
  *     row length and, like it, a multiple of 8 (of 16 for LAUD_E4M3 operands of a product).  Bases are 16-byte aligned.
  *   - No row (rows, M or T = 0): LAUD_OK, nothing is launched.
- *   - Sizes of one tensor are limited by memory only: rows are addressed with 64 bits.
+ *   - Rows are addressed with 64 bits: tensors are limited by memory, and by what one launch takes where an entry point
+ *     says so (LAUD_ERR_UNSUPPORTED beyond).
  *   - Sums, statistics and accumulators are float32; each result is rounded once, to nearest even.
  */
 
@@ -374,7 +375,7 @@ int laud_channel_masker(const void* x, laud_fmap fx, const float* wa, const floa
 /*
  * Quantises x [rows][cols] (dtype, cols a multiple of 8): scale = max(max|x| / 448, 2^-126) over the block, q = e4m3(x / scale), the
  * quotient in float32, ties to even.  A NaN or an infinity makes its block's codes NaN.  block_rows: 1 (activations) or 128
- * (weights).
+ * (weights; then cols at most 2^31 - 128).
  */
 int laud_quantize_e4m3(const void* x, int64_t ldx, int rows, int cols, int dtype, int block_rows, void* q, int64_t ldq,
                        float* scale, void* stream);
@@ -418,7 +419,8 @@ int laud_norm_residual(const laud_norm_block* p, int rows, const void* x, int64_
  * rows at most 2^22 elements apart; sa [M][ceil(K/128)], sb [ceil(N/128)][ceil(K/128)] (laud_quantize_e4m3 with block_rows 1 and
  * 128); out [M][N] of out_dtype (LAUD_F32 or LAUD_BF16), no alias of an input.  Codes are widened
  * to bf16, which holds them exactly; products and sums are float32 for every shape and both types of result, so that the number of
- * rows changes a row's result by the order of its sums only.
+ * rows changes a row's result by the order of its sums only.  At most 2^27 - 16 columns for up to 16 rows; for more rows 2^23 - 8
+ * tiles of 64 x 64 (larger ones where the results are many).
  * Workspace: laud_matmul_e4m3_workspace(M, N, K) bytes; no shape needs any at present (then ws may be NULL).
  */
 size_t laud_matmul_e4m3_workspace(int M, int N, int K);

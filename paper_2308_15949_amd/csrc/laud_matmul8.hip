@@ -340,6 +340,8 @@ __global__ __launch_bounds__(KG * BM / WM * (BN / WN) * kWave) void k_mm8_tile(M
   }
 }
 
+inline double tile_count(const Mm8Args& g, int bm, int bn) { return (double)((g.M - 1) / bm + 1) * ((g.N - 1) / bn + 1); }
+
 template <typename OT, int BM, int BN, int WM, int WN, int NS, int KG = 1>
 int ask_tile_lds() {
   return hipFuncSetAttribute(reinterpret_cast<const void*>(&k_mm8_tile<OT, BM, BN, WM, WN, NS, KG>), hipFuncAttributeMaxDynamicSharedMemorySize,
@@ -347,10 +349,12 @@ int ask_tile_lds() {
 }
 template <typename OT, int BM, int BN, int WM, int WN, int NS, int KG = 1>
 int launch_tile(const Mm8Args& g, hipStream_t st) {
+  constexpr int kThreads = KG * BM / WM * (BN / WN) * kWave;
+  if (!launchable(tile_count(g, BM, BN) + 7, kThreads)) return LAUD_ERR_UNSUPPORTED;  // (so that their number is an int's)
   if (matmul8_init_device() != LAUD_OK) return LAUD_ERR_HIP;
   const int mtiles = (g.M - 1) / BM + 1, ntiles = (g.N - 1) / BN + 1;
-  hipLaunchKernelGGL((k_mm8_tile<OT, BM, BN, WM, WN, NS, KG>), dim3((unsigned)((mtiles * ntiles + 7) / 8 * 8)),
-                     dim3(KG * BM / WM * (BN / WN) * kWave), (TileLds<BM, BN, NS, KG>::kBytes), st, g, mtiles, ntiles);
+  hipLaunchKernelGGL((k_mm8_tile<OT, BM, BN, WM, WN, NS, KG>), dim3((unsigned)((mtiles * ntiles + 7) / 8 * 8)), dim3(kThreads),
+                     (TileLds<BM, BN, NS, KG>::kBytes), st, g, mtiles, ntiles);
   return check_launch();
 }
 
@@ -376,7 +380,6 @@ struct TileTime {
   int bm, bn;
   float block, ends;
 };
-inline double tile_count(const Mm8Args& g, int bm, int bn) { return (double)((g.M - 1) / bm + 1) * ((g.N - 1) / bn + 1); }
 inline float tile_time(const Mm8Args& g, const TileTime& t) {
   return (float)(std::ceil(tile_count(g, t.bm, t.bn) / kComputeUnits) * (g.kb * t.block + t.ends));
 }
@@ -385,6 +388,7 @@ template <typename OT>
 int launch_mm8(const Mm8Args& g, hipStream_t st) {
   if (g.M <= kSplitRows) {
     const int ntiles = (g.N - 1) / 16 + 1;
+    if (!launchable(ntiles, kSplit * kWave)) return LAUD_ERR_UNSUPPORTED;
     hipLaunchKernelGGL((k_mm8_split<OT>), dim3(ntiles), dim3(kSplit * kWave), kSplit * kWave * sizeof(f32x4), st, g);
     return check_launch();
   }
@@ -394,7 +398,6 @@ int launch_mm8(const Mm8Args& g, hipStream_t st) {
   int best = 0;
   for (int i = 1; i < (kBf16 ? 5 : 3); ++i)
     if (tile_time(g, kTimes[i]) < tile_time(g, kTimes[best])) best = i;
-  if (tile_count(g, kTimes[best].bm, kTimes[best].bn) > 1e9) return LAUD_ERR_UNSUPPORTED;
   if constexpr (kBf16) {
     if (best == 4) return launch_tile<OT, 256, 256, 128, 64, 2>(g, st);
     if (best == 3) return launch_tile<OT, 128, 256, 64, 64, 3>(g, st);

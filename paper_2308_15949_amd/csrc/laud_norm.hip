@@ -357,7 +357,7 @@ extern "C" int laud_quantize_e4m3(const void* x, int64_t ldx, int rows, int cols
                                   float* scale, void* stream) {
   using namespace laud;
   if (rows < 0 || cols <= 0 || !float_type(dtype) || (block_rows != 1 && block_rows != kScaleBlock)) return LAUD_ERR_INVALID_ARG;
-  if (cols % 8) return LAUD_ERR_UNSUPPORTED;
+  if (cols % 8 || (block_rows != 1 && !launchable(scale_blocks(cols), 256))) return LAUD_ERR_UNSUPPORTED;
   if (rows == 0) return LAUD_OK;
   if (!x || !q || !scale || !good_ld(ldx, cols, 8) || !good_ld(ldq, cols, 8) || !aligned16(x) || !aligned16(q)) return LAUD_ERR_INVALID_ARG;
   if (rows_meet(x, ldx, elem_bytes(dtype), q, ldq, 1, rows, cols)) return LAUD_ERR_INVALID_ARG;

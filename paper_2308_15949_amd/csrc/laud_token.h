@@ -13,7 +13,7 @@ typedef unsigned int tok_u2 __attribute__((ext_vector_type(2)));
 constexpr int kScaleBlock = 128;       // elements that share a scale along a row
 constexpr float kE4m3Max = 448.f;
 
-inline __host__ __device__ int scale_blocks(int n) { return (n + kScaleBlock - 1) / kScaleBlock; }
+inline __host__ __device__ int scale_blocks(int n) { return n / kScaleBlock + (n % kScaleBlock != 0); }  // (no sum past 2^31)
 
 // ---- reductions whose result every lane gets; data-parallel moves inside a row of sixteen lanes, swaps across rows ---------
 template <int CTRL>
@@ -150,6 +150,8 @@ __device__ __forceinline__ void store4(OT* out, const f32x4& v) {
 }
 
 // ---- host side: argument checks the token operators share ------------------------------------------------------------------
+// whether a launch of so many workgroups has less than 2^32 threads, the most that one takes along a dimension
+inline bool launchable(double groups, int threads) { return groups * threads < 4294967296.0; }
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 inline bool good_ld(int64_t ld, int cols, int step) { return ld >= cols && ld % step == 0; }
 inline bool float_type(int dtype) { return dtype == LAUD_F32 || dtype == LAUD_BF16; }
