@@ -3,6 +3,9 @@ operators from torch tensors, with the host compiler.
 
     python -m paper_2308_15949_amd.build
 
+The library needs hipcc only: where torch cannot be imported the extension is left out, with a line on stderr, and where it does not
+compile the library is there before the error is raised.
+
 Every source is compiled to an object of its own (in parallel), then linked; objects live in
 csrc/_build/ (ignored by git).
 """
@@ -46,8 +49,10 @@ def extension_command() -> list[str]:
 
     import torch
     home = os.path.dirname(torch.__file__)
-    include = [os.path.join(home, "include"), os.path.join(home, "include", "torch", "csrc", "api", "include"), "/opt/rocm/include"]
+    include = [os.path.join(home, "include"), os.path.join(home, "include", "torch", "csrc", "api", "include"),
+               os.path.join(os.environ.get("ROCM_PATH", "/opt/rocm"), "include")]
     return [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-shared", "-fPIC", "-D__HIP_PLATFORM_AMD__=1", "-DUSE_ROCM=1",
+            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}",
             "-I", os.path.join(ROOT, "include"), "-I", sysconfig.get_paths()["include"],
             *(a for d in include for a in ("-isystem", d)), os.path.join(CSRC, "laud_torch.cpp"), "-o", EXTENSION,
             "-L", os.path.join(home, "lib"), "-lc10", "-lc10_hip", "-ltorch_cpu", "-ltorch_python"]
@@ -58,10 +63,17 @@ def build(verbose: bool = True) -> str:
     os.makedirs(OBJ, exist_ok=True)
     objs = [os.path.join(OBJ, s.replace(".hip", ".o")) for s in SOURCES]
     jobs = [[hipcc, *FLAGS, "-c", os.path.join(CSRC, s), "-o", o] for s, o in zip(SOURCES, objs)]
-    jobs.append(extension_command())
-    with ThreadPoolExecutor(max_workers=min(8, len(jobs))) as ex:
+    try:
+        extension = extension_command()
+    except ImportError as e:
+        extension = None
+        sys.stderr.write(f"{os.path.basename(EXTENSION)} (calls of the token operators from torch tensors) is left out: {e}\n")
+    with ThreadPoolExecutor(max_workers=min(8, len(jobs) + 1)) as ex:
+        made = ex.submit(_run, extension, verbose) if extension else None
         list(ex.map(lambda c: _run(c, verbose), jobs))
     _run([hipcc, "--offload-arch=gfx950", "-shared", "-fPIC", *objs, "-o", LIB], verbose)
+    if made:
+        made.result()  # (raises what the extension's compiler said, behind the library's link)
     return LIB
 
 
