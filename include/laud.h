@@ -364,6 +364,8 @@ int laud_channel_masker(const void* x, laud_fmap fx, const float* wa, const floa
  *   - Rows may be further apart than they are long: an `ld` argument is the distance of two rows in elements, at least the
  *     row length and, like it, a multiple of 8 (of 16 for LAUD_E4M3 operands of a product).  Bases are 16-byte aligned.
  *   - No row (rows, M or T = 0): LAUD_OK, nothing is launched.
+ *   - What is written shares no byte with anything else of the call, except where an argument says what it may be
+ *     (LAUD_ERR_INVALID_ARG).
  *   - Rows are addressed with 64 bits: tensors are limited by memory, and by what one launch takes where an entry point
  *     says so (LAUD_ERR_UNSUPPORTED beyond).
  *   - Sums, statistics and accumulators are float32; each result is rounded once, to nearest even.

@@ -451,6 +451,8 @@ extern "C" int laud_matmul_e4m3(const void* a, int64_t lda, const float* sa, con
   if (lda > kMaxLd || ldb > kMaxLd) return LAUD_ERR_UNSUPPORTED;
   const size_t ob = span_bytes(M, ldo, N, elem_bytes(out_dtype));
   if (ranges_meet(a, span_bytes(M, lda, K, 1), out, ob) || ranges_meet(b, span_bytes(N, ldb, K, 1), out, ob)) return LAUD_ERR_INVALID_ARG;
+  const size_t kb = (size_t)scale_blocks(K) * 4, eb = elem_bytes(out_dtype);
+  if (range_meets_rows(sa, M * kb, out, ldo, eb, M, N) || range_meets_rows(sb, scale_blocks(N) * kb, out, ldo, eb, M, N)) return LAUD_ERR_INVALID_ARG;
   Mm8Args g{(const uint8_t*)a, (const uint8_t*)b, sa, sb, out, M, N, K, scale_blocks(K), lda, ldb, ldo};
   clear_stale_error();
   return out_dtype == LAUD_BF16 ? launch_mm8<bf16_t>(g, (hipStream_t)stream) : launch_mm8<float>(g, (hipStream_t)stream);

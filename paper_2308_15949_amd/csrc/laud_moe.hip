@@ -585,6 +585,28 @@ MoeWs moe_ws(const laud_moe_layer* p, int T) {
   return w;
 }
 
+// Whether what a call writes (out, its routing, the workspace) lies over what it reads or over each other; out may be x.
+bool moe_overlaps(const laud_moe_layer* p, int T, const void* x, int64_t ldx, const uint8_t* keep, const void* out, int64_t ldo,
+                  const int32_t* experts, const float* weights, const void* ws, size_t ws_bytes) {
+  struct Range { const void* p; size_t n; };
+  const size_t E = p->E, C = p->C, F = p->F, eb = elem_bytes(p->dtype), wb = p->w_dtype == LAUD_E4M3 ? 1 : eb;
+  const size_t scales = p->w_dtype == LAUD_E4M3 ? E * scale_blocks(p->F) * scale_blocks(p->C) * 4 : 0, chosen = (size_t)T * p->top_k * 4;
+  const Range written[] = {{experts, chosen}, {weights, chosen}, {ws, ws_bytes}};
+  for (const Range& r : {Range{p->router, E * C * eb}, Range{p->up, E * 2 * F * C * wb}, Range{p->down, E * C * F * wb},
+                         Range{p->s_up, 2 * scales}, Range{p->s_down, scales}, Range{keep, (size_t)T}}) {
+    if (range_meets_rows(r.p, r.n, out, ldo, eb, T, p->C)) return true;
+    for (const Range& w : written)
+      if (ranges_meet(r.p, r.n, w.p, w.n)) return true;
+  }
+  for (int i = 0; i < 3; ++i) {
+    const Range& w = written[i];
+    if (range_meets_rows(w.p, w.n, x, ldx, eb, T, p->C) || range_meets_rows(w.p, w.n, out, ldo, eb, T, p->C)) return true;
+    for (int j = 0; j < i; ++j)
+      if (ranges_meet(w.p, w.n, written[j].p, written[j].n)) return true;
+  }
+  return false;
+}
+
 int validate_moe(const laud_moe_layer* p, int T) {
   if (!p || T < 0 || p->C <= 0 || p->F <= 0 || p->E <= 0 || p->top_k <= 0 || p->top_k > p->E || !float_type(p->dtype))
     return LAUD_ERR_INVALID_ARG;
@@ -619,6 +641,7 @@ extern "C" int laud_moe(const laud_moe_layer* p, int T, const void* x, int64_t l
   if (!same_or_apart(x, ldx, eb, out, ldo, eb, T, p->C)) return LAUD_ERR_INVALID_ARG;
   if (!ws || ws_bytes < laud_moe_workspace(p, T)) return LAUD_ERR_WORKSPACE;
   const MoeWs w = moe_ws(p, T);
+  if (moe_overlaps(p, T, x, ldx, keep, out, ldo, experts, weights, ws, w.bytes)) return LAUD_ERR_INVALID_ARG;
   MoeArgs a{};
   a.T = T; a.C = p->C; a.F = p->F; a.E = p->E; a.top_k = p->top_k; a.renormalise = p->renormalise;
   a.Fp = scale_blocks(p->F) * kScaleBlock;

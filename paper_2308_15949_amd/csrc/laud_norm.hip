@@ -335,6 +335,18 @@ extern "C" int laud_norm_residual(const laud_norm_block* p, int rows, const void
       (z && (!same_or_apart(x, ldx, eb, z, ldz, zb, rows, p->C) || (y && !same_or_apart(y, ldy, eb, z, ldz, zb, rows, p->C)))) ||
       (out && z && rows_meet(out, ldo, eb, z, ldz, zb, rows, p->C)))
     return LAUD_ERR_INVALID_ARG;
+  // ... and over nothing that every row reads; the scales over nothing at all
+  const size_t scales = z8 ? (size_t)rows * scale_blocks(p->C) * 4 : 0, vector = (size_t)p->C * 4;
+  const auto over_result = [&](const void* q, size_t n) {
+    return range_meets_rows(q, n, out, ldo, eb, rows, p->C) || range_meets_rows(q, n, z, ldz, zb, rows, p->C);
+  };
+  for (const void* v : {y ? p->post_w : nullptr, y && p->post_w ? p->post_b : nullptr, z ? p->pre_w : nullptr, z ? p->pre_b : nullptr})
+    if (over_result(v, vector) || ranges_meet(v, vector, z_scale, scales)) return LAUD_ERR_INVALID_ARG;
+  const size_t gates = gate ? ((size_t)(rows - 1) / rows_per_gate + 1) * vector : 0;
+  if (over_result(keep, rows) || over_result(gate, gates) || over_result(z_scale, scales) || ranges_meet(keep, rows, z_scale, scales) ||
+      ranges_meet(gate, gates, z_scale, scales) || range_meets_rows(z_scale, scales, x, ldx, eb, rows, p->C) ||
+      range_meets_rows(z_scale, scales, y, ldy, eb, rows, p->C))
+    return LAUD_ERR_INVALID_ARG;
   NormArgs a{};
   a.rows = rows; a.C = p->C; a.kind = p->kind; a.rows_per_gate = rows_per_gate;
   a.eps = p->eps; a.alpha = p->alpha; a.beta = p->beta; a.inv_c = 1.f / (float)p->C;
@@ -360,7 +372,10 @@ extern "C" int laud_quantize_e4m3(const void* x, int64_t ldx, int rows, int cols
   if (cols % 8 || (block_rows != 1 && !launchable(scale_blocks(cols), 256))) return LAUD_ERR_UNSUPPORTED;
   if (rows == 0) return LAUD_OK;
   if (!x || !q || !scale || !good_ld(ldx, cols, 8) || !good_ld(ldq, cols, 8) || !aligned16(x) || !aligned16(q)) return LAUD_ERR_INVALID_ARG;
-  if (rows_meet(x, ldx, elem_bytes(dtype), q, ldq, 1, rows, cols)) return LAUD_ERR_INVALID_ARG;
+  const size_t scales = ((size_t)(rows - 1) / block_rows + 1) * scale_blocks(cols) * 4;
+  if (rows_meet(x, ldx, elem_bytes(dtype), q, ldq, 1, rows, cols) || range_meets_rows(scale, scales, x, ldx, elem_bytes(dtype), rows, cols) ||
+      range_meets_rows(scale, scales, q, ldq, 1, rows, cols))
+    return LAUD_ERR_INVALID_ARG;
   clear_stale_error();
   if (dtype == LAUD_BF16) launch_quant<bf16_t>(x, ldx, rows, cols, block_rows, q, ldq, scale, (hipStream_t)stream);
   else launch_quant<float>(x, ldx, rows, cols, block_rows, q, ldq, scale, (hipStream_t)stream);

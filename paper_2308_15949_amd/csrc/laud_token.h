@@ -161,6 +161,13 @@ inline bool ranges_meet(const void* a, size_t na, const void* b, size_t nb) {
   const char *p = (const char*)a, *q = (const char*)b;
   return p && q && na && nb && p < q + nb && q < p + na;
 }
+// whether n bytes share one with a row array; they may lie between its rows
+inline bool range_meets_rows(const void* p, size_t n, const void* a, int64_t lda, size_t eb, int rows, int cols) {
+  if (!ranges_meet(p, n, a, span_bytes(rows, lda, cols, eb))) return false;
+  if ((uintptr_t)p < (uintptr_t)a) return true;  // (they reach the first row)
+  const size_t pitch = (size_t)lda * eb, d = (size_t)((uintptr_t)p - (uintptr_t)a) % pitch;
+  return d < (size_t)cols * eb || d + n > pitch;
+}
 // whether two row arrays of `rows` rows share a byte; rows at the same distance may lie side by side (columns of one wider array)
 inline bool rows_meet(const void* a, int64_t lda, size_t ea, const void* b, int64_t ldb, size_t eb, int rows, int cols) {
   if (!a || !b || !ranges_meet(a, span_bytes(rows, lda, cols, ea), b, span_bytes(rows, ldb, cols, eb))) return false;
