@@ -104,12 +104,18 @@ __device__ __forceinline__ float block_scale(unsigned top) {
   return s < 0x1p-126f ? 0x1p-126f : s;  // (NaN stays)
 }
 // Codes of f / s, nearest even.  The quotient by the rounded reciprocal and one correction of its remainder is the rounded quotient
-// (a division for every element took twice the instructions of all the rest of a norm); where s is infinite or NaN it is NaN.
+// (a division for every element took twice the instructions of all the rest of a norm); where s is infinite or NaN it is NaN.  What
+// a quotient of 2^-10 (half the least code) leaves over is as small as 2^-56 s: where that is no float, both are taken 2^64 times.
 __device__ __forceinline__ float quotient(float f, float s, float inv) {
   const float q = f * inv;
   return fmaf(fmaf(-q, s, f), inv, q);
 }
-__device__ __forceinline__ tok_u2 codes8(const float (&f)[8], float s) {
+__device__ __forceinline__ tok_u2 codes8(float (&f)[8], float s) {
+  if (s < 0x1p-60f) {
+    s *= 0x1p64f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f[e] *= 0x1p64f;
+  }
   const float inv = 1.f / s;
   tok_u2 q;
 #pragma unroll
