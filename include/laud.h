@@ -401,7 +401,8 @@ typedef struct {
  * The seam between two residual blocks, in one pass over the rows:
  *   p = y, or norm(y; post_w, post_b);   r = x + branch on the rows a block ran on:  r = alpha * x + beta * gate * p  if keep, else x;
  *   out = r;   z = norm(r; pre_w, pre_b), taken from r before its rounding.
- * norm(v) = v / sqrt(mean(v^2) + eps) * w + b (RMS) or (v - mean(v)) / sqrt(var(v) + eps) * w + b (LAYER).
+ * norm(v) = v / sqrt(mean(v^2) + eps) * w + b (RMS) or (v - mean(v)) / sqrt(var(v) + eps) * w + b (LAYER).  Squares are float32:
+ * where their sum passes 2^128 it is infinite, and what it divides is 0.
  *   x     [rows][C]   residual stream
  *   y     [rows][C]   the block's result, or NULL: r = x (only the norm before a block; keep, gate must be NULL)
  *   keep  [rows] bytes or NULL (all kept): a row with 0 passes x on bit for bit; its y is not read
@@ -417,12 +418,12 @@ int laud_norm_residual(const laud_norm_block* p, int rows, const void* x, int64_
 
 /*
  * out[m][n] = sum_k a[m][k] * sa[m][k/128] * b[n][k] * sb[n/128][k/128]: products of 8-bit operands are added over a block of
- * 128, the block's sum takes its two scales, blocks are added in float32.  a [M][K], b [N][K] E4M3, K a multiple of 16, N of 8,
- * rows at most 2^22 elements apart; sa [M][ceil(K/128)], sb [ceil(N/128)][ceil(K/128)] (laud_quantize_e4m3 with block_rows 1 and
- * 128); out [M][N] of out_dtype (LAUD_F32 or LAUD_BF16), no alias of an input.  Codes are widened
- * to bf16, which holds them exactly; products and sums are float32 for every shape and both types of result, so that the number of
- * rows changes a row's result by the order of its sums only.  At most 2^27 - 16 columns for up to 16 rows; for more rows 2^23 - 8
- * tiles of 64 x 64 (larger ones where the results are many).
+ * 128, the block's sum takes its two scales (their product, in float32), blocks are added in float32.  a [M][K], b [N][K] E4M3, K a
+ * multiple of 16, N of 8, rows at most 2^22 elements apart; sa [M][ceil(K/128)], sb [ceil(N/128)][ceil(K/128)]
+ * (laud_quantize_e4m3 with block_rows 1 and 128); out [M][N] of out_dtype (LAUD_F32 or LAUD_BF16), no alias of an input.  Codes
+ * are widened to bf16, which holds them exactly; products and sums are float32 for every shape and both types of result, so that
+ * the number of rows changes a row's result by the order of its sums only.  At most 2^27 - 16 columns for up to 16 rows; for more
+ * rows 2^23 - 8 tiles of 64 x 64 (larger ones where the results are many).
  * Workspace: laud_matmul_e4m3_workspace(M, N, K) bytes; no shape needs any at present (then ws may be NULL).
  */
 size_t laud_matmul_e4m3_workspace(int M, int N, int K);

@@ -34,8 +34,8 @@ __device__ __forceinline__ f32x4 mma_block(const i32x8& a, const i32x8& b) {
 }
 
 // Up to 16 rows: the weights are read once, for all of them.  A workgroup has 16 columns, its waves share the reduction, their sums are
-// added in the waves' order.  Bound by memory and the launch: one row of 4096 x 4096 in 5.2 us (5.6 with all of a wave's blocks asked
-// for at once, 5.2 to 5.3 with sixteen waves).
+// added in the waves' order.  Bound by memory and the launch: one row of 4096 x 4096 in 5.2 us back to back, 5.0 to 6.6 by itself (back
+// to back 5.6 with all of a wave's blocks asked for at once, 5.2 to 5.3 with sixteen waves).
 constexpr int kSplit = 8, kSplitRows = 16;
 template <typename OT>
 __global__ __launch_bounds__(kSplit * kWave) void k_mm8_split(Mm8Args g) {
@@ -76,8 +76,8 @@ __global__ __launch_bounds__(kSplit * kWave) void k_mm8_split(Mm8Args g) {
 // loads, a block of 128 along K at a time, into NS stages that take turns: one barrier a block, the next blocks' loads are under way
 // while this one is multiplied.  A row's eight 16-byte chunks lie XOR-swizzled (chunk ^ row % 8; the swizzle is applied to the global
 // side).  The first operand of the matrix instructions is b: a lane's results are consecutive columns, its row of a - and that row's
-// scale - is one for all of them.  Bound by the matrix cores at their bf16 rate: 8192 x 8192 x 4096 in 421 to 444 us, 1.2 to 1.3 PFLOP/s, where a
-// large bf16 product of the vendor's library reaches 1.1.
+// scale - is one for all of them.  Bound by the matrix cores at their bf16 rate: 8192 x 8192 x 4096 in 412 to 444 us, 1.2 to 1.3
+// PFLOP/s, where a large bf16 product of the vendor's library reaches 1.1.
 template <int BM, int BN, int NS, int KG> struct TileLds {
   static constexpr int kB = 0, kA = BN * kScaleBlock, kSa = kA + BM * kScaleBlock, kSb = kSa + BM * 4, kStage = kSb + 256;
   static constexpr int kGroup = NS * kStage, kBytes = KG * kGroup;
@@ -452,7 +452,8 @@ extern "C" int laud_matmul_e4m3(const void* a, int64_t lda, const float* sa, con
   const size_t ob = span_bytes(M, ldo, N, elem_bytes(out_dtype));
   if (ranges_meet(a, span_bytes(M, lda, K, 1), out, ob) || ranges_meet(b, span_bytes(N, ldb, K, 1), out, ob)) return LAUD_ERR_INVALID_ARG;
   const size_t kb = (size_t)scale_blocks(K) * 4, eb = elem_bytes(out_dtype);
-  if (range_meets_rows(sa, M * kb, out, ldo, eb, M, N) || range_meets_rows(sb, scale_blocks(N) * kb, out, ldo, eb, M, N)) return LAUD_ERR_INVALID_ARG;
+  if (range_meets_rows(sa, M * kb, out, ldo, eb, M, N) || range_meets_rows(sb, scale_blocks(N) * kb, out, ldo, eb, M, N))
+    return LAUD_ERR_INVALID_ARG;
   Mm8Args g{(const uint8_t*)a, (const uint8_t*)b, sa, sb, out, M, N, K, scale_blocks(K), lda, ldb, ldo};
   clear_stale_error();
   return out_dtype == LAUD_BF16 ? launch_mm8<bf16_t>(g, (hipStream_t)stream) : launch_mm8<float>(g, (hipStream_t)stream);

@@ -35,7 +35,7 @@ __device__ __forceinline__ unsigned order_key(float f) {
 constexpr int kRouteThreads = 1024, kLogitWaves = 4;
 
 // The logits of N experts from e0 on, by one wave, D pieces of 16 bytes a lane of every row at a time, whose loads are all under way
-// together (one piece of each row at a time: one token through 2 of 8 experts of 4096 x 2048, bf16, 31.9 us against 29.1).
+// together (one piece of each row at a time: one token through 2 of 8 experts of 4096 x 2048, bf16, 33.3 us against 30.3).
 template <typename ET, int N, int D>
 __device__ __forceinline__ void router_logits(const MoeArgs& a, const ET* x, int e0, float* logits) {
   const int lane = lane_id();
@@ -139,7 +139,8 @@ __global__ __launch_bounds__(kRouteThreads) void k_moe_route(MoeArgs a) {
 }
 
 // A single token's logits, an expert a wave over many workgroups, where one workgroup would wait for its share of the memory's rate;
-// the workgroups of the first product then choose, each for itself.  (One token, 8 of 64 experts of 2048 x 1024, bf16: 32.0 -> 30.9 us.)
+// the workgroups of the first product then choose, each for itself.  (One token, 8 of 64 experts of 2048 x 1024, bf16:
+// 28.9 us against 31.3 routed by one workgroup.)
 template <typename ET>
 __global__ __launch_bounds__(kLogitWaves * kWave) void k_moe_logits(MoeArgs a) {
   const int e = blockIdx.x * kLogitWaves + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
@@ -175,8 +176,9 @@ __device__ __forceinline__ f32x4 mma_stored(const tok_u4& w, const tok_u4 (&x)[W
 }
 // Hidden values are float32.  Through bf16 instructions they go as a sum of three: the eight leading bits (not rounded: a finite value
 // stays finite), the eight behind them and the rest, which hold all 24 (rounded to bf16 alone they would add an error as large as
-// the result's own rounding, in two parts one of 2^-17 of theirs).  k_moe_down splits them in registers, beside its loads of weights;
-// k_moe_down_few, whose lanes hold a part each, finds them split in three planes (split there: one token 34.9 us against 29.5).  Where
+// the result's own rounding, in two parts one of 2^-17 of theirs).  k_moe_down splits them in registers, beside its loads of weights
+// (three planes read instead: 64 tokens 187.6 us against 178.7); k_moe_down_few, whose lanes hold a part each, finds them split in
+// three planes (split there: one token 34.9 us against 29.5).  Where
 // the leading parts' sum is infinite or NaN it is the result: an infinite weight times a part that is zero, or the parts behind an
 // infinity, are none of the formula's.
 __device__ __forceinline__ unsigned leading(float a, float b) {  // of two values, as two bf16
@@ -254,14 +256,14 @@ __device__ __forceinline__ void join_waves(f32x4 (&v)[N], f32x4 (*part)[N][kWave
 
 // Waves of a workgroup, which share the reduction by blocks of 128.  Few waves leave room for more workgroups, which wait for their
 // entries, their weights and each other at different times (16 / 64 tokens, 8 of 64 experts of 2048 x 1024, bf16, eight / four / two
-// waves: 162 / 149 / 159 and 191 / 184 / 194 us; 16 tokens, 6 of 64 of 2048 x 1424, 8 bits, 125 / 102 / 105); float32 blocks need the
-// registers of the longer ones (32 tokens, 2 of 16 experts of 1024 x 1024, eight / four: 58.0 / 60.5).  A single token's workgroups,
-// one or two a compute unit, have eight (30.6 against 31.9 us).
+// waves: 156 / 143 / 153 and 189 / 179 / 189 us; 16 tokens, 6 of 64 of 2048 x 1424, 8 bits, 115 / 111 / 118); float32 blocks need the
+// registers of the longer ones (32 tokens, 2 of 16 experts of 1024 x 1024, eight / four: 61.3 / 62.9).  A single token's workgroups,
+// one or two a compute unit, have eight (29.9 against 31.1 us with four).
 template <int W> constexpr int kSplit = W == W_F32 ? 8 : 4;
 constexpr int kSplitOne = 8;
 
 // h of one expert's entries for 16 hidden channels; ONE: of one entry of the single token.  Bound by memory: 64 experts of 2048 x 1024
-// in bf16, 537 MB, in 109 us, 4.9 TB/s.
+// in bf16, 537 MB, in 108 us, 5.0 TB/s.
 template <int W, bool ONE>
 __global__ __launch_bounds__((ONE ? kSplitOne : kSplit<W>) * kWave) void k_moe_up(MoeArgs a) {
   typedef Weights<W> WT;
@@ -360,7 +362,7 @@ __global__ __launch_bounds__((ONE ? kSplitOne : kSplit<W>) * kWave) void k_moe_u
 }
 
 // One expert's entries for 32 output channels, weighted; k_moe_sum adds each token's entries up.  Bound by memory and, at two blocks of
-// the reduction a wave, by a workgroup's start and end: 64 experts of 2048 x 1024 in bf16, 268 MB, in 64 us, 4.2 TB/s.
+// the reduction a wave, by a workgroup's start and end: 64 experts of 2048 x 1024 in bf16, 268 MB, in 65 us, 4.1 TB/s.
 template <int W>
 __global__ __launch_bounds__(kSplit<W> * kWave) void k_moe_down(MoeArgs a) {
   typedef Weights<W> WT;
@@ -464,10 +466,11 @@ __global__ __launch_bounds__(256) void k_moe_sum(MoeArgs a) {
 // of a matrix instruction's sixteen rows of weights; of the token side, column 0 is the even block and column 1 the odd one, columns
 // 2 to 5 the parts behind the leading ones of both; a half's results stand in its columns.  Sums are added in the waves' order.
 // The layer, with k_moe_down / with this kernel, in us:
-//   8 of 64 experts of 2048 x 1024, bf16    1 token 35.6 / 32.0    4 tokens 89.3 / 83.2    8 tokens 129.5 / 127.6    16 tokens 162.6 / 188.5
-//   6 of 64 experts of 2048 x 1424, e4m3            29.4 / 24.7             65.4 / 58.7              90.9 /  87.3             116.0 / 123.6
-//   2 of  8 experts of 4096 x 2048, bf16            37.3 / 33.5             76.7 / 75.3              96.0 / 106.9
-// (Two pairs of blocks at a time take 78 registers in bf16, four take 140 and leave room for one workgroup of 8 waves a compute unit
+//   8 of 64 experts of 2048 x 1024, bf16    1 token 32.6 / 29.9    4 tokens 84.2 / 82.7    8 tokens 119.2 / 127.9    16 tokens 148.2 / 190.6
+//   6 of 64 experts of 2048 x 1424, e4m3            27.0 / 22.3             62.7 / 57.5              88.0 /  86.9             111.3 / 126.4
+//   2 of  8 experts of 4096 x 2048, bf16            34.3 / 29.6             74.1 / 73.9              91.3 / 105.4
+//   2 of 16 experts of 1024 x 1024, float32                                 32.8 / 28.2              51.2 /  45.9              59.2 /  61.0
+// (Two pairs of blocks at a time take 78 registers in bf16, four took 140 and leave room for one workgroup of 8 waves a compute unit
 // instead of two: 54.6 against 62.5 us for two tokens of the last one.)
 constexpr int kFewColumns = 8;
 template <int W> constexpr int kPairs = W == W_F32 ? 1 : 2;  // pairs whose loads a wave has under way together

@@ -8,7 +8,9 @@ namespace {
 // Bound by memory: x and y are read once, out and z written once.  A row belongs to TPR threads, which keep it in registers from its
 // only read to its last write: chunk j of a thread is eight elements, chunks of neighbouring threads lie side by side.  A workgroup
 // goes from row to row with the norms' vectors in registers and requests the next row's x and y before it finishes a row, four waves
-// a SIMD (128 registers): 16384 x 4096 bf16 to 8 bits, a quarter of the rows skipped, 109 -> 86 us, 5.1 TB/s of a copy's 5.2.  More
+// a SIMD (128 registers): 16384 x 4096 bf16 to 8 bits, a quarter of the rows skipped, 109 -> 86 us, 5.1 TB/s of a copy's 5.2.  Bf16
+// rows up to 4096 channels fit; float32 rows of two pieces a thread keep up to 32 registers of a lane in memory and rows of four pieces
+// 32 to 93: 8192 x 4096 float32 at 5.2 TB/s, 4.5 to 8 bits, 4096 x 8192 4.0; 2048 x 16384 bf16 at 4.5, 1024 x 32768 at 3.0.  More
 // threads a row for few rows: 4 x 2048 in 2.8 us with 256, 3.2 with 128, 4.3 with 64 threads; 8192 x 2048 26.1 / 26.9 / 34.6.
 constexpr int kMaxC = 32768;
 constexpr int kMostGroups = 1 << 20;   // workgroups of a launch (threads are counted in 32 bits); longer lists loop
@@ -232,7 +234,7 @@ void launch_norm(const NormArgs& a, hipStream_t st) {
 }
 
 // ---- quantisation ---------------------------------------------------------------------------------------------------------
-// One scale for 128 elements of a row: sixteen lanes a block, one read of x.  Bound by memory: 16384 x 4096 bf16 in 38.9 us, 5.2 TB/s.
+// One scale for 128 elements of a row: sixteen lanes a block, one read of x.  Bound by memory: 16384 x 4096 bf16 in 38.7 us, 5.2 TB/s.
 template <typename ET>
 __global__ __launch_bounds__(256) void k_quant_rows(const ET* __restrict__ x, int64_t ldx, long long blocks, int kb, int cols,
                                                     uint8_t* __restrict__ q, int64_t ldq, float* __restrict__ scale) {
@@ -252,7 +254,8 @@ __global__ __launch_bounds__(256) void k_quant_rows(const ET* __restrict__ x, in
   }
 }
 
-// One scale for 128 rows of 128 elements: a workgroup a block, which stays in registers between its maximum and its codes.
+// One scale for 128 rows of 128 elements: a workgroup a block, which stays in registers between its maximum and its codes.  Bound by
+// memory: 8192 x 4096 bf16 in 21 us, 4.7 TB/s, float32 in 33, 5.1.
 template <typename ET>
 __global__ __launch_bounds__(256) void k_quant_square(const ET* __restrict__ x, int64_t ldx, int rows, int kb, int cols,
                                                       uint8_t* __restrict__ q, int64_t ldq, float* __restrict__ scale) {
