@@ -462,6 +462,85 @@ int laud_moe(const laud_moe_layer* p, int T, const void* x, int64_t ldx, const u
              int32_t* experts, float* weights, void* ws, size_t ws_bytes, void* stream);
 
 /*
+ * ---- Attention of a token block -------------------------------------------------------------------------------------------
+ * The mixing step between a block's projections: over the tokens of this call (laud_attention), or of new tokens over a cache of
+ * earlier tokens' keys and values (laud_cache_attention).  The conventions of the token operators hold.  Rows of q and out are
+ * [token][heads][D], rows of k and v [token][kv_heads][D]: columns of one wider array (a projection's result) will do.
+ * Query head h belongs to key head h / (heads / kv_heads).
+ *   - Sequences lie one behind the other: offsets [B + 1] int32 (device) names the rows offsets[b] .. offsets[b + 1] - 1 of sequence b,
+ *     ascending, within 0 .. T; a sequence may have no row.  Rows outside all sequences are not read, and left as they were.
+ *   - Weights are softmax(scale * q k) over the tokens that a query sees, and nothing else of the call has any part in its result
+ *     (a NaN or an infinity in a token that it does not see stays there).  A score of -infinity has no weight; a query that sees
+ *     nothing, or has no weight, gets zeros.
+ *   - Scores, statistics and sums are float32.  With bf16 rows a weight is rounded to bf16 where it meets its value (2^-9 of itself,
+ *     the instructions' operand); with float32 rows it is not.
+ */
+typedef struct {
+  int32_t heads, kv_heads; /* heads: a multiple of kv_heads */
+  int32_t D;               /* width of a head: a multiple of 8, at most 128 (LAUD_ERR_UNSUPPORTED beyond) */
+  int32_t dtype;           /* LAUD_F32 or LAUD_BF16: q, k, v and out */
+  int32_t causal;          /* non-zero: a query sees its own token and those before it; else all of its sequence */
+  float scale;             /* of the products, positive and finite (1 / sqrt(D)) */
+} laud_heads;
+
+/*
+ * out = attention of every token over its sequence.
+ *   q, out [T] rows, k, v [T] rows; out may be q.  Rows at most 2^22 elements apart.
+ *   keep [T] bytes or NULL: a token with 0 (the masker's) is no key, and its row of out is zeros
+ */
+int laud_attention(const laud_heads* p, int B, const int32_t* offsets, int T, const void* q, int64_t ldq, const void* k, int64_t ldk,
+                   const void* v, int64_t ldv, const uint8_t* keep, void* out, int64_t ldo, void* stream);
+
+/* A cache of keys and values in pages.  Device pointers, dense; 16-byte aligned. */
+typedef struct {
+  int32_t pages, page;  /* number of pages; tokens a page holds: 16, 32, 64, 128 or 256; pages * page below 2^31 */
+  int32_t kv_heads, D;  /* as in laud_heads; D a multiple of 16 for LAUD_E4M3 */
+  int32_t dtype;        /* LAUD_F32, LAUD_BF16 or LAUD_E4M3 */
+  void* k;              /* [pages][kv_heads][page][D] */
+  void* v;
+  float* k_scale;       /* LAUD_E4M3: [pages][kv_heads][page], a scale for each token's row of D, as laud_quantize_e4m3 defines it; else */
+  float* v_scale;       /* unused */
+} laud_cache;
+
+/*
+ * Which rows of a call belong to which sequence, and where its tokens are in the cache: the rows of sequence b are the last
+ * ones of its lens[b] tokens (row i of n is at position lens[b] - n + i), position j is row j % page of page table[b][j / page].
+ * Device pointers.  A position before the first or past the table, and one whose page is not 0 .. pages - 1, is no place: nothing
+ * is written there, zeros are read, no query sees it.
+ */
+typedef struct {
+  int32_t B;
+  int32_t table_ld;       /* pages of a row of table, at least 1; table_ld * page below 2^31 */
+  const int32_t* offsets; /* [B + 1] */
+  const int32_t* lens;    /* [B] */
+  const int32_t* table;   /* [B][table_ld] */
+  const int32_t* prefix;  /* [ceil(prefix_len / page)] pages of the tokens that come before the first of every sequence, or NULL */
+  int32_t prefix_len;     /* their number (0: none); laud_cache_attention only */
+} laud_batch;
+
+/*
+ * laud_cache_write puts the rows k, v [T] of dtype (LAUD_F32 or LAUD_BF16: the cache's type, or any of them into LAUD_E4M3) where the
+ * batch says, quantised by the way; laud_cache_read brings the rows from there, code * scale rounded once.  Two rows of a
+ * call that are written to one place leave it undefined.  T * kv_heads is below 2^31 (LAUD_ERR_UNSUPPORTED beyond).
+ */
+int laud_cache_write(const laud_cache* c, const laud_batch* b, int T, const void* k, int64_t ldk, const void* v, int64_t ldv, int dtype,
+                     void* stream);
+int laud_cache_read(const laud_cache* c, const laud_batch* b, int T, void* k, int64_t ldk, void* v, int64_t ldv, int dtype,
+                    void* stream);
+
+/*
+ * out = attention of new tokens (one, or some) over the cached tokens of their sequence, themselves among them, and over
+ * the prefix: a query sees the whole prefix, and the positions up to its own (all of them where p->causal is 0).  The prefix is read once for all
+ * sequences.  p->dtype is the cache's type, or LAUD_BF16 where that is LAUD_E4M3.
+ *   q, out [T] rows; out may be q
+ * Long sequences are shared out over workgroups, by the table's size and the number of rows; their parts are joined in order.
+ * Workspace: laud_cache_attention_workspace(p, c, b, T) bytes (0 for shapes that need none, and for arguments that the call refuses).
+ */
+size_t laud_cache_attention_workspace(const laud_heads* p, const laud_cache* c, const laud_batch* b, int T);
+int laud_cache_attention(const laud_heads* p, const laud_cache* c, const laud_batch* b, int T, const void* q, int64_t ldq, void* out,
+                         int64_t ldo, void* ws, size_t ws_bytes, void* stream);
+
+/*
  * Instrumentation (host side; not part of the paper's method): per-stage GPU time of the
  * kernels the entry points launch.  While enabled, every stage is bracketed by a pair of HIP
  * events recorded on the call's stream (at most 65536 stage launches are kept per collection;

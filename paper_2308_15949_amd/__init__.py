@@ -13,4 +13,6 @@ from .binding import (  # noqa: F401
     make_bottleneck, status_string, workspace_size,
     E4M3, MoeLayer, NormBlock, laud_matmul_e4m3, laud_moe, laud_norm_residual, laud_quantize_e4m3, make_moe, make_norm_block,
     matmul_e4m3_workspace, moe_workspace,
+    Batch, Cache, Heads, cache_attention_workspace, laud_attention, laud_cache_attention, laud_cache_read, laud_cache_write, make_batch,
+    make_cache, make_heads,
 )

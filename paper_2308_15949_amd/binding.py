@@ -29,7 +29,8 @@ EXPORTS = ["laud_status_string", "laud_abi_version", "laud_workspace_size", "lau
            "laud_init", "laud_dyn_bottleneck_noalloc", "laud_probe_mfma", "laud_probe_copy", "laud_probe_read",
            "laud_packed_weights_size", "laud_pack_weights",
            "laud_norm_residual", "laud_quantize_e4m3", "laud_matmul_e4m3_workspace", "laud_matmul_e4m3", "laud_moe_workspace",
-           "laud_moe"]
+           "laud_moe",
+           "laud_attention", "laud_cache_write", "laud_cache_read", "laud_cache_attention_workspace", "laud_cache_attention"]
 STAGE_COUNT = 13
 
 
@@ -58,6 +59,21 @@ class MoeLayer(C.Structure):
     _fields_ = [("C", C.c_int32), ("F", C.c_int32), ("E", C.c_int32), ("top_k", C.c_int32), ("dtype", C.c_int32),
                 ("w_dtype", C.c_int32), ("router", C.c_void_p), ("up", C.c_void_p), ("down", C.c_void_p), ("s_up", C.c_void_p),
                 ("s_down", C.c_void_p), ("renormalise", C.c_int32), ("scale", C.c_float)]
+
+
+class Heads(C.Structure):
+    _fields_ = [("heads", C.c_int32), ("kv_heads", C.c_int32), ("D", C.c_int32), ("dtype", C.c_int32), ("causal", C.c_int32),
+                ("scale", C.c_float)]
+
+
+class Cache(C.Structure):
+    _fields_ = [("pages", C.c_int32), ("page", C.c_int32), ("kv_heads", C.c_int32), ("D", C.c_int32), ("dtype", C.c_int32),
+                ("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p)]
+
+
+class Batch(C.Structure):
+    _fields_ = [("B", C.c_int32), ("table_ld", C.c_int32), ("offsets", C.c_void_p), ("lens", C.c_void_p), ("table", C.c_void_p),
+                ("prefix", C.c_void_p), ("prefix_len", C.c_int32)]
 
 
 class LaudError(RuntimeError):
@@ -154,6 +170,14 @@ def load() -> C.CDLL:
     lib.laud_moe_workspace.argtypes = [C.POINTER(MoeLayer), i32]
     lib.laud_moe.restype = i32
     lib.laud_moe.argtypes = [C.POINTER(MoeLayer), i32, vp, i64, vp, vp, i64, vp, vp, vp, sz, vp]
+    lib.laud_attention.restype = i32
+    lib.laud_attention.argtypes = [C.POINTER(Heads), i32, vp, i32, vp, i64, vp, i64, vp, i64, vp, vp, i64, vp]
+    lib.laud_cache_write.restype = lib.laud_cache_read.restype = i32
+    lib.laud_cache_write.argtypes = lib.laud_cache_read.argtypes = [C.POINTER(Cache), C.POINTER(Batch), i32, vp, i64, vp, i64, i32, vp]
+    lib.laud_cache_attention_workspace.restype = sz
+    lib.laud_cache_attention_workspace.argtypes = [C.POINTER(Heads), C.POINTER(Cache), C.POINTER(Batch), i32]
+    lib.laud_cache_attention.restype = i32
+    lib.laud_cache_attention.argtypes = [C.POINTER(Heads), C.POINTER(Cache), C.POINTER(Batch), i32, vp, i64, vp, i64, vp, sz, vp]
     lib.laud_stage_timing_enable.restype = i32
     lib.laud_stage_timing_enable.argtypes = [i32]
     lib.laud_stage_timing_read.restype = i32
@@ -414,7 +438,8 @@ def _token_calls():
     if torch.cuda.is_available():
         torch.cuda.current_stream()  # initialises torch's device state, which the extension takes for granted
     _laud_torch.bind(*(C.cast(f, C.c_void_p).value for f in (lib.laud_norm_residual, lib.laud_quantize_e4m3, lib.laud_matmul_e4m3,
-                                                              lib.laud_moe)))
+                                                              lib.laud_moe, lib.laud_attention, lib.laud_cache_write,
+                                                              lib.laud_cache_read, lib.laud_cache_attention)))
     _calls = _laud_torch
     return _calls
 
@@ -510,6 +535,94 @@ def laud_moe(p: MoeLayer, x, keep, out, experts, weights, ws) -> None:
     s = (_calls or _token_calls()).moe(p, x, keep, out, experts, weights, ws)
     if s:
         raise LaudError(s, "laud_moe")
+
+
+# ----- attention of a token block ------------------------------------------------------------------------------------------------
+def make_heads(heads: int, kv_heads: int, d: int, dtype, causal: bool, scale: float | None = None) -> Heads:
+    """Descriptor of an attention's heads; dtype: torch's type of the rows; scale None: 1 / sqrt(d)."""
+    import torch
+    if dtype not in (torch.float32, torch.bfloat16) or d <= 0:
+        _bad("make_heads")
+    return Heads(int(heads), int(kv_heads), int(d), BF16 if dtype == torch.bfloat16 else F32, 1 if causal else 0,
+                 float(d) ** -0.5 if scale is None else float(scale))
+
+
+def _of_one_device(where: str, *tensors) -> None:
+    if len({t.device for t in tensors if t is not None}) != 1:
+        _bad(where)
+
+
+def make_cache(k, v, k_scale=None, v_scale=None) -> Cache:
+    """Descriptor of a paged cache over device tensors k, v [pages][kv_heads][page][D] (float32, bf16, or float8_e4m3fn with k_scale,
+    v_scale [pages][kv_heads][page] float32), which it holds."""
+    where = "make_cache"
+    if k.dim() != 4 or _dtype_of(k) < 0 or (k_scale is None) != (v_scale is None) or (_dtype_of(k) == E4M3) != (k_scale is not None):
+        _bad(where)
+    pages, h, page, d = (int(n) for n in k.shape)
+    _of_one_device(where, k, v, k_scale, v_scale)
+    code = _dtype_of(k)
+    c = Cache(pages, page, h, d, code, _dense(k, k.shape, code, where), _dense(v, k.shape, code, where),
+              _dense(k_scale, (pages, h, page), F32, where), _dense(v_scale, (pages, h, page), F32, where))
+    c.held = (k, v, k_scale, v_scale)
+    return c
+
+
+def _indices(t, dim: int, where: str):
+    import torch
+    if t is None:
+        return None
+    if not (t.is_cuda and t.dtype == torch.int32 and t.dim() == dim and t.is_contiguous()):
+        _bad(where)
+    return t.data_ptr()
+
+
+def make_batch(offsets, lens, table, prefix=None, prefix_len: int = 0) -> Batch:
+    """Descriptor of a batch over int32 device tensors: offsets [B + 1], lens [B], table [B][pages of the longest], and prefix [pages],
+    those of the prefix_len tokens that come before every sequence's own.  It holds the tensors; their contents may change between calls."""
+    where = "make_batch"
+    v = [_indices(t, n, where) for t, n in ((offsets, 1), (lens, 1), (table, 2), (prefix, 1))]
+    _of_one_device(where, offsets, lens, table, prefix)
+    n = int(lens.shape[0])
+    if offsets.shape[0] != n + 1 or table.shape[0] != n or (n and not table.shape[1]) or prefix_len < 0 or (prefix_len and prefix is None):
+        _bad(where)
+    b = Batch(n, int(table.shape[1]), *v, int(prefix_len))
+    b.held, b.prefix_pages = (offsets, lens, table, prefix), 0 if prefix is None else int(prefix.shape[0])
+    return b
+
+
+def laud_attention(p: Heads, offsets, q, k, v, keep, out) -> None:
+    """q, out [T][heads * D] and k, v [T][kv_heads * D] of one type, rows any distance apart; offsets [B + 1] int32; keep [T] bytes or
+    None."""
+    s = (_calls or _token_calls()).attention(p, offsets, q, k, v, keep, out)
+    if s:
+        raise LaudError(s, "laud_attention")
+
+
+def laud_cache_write(c: Cache, b: Batch, k, v) -> None:
+    """Rows k, v [T][kv_heads * D] to their places in the cache."""
+    s = (_calls or _token_calls()).cache_write(c, b, k, v)
+    if s:
+        raise LaudError(s, "laud_cache_write")
+
+
+def laud_cache_read(c: Cache, b: Batch, k, v) -> None:
+    """Rows k, v [T][kv_heads * D] from their places in the cache."""
+    s = (_calls or _token_calls()).cache_read(c, b, k, v)
+    if s:
+        raise LaudError(s, "laud_cache_read")
+
+
+def cache_attention_workspace(p: Heads, c: Cache, b: Batch, t: int) -> int:
+    return int(load().laud_cache_attention_workspace(C.byref(p), C.byref(c), C.byref(b), int(t)))
+
+
+def laud_cache_attention(p: Heads, c: Cache, b: Batch, q, out, ws=None) -> None:
+    """q, out [T][heads * D]: new tokens over the cached ones of their sequences."""
+    if b.prefix_len > getattr(b, "prefix_pages", b.prefix_len) * c.page:
+        _bad("laud_cache_attention")
+    s = (_calls or _token_calls()).cache_attention(p, c, b, q, out, ws)
+    if s:
+        raise LaudError(s, "laud_cache_attention")
 
 
 def laud_stage_timing_enable(on: bool) -> None:

@@ -23,7 +23,7 @@ OBJ = os.path.join(CSRC, "_build")
 LIB = os.path.join(HERE, "liblaud.so")
 EXTENSION = os.path.join(HERE, "_laud_torch.so")
 SOURCES = ["laud_api.hip", "laud_mask.hip", "laud_chanmask.hip", "laud_static.hip", "laud_se.hip", "laud_gemm.hip", "laud_pipe_a.hip", "laud_pipe_b.hip", "laud_pipe_c.hip", "laud_group.hip", "laud_group_fused.hip", "laud_skinny.hip", "laud_narrow.hip", "laud_first.hip",
-           "laud_probe.hip", "laud_tail.hip", "laud_head.hip", "laud_norm.hip", "laud_matmul8.hip", "laud_moe.hip"]
+           "laud_probe.hip", "laud_tail.hip", "laud_head.hip", "laud_norm.hip", "laud_matmul8.hip", "laud_moe.hip", "laud_attend.hip", "laud_cache.hip", "laud_cached.hip"]
 # packed-fp32 code generation is switched off for device code (the host pass warns that it
 # does not know the feature; that is harmless).
 FLAGS = ["-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC",

@@ -145,6 +145,10 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t bytes_of(const void* base, lon
 __device__ __forceinline__ tok_u4 load16(__amdgpu_buffer_rsrc_t r, unsigned off) {
   return __builtin_bit_cast(tok_u4, __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, 0));
 }
+__device__ __forceinline__ tok_u2 load8(__amdgpu_buffer_rsrc_t r, unsigned off) {
+  return __builtin_bit_cast(tok_u2, __builtin_amdgcn_raw_buffer_load_b64(r, off, 0, 0));
+}
+__device__ __forceinline__ unsigned load4(__amdgpu_buffer_rsrc_t r, unsigned off) { return __builtin_amdgcn_raw_buffer_load_b32(r, off, 0, 0); }
 // Four consecutive results of a row.
 template <typename OT>
 __device__ __forceinline__ void store4(OT* out, const f32x4& v) {

@@ -19,6 +19,10 @@ decltype(&laud_norm_residual) p_norm = nullptr;
 decltype(&laud_quantize_e4m3) p_quantize = nullptr;
 decltype(&laud_matmul_e4m3) p_matmul = nullptr;
 decltype(&laud_moe) p_moe = nullptr;
+decltype(&laud_attention) p_attention = nullptr;
+decltype(&laud_cache_write) p_cache_write = nullptr;
+decltype(&laud_cache_read) p_cache_read = nullptr;
+decltype(&laud_cache_attention) p_cache_attention = nullptr;
 
 struct Refused {};  // an argument that does not fit: LAUD_ERR_INVALID_ARG
 
@@ -188,28 +192,77 @@ PyObject* moe(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return status_of(n, 7, [&] {
+    const auto p = descriptor<laud_heads>(a[0]);
+    const at::Tensor& offsets = tensor(a[1]);
+    if (offsets.scalar_type() != at::kInt || offsets.dim() != 1 || !offsets.is_contiguous() || offsets.size(0) < 1 || offsets.size(0) > INT32_MAX)
+      throw Refused{};
+    const Rows q = rows(a[2]);
+    const int64_t c = (int64_t)p.heads * p.D, ck = (int64_t)p.kv_heads * p.D;
+    const Rows k = rows(a[3], q.n, ck), v = rows(a[4], q.n, ck), out = rows(a[6], q.n, c);
+    if (q.c != c || q.code != p.dtype || k.code != p.dtype || v.code != p.dtype || out.code != p.dtype) throw Refused{};
+    return p_attention(&p, (int)offsets.size(0) - 1, static_cast<const int32_t*>(offsets.data_ptr()), (int)q.n, q.p, q.ld, k.p, k.ld, v.p, v.ld,
+                       bytes(a[5], q.n), out.p, out.ld, stream());
+  });
+}
+
+template <typename F>
+PyObject* cache_rows(F* call, PyObject* const* a, Py_ssize_t n) {
+  return status_of(n, 4, [&] {
+    const auto c = descriptor<laud_cache>(a[0]);
+    const auto b = descriptor<laud_batch>(a[1]);
+    const Rows k = rows(a[2]), v = rows(a[3], k.n, k.c);
+    if (k.c != (int64_t)c.kv_heads * c.D || k.code != v.code) throw Refused{};
+    return call(&c, &b, (int)k.n, k.p, k.ld, v.p, v.ld, k.code, stream());
+  });
+}
+PyObject* cache_write(PyObject*, PyObject* const* a, Py_ssize_t n) { return cache_rows(p_cache_write, a, n); }
+PyObject* cache_read(PyObject*, PyObject* const* a, Py_ssize_t n) { return cache_rows(p_cache_read, a, n); }
+
+PyObject* cache_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return status_of(n, 6, [&] {
+    const auto p = descriptor<laud_heads>(a[0]);
+    const auto c = descriptor<laud_cache>(a[1]);
+    const auto b = descriptor<laud_batch>(a[2]);
+    const Rows q = rows(a[3]), out = rows(a[4], q.n, q.c);
+    if (q.c != (int64_t)p.heads * p.D || q.code != p.dtype || out.code != p.dtype) throw Refused{};
+    size_t ws_bytes;
+    void* ws = space(a[5], &ws_bytes);
+    return p_cache_attention(&p, &c, &b, (int)q.n, q.p, q.ld, out.p, out.ld, ws, ws_bytes, stream());
+  });
+}
+
 template <typename F>
 void take(F& f, PyObject* address) { f = reinterpret_cast<F>(PyLong_AsVoidPtr(address)); }
 
 PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  if (n != 4) {
-    PyErr_SetString(PyExc_TypeError, "4 addresses");
+  if (n != 8) {
+    PyErr_SetString(PyExc_TypeError, "8 addresses");
     return nullptr;
   }
   take(p_norm, a[0]);
   take(p_quantize, a[1]);
   take(p_matmul, a[2]);
   take(p_moe, a[3]);
+  take(p_attention, a[4]);
+  take(p_cache_write, a[5]);
+  take(p_cache_read, a[6]);
+  take(p_cache_attention, a[7]);
   if (PyErr_Occurred()) return nullptr;
   Py_RETURN_NONE;
 }
 
 #define LAUD_METHOD(f, doc) {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)), METH_FASTCALL, doc}
-PyMethodDef methods[] = {LAUD_METHOD(bind, "bind(norm_residual, quantize_e4m3, matmul_e4m3, moe): addresses of the entry points"),
+PyMethodDef methods[] = {LAUD_METHOD(bind, "bind(norm_residual, quantize_e4m3, matmul_e4m3, moe, attention, cache_write, cache_read, cache_attention): addresses of the entry points"),
                          LAUD_METHOD(norm_residual, "norm_residual(block, x, y, keep, gate, rows_per_gate, out, z, z_scale) -> status"),
                          LAUD_METHOD(quantize, "quantize(x, q, scale, block_rows) -> status"),
                          LAUD_METHOD(matmul, "matmul(a, sa, b, sb, out, ws) -> status"),
                          LAUD_METHOD(moe, "moe(layer, x, keep, out, experts, weights, ws) -> status"),
+                         LAUD_METHOD(attention, "attention(heads, offsets, q, k, v, keep, out) -> status"),
+                         LAUD_METHOD(cache_write, "cache_write(cache, batch, k, v) -> status"),
+                         LAUD_METHOD(cache_read, "cache_read(cache, batch, k, v) -> status"),
+                         LAUD_METHOD(cache_attention, "cache_attention(heads, cache, batch, q, out, ws) -> status"),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_laud_torch", "Calls of liblaud.so from torch tensors.", -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -72,6 +72,14 @@ struct Rsrc { const char* base; unsigned bytes; };
 typedef unsigned Chunk __attribute__((ext_vector_type(4)));
 unsigned load_dword(const Rsrc& r, unsigned voff, unsigned soff);  // zero past the descriptor's end
 uint8_t load_byte(const Rsrc& r, unsigned voff, unsigned soff);
+typedef unsigned Two __attribute__((ext_vector_type(2)));
+static inline Two load_pair(const Rsrc& r, unsigned voff, unsigned soff) { return Two{load_dword(r, voff, soff), load_dword(r, voff + 4, soff)}; }
+typedef short Turned __attribute__((ext_vector_type(4)));
+static inline Turned read_turned(const char* at) {  // a transposing LDS read: the lane's own eight bytes stand for the others'
+  Turned t;
+  memcpy(&t, at, 8);
+  return t;
+}
 Chunk load_chunk(const Rsrc& r, unsigned voff, unsigned soff);
 void store_chunk(const Chunk& c, const Rsrc& r, unsigned voff, unsigned soff);  // dropped past the descriptor's end
 void load_to_lds(const Rsrc& r, unsigned voff, unsigned soff, unsigned lds_base);
@@ -111,6 +119,7 @@ static inline int lanes_below(unsigned mask, int first) {  // set bits of 32 lan
 #define __builtin_amdgcn_raw_buffer_load_b128(r, v, s, a) host::load_chunk(r, v, s)
 #define __builtin_amdgcn_raw_buffer_store_b128(c, r, v, s, a) host::store_chunk(c, r, v, s)
 #define __builtin_amdgcn_raw_buffer_load_b8(r, v, s, a) host::load_byte(r, v, s)
+#define __builtin_amdgcn_raw_buffer_load_b64(r, v, s, a) host::load_pair(r, v, s)
 #define __builtin_amdgcn_raw_buffer_load_b32(r, v, s, a) host::load_dword(r, v, s)
 #define __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, x, y, z) (c)
 #define __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, x, y, z) (c)
@@ -122,6 +131,9 @@ static inline int lanes_below(unsigned mask, int first) {  // set bits of 32 lan
 #define __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, x, y, z, u, v, w) (c)
 #define __builtin_amdgcn_cvt_pk_fp8_f32(a, b, old, hi) (old)
 #define __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, s, hi) host::Zero()
+#define __builtin_amdgcn_ds_read_tr16_b64_v4i16(p) host::read_turned((const char*)(p))
+#define __builtin_amdgcn_perm(a, b, s) ((a) ^ (b))
+#define __builtin_amdgcn_exp2f(x) exp2f(x)
 #define atomicAdd(p, v) __atomic_fetch_add(p, v, __ATOMIC_RELAXED)
 #define __builtin_amdgcn_readfirstlane(x) (x)
 #define __builtin_amdgcn_sched_barrier(x)

@@ -1,0 +1,114 @@
+"""Which memory the attention kernels touch, checked on the CPU as in test_token_memory.py: every operand, index array, cache and
+workspace between two pages that nobody may touch; sequences of every length from none on, rows behind the last one, pages that are
+none, lengths past the table and below the new tokens, offsets that are out of order."""
+import ctypes as C
+
+import numpy as np
+import pytest
+
+from paper_2308_15949_amd import binding as B
+from test_memory_bounds import Call, in_a_process_of_its_own, lib  # noqa: F401  (lib: the fixture that builds the sources for the host)
+from test_token_memory import floats, ok, rows
+
+
+def ints(call, values):
+    a = np.asarray(values, np.int32)
+    return call.buf(a.nbytes, a)
+
+
+def offsets_of(new, start=0):
+    return np.concatenate(([start], start + np.cumsum(new)))
+
+
+def attention(call, new, T, heads, kv_heads, D, dtype, causal, extra, keep, offsets=None, in_place=False):
+    p = B.Heads(heads, kv_heads, D, dtype, causal, 0.1)
+    q, ldq = rows(call, T, heads * D, dtype, extra)
+    k, ldk = rows(call, T, kv_heads * D, dtype, 2 * extra)
+    v, ldv = rows(call, T, kv_heads * D, dtype, 3 * extra)
+    out, ldo = (q, ldq) if in_place else rows(call, T, heads * D, dtype, extra)
+    offs = offsets_of(new) if offsets is None else offsets
+    kept = call.buf(T, (call.rng.random(T) < 0.5).astype(np.uint8)) if keep else None
+    ok(call.host.laud_attention(C.byref(p), len(offs) - 1, ints(call, offs), T, q, ldq, k, ldk, v, ldv, kept, out, ldo, None))
+
+
+def cache_and_batch(call, new, lens, kv_heads, D, cache, page, table_ld, prefix_len, offsets, bad_pages):
+    pages = sum(-(-max(n, 0) // page) for n in lens) + -(-prefix_len // page) + 1
+    k, v = (rows(call, pages * kv_heads * page, D, cache)[0] for _ in range(2))
+    s = [floats(call, pages * kv_heads * page) for _ in range(2)] if cache == B.E4M3 else [None, None]
+    c = B.Cache(pages, page, kv_heads, D, cache, k, v, *s)
+    order = call.rng.permutation(pages)
+    shared = -(-prefix_len // page)
+    table, at = np.full((len(lens), table_ld), -1), shared
+    for b, n in enumerate(lens):
+        need = min(-(-max(n, 0) // page), table_ld)
+        table[b, :need] = order[at:at + need]
+        at += need
+    if bad_pages:
+        table[:, ::3] = [[pages], [-5], [2 ** 31 - 1]][len(new) % 3]
+    offs = offsets_of(new) if offsets is None else offsets
+    b = B.Batch(len(lens), table_ld, ints(call, offs), ints(call, lens), ints(call, table), ints(call, order[:shared]) if shared else None, prefix_len)
+    return c, b
+
+
+def cached(call, new, lens, T, heads, kv_heads, D, dtype, cache, page, extra=0, prefix_len=0, causal=1, offsets=None, bad_pages=False, spare=2):
+    longest = max([-(-max(n, 0) // page) for n in lens] + [1])
+    c, b = cache_and_batch(call, new, lens, kv_heads, D, cache, page, max(longest + spare, 1), prefix_len, offsets, bad_pages)
+    k, ldk = rows(call, T, kv_heads * D, dtype, extra)
+    v, ldv = rows(call, T, kv_heads * D, dtype, 2 * extra)
+    ok(call.host.laud_cache_write(C.byref(c), C.byref(b), T, k, ldk, v, ldv, dtype, None))
+    p = B.Heads(heads, kv_heads, D, dtype, causal, 0.1)
+    q, ldq = rows(call, T, heads * D, dtype, extra)
+    out, ldo = rows(call, T, heads * D, dtype, 2 * extra)
+    n = call.host.laud_cache_attention_workspace(C.byref(p), C.byref(c), C.byref(b), T)
+    ws = call.buf(n) if n else None
+    if n:
+        C.memset(ws, 0x7b, n)
+    if dtype == cache or dtype == B.BF16:
+        ok(call.host.laud_cache_attention(C.byref(p), C.byref(c), C.byref(b), T, q, ldq, out, ldo, ws, n, None))
+    ok(call.host.laud_cache_read(C.byref(c), C.byref(b), T, k, ldk, v, ldv, dtype, None))
+
+
+F, H, E = B.F32, B.BF16, B.E4M3
+CASES = {
+    # every width of a tile, sequences that end inside it, of one token and none, tokens behind the last one
+    "attend_bf16": (attention, [5, 0, 130, 1, 64], 203, 4, 2, 128, H, 1, 8, False),
+    "attend_bf16_64": (attention, [129, 63, 1], 193, 3, 3, 64, H, 0, 0, True),
+    "attend_bf16_80": (attention, [200], 200, 8, 1, 80, H, 1, 8, True),
+    "attend_bf16_8": (attention, [70, 3], 80, 2, 1, 8, H, 1, 24, False, None, True),
+    "attend_f32": (attention, [33, 129, 0, 2], 170, 2, 2, 128, F, 1, 8, True),
+    "attend_f32_40": (attention, [1, 96, 31], 128, 5, 1, 40, F, 0, 0, False, None, True),
+    "attend_many": (attention, [2] * 70 + [0] * 70 + [1], 141, 1, 1, 64, H, 1, 0, False),
+    "attend_odd_offsets": (attention, [], 150, 2, 1, 64, H, 1, 0, True, [140, 20, -7, 400, 90, 130]),
+    # caches of every type and page, one new token and many, parts and none
+    "cached_bf16": (cached, [1, 1, 1], [300, 1, 17], 3, 8, 2, 128, H, H, 16),
+    "cached_bf16_tail": (cached, [1, 3, 0, 2], [63, 64, 100, 2], 9, 4, 4, 64, H, H, 32, 8),
+    "cached_bf16_rows": (cached, [40, 25], [190, 25], 70, 4, 1, 128, H, H, 64, 8),
+    "cached_bf16_many_rows": (cached, [150, 20], [150, 400], 170, 4, 1, 80, H, H, 256, 0),
+    "cached_e4m3": (cached, [1, 1], [513, 40], 2, 16, 2, 128, H, E, 128),
+    "cached_e4m3_rows": (cached, [30, 9], [200, 9], 39, 3, 1, 48, H, E, 16, 8),
+    "cached_e4m3_many_rows": (cached, [90], [700], 90, 5, 1, 128, H, E, 32),
+    "cached_f32": (cached, [1, 2], [150, 33], 3, 6, 2, 128, F, F, 16, 8),
+    "cached_f32_rows": (cached, [17, 40], [17, 90], 57, 2, 2, 24, F, F, 64),
+    "cached_f32_e4m3_rows_only": (cached, [17, 40], [17, 90], 57, 2, 2, 32, F, E, 64),
+    "cached_prefix": (cached, [1, 1, 1, 2], [20, 0, 1, 70], 6, 8, 2, 128, H, H, 16, 8, 600),
+    "cached_prefix_e4m3": (cached, [2] * 9, [31] * 9, 18, 10, 2, 64, H, E, 64, 0, 1000),
+    "cached_prefix_f32": (cached, [3, 3], [5, 3], 6, 4, 1, 40, F, F, 16, 0, 37),
+    "cached_whole": (cached, [4, 1], [50, 3], 5, 4, 2, 64, H, H, 16, 0, 0, 0),
+    # lengths below the new tokens' number, negative ones, past the table; pages that are none
+    "cached_short_lens": (cached, [4, 5, 2, 1], [2, -3, 0, 1], 12, 4, 2, 64, H, H, 16),
+    "cached_past_table": (cached, [2, 2], [700, 500], 4, 4, 2, 64, H, E, 16, 0, 0, 1, None, False, -30),
+    "cached_bad_pages": (cached, [2, 1], [200, 90], 3, 4, 2, 128, H, H, 16, 0, 0, 1, None, True),
+    "cached_bad_pages_e4m3": (cached, [2, 1, 1], [200, 90, 5], 4, 4, 2, 64, H, E, 16, 0, 40, 1, None, True),
+    "cached_bad_pages_f32": (cached, [2], [200], 2, 4, 2, 64, F, F, 32, 0, 0, 1, None, True),
+    "cached_odd_offsets": (cached, [], [100, 40, 30], 20, 2, 1, 64, H, H, 16, 0, 0, 1, [15, 3, 90, -2]),
+    "cached_many": (cached, [1, 0] * 70, [9, 3] * 70, 75, 2, 1, 64, H, H, 16),
+}
+
+
+@pytest.mark.parametrize("front", [0, 1])
+@pytest.mark.parametrize("name", CASES)
+def test_kernels_stay_inside_their_buffers(lib, name, front, capfd):  # noqa: F811
+    def body():
+        f, *args = CASES[name]
+        f(Call(lib, front), *args)
+    in_a_process_of_its_own(body, capfd)
