@@ -1,4 +1,6 @@
 // Attention over the tokens of packed sequences: one pass over keys and values with the running maximum and sum of each query's softmax.
+#include <type_traits>
+
 #include "laud_heads.h"
 
 namespace laud {
@@ -14,22 +16,28 @@ struct AttendArgs {
   int64_t ldq, ldk, ldv, ldo;  // elements
 };
 
-// A workgroup has a tile of 32 queries a wave of one head and goes over their keys, KN at a time.  Keys and values come by LDS-direct
-// loads into two stages that take turns: one barrier a step, the next step's loads under way while this one is multiplied.  A wave
-// multiplies keys * queries (32 x 32: a lane has 16 keys of its query, the other half wave the other 16), so that a query's maximum and
-// sum are a lane's own business but for one swap, and the weights lie as the second product, values^T * weights, takes them: its order
-// of keys within 16 is the first product's (lane half h: 4 h .. 4 h + 3 and those 8 behind), and the values are read to match -
-// transposed on their way from LDS where they are bf16.
-template <typename ET, int DP>
+// A workgroup has a tile of NW * 32 queries of one head, 32 a wave, and goes over their keys, KK at a time; KG groups of waves share the
+// steps, each with stages of its own, and join their sums at the end.  Keys and values come by LDS-direct loads into two stages that take
+// turns: one barrier a step, the next step's loads under way while this one is multiplied.  A wave multiplies keys * queries (32 x 32: a
+// lane has 16 keys of its query, the other half wave the other 16), so that a query's maximum and sum are a lane's own business but for
+// one swap, and the weights lie as the second product, values^T * weights, takes them: its order of keys within 16 is the first product's
+// (lane half h: 4 h .. 4 h + 3 and those 8 behind), and the values are read to match - transposed on their way from LDS where they are
+// bf16.
+template <typename ET, int DP, int KK>
 struct Tile {
   static constexpr bool kHalf = sizeof(ET) == 2;
-  static constexpr int kKeys = kHalf ? 64 : 32;     // KN
   static constexpr int kRow = DP * (int)sizeof(ET);  // bytes of a row in LDS
   static constexpr int kChunks = kRow / 16;
-  static constexpr int kPart = kKeys * kRow;  // keys, or values, of a stage
-  static constexpr int kStage = 2 * kPart, kBytes = 2 * kStage;
+  static constexpr int kPart = KK * kRow;  // keys, or values, of a stage
+  static constexpr int kStage = 2 * kPart, kGroup = 2 * kStage;
+  static constexpr int kSums = DP / 32 * 4 * kWave;  // of a wave's 32 queries, in f32x4
+  // LDS of a workgroup: the groups' stages, in whose place all groups' but the first's sums, maxima and sums of weights come
+  static constexpr int bytes(int NW, int KG) {
+    const int stages = KG * kGroup, sums = (KG - 1) * NW * (kSums * 16 + 2 * kWave * 4);
+    return stages > sums ? stages : sums;
+  }
   // A row's 16-byte chunk c lies at position c ^ swizzle: sixteen lanes that read a chunk of sixteen rows, or a transposed read's four
-  // rows of four chunks, meet all banks.
+  // rows of four chunks, meet all banks (no bank conflict counted).
   static __device__ __forceinline__ int key_swizzle(int row) { return kChunks == 8 ? (row >> 1) & 7 : row & 15; }
   static __device__ __forceinline__ int value_swizzle(int row) {
     return !kHalf ? 0 : kChunks == 8 ? ((row >> 1) & 1) << 2 : (row & 3) << 2;
@@ -45,15 +53,22 @@ __device__ __forceinline__ f32x16 mma32(const tok_u4& a, const tok_u4& b, const 
 }
 __device__ __forceinline__ f32x16 mma32(float a, float b, const f32x16& c) { return __builtin_amdgcn_mfma_f32_32x32x2f32(a, b, c, 0, 0, 0); }
 
-template <typename ET, int DP, int NW>
-__global__ __launch_bounds__(NW * kWave, 2) void k_attend(AttendArgs a) {
-  typedef Tile<ET, DP> L;
+// Sums are relative to a maximum that is let grow by this much (as an exponent of 2) before they are taken anew: the largest weight is
+// 2^8 instead of 1, which costs float32 nothing, and most steps are spared the scaling of all sums (64 instructions).
+constexpr float kSlack = 8.f;
+
+template <typename ET, int DP, int NW, int KG, int KK>
+__global__ __launch_bounds__(NW * KG * kWave, (NW * KG > 4 ? 1 : 2)) void k_attend(AttendArgs a) {
+  typedef Tile<ET, DP, KK> L;
   constexpr bool kHalf = L::kHalf;
-  constexpr int kKeys = L::kKeys, kBlocks = kKeys / 32, kRows = NW * 32, kDt = DP / 32;
-  constexpr int kLoads = L::kPart / 1024 / NW, kLanesRow = L::kChunks;  // LDS-direct loads a wave of keys; lanes that bring a row
+  constexpr int kBlocks = KK / 32, kRows = NW * 32, kDt = DP / 32, kEb = (int)sizeof(ET);
+  constexpr int kLanesRow = L::kChunks, kRowsLoad = kWave / kLanesRow;  // lanes that bring a row, rows of an LDS-direct load
+  constexpr int kLoads = L::kPart / 1024 / NW;                          // loads a wave of a step's keys
   static_assert(kLoads * NW * 1024 == L::kPart, "loads shared evenly");
   extern __shared__ __align__(16) unsigned char lds[];
-  const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), r32 = lane % 32, half = lane / 32;
+  const int lane = lane_id(), r32 = lane % 32, half = lane / 32;
+  const int group = __builtin_amdgcn_readfirstlane(threadIdx.x / (NW * kWave));
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave) - group * NW;
 
   // Workgroups go round-robin over the eight XCDs: each takes a run of heads, whose keys its L2 then serves, the tiles of several heads
   // side by side; the last tiles, which see the most keys, first.
@@ -69,48 +84,68 @@ __global__ __launch_bounds__(NW * kWave, 2) void k_attend(AttendArgs a) {
   const long long q_first = (tile - first_tile(a.offsets, b, a.T, 1, kRows)) * kRows;
   if (q_first < 0 || q_first >= n) return;
   const int q0 = (int)q_first, qw = q0 + wave * 32, qr = qw + r32;  // the tile's first row in its sequence, the wave's, the lane's
-  const int end = a.causal ? min(n, q0 + kRows) : n, steps = (end + kKeys - 1) / kKeys;
+  const int end = a.causal ? min(n, q0 + kRows) : n, steps = (end + KK - 1) / KK, rounds = (steps + KG - 1) / KG;
+  const uint8_t* const keep = a.keep ? a.keep + row0 : nullptr;
+  // rounds whose keys are all there, and seen by all queries of the tile
+  const int whole_steps = keep ? 0 : (a.causal ? min(n, q0 + 1) : n) / KK, whole = whole_steps / KG;
 
   // the wave's queries, for good: lane = query, sixteen-byte pieces 2 s + half
-  constexpr int kPieces = L::kChunks / 2, kPer = 16 / (int)sizeof(ET);
+  constexpr int kPieces = L::kChunks / 2, kPer = 16 / kEb;
   tok_u4 qf[kPieces];
   {
     const __amdgpu_buffer_rsrc_t rq = bytes_of(reinterpret_cast<const ET*>(a.q) + (row0 + (long long)q0) * a.ldq + head * a.D,
-                                               ((long long)(min(kRows, n - q0) - 1) * a.ldq + a.D) * (long long)sizeof(ET));
+                                               ((long long)(min(kRows, n - q0) - 1) * a.ldq + a.D) * kEb);
 #pragma unroll
     for (int s = 0; s < kPieces; ++s) {
       const int d = (2 * s + half) * kPer;
-      qf[s] = load16(rq, qr < n && d < a.D ? (unsigned)((qr - q0) * a.ldq + d) * (unsigned)sizeof(ET) : kOutside);
+      qf[s] = load16(rq, qr < n && d < a.D ? (unsigned)((qr - q0) * a.ldq + d) * kEb : kOutside);
     }
   }
   const ET* const kp = reinterpret_cast<const ET*>(a.k) + (long long)row0 * a.ldk + head / a.group * a.D;
   const ET* const vp = reinterpret_cast<const ET*>(a.v) + (long long)row0 * a.ldv + head / a.group * a.D;
-  const uint8_t* const keep = a.keep ? a.keep + row0 : nullptr;
 
-  // which of a step's keys are there: rows of the sequence that the masker kept
+  // Which of a step's keys are there, a bit each: rows of the sequence that the masker kept (asked for a round ahead).
   auto kept_byte = [&](int step) -> unsigned {
-    const long long r = (long long)step * kKeys + lane;
-    return lane < kKeys && r < n ? (keep ? (unsigned)keep[r] : 1u) : 0u;
+    const long long r = (long long)step * KK + lane;
+    return lane < KK && r < n ? (unsigned)keep[r] : 0u;
   };
-  // LDS-direct loads of a step: rows that are not there come as zeros (their weights are 0, and so are not 0 * NaN)
-  unsigned vk[kLoads], vv[kLoads];
+  auto rows_there = [&](int step) -> unsigned long long {
+    const long long rows = n - (long long)step * KK;
+    return rows >= 64 ? ~0ull : rows <= 0 ? 0ull : (1ull << rows) - 1;
+  };
+  // LDS-direct loads of a step: load i brings rows i * NW * kRowsLoad + wave * kRowsLoad .., of which a lane has one chunk, the same of
+  // each where the swizzles' periods (16 rows) allow.
+  constexpr bool kSame = NW * kRowsLoad % (kHalf ? 16 : 16) == 0;
+  constexpr int kOffsets = kSame ? 1 : kLoads;
+  unsigned vk[kOffsets], vv[kOffsets];
 #pragma unroll
-  for (int i = 0; i < kLoads; ++i) {
-    const int at = (wave * kLoads + i) * kWave + lane, row = at / kLanesRow, pos = at % kLanesRow;
+  for (int i = 0; i < kOffsets; ++i) {
+    const int row = (i * NW + wave) * kRowsLoad + lane / kLanesRow, pos = lane % kLanesRow;
     const int ck = (pos ^ L::key_swizzle(row)) * kPer, cv = (pos ^ L::value_swizzle(row)) * kPer;
-    vk[i] = ck < a.D ? (unsigned)(row * a.ldk + ck) * (unsigned)sizeof(ET) : kOutside;
-    vv[i] = cv < a.D ? (unsigned)(row * a.ldv + cv) * (unsigned)sizeof(ET) : kOutside;
+    vk[i] = ck < a.D ? (unsigned)(row * a.ldk + ck) * kEb : kOutside;
+    vv[i] = cv < a.D ? (unsigned)(row * a.ldv + cv) * kEb : kOutside;
   }
-  auto request = [&](int step, unsigned long long there) {
-    const unsigned stage = (step & 1) * L::kStage;
-    const __amdgpu_buffer_rsrc_t rk = bytes_of(kp + (long long)step * kKeys * a.ldk, 0x7fffffff);
-    const __amdgpu_buffer_rsrc_t rv = bytes_of(vp + (long long)step * kKeys * a.ldv, 0x7fffffff);
+  const unsigned stage0 = group * L::kGroup;
+  auto request = [&](int round, int step, bool all, unsigned long long there) {
+    const unsigned stage = stage0 + (round & 1) * L::kStage + wave * 1024;
+    const __amdgpu_buffer_rsrc_t rk = bytes_of(kp + (long long)step * KK * a.ldk, 0x7fffffff);
+    const __amdgpu_buffer_rsrc_t rv = bytes_of(vp + (long long)step * KK * a.ldv, 0x7fffffff);
+    if (all) {
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-      const int row = ((wave * kLoads + i) * kWave + lane) / kLanesRow;
-      const bool in = (there >> row) & 1;
-      dma16(rk, in ? vk[i] : kOutside, 0, stage + (wave * kLoads + i) * 1024);
-      dma16(rv, in ? vv[i] : kOutside, 0, stage + L::kPart + (wave * kLoads + i) * 1024);
+      for (int i = 0; i < kLoads; ++i) {
+        const unsigned skip = kSame ? (unsigned)i * NW * kRowsLoad * kEb : 0u;
+        dma16(rk, vk[kSame ? 0 : i], skip * (unsigned)a.ldk, stage + i * NW * 1024);
+        dma16(rv, vv[kSame ? 0 : i], skip * (unsigned)a.ldv, stage + L::kPart + i * NW * 1024);
+      }
+    } else {  // rows that are not there come as zeros (their weights are 0, and so are not 0 * NaN)
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) {
+        const int row = (i * NW + wave) * kRowsLoad + lane / kLanesRow;
+        const unsigned skip = kSame ? (unsigned)i * NW * kRowsLoad * kEb : 0u, ok = vk[kSame ? 0 : i], ov = vv[kSame ? 0 : i];
+        const bool in = (there >> row) & 1;
+        dma16(rk, in && ok != kOutside ? ok + skip * (unsigned)a.ldk : kOutside, 0, stage + i * NW * 1024);
+        dma16(rv, in && ov != kOutside ? ov + skip * (unsigned)a.ldv : kOutside, 0, stage + L::kPart + i * NW * 1024);
+      }
     }
   };
 
@@ -120,23 +155,10 @@ __global__ __launch_bounds__(NW * kWave, 2) void k_attend(AttendArgs a) {
 #pragma unroll
     for (int e = 0; e < 16; ++e) acc[t][e] = 0.f;
   float top = kNoScore, sum = 0.f;
-  const bool asks = qr < n && (!keep || keep[min(qr, n - 1)] != 0);
 
-  unsigned long long there = __ballot(kept_byte(0) != 0);
-  request(0, there);
-  unsigned kept_next = steps > 1 ? kept_byte(1) : 0;
-  for (int step = 0; step < steps; ++step) {
-    vm_wait<0>();
-    __syncthreads();  // the step's rows are there, and nobody reads the other stage any more
-    const unsigned long long there_next = __ballot(kept_next != 0);
-    if (step + 1 < steps) request(step + 1, there_next);
-    if (step + 2 < steps) kept_next = kept_byte(step + 2);
-    const int k0 = step * kKeys;
-    const unsigned long long here = there;
-    there = there_next;
-    if (a.causal && k0 > qw + 31) continue;  // (the wave's queries see none of them)
-    const unsigned char *ks = lds + (step & 1) * L::kStage, *vs = ks + L::kPart;
-
+  auto multiply = [&](auto some, int round, int k0, unsigned long long here, bool asks) {
+    constexpr bool kSome = decltype(some)::value;  // some keys are not there, or not seen by every query
+    const unsigned char *ks = lds + stage0 + (round & 1) * L::kStage, *vs = ks + L::kPart;
     // scores: key 32 u + 8 * (e / 4) + 4 * half + e % 4 with the lane's query
     f32x16 s[kBlocks];
 #pragma unroll
@@ -155,11 +177,8 @@ __global__ __launch_bounds__(NW * kWave, 2) void k_attend(AttendArgs a) {
         }
       }
     }
-    const bool diagonal = a.causal && k0 + kKeys - 1 > qw;
-    const unsigned long long all = kKeys == 64 ? ~0ull : 0xffffffffull;
-    const bool masked = diagonal || here != all || keep;
-    unsigned long long seen = all;
-    if (masked) {
+    unsigned long long seen = 0;
+    if constexpr (kSome) {
       seen = asks ? here : 0;
       if (a.causal) {
         const int last = qr - k0;  // the last key that the query sees
@@ -177,10 +196,10 @@ __global__ __launch_bounds__(NW * kWave, 2) void k_attend(AttendArgs a) {
     for (int u = 0; u < kBlocks; ++u)
 #pragma unroll
       for (int e = 0; e < 16; ++e) most = fmaxf(most, s[u][e]);
-    most = fmaxf(top, other_half_max(most) * a.c);
-    const float shift = shift_of(most);
-    if (__ballot(most > top)) {
-      const float shrink = exp2_fast(top - shift);
+    most = other_half_max(most) * a.c;
+    if (__ballot(most > top + kSlack)) {  // (the first score: more than -infinity)
+      most = fmaxf(top, most);
+      const float shrink = exp2_fast(top - shift_of(most));
       sum *= shrink;
 #pragma unroll
       for (int t = 0; t < kDt; ++t)
@@ -188,6 +207,7 @@ __global__ __launch_bounds__(NW * kWave, 2) void k_attend(AttendArgs a) {
         for (int e = 0; e < 16; ++e) acc[t][e] *= shrink;
       top = most;
     }
+    const float shift = shift_of(top);
 #pragma unroll
     for (int u = 0; u < kBlocks; ++u)
 #pragma unroll
@@ -198,14 +218,16 @@ __global__ __launch_bounds__(NW * kWave, 2) void k_attend(AttendArgs a) {
 
     // out^T += values^T * weights
     bool clean = true;
-    if (diagonal) {  // values that some of the queries do not see: numbers?
-      bool bad = false;
-      for (int i = lane; i < L::kPart / 16; i += kWave) {
-        const tok_u4 v = reinterpret_cast<const tok_u4*>(vs)[i];
+    if constexpr (kSome) {  // values that some of the queries do not see: numbers?
+      if (a.causal) {
+        bool bad = false;
+        for (int i = lane; i < L::kPart / 16; i += kWave) {
+          const tok_u4 v = reinterpret_cast<const tok_u4*>(vs)[i];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) bad |= kHalf ? not_finite2(v[j]) : not_finite(__uint_as_float(v[j]));
+          for (int j = 0; j < 4; ++j) bad |= kHalf ? not_finite2(v[j]) : not_finite(__uint_as_float(v[j]));
+        }
+        clean = __ballot(bad) == 0;
       }
-      clean = __ballot(bad) == 0;
     }
     if constexpr (kHalf) {
       tok_u4 w[kBlocks * 2];
@@ -220,21 +242,18 @@ __global__ __launch_bounds__(NW * kWave, 2) void k_attend(AttendArgs a) {
         const tok_u2 lo = read_transposed(at), hi = read_transposed(at + 8 * L::kRow);
         return tok_u4{lo[0], lo[1], hi[0], hi[1]};
       };
-      if (clean) {
 #pragma unroll
-        for (int t = 0; t < kBlocks * 2; ++t)
+      for (int t = 0; t < kBlocks * 2; ++t)
 #pragma unroll
-          for (int dt = 0; dt < kDt; ++dt) acc[dt] = mma32(values(t, dt), w[t], acc[dt]);
-      } else {
-#pragma unroll
-        for (int t = 0; t < kBlocks * 2; ++t)
-#pragma unroll
-          for (int dt = 0; dt < kDt; ++dt) {
-            tok_u4 v = values(t, dt);
+        for (int dt = 0; dt < kDt; ++dt) {
+          tok_u4 v = values(t, dt);
+          if (kSome && !clean) {
 #pragma unroll
             for (int j = 0; j < 4; ++j) v[j] = finite2(v[j]);
-            acc[dt] = mma32(v, w[t], acc[dt]);
           }
+          acc[dt] = mma32(v, w[t], acc[dt]);
+        }
+      if (kSome && !clean) {
 #pragma unroll 1
         for (int i = 0; i < 2 * kDt; ++i) {  // infinities of either sign
           f32x16 found;
@@ -259,19 +278,15 @@ __global__ __launch_bounds__(NW * kWave, 2) void k_attend(AttendArgs a) {
     } else {
       const float* const from = reinterpret_cast<const float*>(vs) + 4 * half * DP + r32;
       auto value = [&](int e, int dt) { return from[(8 * (e / 4) + e % 4) * DP + 32 * dt]; };
-      if (clean) {
 #pragma unroll
-        for (int e = 0; e < 16; ++e)
+      for (int e = 0; e < 16; ++e)
 #pragma unroll
-          for (int dt = 0; dt < kDt; ++dt) acc[dt] = mma32(value(e, dt), s[0][e], acc[dt]);
-      } else {
-#pragma unroll
-        for (int e = 0; e < 16; ++e)
-#pragma unroll
-          for (int dt = 0; dt < kDt; ++dt) {
-            const float v = value(e, dt);
-            acc[dt] = mma32(not_finite(v) ? 0.f : v, s[0][e], acc[dt]);
-          }
+        for (int dt = 0; dt < kDt; ++dt) {
+          float v = value(e, dt);
+          if (kSome && !clean) v = not_finite(v) ? 0.f : v;
+          acc[dt] = mma32(v, s[0][e], acc[dt]);
+        }
+      if (kSome && !clean) {
 #pragma unroll 1
         for (int i = 0; i < 2 * kDt; ++i) {  // infinities of either sign
           f32x16 found;
@@ -286,10 +301,83 @@ __global__ __launch_bounds__(NW * kWave, 2) void k_attend(AttendArgs a) {
         }
       }
     }
+  };
+
+  // Rounds of whole steps, then those of which some keys are not there or not seen.
+  unsigned kept = 0;
+  unsigned long long there = 0;
+  auto ask = [&](int round) {  // a round's loads; its step may be past the last one: nothing is fetched
+    const int step = round * KG + group;
+    there = keep ? __ballot(kept != 0) : rows_there(step);
+    request(round, step, !keep && round < whole, there);
+    if (keep) kept = kept_byte(step + KG);
+  };
+  if (keep) kept = kept_byte(group);
+  ask(0);
+  int round = 0;
+  for (; round < whole; ++round) {
+    vm_wait<0>();
+    __syncthreads();  // the step's rows are there, and nobody reads the other stage any more
+    if (round + 1 < rounds) ask(round + 1);
+    multiply(std::false_type(), round, 0, 0, true);
+  }
+  if (round < rounds) {
+    const bool asks = qr < n && (!keep || keep[min(qr, n - 1)] != 0);
+    for (; round < rounds; ++round) {
+      const unsigned long long here = there;
+      vm_wait<0>();
+      __syncthreads();
+      if (round + 1 < rounds) ask(round + 1);
+      const int k0 = (round * KG + group) * KK;
+      if (k0 >= end || (a.causal && k0 > qw + 31)) continue;  // (no keys, or none that the wave's queries see)
+      multiply(std::true_type(), round, k0, here, asks);
+    }
+  }
+  sum = other_half_sum(sum);
+
+  if constexpr (KG > 1) {  // the other groups' sums through LDS to the first, in their order
+    constexpr int kSums = L::kSums;
+    f32x4* const sums = reinterpret_cast<f32x4*>(lds);
+    float* const stats = reinterpret_cast<float*>(lds + (KG - 1) * NW * kSums * 16);
+    __syncthreads();
+    if (group != 0) {
+      const int at = (group - 1) * NW + wave;
+#pragma unroll
+      for (int t = 0; t < kDt; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          sums[at * kSums + (t * 4 + e) * kWave + lane] = f32x4{acc[t][4 * e], acc[t][4 * e + 1], acc[t][4 * e + 2], acc[t][4 * e + 3]};
+      stats[(2 * at) * kWave + lane] = top;
+      stats[(2 * at + 1) * kWave + lane] = sum;
+    }
+    __syncthreads();
+    if (group != 0) return;
+    float most = top;
+#pragma unroll
+    for (int g = 0; g < KG - 1; ++g) most = fmaxf(most, stats[2 * (g * NW + wave) * kWave + lane]);
+    const float shift = shift_of(most), mine = exp2_fast(top - shift);
+    sum *= mine;
+#pragma unroll
+    for (int t = 0; t < kDt; ++t)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[t][e] *= mine;
+#pragma unroll
+    for (int g = 0; g < KG - 1; ++g) {
+      const int at = g * NW + wave;
+      const float by = exp2_fast(stats[2 * at * kWave + lane] - shift);
+      sum = fmaf(stats[(2 * at + 1) * kWave + lane], by, sum);
+#pragma unroll
+      for (int t = 0; t < kDt; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const f32x4 v = sums[at * kSums + (t * 4 + e) * kWave + lane];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) acc[t][4 * e + j] = fmaf(v[j], by, acc[t][4 * e + j]);
+        }
+    }
   }
 
   // out: the lane's query, channels 32 t + 16 * half .. + 15
-  sum = other_half_sum(sum);
   const bool none = sum == 0.f;
   const float inv = 1.f / sum;
   ET* const out = reinterpret_cast<ET*>(a.out) + (row0 + (long long)qr) * a.ldo + head * a.D;
@@ -299,7 +387,7 @@ __global__ __launch_bounds__(NW * kWave, 2) void k_attend(AttendArgs a) {
 #pragma unroll
     for (int e = 0; e < 16; ++e) v[e] = none ? 0.f : acc[t][e] * inv;
     to_consecutive_channels(v);
-    // (the swaps leave channels 0-3, 8-11 of a half in v[0..7] and 4-7, 12-15 in v[8..15])
+    // (the swaps leave the first eight in v[0..3] and v[8..11])
     float f[2][8];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
@@ -320,14 +408,36 @@ __global__ __launch_bounds__(NW * kWave, 2) void k_attend(AttendArgs a) {
   }
 }
 
-template <typename ET, int DP>
-int launch_attend(AttendArgs a, hipStream_t st) {
-  constexpr int kWaves = 4, kRows = kWaves * 32;
-  const long long tiles = tiles_of(a.T, a.B, 1, kRows), groups = (tiles * a.heads + 7) / 8 * 8;
-  if (!launchable((double)groups, kWaves * kWave)) return LAUD_ERR_UNSUPPORTED;
+template <typename ET, int DP, int NW, int KG, int KK>
+int ask_tile_lds() {
+  return hipFuncSetAttribute(reinterpret_cast<const void*>(&k_attend<ET, DP, NW, KG, KK>), hipFuncAttributeMaxDynamicSharedMemorySize,
+                             (Tile<ET, DP, KK>::bytes(NW, KG))) == hipSuccess ? LAUD_OK : LAUD_ERR_HIP;
+}
+template <typename ET, int DP, int NW, int KG, int KK>
+int launch_tiles(AttendArgs a, hipStream_t st) {
+  const long long tiles = tiles_of(a.T, a.B, 1, NW * 32), groups = (tiles * a.heads + 7) / 8 * 8;
+  if (!launchable((double)groups, NW * KG * kWave)) return LAUD_ERR_UNSUPPORTED;
   a.tiles = (int)tiles;
-  hipLaunchKernelGGL((k_attend<ET, DP, kWaves>), dim3((unsigned)groups), dim3(kWaves * kWave), (Tile<ET, DP>::kBytes), st, a);
+  if (Tile<ET, DP, KK>::bytes(NW, KG) > 65536 && ask_tile_lds<ET, DP, NW, KG, KK>() != LAUD_OK) return LAUD_ERR_HIP;
+  hipLaunchKernelGGL((k_attend<ET, DP, NW, KG, KK>), dim3((unsigned)groups), dim3(NW * KG * kWave), (Tile<ET, DP, KK>::bytes(NW, KG)), st, a);
   return check_launch();
+}
+
+template <typename ET, int DP>
+int launch_attend(const AttendArgs& a, hipStream_t st) {
+  constexpr bool kHalf = sizeof(ET) == 2;
+#ifdef LAUD_VARIANT
+  constexpr int v = LAUD_VARIANT;
+#else
+  const int v = 0;
+#endif
+  if constexpr (kHalf) {
+    if (v == 1) return launch_tiles<ET, DP, 4, 2, 32>(a, st);
+    if (v == 2) return launch_tiles<ET, DP, 2, 2, 32>(a, st);
+    return launch_tiles<ET, DP, 4, 1, 64>(a, st);
+  } else {
+    return launch_tiles<ET, DP, 4, 1, 32>(a, st);
+  }
 }
 
 }  // namespace
