@@ -23,19 +23,23 @@ struct AttendArgs {
 // one swap, and the weights lie as the second product, values^T * weights, takes them: its order of keys within 16 is the first product's
 // (lane half h: 4 h .. 4 h + 3 and those 8 behind), and the values are read to match - transposed on their way from LDS where they are
 // bf16.
-template <typename ET, int DP, int KK>
+constexpr int kMaskWords = 128;  // 64 keys' bits each: two windows of 4096 keys
+template <typename ET, int DP, int KK, int NS>
 struct Tile {
   static constexpr bool kHalf = sizeof(ET) == 2;
   static constexpr int kRow = DP * (int)sizeof(ET);  // bytes of a row in LDS
   static constexpr int kChunks = kRow / 16;
   static constexpr int kPart = KK * kRow;  // keys, or values, of a stage
-  static constexpr int kStage = 2 * kPart, kGroup = 2 * kStage;
+  static constexpr int kStage = 2 * kPart, kGroup = NS * kStage;
   static constexpr int kSums = DP / 32 * 4 * kWave;  // of a wave's 32 queries, in f32x4
   // LDS of a workgroup: the groups' stages, in whose place all groups' but the first's sums, maxima and sums of weights come
   static constexpr int bytes(int NW, int KG) {
     const int stages = KG * kGroup, sums = (KG - 1) * NW * (kSums * 16 + 2 * kWave * 4);
     return stages > sums ? stages : sums;
   }
+  // behind them the masker's bits, and two flags a group
+  static constexpr int with_masks(int NW, int KG) { return bytes(NW, KG) + kMaskWords * 8; }
+  static constexpr int all_bytes(int NW, int KG) { return with_masks(NW, KG) + 2 * KG * 4; }
   // A row's 16-byte chunk c lies at position c ^ swizzle: sixteen lanes that read a chunk of sixteen rows, or a transposed read's four
   // rows of four chunks, meet all banks (no bank conflict counted).
   static __device__ __forceinline__ int key_swizzle(int row) { return kChunks == 8 ? (row >> 1) & 7 : row & 15; }
@@ -53,13 +57,21 @@ __device__ __forceinline__ f32x16 mma32(const tok_u4& a, const tok_u4& b, const 
 }
 __device__ __forceinline__ f32x16 mma32(float a, float b, const f32x16& c) { return __builtin_amdgcn_mfma_f32_32x32x2f32(a, b, c, 0, 0, 0); }
 
+// a pointer that is the same for the wave, in scalar registers (the descriptors of LDS-direct loads)
+template <typename T>
+__device__ __forceinline__ const T* scalar_pointer(const T* p) {
+  const unsigned long long at = (unsigned long long)(uintptr_t)p;
+  const unsigned lo = __builtin_amdgcn_readfirstlane((int)at), hi = __builtin_amdgcn_readfirstlane((int)(at >> 32));
+  return reinterpret_cast<const T*>((uintptr_t)((unsigned long long)hi << 32 | lo));
+}
+
 // Sums are relative to a maximum that is let grow by this much (as an exponent of 2) before they are taken anew: the largest weight is
 // 2^8 instead of 1, which costs float32 nothing, and most steps are spared the scaling of all sums (64 instructions).
 constexpr float kSlack = 8.f;
 
-template <typename ET, int DP, int NW, int KG, int KK>
-__global__ __launch_bounds__(NW * KG * kWave, (NW * KG > 4 ? 1 : 2)) void k_attend(AttendArgs a) {
-  typedef Tile<ET, DP, KK> L;
+template <typename ET, int DP, int NW, int KG, int KK, int NS>
+__global__ __launch_bounds__(NW * KG * kWave, 2) void k_attend(AttendArgs a) {
+  typedef Tile<ET, DP, KK, NS> L;
   constexpr bool kHalf = L::kHalf;
   constexpr int kBlocks = KK / 32, kRows = NW * 32, kDt = DP / 32, kEb = (int)sizeof(ET);
   constexpr int kLanesRow = L::kChunks, kRowsLoad = kWave / kLanesRow;  // lanes that bring a row, rows of an LDS-direct load
@@ -104,18 +116,30 @@ __global__ __launch_bounds__(NW * KG * kWave, (NW * KG > 4 ? 1 : 2)) void k_atte
   const ET* const kp = reinterpret_cast<const ET*>(a.k) + (long long)row0 * a.ldk + head / a.group * a.D;
   const ET* const vp = reinterpret_cast<const ET*>(a.v) + (long long)row0 * a.ldv + head / a.group * a.D;
 
-  // Which of a step's keys are there, a bit each: rows of the sequence that the masker kept (asked for a round ahead).
-  auto kept_byte = [&](int step) -> unsigned {
-    const long long r = (long long)step * KK + lane;
-    return lane < KK && r < n ? (unsigned)keep[r] : 0u;
+  // Which of a step's keys are there, a bit each: rows of the sequence that the masker kept.  Its bytes become bits, 4096 keys at a time,
+  // a window ahead of the keys that are asked for.
+  unsigned long long* const words = reinterpret_cast<unsigned long long*>(lds + L::bytes(NW, KG));
+  auto fill_window = [&](int w) {
+    const int words_there = (int)min((n - (long long)w * 4096 + 63) / 64, 64ll);
+    for (int i = group * NW + wave; i < words_there; i += NW * KG) {
+      const long long r = ((long long)w * 64 + i) * 64 + lane;
+      const unsigned long long m = __ballot(r < n && keep[r] != 0);
+      if (lane == 0) words[(w & 1) * 64 + i] = m;
+    }
   };
   auto rows_there = [&](int step) -> unsigned long long {
-    const long long rows = n - (long long)step * KK;
-    return rows >= 64 ? ~0ull : rows <= 0 ? 0ull : (1ull << rows) - 1;
+    const long long first = (long long)step * KK, rows = n - first;
+    if (rows <= 0) return 0;
+    if (keep) {
+      const unsigned long long m = words[(first / 64) % kMaskWords] >> (first % 64);
+      return (unsigned long long)__builtin_amdgcn_readfirstlane((int)m) & 0xffffffffull |
+             (unsigned long long)(unsigned)__builtin_amdgcn_readfirstlane((int)(m >> 32)) << 32;
+    }
+    return rows >= 64 ? ~0ull : (1ull << rows) - 1;
   };
   // LDS-direct loads of a step: load i brings rows i * NW * kRowsLoad + wave * kRowsLoad .., of which a lane has one chunk, the same of
   // each where the swizzles' periods (16 rows) allow.
-  constexpr bool kSame = NW * kRowsLoad % (kHalf ? 16 : 16) == 0;
+  constexpr bool kSame = NW * kRowsLoad % 16 == 0;
   constexpr int kOffsets = kSame ? 1 : kLoads;
   unsigned vk[kOffsets], vv[kOffsets];
 #pragma unroll
@@ -126,10 +150,10 @@ __global__ __launch_bounds__(NW * KG * kWave, (NW * KG > 4 ? 1 : 2)) void k_atte
     vv[i] = cv < a.D ? (unsigned)(row * a.ldv + cv) * kEb : kOutside;
   }
   const unsigned stage0 = group * L::kGroup;
-  auto request = [&](int round, int step, bool all, unsigned long long there) {
-    const unsigned stage = stage0 + (round & 1) * L::kStage + wave * 1024;
-    const __amdgpu_buffer_rsrc_t rk = bytes_of(kp + (long long)step * KK * a.ldk, 0x7fffffff);
-    const __amdgpu_buffer_rsrc_t rv = bytes_of(vp + (long long)step * KK * a.ldv, 0x7fffffff);
+  auto request = [&](int stage_of, int step, bool all) {
+    const unsigned stage = __builtin_amdgcn_readfirstlane(stage0 + stage_of * L::kStage + wave * 1024);
+    const __amdgpu_buffer_rsrc_t rk = bytes_of(scalar_pointer(kp + (long long)step * KK * a.ldk), 0x7fffffff);
+    const __amdgpu_buffer_rsrc_t rv = bytes_of(scalar_pointer(vp + (long long)step * KK * a.ldv), 0x7fffffff);
     if (all) {
 #pragma unroll
       for (int i = 0; i < kLoads; ++i) {
@@ -138,11 +162,11 @@ __global__ __launch_bounds__(NW * KG * kWave, (NW * KG > 4 ? 1 : 2)) void k_atte
         dma16(rv, vv[kSame ? 0 : i], skip * (unsigned)a.ldv, stage + L::kPart + i * NW * 1024);
       }
     } else {  // rows that are not there come as zeros (their weights are 0, and so are not 0 * NaN)
+      const unsigned long long there = rows_there(step);
 #pragma unroll
       for (int i = 0; i < kLoads; ++i) {
-        const int row = (i * NW + wave) * kRowsLoad + lane / kLanesRow;
         const unsigned skip = kSame ? (unsigned)i * NW * kRowsLoad * kEb : 0u, ok = vk[kSame ? 0 : i], ov = vv[kSame ? 0 : i];
-        const bool in = (there >> row) & 1;
+        const bool in = (unsigned)(there >> (i * NW + wave) * kRowsLoad) >> lane / kLanesRow & 1;
         dma16(rk, in && ok != kOutside ? ok + skip * (unsigned)a.ldk : kOutside, 0, stage + i * NW * 1024);
         dma16(rv, in && ov != kOutside ? ov + skip * (unsigned)a.ldv : kOutside, 0, stage + L::kPart + i * NW * 1024);
       }
@@ -156,19 +180,29 @@ __global__ __launch_bounds__(NW * KG * kWave, (NW * KG > 4 ? 1 : 2)) void k_atte
     for (int e = 0; e < 16; ++e) acc[t][e] = 0.f;
   float top = kNoScore, sum = 0.f;
 
-  auto multiply = [&](auto some, int round, int k0, unsigned long long here, bool asks) {
+  // which keys of a step the lane's query sees
+  auto seen_of = [&](int k0, unsigned long long here, bool asks) -> unsigned long long {
+    if (!asks) return 0;
+    if (!a.causal) return here;
+    const int last = qr - k0;
+    return last < 0 ? 0 : last >= 63 ? here : here & ((2ull << last) - 1);
+  };
+  auto multiply = [&](auto some, int stage_of, int k0, unsigned long long here, bool asks) {
     constexpr bool kSome = decltype(some)::value;  // some keys are not there, or not seen by every query
-    const unsigned char *ks = lds + stage0 + (round & 1) * L::kStage, *vs = ks + L::kPart;
+    const unsigned char *ks = lds + stage0 + stage_of * L::kStage, *vs = ks + L::kPart;
     // scores: key 32 u + 8 * (e / 4) + 4 * half + e % 4 with the lane's query
     f32x16 s[kBlocks];
 #pragma unroll
-    for (int u = 0; u < kBlocks; ++u) {
+    for (int u = 0; u < kBlocks; ++u)
 #pragma unroll
       for (int e = 0; e < 16; ++e) s[u][e] = 0.f;
-      const unsigned char* const row = ks + (u * 32 + r32) * L::kRow;
+    const unsigned char* const row = ks + r32 * L::kRow;
+    __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-      for (int i = 0; i < kPieces; ++i) {
-        const tok_u4 kf = *reinterpret_cast<const tok_u4*>(row + (((2 * i + half) ^ L::key_swizzle(r32)) << 4));
+    for (int i = 0; i < kPieces; ++i)
+#pragma unroll
+      for (int u = 0; u < kBlocks; ++u) {
+        const tok_u4 kf = *reinterpret_cast<const tok_u4*>(row + u * 32 * L::kRow + (((2 * i + half) ^ L::key_swizzle(r32)) << 4));
         if constexpr (kHalf) {
           s[u] = mma32(kf, qf[i], s[u]);
         } else {
@@ -176,20 +210,18 @@ __global__ __launch_bounds__(NW * KG * kWave, (NW * KG > 4 ? 1 : 2)) void k_atte
           for (int j = 0; j < 4; ++j) s[u] = mma32(__uint_as_float(kf[j]), __uint_as_float(qf[i][j]), s[u]);
         }
       }
-    }
-    unsigned long long seen = 0;
+    __builtin_amdgcn_s_setprio(0);
     if constexpr (kSome) {
-      seen = asks ? here : 0;
-      if (a.causal) {
-        const int last = qr - k0;  // the last key that the query sees
-        seen &= last < 0 ? 0 : last >= 63 ? ~0ull : (2ull << last) - 1;
+      const unsigned long long seen = seen_of(k0, here, asks) >> (4 * half);
+#pragma unroll
+      for (int u = 0; u < kBlocks; ++u) {
+        const unsigned bits = (unsigned)(seen >> (32 * u));
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const unsigned m = (unsigned)((int)(bits << (31 - 8 * (e / 4) - e % 4)) >> 31);  // all bits, or none
+          s[u][e] = __uint_as_float((__float_as_uint(s[u][e]) & m) | (__float_as_uint(kNoScore) & ~m));
+        }
       }
-      seen >>= 4 * half;
-#pragma unroll
-      for (int u = 0; u < kBlocks; ++u)
-#pragma unroll
-        for (int e = 0; e < 16; ++e)
-          if (!((seen >> (32 * u + 8 * (e / 4) + e % 4)) & 1)) s[u][e] = kNoScore;
     }
     float most = s[0][0];
 #pragma unroll
@@ -217,18 +249,7 @@ __global__ __launch_bounds__(NW * KG * kWave, (NW * KG > 4 ? 1 : 2)) void k_atte
       }
 
     // out^T += values^T * weights
-    bool clean = true;
-    if constexpr (kSome) {  // values that some of the queries do not see: numbers?
-      if (a.causal) {
-        bool bad = false;
-        for (int i = lane; i < L::kPart / 16; i += kWave) {
-          const tok_u4 v = reinterpret_cast<const tok_u4*>(vs)[i];
-#pragma unroll
-          for (int j = 0; j < 4; ++j) bad |= kHalf ? not_finite2(v[j]) : not_finite(__uint_as_float(v[j]));
-        }
-        clean = __ballot(bad) == 0;
-      }
-    }
+    __builtin_amdgcn_s_setprio(1);
     if constexpr (kHalf) {
       tok_u4 w[kBlocks * 2];
 #pragma unroll
@@ -237,100 +258,117 @@ __global__ __launch_bounds__(NW * KG * kWave, (NW * KG > 4 ? 1 : 2)) void k_atte
         for (int j = 0; j < 4; ++j) w[t][j] = pack_bf16(s[t / 2][8 * (t % 2) + 2 * j], s[t / 2][8 * (t % 2) + 2 * j + 1]);
       const int i16 = lane % 16, low = (lane / 16) % 2 * 2 + i16 % 4 / 2;
       const unsigned char* const from = vs + (4 * half + i16 / 4) * L::kRow + i16 % 2 * 8;
-      auto values = [&](int t, int dt) {
-        const unsigned char* const at = from + 16 * t * L::kRow + (((4 * dt + low) ^ L::value_swizzle(i16 / 4)) << 4);
-        const tok_u2 lo = read_transposed(at), hi = read_transposed(at + 8 * L::kRow);
-        return tok_u4{lo[0], lo[1], hi[0], hi[1]};
-      };
 #pragma unroll
       for (int t = 0; t < kBlocks * 2; ++t)
 #pragma unroll
         for (int dt = 0; dt < kDt; ++dt) {
-          tok_u4 v = values(t, dt);
-          if (kSome && !clean) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) v[j] = finite2(v[j]);
-          }
-          acc[dt] = mma32(v, w[t], acc[dt]);
+          const unsigned char* const at = from + 16 * t * L::kRow + (((4 * dt + low) ^ L::value_swizzle(i16 / 4)) << 4);
+          const tok_u2 lo = read_transposed(at), hi = read_transposed(at + 8 * L::kRow);
+          acc[dt] = mma32(tok_u4{lo[0], lo[1], hi[0], hi[1]}, w[t], acc[dt]);
         }
-      if (kSome && !clean) {
-#pragma unroll 1
-        for (int i = 0; i < 2 * kDt; ++i) {  // infinities of either sign
-          f32x16 found;
-#pragma unroll
-          for (int e = 0; e < 16; ++e) found[e] = 0.f;
-#pragma unroll 1
-          for (int t = 0; t < kBlocks * 2; ++t) {
-            tok_u4 v = values(t, i / 2), sees;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              v[j] = endless2(v[j], i % 2);
-              const int key = 16 * t + 8 * (j / 2) + j % 2 * 2;  // (of seen, which is shifted by the lane's half)
-              sees[j] = ((seen >> key) & 1 ? 0x3f80u : 0u) | ((seen >> key) & 2 ? 0x3f800000u : 0u);
-            }
-            found = mma32(v, sees, found);
-          }
-#pragma unroll
-          for (int t = 0; t < kDt; ++t)
-            if (t == i / 2) add_endless(acc[t], found, i % 2);
-        }
-      }
     } else {
       const float* const from = reinterpret_cast<const float*>(vs) + 4 * half * DP + r32;
-      auto value = [&](int e, int dt) { return from[(8 * (e / 4) + e % 4) * DP + 32 * dt]; };
 #pragma unroll
       for (int e = 0; e < 16; ++e)
 #pragma unroll
-        for (int dt = 0; dt < kDt; ++dt) {
-          float v = value(e, dt);
-          if (kSome && !clean) v = not_finite(v) ? 0.f : v;
-          acc[dt] = mma32(v, s[0][e], acc[dt]);
-        }
-      if (kSome && !clean) {
-#pragma unroll 1
-        for (int i = 0; i < 2 * kDt; ++i) {  // infinities of either sign
-          f32x16 found;
+        for (int dt = 0; dt < kDt; ++dt) acc[dt] = mma32(from[(8 * (e / 4) + e % 4) * DP + 32 * dt], s[0][e], acc[dt]);
+    }
+    __builtin_amdgcn_s_setprio(0);
+  };
+
+  // 0 * NaN is NaN, so where some queries of a tile do not see all of a step's keys, values that are not finite must not meet the matrix
+  // instructions.  They become zeros in LDS, and are added to the queries that see them one by one, from memory.
+  int* const found = reinterpret_cast<int*>(lds + L::with_masks(NW, KG));  // [2][KG]
+  auto take_out = [&](int stage_of, int turn) {
+    tok_u4* const vs = reinterpret_cast<tok_u4*>(lds + stage0 + stage_of * L::kStage + L::kPart);
+    bool bad = false;
 #pragma unroll
-          for (int e = 0; e < 16; ++e) found[e] = 0.f;
-#pragma unroll 1
-          for (int e = 0; e < 16; ++e)
-            found = mma32(endless(value(e, i / 2), i % 2), (seen >> (8 * (e / 4) + e % 4)) & 1 ? 1.f : 0.f, found);
+    for (int i = 0; i < L::kPart / 16 / (NW * kWave); ++i) {
+      const int at = (i * NW + wave) * kWave + lane;
+      tok_u4 v = vs[at];
+      bool here = false;
 #pragma unroll
-          for (int t = 0; t < kDt; ++t)
-            if (t == i / 2) add_endless(acc[t], found, i % 2);
-        }
+      for (int j = 0; j < 4; ++j) here |= kHalf ? not_finite2(v[j]) : not_finite(__uint_as_float(v[j]));
+      if (here) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = kHalf ? finite2(v[j]) : not_finite(__uint_as_float(v[j])) ? 0u : v[j];
+        vs[at] = v;
+        bad = true;
       }
+    }
+    if (__ballot(bad) && lane == 0) found[turn * KG + group] = 1;
+  };
+  auto add_back = [&](int k0, unsigned long long here, bool asks) {
+    const unsigned long long seen = seen_of(k0, here, asks);
+#pragma unroll 1
+    for (int j = 0; j < KK; ++j) {
+      if (!((here >> j) & 1)) continue;
+      const __amdgpu_buffer_rsrc_t row = bytes_of(vp + (long long)(k0 + j) * a.ldv, a.D * kEb);
+      const bool sees = (seen >> j) & 1;
+#pragma unroll
+      for (int t = 0; t < kDt; ++t)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          float v[4];
+          if constexpr (kHalf) {
+            const tok_u2 x = load8(row, half * 8 + (32 * t + 8 * g) * 2);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = __uint_as_float(e % 2 ? x[e / 2] & 0xffff0000u : x[e / 2] << 16);
+          } else {
+            const tok_u4 x = load16(row, half * 16 + (32 * t + 8 * g) * 4);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = __uint_as_float(x[e]);
+          }
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[t][4 * g + e] += sees && not_finite(v[e]) ? v[e] : 0.f;
+        }
     }
   };
 
-  // Rounds of whole steps, then those of which some keys are not there or not seen.
-  unsigned kept = 0;
-  unsigned long long there = 0;
-  auto ask = [&](int round) {  // a round's loads; its step may be past the last one: nothing is fetched
+  // Rounds of whole steps, then those of which some keys are not there or not seen.  Loads are asked for NS - 1 rounds ahead; behind the
+  // last round they fetch nothing, so that what is under way is always as much.
+  int now = 0, fill = NS - 1;  // stages of this round and of the one asked for
+  auto ask = [&](int round, int stage_of) {
     const int step = round * KG + group;
-    there = keep ? __ballot(kept != 0) : rows_there(step);
-    request(round, step, !keep && round < whole, there);
-    if (keep) kept = kept_byte(step + KG);
+    request(stage_of, step, round < whole);
   };
-  if (keep) kept = kept_byte(group);
-  ask(0);
+  if (keep) {
+    fill_window(0);
+    fill_window(1);
+    __syncthreads();
+  }
+#pragma unroll
+  for (int r = 0; r < NS - 1; ++r) ask(r, r);
   int round = 0;
-  for (; round < whole; ++round) {
-    vm_wait<0>();
-    __syncthreads();  // the step's rows are there, and nobody reads the other stage any more
-    if (round + 1 < rounds) ask(round + 1);
-    multiply(std::false_type(), round, 0, 0, true);
+  auto begin = [&] {  // the round's rows are there, and nobody reads the stage of the one before any more
+    vm_wait<(NS - 2) * 2 * kLoads>();
+    __syncthreads();
+    ask(round + NS - 1, fill);
+  };
+  auto next = [&] {
+    fill = now;
+    now = now + 1 < NS ? now + 1 : 0;
+  };
+  for (; round < whole; ++round, next()) {
+    begin();
+    multiply(std::false_type(), now, 0, 0, true);
   }
   if (round < rounds) {
     const bool asks = qr < n && (!keep || keep[min(qr, n - 1)] != 0);
-    for (; round < rounds; ++round) {
-      const unsigned long long here = there;
-      vm_wait<0>();
-      __syncthreads();
-      if (round + 1 < rounds) ask(round + 1);
-      const int k0 = (round * KG + group) * KK;
+    if (threadIdx.x < 2 * KG) found[threadIdx.x] = 0;
+    for (; round < rounds; ++round, next()) {
+      const int k0 = (round * KG + group) * KK, turn = round & 1;
+      begin();
+      if (keep && round > 0 && k0 / 4096 * 4096 == k0 - group * KK) fill_window(k0 / 4096 + 1);  // (in the place of the window before)
+      if (a.causal) {
+        take_out(now, turn);
+        __syncthreads();
+        if (threadIdx.x < KG) found[(turn ^ 1) * KG + threadIdx.x] = 0;  // (the next round's, whose last reader has passed this barrier)
+      }
       if (k0 >= end || (a.causal && k0 > qw + 31)) continue;  // (no keys, or none that the wave's queries see)
-      multiply(std::true_type(), round, k0, here, asks);
+      const unsigned long long here = rows_there(k0 / KK);
+      multiply(std::true_type(), now, k0, here, asks);
+      if (a.causal && found[turn * KG + group]) add_back(k0, here, asks);
     }
   }
   sum = other_half_sum(sum);
@@ -339,6 +377,7 @@ __global__ __launch_bounds__(NW * KG * kWave, (NW * KG > 4 ? 1 : 2)) void k_atte
     constexpr int kSums = L::kSums;
     f32x4* const sums = reinterpret_cast<f32x4*>(lds);
     float* const stats = reinterpret_cast<float*>(lds + (KG - 1) * NW * kSums * 16);
+    vm_wait<0>();  // (no load into LDS is left behind)
     __syncthreads();
     if (group != 0) {
       const int at = (group - 1) * NW + wave;
@@ -408,36 +447,30 @@ __global__ __launch_bounds__(NW * KG * kWave, (NW * KG > 4 ? 1 : 2)) void k_atte
   }
 }
 
-template <typename ET, int DP, int NW, int KG, int KK>
+template <typename ET, int DP, int NW, int KG, int KK, int NS>
 int ask_tile_lds() {
-  return hipFuncSetAttribute(reinterpret_cast<const void*>(&k_attend<ET, DP, NW, KG, KK>), hipFuncAttributeMaxDynamicSharedMemorySize,
-                             (Tile<ET, DP, KK>::bytes(NW, KG))) == hipSuccess ? LAUD_OK : LAUD_ERR_HIP;
+  return hipFuncSetAttribute(reinterpret_cast<const void*>(&k_attend<ET, DP, NW, KG, KK, NS>), hipFuncAttributeMaxDynamicSharedMemorySize,
+                             (Tile<ET, DP, KK, NS>::all_bytes(NW, KG))) == hipSuccess ? LAUD_OK : LAUD_ERR_HIP;
 }
-template <typename ET, int DP, int NW, int KG, int KK>
+template <typename ET, int DP, int NW, int KG, int KK, int NS>
 int launch_tiles(AttendArgs a, hipStream_t st) {
   const long long tiles = tiles_of(a.T, a.B, 1, NW * 32), groups = (tiles * a.heads + 7) / 8 * 8;
   if (!launchable((double)groups, NW * KG * kWave)) return LAUD_ERR_UNSUPPORTED;
   a.tiles = (int)tiles;
-  if (Tile<ET, DP, KK>::bytes(NW, KG) > 65536 && ask_tile_lds<ET, DP, NW, KG, KK>() != LAUD_OK) return LAUD_ERR_HIP;
-  hipLaunchKernelGGL((k_attend<ET, DP, NW, KG, KK>), dim3((unsigned)groups), dim3(NW * KG * kWave), (Tile<ET, DP, KK>::bytes(NW, KG)), st, a);
+  constexpr int lds = Tile<ET, DP, KK, NS>::all_bytes(NW, KG);
+  if (lds > 65536 && ask_tile_lds<ET, DP, NW, KG, KK, NS>() != LAUD_OK) return LAUD_ERR_HIP;
+  hipLaunchKernelGGL((k_attend<ET, DP, NW, KG, KK, NS>), dim3((unsigned)groups), dim3(NW * KG * kWave), lds, st, a);
   return check_launch();
 }
 
 template <typename ET, int DP>
 int launch_attend(const AttendArgs& a, hipStream_t st) {
   constexpr bool kHalf = sizeof(ET) == 2;
-#ifdef LAUD_VARIANT
-  constexpr int v = LAUD_VARIANT;
-#else
-  const int v = 0;
+#ifdef LAUD_TILE
+  return launch_tiles<ET, DP, LAUD_TILE>(a, st);
 #endif
-  if constexpr (kHalf) {
-    if (v == 1) return launch_tiles<ET, DP, 4, 2, 32>(a, st);
-    if (v == 2) return launch_tiles<ET, DP, 2, 2, 32>(a, st);
-    return launch_tiles<ET, DP, 4, 1, 64>(a, st);
-  } else {
-    return launch_tiles<ET, DP, 4, 1, 32>(a, st);
-  }
+  if constexpr (kHalf) return launch_tiles<ET, DP, 4, 1, 64, 2>(a, st);
+  else return launch_tiles<ET, DP, 4, 1, 32, 2>(a, st);
 }
 
 }  // namespace
