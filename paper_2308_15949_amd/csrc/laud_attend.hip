@@ -57,14 +57,6 @@ __device__ __forceinline__ f32x16 mma32(const tok_u4& a, const tok_u4& b, const 
 }
 __device__ __forceinline__ f32x16 mma32(float a, float b, const f32x16& c) { return __builtin_amdgcn_mfma_f32_32x32x2f32(a, b, c, 0, 0, 0); }
 
-// a pointer that is the same for the wave, in scalar registers (the descriptors of LDS-direct loads)
-template <typename T>
-__device__ __forceinline__ const T* scalar_pointer(const T* p) {
-  const unsigned long long at = (unsigned long long)(uintptr_t)p;
-  const unsigned lo = __builtin_amdgcn_readfirstlane((int)at), hi = __builtin_amdgcn_readfirstlane((int)(at >> 32));
-  return reinterpret_cast<const T*>((uintptr_t)((unsigned long long)hi << 32 | lo));
-}
-
 // Sums are relative to a maximum that is let grow by this much (as an exponent of 2) before they are taken anew: the largest weight is
 // 2^8 instead of 1, which costs float32 nothing, and most steps are spared the scaling of all sums (64 instructions).
 constexpr float kSlack = 8.f;

@@ -6,12 +6,13 @@ namespace {
 
 struct CachedArgs {
   int heads, group, kv_heads, D, causal, B, T, pages, page_bits, table_ld, prefix_len;
-  int tiles, splits;      // tiles of query rows; parts that a tile's keys are shared out over
-  int parts, first_part;  // all parts that are joined; the first of this launch
-  int shared;             // the prefix: every token's rows over the same keys
-  int by_xcd;
+  // of the sequences' own keys, and of the prefix, whose workgroups come first: tiles of query rows, and parts that a tile's keys are
+  // shared out over; all parts of a row are joined, its own first
+  int tiles, splits, prefix_tiles, prefix_splits;
+  unsigned prefix_groups;
+  int by_xcd, prefix_by_xcd;
   float c;                // scale * log2(e)
-  const int32_t *offsets, *lens, *table;
+  const int32_t *offsets, *lens, *table, *prefix;
   const uint8_t *k, *v;
   const float *ks, *vs;
   const void* q;
@@ -20,11 +21,18 @@ struct CachedArgs {
   int64_t ldq, ldo;
 };
 
+#ifndef LAUD_G8
+#define LAUD_G8 2
+#endif
 constexpr int kWaves = 4, kMaxParts = 64, kPartStep = 128;
 // Keys of a part: the same for every tile of a sequence, so that whoever joins the parts knows how many there are.
 __device__ __forceinline__ int part_keys(int len, int splits) {
   const int each = (len + splits - 1) / splits;
   return max((each + kPartStep - 1) / kPartStep * kPartStep, kPartStep);
+}
+__device__ __forceinline__ int parts_of(int len, int splits) {  // how many of them have keys; one where there are none
+  const int each = part_keys(len, splits);
+  return max((len + each - 1) / each, 1);
 }
 __device__ __forceinline__ int cached_tokens(const CachedArgs& a, int b) {
   const long long room = (long long)a.table_ld << a.page_bits;
@@ -36,20 +44,22 @@ __device__ __forceinline__ int cached_tokens(const CachedArgs& a, int b) {
 // results are keys 4 * (l / 16) .. +3 of its query, l % 16), and of the values keys 4 * (l / 16) .. +3, elements kEach * (l % 16) .. of
 // each: all of a row's bytes come in one piece a lane, straight into registers, and with element e of every lane the matrix instruction
 // makes channels kEach * m + e, m = 0 .. 15.  Nothing has to change lanes between the two products.
-template <typename CT, int DP> struct Operands;
+template <typename CT, int DP, int GROUPS> struct Operands;
 
-template <int DP>
-struct Operands<bf16_t, DP> {
-  static constexpr int kGroups = 2, kEach = DP / 16, kPieces = DP / 32, kQuery = DP / 32;
+template <int DP, int GROUPS>
+struct Operands<bf16_t, DP, GROUPS> {
+  static constexpr int kGroups = GROUPS, kEach = DP / 16, kPieces = DP / 32, kQuery = DP / 32;
   static constexpr int kBytes = 2;
   tok_u4 k[kGroups][kPieces];
   unsigned v[kGroups][4][kEach / 2];
-  __device__ __forceinline__ void load(int u, __amdgpu_buffer_rsrc_t rk, __amdgpu_buffer_rsrc_t rv, int D, int r16, int quarter) {
+  __device__ __forceinline__ void load_keys(int u, __amdgpu_buffer_rsrc_t rk, int D, int r16, int quarter) {
 #pragma unroll
     for (int s = 0; s < kPieces; ++s) {
       const int d = 32 * s + 8 * quarter;
       k[u][s] = load16(rk, d < D ? (unsigned)(r16 * D + d) * 2u : kOutside);
     }
+  }
+  __device__ __forceinline__ void load_values(int u, __amdgpu_buffer_rsrc_t rv, int D, int r16, int quarter) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const unsigned at = r16 * kEach < D ? (unsigned)((4 * quarter + j) * D + r16 * kEach) * 2u : kOutside;
@@ -66,28 +76,41 @@ struct Operands<bf16_t, DP> {
   }
   static __device__ __forceinline__ int query_at(int s, int quarter) { return 32 * s + 8 * quarter; }  // eight elements
   __device__ __forceinline__ bf16x8 key(int u, int s) const { return __builtin_bit_cast(bf16x8, k[u][s]); }
-  // element e of the lane's eight keys
-  __device__ __forceinline__ tok_u4 value(int e) const {
+  // element e of the lane's eight keys of groups 2 h and 2 h + 1
+  __device__ __forceinline__ tok_u4 value(int h, int e) const {
     tok_u4 r;
 #pragma unroll
     for (int p = 0; p < 4; ++p)
-      r[p] = __builtin_amdgcn_perm(v[p / 2][p % 2 * 2 + 1][e / 2], v[p / 2][p % 2 * 2][e / 2], e % 2 ? 0x07060302u : 0x05040100u);
+      r[p] = __builtin_amdgcn_perm(v[2 * h + p / 2][p % 2 * 2 + 1][e / 2], v[2 * h + p / 2][p % 2 * 2][e / 2], e % 2 ? 0x07060302u : 0x05040100u);
     return r;
   }
+  __device__ __forceinline__ bool take_out() {
+    bool bad = false;
+#pragma unroll
+    for (int i = 0; i < kGroups * 4 * (kEach / 2); ++i) {
+      unsigned& x = v[i / (2 * kEach)][i / (kEach / 2) % 4][i % (kEach / 2)];
+      bad |= not_finite2(x);
+      x = finite2(x);
+    }
+    return bad;
+  }
+  static __device__ __forceinline__ float value_at(const uint8_t* p, int i) { return bf16_to_f32(reinterpret_cast<const bf16_t*>(p)[i]); }
 };
 
-template <int DP>
-struct Operands<uint8_t, DP> {
-  static constexpr int kGroups = 2, kEach = DP / 16, kPieces = DP / 64, kQuery = DP / 32;
+template <int DP, int GROUPS>
+struct Operands<uint8_t, DP, GROUPS> {
+  static constexpr int kGroups = GROUPS, kEach = DP / 16, kPieces = DP / 64, kQuery = DP / 32;
   static constexpr int kBytes = 1;
   tok_u4 k[kGroups][kPieces];
   unsigned v[kGroups][4][kEach / 4];
-  __device__ __forceinline__ void load(int u, __amdgpu_buffer_rsrc_t rk, __amdgpu_buffer_rsrc_t rv, int D, int r16, int quarter) {
+  __device__ __forceinline__ void load_keys(int u, __amdgpu_buffer_rsrc_t rk, int D, int r16, int quarter) {
 #pragma unroll
     for (int s = 0; s < kPieces; ++s) {
       const int d = 64 * s + 16 * quarter;
       k[u][s] = load16(rk, d < D ? (unsigned)(r16 * D + d) : kOutside);
     }
+  }
+  __device__ __forceinline__ void load_values(int u, __amdgpu_buffer_rsrc_t rv, int D, int r16, int quarter) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const unsigned at = r16 * kEach < D ? (unsigned)((4 * quarter + j) * D + r16 * kEach) : kOutside;
@@ -102,11 +125,11 @@ struct Operands<uint8_t, DP> {
   }
   static __device__ __forceinline__ int query_at(int s, int quarter) { return 64 * (s / 2) + 16 * quarter + 8 * (s % 2); }
   __device__ __forceinline__ bf16x8 key(int u, int s) const { return widen8(k[u][s / 2][s % 2 * 2], k[u][s / 2][s % 2 * 2 + 1]); }
-  __device__ __forceinline__ tok_u4 value(int e) const {
+  __device__ __forceinline__ tok_u4 value(int h, int e) const {
     tok_u4 r;
 #pragma unroll
     for (int p = 0; p < 4; ++p) {  // codes e and its neighbour of two keys, the asked one widened
-      const unsigned w = __builtin_amdgcn_perm(v[p / 2][p % 2 * 2 + 1][e / 4], v[p / 2][p % 2 * 2][e / 4], e % 4 / 2 ? 0x07030602u : 0x05010400u);
+      const unsigned w = __builtin_amdgcn_perm(v[2 * h + p / 2][p % 2 * 2 + 1][e / 4], v[2 * h + p / 2][p % 2 * 2][e / 4], e % 4 / 2 ? 0x07030602u : 0x05010400u);
       bf16x2 h;
       if (e % 2) h = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, true);
       else h = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, false);
@@ -114,20 +137,33 @@ struct Operands<uint8_t, DP> {
     }
     return r;
   }
+  __device__ __forceinline__ bool take_out() {
+    bool bad = false;
+#pragma unroll
+    for (int i = 0; i < kGroups * 4 * (kEach / 4); ++i) {
+      unsigned& x = v[i / kEach][i / (kEach / 4) % 4][i % (kEach / 4)];
+      bad |= nan_codes(x) != 0;
+      x = finite4(x);
+    }
+    return bad;
+  }
+  static __device__ __forceinline__ float value_at(const uint8_t* p, int i) { return (p[i] & 0x7f) == 0x7f ? __builtin_nanf("") : 0.f; }
 };
 
-template <int DP>
-struct Operands<float, DP> {
-  static constexpr int kGroups = 1, kEach = DP / 16, kPieces = DP / 16, kQuery = DP / 16;
+template <int DP, int GROUPS>
+struct Operands<float, DP, GROUPS> {
+  static constexpr int kGroups = GROUPS, kEach = DP / 16, kPieces = DP / 16, kQuery = DP / 16;
   static constexpr int kBytes = 4;
   tok_u4 k[kGroups][kPieces];
   float v[kGroups][4][kEach];
-  __device__ __forceinline__ void load(int u, __amdgpu_buffer_rsrc_t rk, __amdgpu_buffer_rsrc_t rv, int D, int r16, int quarter) {
+  __device__ __forceinline__ void load_keys(int u, __amdgpu_buffer_rsrc_t rk, int D, int r16, int quarter) {
 #pragma unroll
     for (int s = 0; s < kPieces; ++s) {
       const int d = 16 * s + 4 * quarter;
       k[u][s] = load16(rk, d < D ? (unsigned)(r16 * D + d) * 4u : kOutside);
     }
+  }
+  __device__ __forceinline__ void load_values(int u, __amdgpu_buffer_rsrc_t rv, int D, int r16, int quarter) {
 #pragma unroll
     for (int j = 0; j < 4; ++j)
 #pragma unroll
@@ -138,6 +174,17 @@ struct Operands<float, DP> {
       }
   }
   static __device__ __forceinline__ int query_at(int s, int quarter) { return 16 * s + 4 * quarter; }  // four elements
+  __device__ __forceinline__ bool take_out() {
+    bool bad = false;
+#pragma unroll
+    for (int i = 0; i < 4 * kEach; ++i) {
+      float& x = v[0][i / kEach][i % kEach];
+      bad |= not_finite(x);
+      if (not_finite(x)) x = 0.f;
+    }
+    return bad;
+  }
+  static __device__ __forceinline__ float value_at(const uint8_t* p, int i) { return reinterpret_cast<const float*>(p)[i]; }
 };
 
 __device__ __forceinline__ f32x4 mma4(float a, float b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0); }
@@ -145,8 +192,8 @@ __device__ __forceinline__ f32x4 mma4(float a, float b, f32x4 c) { return __buil
 // Sixteen query rows a row tile (RT of them a workgroup): the tokens of a sequence times the query heads of a key head, so that a key is
 // fetched once for all of them.  Four waves share a part's keys, each takes every fourth step of 16 or 32 keys; their sums are joined through LDS.
 template <typename ET, typename CT, int DP, int RT>
-__global__ __launch_bounds__(kWaves * kWave, (RT > 2 ? 1 : 2)) void k_cached(CachedArgs a) {
-  typedef Operands<CT, DP> O;
+__global__ __launch_bounds__(kWaves * kWave, 2) void k_cached(CachedArgs a) {
+  typedef Operands<CT, DP, (sizeof(CT) == 4 ? 1 : sizeof(CT) == 1 && RT == 1 ? LAUD_G8 : 2)> O;
   constexpr bool kWide = sizeof(CT) == 4;  // float32 instructions
   constexpr int kGroups = O::kGroups, kKeys = 16 * kGroups, kRows = 16 * RT, kEach = O::kEach, kLdRow = DP + 4;
   extern __shared__ __align__(16) unsigned char lds[];
@@ -155,60 +202,75 @@ __global__ __launch_bounds__(kWaves * kWave, (RT > 2 ? 1 : 2)) void k_cached(Cac
   const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), r16 = lane % 16, quarter = lane / 16;
 
   // Which rows, key head and part.  Where several tiles read the same keys they go to one XCD, one behind the other.
+  const bool shared = blockIdx.x < a.prefix_groups;  // the prefix: every token's rows over the same keys
+  const unsigned id = shared ? blockIdx.x : blockIdx.x - a.prefix_groups;
+  const unsigned tiles = shared ? a.prefix_tiles : a.tiles, splits = shared ? a.prefix_splits : a.splits;
   int tile, hk, split;
-  if (a.by_xcd) {
-    const unsigned j = blockIdx.x / 8;
-    const unsigned g = j / a.tiles * 8 + blockIdx.x % 8;
-    tile = j % a.tiles;
+  if (shared ? a.prefix_by_xcd : a.by_xcd) {
+    const unsigned j = id / 8;
+    const unsigned g = j / tiles * 8 + id % 8;
+    tile = j % tiles;
     hk = g % a.kv_heads;
     split = g / a.kv_heads;
   } else {
-    split = blockIdx.x % a.splits;
-    const unsigned j = blockIdx.x / a.splits;
+    split = id % splits;
+    const unsigned j = id / splits;
     hk = j % a.kv_heads;
     tile = j / a.kv_heads;
   }
   int b = 0, row0 = 0, n = a.T, len = a.prefix_len;
-  const int32_t* table = a.table;
-  if (!a.shared) {
+  const int32_t* table = a.prefix;
+  if (!shared) {
     b = last_not_above(a.B, [&](int i) { return first_tile(a.offsets, i, a.T, a.group, kRows) <= tile; });
     row0 = row_at(a.offsets, b, a.T);
     n = row_at(a.offsets, b + 1, a.T) - row0;
     if ((long long)tile < first_tile(a.offsets, b, a.T, a.group, kRows)) return;
     tile -= (int)first_tile(a.offsets, b, a.T, a.group, kRows);
     len = cached_tokens(a, b);
-    table += (long long)b * a.table_ld;
+    table = a.table + (long long)b * a.table_ld;
   }
   if (n <= 0) return;
   const unsigned rows = (unsigned)n * (unsigned)a.group, first_row = (unsigned)tile * kRows;  // (T * heads is below 2^31)
   if (first_row >= rows) return;
   const int there = (int)min((unsigned)kRows, rows - first_row);  // rows of this tile
-  const int each = part_keys(len, a.splits);
+  const int each = part_keys(len, splits);
   if (split > 0 && (long long)split * each >= len) return;
-  const long long past = (long long)(a.shared ? len : a.lens[b]) - n;  // position of the first token
-  const bool causal = a.causal && !a.shared;
+  const long long past = (long long)(shared ? len : a.lens[b]) - n;  // position of the first token
+  const bool causal = a.causal && !shared;
   auto limit_of = [&](unsigned row) -> int {  // keys that a row sees
     return causal ? (int)min(max(past + row / (unsigned)a.group + 1, 0ll), (long long)len) : len;
   };
   const int begin = split * each;
-  const int end = min(min(begin + each, len), limit_of(first_row + there - 1)), all_see = limit_of(first_row);
+  const int end = __builtin_amdgcn_readfirstlane(min(min(begin + each, len), limit_of(first_row + there - 1)));
+  const int all_see = __builtin_amdgcn_readfirstlane(limit_of(first_row));  // keys that every row sees
 
-  // queries, for good
+  // Queries: one row tile stays in registers; several lie in LDS, where every wave reads them step by step (in registers as well they
+  // would push sums out into memory).
+  constexpr bool kQueryLds = RT > 1;
+  constexpr int kQueryRow = DP * (int)sizeof(ET) + 16;
+  static_assert(kRows * kQueryRow <= kWaves * 16 * kLdRow * 4, "queries lie where the waves' sums come later");
   int limit[RT];
-  tok_u4 q[RT][O::kQuery];
+  tok_u4 q[O::kQuery];
 #pragma unroll
   for (int t = 0; t < RT; ++t) {
     const unsigned row = first_row + t * 16 + r16, token = row / (unsigned)a.group;
     const bool in = t * 16 + r16 < there;
     limit[t] = in ? limit_of(row) : 0;
+    if (kQueryLds && t % kWaves != wave) continue;
     const ET* const from = reinterpret_cast<const ET*>(a.q) + (long long)(row0 + token) * a.ldq + (hk * a.group + (row - token * a.group)) * a.D;
 #pragma unroll
     for (int s = 0; s < O::kQuery; ++s) {
       const int d = O::query_at(s, quarter);
-      q[t][s] = tok_u4{0, 0, 0, 0};
-      if (in && d < a.D) q[t][s] = *reinterpret_cast<const tok_u4*>(from + d);
+      q[s] = tok_u4{0, 0, 0, 0};
+      if (in && d < a.D) q[s] = *reinterpret_cast<const tok_u4*>(from + d);
+      if constexpr (kQueryLds) *reinterpret_cast<tok_u4*>(lds + (t * 16 + r16) * kQueryRow + d * (int)sizeof(ET)) = q[s];
     }
   }
+  if constexpr (kQueryLds) __syncthreads();
+  auto query = [&](int t, int i) {
+    if constexpr (kQueryLds) return *reinterpret_cast<const tok_u4*>(lds + (t * 16 + r16) * kQueryRow + O::query_at(i, quarter) * (int)sizeof(ET));
+    else return q[i];
+  };
 
   f32x4 acc[RT][kEach];
   float top[RT], sum[RT];
@@ -220,74 +282,93 @@ __global__ __launch_bounds__(kWaves * kWave, (RT > 2 ? 1 : 2)) void k_cached(Cac
     for (int e = 0; e < kEach; ++e) acc[t][e] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
 
-  // A step's operands, and how many keys of each sixteen there are (a page that is none has none).
-  struct Step {
-    O o;
-    f32x4 ks[kGroups], vs[kGroups];
+  // Where a step's keys are: of each sixteen how many (a page that is none has none), and the first one's row of the cache.
+  struct Place {
     int valid[kGroups];
+    long long at[kGroups];
   };
-  auto page_at = [&](int key, int u) {
-    const int pos = key + 16 * u;
-    return pos < end ? table[pos >> a.page_bits] : -1;
-  };
-  auto load = [&](Step& s, int key, const int (&page)[kGroups]) {
+  auto place_of = [&](int key) {
+    Place s;
 #pragma unroll
     for (int u = 0; u < kGroups; ++u) {
-      const int pos = key + 16 * u, pg = __builtin_amdgcn_readfirstlane(page[u]);
-      const bool ok = pos < end && (unsigned)pg < (unsigned)a.pages;
+      const int pos = key + 16 * u, pg = pos < end ? __builtin_amdgcn_readfirstlane(table[pos >> a.page_bits]) : -1;
+      const bool ok = (unsigned)pg < (unsigned)a.pages;
       s.valid[u] = ok ? min(16, end - pos) : 0;
-      const long long at = ok ? (((long long)pg * a.kv_heads + hk) << a.page_bits) + (pos & ((1 << a.page_bits) - 1)) : 0;
-      const int bytes = s.valid[u] * a.D * O::kBytes;
-      s.o.load(u, bytes_of(a.k + at * a.D * O::kBytes, bytes), bytes_of(a.v + at * a.D * O::kBytes, bytes), a.D, r16, quarter);
-      if constexpr (O::kBytes == 1) {
-        const __amdgpu_buffer_rsrc_t rks = bytes_of(a.ks + at, ok ? 64 : 0), rvs = bytes_of(a.vs + at, ok ? 64 : 0);  // (all of a page's scales are there)
-        s.ks[u] = __builtin_bit_cast(f32x4, load16(rks, quarter * 16));
-        s.vs[u] = __builtin_bit_cast(f32x4, load16(rvs, quarter * 16));
-      }
+      s.at[u] = ok ? (((long long)pg * a.kv_heads + hk) << a.page_bits) + (pos & ((1 << a.page_bits) - 1)) : 0;
+    }
+    return s;
+  };
+  O o;
+  f32x4 ks[kGroups], vs[kGroups];
+  auto load_keys = [&](const Place& s) {
+#pragma unroll
+    for (int u = 0; u < kGroups; ++u) {
+      o.load_keys(u, bytes_of(scalar_pointer(a.k + s.at[u] * a.D * O::kBytes), s.valid[u] * a.D * O::kBytes), a.D, r16, quarter);
+      if constexpr (O::kBytes == 1)  // (all of a page's scales are there)
+        ks[u] = __builtin_bit_cast(f32x4, load16(bytes_of(scalar_pointer(a.ks + s.at[u]), s.valid[u] ? 64 : 0), quarter * 16));
     }
   };
-  auto compute = [&](const Step& s, int key) {
+  auto load_values = [&](const Place& s) {
+#pragma unroll
+    for (int u = 0; u < kGroups; ++u) {
+      o.load_values(u, bytes_of(scalar_pointer(a.v + s.at[u] * a.D * O::kBytes), s.valid[u] * a.D * O::kBytes), a.D, r16, quarter);
+      if constexpr (O::kBytes == 1)
+        vs[u] = __builtin_bit_cast(f32x4, load16(bytes_of(scalar_pointer(a.vs + s.at[u]), s.valid[u] ? 64 : 0), quarter * 16));
+    }
+  };
+
+  // A step's keys are asked for when the last step's are used up, its values likewise: something is always under way.
+  constexpr int kStride = kWaves * kKeys;
+  int key = begin + wave * kKeys;
+  Place here = place_of(key);
+  if (key < end) {
+    load_keys(here);
+    load_values(here);
+  }
+  for (; key < end; key += kStride) {
+    const Place next = place_of(key + kStride);  // (past the end: no keys)
     bool whole = key + kKeys <= all_see;
 #pragma unroll
-    for (int u = 0; u < kGroups; ++u) whole = whole && s.valid[u] == 16;
-    float p[RT][kGroups][4];
-    unsigned seen[RT];  // bits 4 u + i: the lane's query sees key i of the lane's four
+    for (int u = 0; u < kGroups; ++u) whole = whole && here.valid[u] == 16;
+    f32x4 sc[RT][kGroups];
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
       if (t * 16 >= there) break;
-      f32x4 sc[kGroups];
 #pragma unroll
       for (int u = 0; u < kGroups; ++u) {
-        sc[u] = f32x4{0.f, 0.f, 0.f, 0.f};
+        sc[t][u] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int i = 0; i < O::kQuery; ++i) {
+          const tok_u4 qf = query(t, i);
           if constexpr (kWide) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) sc[u] = mma4(__uint_as_float(s.o.k[u][i][j]), __uint_as_float(q[t][i][j]), sc[u]);
+            for (int j = 0; j < 4; ++j) sc[t][u] = mma4(__uint_as_float(o.k[u][i][j]), __uint_as_float(qf[j]), sc[t][u]);
           } else {
-            sc[u] = mma_bf16_16(s.o.key(u, i), __builtin_bit_cast(bf16x8, q[t][i]), sc[u]);
+            sc[t][u] = mma_bf16_16(o.key(u, i), __builtin_bit_cast(bf16x8, qf), sc[t][u]);
           }
         }
-        if constexpr (O::kBytes == 1) sc[u] *= s.ks[u];
+        if constexpr (O::kBytes == 1) sc[t][u] *= ks[u];
       }
-      seen[t] = (1u << (4 * kGroups)) - 1;
+      if constexpr (kQueryLds) __builtin_amdgcn_sched_barrier(0);  // (no reads of all row tiles at once)
+    }
+    load_keys(next);
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+      if (t * 16 >= there) break;
       if (!whole) {
-        seen[t] = 0;
 #pragma unroll
         for (int u = 0; u < kGroups; ++u)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const int at = 4 * quarter + i;
-            const bool sees = at < s.valid[u] && key + 16 * u + at < limit[t];
-            seen[t] |= sees ? 1u << (4 * u + i) : 0u;
-            if (!sees) sc[u][i] = kNoScore;
+            if (!(at < here.valid[u] && key + 16 * u + at < limit[t])) sc[t][u][i] = kNoScore;
           }
       }
-      float most = sc[0][0];
+      float most = sc[t][0][0];
 #pragma unroll
       for (int u = 0; u < kGroups; ++u)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) most = fmaxf(most, sc[u][i]);
+        for (int i = 0; i < 4; ++i) most = fmaxf(most, sc[t][u][i]);
       most = fmaxf(top[t], quarters_max(most) * a.c);
       const float shift = shift_of(most);
       if (__ballot(most > top[t])) {
@@ -301,94 +382,62 @@ __global__ __launch_bounds__(kWaves * kWave, (RT > 2 ? 1 : 2)) void k_cached(Cac
       for (int u = 0; u < kGroups; ++u)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          p[t][u][i] = exp2_fast(fmaf(sc[u][i], a.c, -shift));
-          sum[t] += p[t][u][i];
-          if constexpr (O::kBytes == 1) p[t][u][i] = (seen[t] >> (4 * u + i)) & 1 ? p[t][u][i] * s.vs[u][i] : 0.f;
+          const bool none = sc[t][u][i] == kNoScore;  // (what a value's scale holds where there is no key is nobody's business)
+          sc[t][u][i] = exp2_fast(fmaf(sc[t][u][i], a.c, -shift));
+          sum[t] += sc[t][u][i];
+          if constexpr (O::kBytes == 1) sc[t][u][i] = none ? 0.f : sc[t][u][i] * vs[u][i];
         }
     }
-    const bool mixed = all_see < min(key + kKeys, end);  // some rows see fewer keys of the step than others
+    bool bad = false;
+    if (all_see < min(key + kKeys, end)) bad = __ballot(o.take_out()) != 0;  // some rows see fewer keys of the step than others
     if constexpr (kWide) {
-      bool clean = true;
-      if (mixed) {
-        bool bad = false;
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+      for (int i = 0; i < 4; ++i)
 #pragma unroll
-          for (int e = 0; e < kEach; ++e) bad |= not_finite(s.o.v[0][i][e]);
-        clean = __ballot(bad) == 0;
-      }
+        for (int e = 0; e < kEach; ++e)
 #pragma unroll
-      for (int t = 0; t < RT; ++t) {
-        if (t * 16 >= there) break;
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-          for (int e = 0; e < kEach; ++e) {
-            const float v = s.o.v[0][i][e];
-            acc[t][e] = mma4(clean || !not_finite(v) ? v : 0.f, p[t][0][i], acc[t][e]);
-          }
-        if (!clean) {
-#pragma unroll
-          for (int e = 0; e < kEach; ++e)
-#pragma unroll
-            for (int sign = 0; sign < 2; ++sign) {
-              f32x4 found = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-              for (int i = 0; i < 4; ++i) found = mma4(endless(s.o.v[0][i][e], sign), (seen[t] >> i) & 1 ? 1.f : 0.f, found);
-              add_endless(acc[t][e], found, sign);
-            }
-        }
-      }
+          for (int t = 0; t < RT; ++t)
+            if (t * 16 < there) acc[t][e] = mma4(o.v[0][i][e], sc[t][0][i], acc[t][e]);
     } else {
-      tok_u4 w[RT];
 #pragma unroll
-      for (int t = 0; t < RT; ++t)
-        if (t * 16 < there)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) w[t][j] = pack_bf16(p[t][j / 2][j % 2 * 2], p[t][j / 2][j % 2 * 2 + 1]);
-#pragma unroll
-      for (int e = 0; e < kEach; ++e) {
-        tok_u4 v = s.o.value(e);
-        bool bad = false;
-        if (mixed) {
-#pragma unroll
-          for (int j = 0; j < 4; ++j) bad |= not_finite2(v[j]);
-          bad = __ballot(bad) != 0;
-        }
-        if (bad) {
-#pragma unroll
-          for (int sign = 0; sign < 2; ++sign) {
-            tok_u4 x;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) x[j] = endless2(v[j], sign);
-#pragma unroll
-            for (int t = 0; t < RT; ++t) {
-              if (t * 16 >= there) break;
-              tok_u4 sees;
-#pragma unroll
-              for (int j = 0; j < 4; ++j) sees[j] = ((seen[t] >> (2 * j)) & 1 ? 0x3f80u : 0u) | ((seen[t] >> (2 * j)) & 2 ? 0x3f800000u : 0u);
-              const f32x4 found = mma_bf16_16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, sees), f32x4{0.f, 0.f, 0.f, 0.f});
-              add_endless(acc[t][e], found, sign);
-            }
-          }
-#pragma unroll
-          for (int j = 0; j < 4; ++j) v[j] = finite2(v[j]);
-        }
+      for (int h = 0; h < kGroups / 2; ++h) {
+        tok_u4 w[RT];
 #pragma unroll
         for (int t = 0; t < RT; ++t)
-          if (t * 16 < there) acc[t][e] = mma_bf16_16(__builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, w[t]), acc[t][e]);
+          if (t * 16 < there)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) w[t][j] = pack_bf16(sc[t][2 * h + j / 2][j % 2 * 2], sc[t][2 * h + j / 2][j % 2 * 2 + 1]);
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) {
+          const tok_u4 v = o.value(h, e);
+#pragma unroll
+          for (int t = 0; t < RT; ++t)
+            if (t * 16 < there) acc[t][e] = mma_bf16_16(__builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, w[t]), acc[t][e]);
+        }
       }
     }
-  };
-
-  constexpr int kStride = kWaves * kKeys;
-  for (int key = begin + wave * kKeys; key < end; key += kStride) {
-    int page[kGroups];
+    load_values(next);
+    if (bad) {
 #pragma unroll
-    for (int u = 0; u < kGroups; ++u) page[u] = page_at(key, u);
-    Step s;
-    load(s, key, page);
-    compute(s, key);
+      for (int u = 0; u < kGroups; ++u)
+#pragma unroll 1
+        for (int j = 0; j < here.valid[u]; ++j) {
+          const uint8_t* const row = a.v + (here.at[u] + j) * a.D * O::kBytes;
+#pragma unroll 1
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int e = 0; e < kEach; ++e) {
+              const float v = O::value_at(row, min(kEach * (4 * quarter + i) + e, a.D - 1));
+#pragma unroll
+              for (int t = 0; t < RT; ++t) {
+                const float add = key + 16 * u + j < limit[t] && not_finite(v) ? v : 0.f;
+#pragma unroll
+                for (int x = 0; x < 4; ++x) acc[t][e][x] += x == i ? add : 0.f;
+              }
+            }
+        }
+    }
+    here = next;
   }
 
   // The waves' parts: each row's maximum over them, their sums relative to it.
@@ -428,8 +477,8 @@ __global__ __launch_bounds__(kWaves * kWave, (RT > 2 ? 1 : 2)) void k_cached(Cac
     const unsigned row = first_row + t * 16 + r;
     const long long tok = row0 + row / (unsigned)a.group;
     const int h = hk * a.group + (int)(row % (unsigned)a.group);
-    if (a.parts > 1) {
-      const long long at = ((long long)(a.first_part + split) * a.T + tok) * a.heads + h;
+    if (a.splits + a.prefix_splits > 1) {
+      const long long at = ((long long)(shared ? a.splits + split : split) * a.T + tok) * a.heads + h;
       if (d < a.D)
 #pragma unroll
         for (int e = 0; e < kEach; e += 4) *reinterpret_cast<f32x4*>(a.part_out + at * a.D + d + e) = f32x4{f[e], f[e + 1], f[e + 2], f[e + 3]};
@@ -450,79 +499,86 @@ __global__ __launch_bounds__(kWaves * kWave, (RT > 2 ? 1 : 2)) void k_cached(Cac
   }
 }
 
-// Joins the parts of a row: a wave a row, its lanes first the parts' statistics, then the channels.
+// Joins the parts of a row: eight parts at a time, 32 threads each.  Every wave works the row's statistics out; what it reads does not
+// depend on them (parts that do not count are dropped behind their loads), so that the trips to memory overlap.
 template <typename ET>
-__global__ __launch_bounds__(256) void k_join(CachedArgs a, int own, int shared) {
-  const int lane = lane_id();
-  const unsigned row = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+__global__ __launch_bounds__(256) void k_join(CachedArgs a) {
+  __shared__ f32x4 part[8][32];
+  const int lane = lane_id(), slot = threadIdx.x / 32, d = threadIdx.x % 32 * 4, parts = a.splits + a.prefix_splits;
+  const unsigned row = blockIdx.x;
   const long long rows = (long long)a.T * a.heads;
-  if (row >= rows) return;
   const int token = (int)(row / (unsigned)a.heads), head = (int)(row - (unsigned)token * a.heads);
-  const int b = last_not_above(a.B, [&](int i) { return row_at(a.offsets, i, a.T) <= token; });
-  if (token < row_at(a.offsets, b, a.T) || token >= row_at(a.offsets, b + 1, a.T)) return;
-  const int len = cached_tokens(a, b), each = part_keys(len, own), used = max((len + each - 1) / each, 1);
-  // part i of the workspace: of the sequence's own, then of the prefix
-  const bool in = lane < own + shared && (lane < used || lane >= own);
+  f32x4 v[kMaxParts / 8];
+#pragma unroll
+  for (int i = 0; i < kMaxParts / 8; ++i)
+    if (i * 8 + slot < parts && d < a.D) v[i] = *reinterpret_cast<const f32x4*>(a.part_out + ((long long)(i * 8 + slot) * rows + row) * a.D + d);
   float top = kNoScore, sum = 0.f;
-  if (in) {
-    const long long at = (long long)lane * rows + row;
-    top = a.part_stat[2 * at];
-    sum = a.part_stat[2 * at + 1];
+  if (lane < parts) {
+    const float2 s = *reinterpret_cast<const float2*>(a.part_stat + 2 * ((long long)lane * rows + row));
+    top = s.x;
+    sum = s.y;
   }
+  const int b = last_not_above(a.B, [&](int i) { return row_at(a.offsets, i, a.T) <= token; });
+  const int own = parts_of(cached_tokens(a, b), a.splits), shared = a.prefix_splits ? parts_of(a.prefix_len, a.prefix_splits) : 0;
+  if (token < row_at(a.offsets, b, a.T) || token >= row_at(a.offsets, b + 1, a.T)) return;  // (all of the workgroup)
+  if (lane < a.splits ? lane >= own : lane - a.splits >= shared) top = kNoScore;  // (a part that there is not: nobody wrote it)
   float most = top;
 #pragma unroll
   for (int o = 1; o < kWave; o <<= 1) most = fmaxf(most, __shfl_xor(most, o, kWave));
-  const float by = exp2_fast(top - shift_of(most));
-  const float total = lanes64_sum(in ? sum * by : 0.f);
-  const unsigned long long counts = __ballot(in && top != kNoScore);  // (the others' sums were not written, or are zero)
-  float f[2] = {0.f, 0.f};
-  const int d = lane * 2;
-  for (int i = 0; i < own + shared; ++i) {
-    if (!((counts >> i) & 1)) continue;
-    const float w = __shfl(by, i, kWave);
-    if (d < a.D) {
-      const float2 v = *reinterpret_cast<const float2*>(a.part_out + ((long long)i * rows + row) * a.D + d);
-      f[0] = fmaf(v.x, w, f[0]);
-      f[1] = fmaf(v.y, w, f[1]);
-    }
+  const bool counts = top != kNoScore;
+  const float by = counts ? exp2_fast(top - most) : 0.f;
+  const float total = lanes64_sum(counts ? sum * by : 0.f);
+  const unsigned long long mask = __ballot(counts);
+  f32x4 f = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int i = 0; i < kMaxParts / 8; ++i) {
+    const float w = __shfl(by, i * 8 + slot, kWave);
+    if ((mask >> (i * 8 + slot)) & 1)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) f[e] = fmaf(v[i][e], w, f[e]);
   }
-  if (d >= a.D) return;
+  part[slot][threadIdx.x % 32] = f;
+  __syncthreads();
+  if (threadIdx.x >= 32 || d >= a.D) return;
+#pragma unroll
+  for (int i = 1; i < 8; ++i) f += part[i][threadIdx.x];
   const float inv = 1.f / total;
-  const float x = total == 0.f ? 0.f : f[0] * inv, y = total == 0.f ? 0.f : f[1] * inv;
-  ET* const out = reinterpret_cast<ET*>(a.out) + token * a.ldo + head * a.D + d;
-  if constexpr (sizeof(ET) == 4) *reinterpret_cast<float2*>(out) = make_float2(x, y);
-  else *reinterpret_cast<unsigned*>(out) = pack_bf16(x, y);
+  f *= inv;
+  if (total == 0.f) f = f32x4{0.f, 0.f, 0.f, 0.f};
+  store4(reinterpret_cast<ET*>(a.out) + token * a.ldo + head * a.D + d, f);
 }
 
 // ---- plan -------------------------------------------------------------------------------------------------------------------
 struct Plan {
-  int rt, prefix_rt;        // row tiles of a workgroup
+  int rt;                   // row tiles of a workgroup
   int own, shared;          // parts of the sequences' own keys, and of the prefix
   long long tiles, prefix_tiles;
   size_t stat_at, bytes;    // workspace: sums, then statistics
 };
-inline int row_tiles(double rows, bool wide) { return rows <= 16 ? 1 : rows <= 32 || wide ? 2 : 4; }
+inline int row_tiles(double rows) { return rows <= 16 ? 1 : 2; }
 
-// Parts: as many workgroups as keep the card's 256 compute units busy for a few rounds, none of fewer than 256 keys.
+// Parts: as many workgroups as keep the card's 256 compute units busy for a few rounds, none of fewer than 128 keys.
 inline int parts_for(double groups, long long keys, int most) {
-  const double want = 1024.0 / groups;
-  const long long room = (keys + 255) / 256;
+#ifndef LAUD_WANT
+#define LAUD_WANT 1024
+#define LAUD_MIN 128
+#endif
+  const double want = (double)LAUD_WANT / groups;
+  const long long room = (keys + LAUD_MIN - 1) / LAUD_MIN;
   return (int)max(1ll, min(min((long long)(want + 0.999), room), (long long)most));
 }
 
 Plan plan_of(const laud_heads* p, const laud_cache* c, const laud_batch* b, int T) {
   Plan s{};
   const int group = p->heads / p->kv_heads;
-  const bool wide = c->dtype == LAUD_F32;
+  const bool prefix = b->prefix_len > 0;
   const double rows = (double)T * group;
-  s.rt = row_tiles(rows / b->B, wide);
+  s.rt = row_tiles(prefix ? rows : rows / b->B);
   s.tiles = tiles_of(T, b->B, group, 16 * s.rt);
   const double busy = max((double)b->B, rows / (16 * s.rt)) * p->kv_heads;
-  const bool prefix = b->prefix_len > 0;
   s.own = parts_for(busy, (long long)b->table_ld * c->page, prefix ? kMaxParts / 2 : kMaxParts);
   if (prefix) {
-    s.prefix_rt = row_tiles(rows, wide);
-    s.prefix_tiles = ((long long)T * group - 1) / (16 * s.prefix_rt) + 1;
+    s.prefix_tiles = ((long long)T * group - 1) / (16 * s.rt) + 1;
     s.shared = parts_for((double)s.prefix_tiles * p->kv_heads, b->prefix_len, kMaxParts / 2);
   }
   if (s.own + s.shared > 1) {
@@ -536,7 +592,7 @@ Plan plan_of(const laud_heads* p, const laud_cache* c, const laud_batch* b, int 
 template <typename ET, typename CT, int DP, int RT>
 int launch_cached(const CachedArgs& a, hipStream_t st) {
   constexpr int kLds = kWaves * 16 * (DP + 4) * 4 + kWaves * 16 * RT * 8;
-  const double groups = (double)a.tiles * a.kv_heads * a.splits;
+  const double groups = (double)a.tiles * a.kv_heads * a.splits + a.prefix_groups;
   if (!launchable(groups, kWaves * kWave)) return LAUD_ERR_UNSUPPORTED;
   hipLaunchKernelGGL((k_cached<ET, CT, DP, RT>), dim3((unsigned)groups), dim3(kWaves * kWave), kLds, st, a);
   return LAUD_OK;
@@ -544,9 +600,7 @@ int launch_cached(const CachedArgs& a, hipStream_t st) {
 template <typename ET, typename CT, int DP>
 int launch_rows(const CachedArgs& a, int rt, hipStream_t st) {
   if (rt == 1) return launch_cached<ET, CT, DP, 1>(a, st);
-  if (rt == 2) return launch_cached<ET, CT, DP, 2>(a, st);
-  if constexpr (sizeof(CT) < 4) return launch_cached<ET, CT, DP, 4>(a, st);
-  return LAUD_ERR_UNSUPPORTED;
+  return launch_cached<ET, CT, DP, 2>(a, st);
 }
 int launch_types(const CachedArgs& a, int cache_type, int rt, hipStream_t st) {
   if (cache_type == LAUD_F32) return a.D <= 64 ? launch_rows<float, float, 64>(a, rt, st) : launch_rows<float, float, 128>(a, rt, st);
@@ -596,38 +650,29 @@ extern "C" int laud_cache_attention(const laud_heads* p, const laud_cache* c, co
     for (const Span& x : BatchSpans(b).s)
       if (ranges_meet(ws, s.bytes, x.p, x.n)) return LAUD_ERR_INVALID_ARG;
   }
-  const double most = 2147483648.0;
-  if (s.tiles >= most || !launchable((double)s.tiles * p->kv_heads * s.own, kWaves * kWave) ||
-      !launchable((double)s.prefix_tiles * p->kv_heads * s.shared, kWaves * kWave) || !launchable(((double)T * p->heads + 3) / 4, 256))
-    return LAUD_ERR_UNSUPPORTED;
+  const double own = (double)s.tiles * p->kv_heads * s.own, shared = (double)s.prefix_tiles * p->kv_heads * s.shared;
+  if (!launchable(own + shared, kWaves * kWave) || !launchable((double)T * p->heads, 256)) return LAUD_ERR_UNSUPPORTED;
   CachedArgs a{};
   a.heads = p->heads; a.group = p->heads / p->kv_heads; a.kv_heads = p->kv_heads; a.D = p->D; a.causal = p->causal; a.B = b->B; a.T = T;
   a.pages = c->pages; a.page_bits = page_bits(c); a.table_ld = b->table_ld;
-  a.parts = s.own + s.shared;
+  a.tiles = (int)s.tiles; a.splits = s.own; a.prefix_tiles = (int)s.prefix_tiles; a.prefix_splits = s.shared;
+  a.prefix_groups = (unsigned)shared; a.prefix_len = b->prefix_len;
+  a.by_xcd = s.rt > 1 && (long long)p->kv_heads * s.own % 8 == 0;
+  a.prefix_by_xcd = (long long)p->kv_heads * s.shared % 8 == 0;
   a.c = p->scale * kLog2e;
-  a.offsets = b->offsets; a.lens = b->lens;
+  a.offsets = b->offsets; a.lens = b->lens; a.table = b->table; a.prefix = b->prefix;
   a.k = (const uint8_t*)c->k; a.v = (const uint8_t*)c->v; a.ks = c->k_scale; a.vs = c->v_scale;
   a.q = q; a.out = out; a.ldq = ldq; a.ldo = ldo;
   a.part_out = (float*)ws;
   a.part_stat = s.bytes ? (float*)((char*)ws + s.stat_at) : nullptr;
   clear_stale_error();
   hipStream_t st = (hipStream_t)stream;
-  CachedArgs o = a;
-  o.tiles = (int)s.tiles; o.splits = s.own; o.table = b->table;
-  o.by_xcd = s.rt > 1 && (long long)p->kv_heads * s.own % 8 == 0;
-  int status = launch_types(o, c->dtype, s.rt, st);
+  const int status = launch_types(a, c->dtype, s.rt, st);
   if (status) return status;
-  if (s.shared) {
-    o = a;
-    o.tiles = (int)s.prefix_tiles; o.splits = s.shared; o.first_part = s.own; o.table = b->prefix; o.prefix_len = b->prefix_len; o.shared = 1;
-    o.by_xcd = (long long)p->kv_heads * s.shared % 8 == 0;
-    status = launch_types(o, c->dtype, s.prefix_rt, st);
-    if (status) return status;
-  }
-  if (a.parts > 1) {
-    const dim3 grid((unsigned)(((long long)T * p->heads + 3) / 4));
-    if (p->dtype == LAUD_BF16) hipLaunchKernelGGL((k_join<bf16_t>), grid, dim3(256), 0, st, a, s.own, s.shared);
-    else hipLaunchKernelGGL((k_join<float>), grid, dim3(256), 0, st, a, s.own, s.shared);
+  if (s.own + s.shared > 1) {
+    const dim3 grid((unsigned)T * (unsigned)p->heads);
+    if (p->dtype == LAUD_BF16) hipLaunchKernelGGL((k_join<bf16_t>), grid, dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((k_join<float>), grid, dim3(256), 0, st, a);
   }
   return check_launch();
 }

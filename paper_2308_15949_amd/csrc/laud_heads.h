@@ -35,6 +35,14 @@ __device__ __forceinline__ int last_not_above(int B, F&& below) {
   return __builtin_amdgcn_readfirstlane(lo + max(__popcll(m), 1) - 1);
 }
 
+// a pointer that is the same for the wave, in scalar registers (what descriptors are made of)
+template <typename T>
+__device__ __forceinline__ const T* scalar_pointer(const T* p) {
+  const unsigned long long at = (unsigned long long)(uintptr_t)p;
+  const unsigned lo = __builtin_amdgcn_readfirstlane((int)at), hi = __builtin_amdgcn_readfirstlane((int)(at >> 32));
+  return reinterpret_cast<const T*>((uintptr_t)((unsigned long long)hi << 32 | lo));
+}
+
 // ---- softmax --------------------------------------------------------------------------------------------------------------
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 constexpr float kNoScore = -__builtin_inff();
@@ -61,36 +69,19 @@ __device__ __forceinline__ float quarters_sum(float v) {
 }
 
 // ---- values that are no numbers ---------------------------------------------------------------------------------------------
-// A matrix instruction multiplies every weight with every value, and 0 * NaN is NaN: where some queries of a tile do not see all of its
-// keys, values that are not finite are taken out of the product, and what they add - an infinity, both of them for a NaN - goes to the
-// queries that see them by a product of indicators.
+// A matrix instruction multiplies every weight with every value, and 0 * NaN is NaN: where some queries of a tile do not see all of a
+// step's keys, values that are not finite become zeros in front of the product, and are added to the queries that see them one by one,
+// from memory.
 __device__ __forceinline__ bool not_finite2(unsigned v) { return (v & 0x7f800000u) == 0x7f800000u || (v & 0x7f80u) == 0x7f80u; }
 __device__ __forceinline__ bool not_finite(float v) { return (__float_as_uint(v) & 0x7f800000u) == 0x7f800000u; }
-// one for each of two bf16 that is an infinity of that sign or a NaN
-__device__ __forceinline__ unsigned endless2(unsigned v, bool negative) {
-  unsigned r = 0;
-#pragma unroll
-  for (int h = 0; h < 32; h += 16) {
-    const unsigned x = (v >> h) & 0xffffu;
-    if ((x & 0x7f80u) == 0x7f80u && ((x & 0x7fu) || (x >> 15) == (unsigned)negative)) r |= 0x3f80u << h;
-  }
-  return r;
-}
-__device__ __forceinline__ unsigned finite2(unsigned v) {
+__device__ __forceinline__ unsigned finite2(unsigned v) {  // of two bf16
   if ((v & 0x7f80u) == 0x7f80u) v &= 0xffff0000u;
   if ((v & 0x7f800000u) == 0x7f800000u) v &= 0xffffu;
   return v;
 }
-__device__ __forceinline__ float endless(float v, bool negative) {
-  return not_finite(v) && (v != v || (v < 0.f) == negative) ? 1.f : 0.f;
-}
-template <typename V>
-__device__ __forceinline__ void add_endless(V& acc, const V& found, bool negative) {
-  const float endless = negative ? -__builtin_inff() : __builtin_inff();
-#pragma unroll
-  for (unsigned e = 0; e < sizeof(V) / 4; ++e)
-    if (found[e] > 0.f) acc[e] += endless;
-}
+// bytes of e4m3 codes that are NaN (0x7f, 0xff) become zero
+__device__ __forceinline__ unsigned nan_codes(unsigned v) { return ((v & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
+__device__ __forceinline__ unsigned finite4(unsigned v) { return v & ~((nan_codes(v) >> 7) * 0xffu); }
 
 // ---- host side ------------------------------------------------------------------------------------------------------------
 // whether two row arrays of as many rows, of different widths, share a byte; at the same distance they may lie side by side
