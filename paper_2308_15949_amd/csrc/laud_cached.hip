@@ -21,9 +21,6 @@ struct CachedArgs {
   int64_t ldq, ldo;
 };
 
-#ifndef LAUD_G8
-#define LAUD_G8 2
-#endif
 constexpr int kWaves = 4, kMaxParts = 64, kPartStep = 128;
 // Keys of a part: the same for every tile of a sequence, so that whoever joins the parts knows how many there are.
 __device__ __forceinline__ int part_keys(int len, int splits) {
@@ -189,11 +186,14 @@ struct Operands<float, DP, GROUPS> {
 
 __device__ __forceinline__ f32x4 mma4(float a, float b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0); }
 
+// the values of four lanes in a row, in each of them
+__device__ __forceinline__ f32x4 of_four(float v) { return f32x4{dpp_movf<0x00>(v), dpp_movf<0x55>(v), dpp_movf<0xAA>(v), dpp_movf<0xFF>(v)}; }
+
 // Sixteen query rows a row tile (RT of them a workgroup): the tokens of a sequence times the query heads of a key head, so that a key is
 // fetched once for all of them.  Four waves share a part's keys, each takes every fourth step of 16 or 32 keys; their sums are joined through LDS.
 template <typename ET, typename CT, int DP, int RT>
 __global__ __launch_bounds__(kWaves * kWave, 2) void k_cached(CachedArgs a) {
-  typedef Operands<CT, DP, (sizeof(CT) == 4 ? 1 : sizeof(CT) == 1 && RT == 1 ? LAUD_G8 : 2)> O;
+  typedef Operands<CT, DP, (sizeof(CT) == 4 ? 1 : 2)> O;
   constexpr bool kWide = sizeof(CT) == 4;  // float32 instructions
   constexpr int kGroups = O::kGroups, kKeys = 16 * kGroups, kRows = 16 * RT, kEach = O::kEach, kLdRow = DP + 4;
   extern __shared__ __align__(16) unsigned char lds[];
@@ -299,13 +299,13 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void k_cached(CachedArgs a) {
     return s;
   };
   O o;
-  f32x4 ks[kGroups], vs[kGroups];
+  float ks[kGroups], vs[kGroups];  // scales: of four lanes in a row each has one of their four keys'
   auto load_keys = [&](const Place& s) {
 #pragma unroll
     for (int u = 0; u < kGroups; ++u) {
       o.load_keys(u, bytes_of(scalar_pointer(a.k + s.at[u] * a.D * O::kBytes), s.valid[u] * a.D * O::kBytes), a.D, r16, quarter);
       if constexpr (O::kBytes == 1)  // (all of a page's scales are there)
-        ks[u] = __builtin_bit_cast(f32x4, load16(bytes_of(scalar_pointer(a.ks + s.at[u]), s.valid[u] ? 64 : 0), quarter * 16));
+        ks[u] = __uint_as_float(load4(bytes_of(scalar_pointer(a.ks + s.at[u]), s.valid[u] ? 64 : 0), quarter * 16 + r16 % 4 * 4));
     }
   };
   auto load_values = [&](const Place& s) {
@@ -313,7 +313,7 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void k_cached(CachedArgs a) {
     for (int u = 0; u < kGroups; ++u) {
       o.load_values(u, bytes_of(scalar_pointer(a.v + s.at[u] * a.D * O::kBytes), s.valid[u] * a.D * O::kBytes), a.D, r16, quarter);
       if constexpr (O::kBytes == 1)
-        vs[u] = __builtin_bit_cast(f32x4, load16(bytes_of(scalar_pointer(a.vs + s.at[u]), s.valid[u] ? 64 : 0), quarter * 16));
+        vs[u] = __uint_as_float(load4(bytes_of(scalar_pointer(a.vs + s.at[u]), s.valid[u] ? 64 : 0), quarter * 16 + r16 % 4 * 4));
     }
   };
 
@@ -347,7 +347,7 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void k_cached(CachedArgs a) {
             sc[t][u] = mma_bf16_16(o.key(u, i), __builtin_bit_cast(bf16x8, qf), sc[t][u]);
           }
         }
-        if constexpr (O::kBytes == 1) sc[t][u] *= ks[u];
+        if constexpr (O::kBytes == 1) sc[t][u] *= of_four(ks[u]);
       }
       if constexpr (kQueryLds) __builtin_amdgcn_sched_barrier(0);  // (no reads of all row tiles at once)
     }
@@ -379,14 +379,17 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void k_cached(CachedArgs a) {
         top[t] = most;
       }
 #pragma unroll
-      for (int u = 0; u < kGroups; ++u)
+      for (int u = 0; u < kGroups; ++u) {
+        f32x4 by = {1.f, 1.f, 1.f, 1.f};
+        if constexpr (O::kBytes == 1) by = of_four(vs[u]);  // (all lanes take part)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const bool none = sc[t][u][i] == kNoScore;  // (what a value's scale holds where there is no key is nobody's business)
           sc[t][u][i] = exp2_fast(fmaf(sc[t][u][i], a.c, -shift));
           sum[t] += sc[t][u][i];
-          if constexpr (O::kBytes == 1) sc[t][u][i] = none ? 0.f : sc[t][u][i] * vs[u][i];
+          if constexpr (O::kBytes == 1) sc[t][u][i] = none ? 0.f : sc[t][u][i] * by[i];
         }
+      }
     }
     bool bad = false;
     if (all_see < min(key + kKeys, end)) bad = __ballot(o.take_out()) != 0;  // some rows see fewer keys of the step than others
@@ -559,12 +562,8 @@ inline int row_tiles(double rows) { return rows <= 16 ? 1 : 2; }
 
 // Parts: as many workgroups as keep the card's 256 compute units busy for a few rounds, none of fewer than 128 keys.
 inline int parts_for(double groups, long long keys, int most) {
-#ifndef LAUD_WANT
-#define LAUD_WANT 1024
-#define LAUD_MIN 128
-#endif
-  const double want = (double)LAUD_WANT / groups;
-  const long long room = (keys + LAUD_MIN - 1) / LAUD_MIN;
+  const double want = 1024.0 / groups;
+  const long long room = (keys + kPartStep - 1) / kPartStep;
   return (int)max(1ll, min(min((long long)(want + 0.999), room), (long long)most));
 }
 
