@@ -24,14 +24,15 @@ struct AttendArgs {
 // (lane half h: 4 h .. 4 h + 3 and those 8 behind), and the values are read to match - transposed on their way from LDS where they are
 // bf16.
 constexpr int kMaskWords = 128;  // 64 keys' bits each: two windows of 4096 keys
-template <typename ET, int DP, int KK, int NS>
+template <typename ET, int DC, int KK>
 struct Tile {
+  static constexpr int DP = DC <= 64 ? 64 : 128;  // channels of a row in LDS; the first DC of them are multiplied
   static constexpr bool kHalf = sizeof(ET) == 2;
   static constexpr int kRow = DP * (int)sizeof(ET);  // bytes of a row in LDS
   static constexpr int kChunks = kRow / 16;
   static constexpr int kPart = KK * kRow;  // keys, or values, of a stage
-  static constexpr int kStage = 2 * kPart, kGroup = NS * kStage;
-  static constexpr int kSums = DP / 32 * 4 * kWave;  // of a wave's 32 queries, in f32x4
+  static constexpr int kGroup = 4 * kPart;  // two stages of keys, two of values
+  static constexpr int kSums = DC / 32 * 4 * kWave;  // of a wave's 32 queries, in f32x4
   // LDS of a workgroup: the groups' stages, in whose place all groups' but the first's sums, maxima and sums of weights come
   static constexpr int bytes(int NW, int KG) {
     const int stages = KG * kGroup, sums = (KG - 1) * NW * (kSums * 16 + 2 * kWave * 4);
@@ -61,11 +62,12 @@ __device__ __forceinline__ f32x16 mma32(float a, float b, const f32x16& c) { ret
 // 2^8 instead of 1, which costs float32 nothing, and most steps are spared the scaling of all sums (64 instructions).
 constexpr float kSlack = 8.f;
 
-template <typename ET, int DP, int NW, int KG, int KK, int NS>
+template <typename ET, int DC, int NW, int KG, int KK>
 __global__ __launch_bounds__(NW * KG * kWave, 2) void k_attend(AttendArgs a) {
-  typedef Tile<ET, DP, KK, NS> L;
+  typedef Tile<ET, DC, KK> L;
+  constexpr int DP = L::DP;
   constexpr bool kHalf = L::kHalf;
-  constexpr int kBlocks = KK / 32, kRows = NW * 32, kDt = DP / 32, kEb = (int)sizeof(ET);
+  constexpr int kBlocks = KK / 32, kRows = NW * 32, kDt = DC / 32, kEb = (int)sizeof(ET);
   constexpr int kLanesRow = L::kChunks, kRowsLoad = kWave / kLanesRow;  // lanes that bring a row, rows of an LDS-direct load
   constexpr int kLoads = L::kPart / 1024 / NW;                          // loads a wave of a step's keys
   static_assert(kLoads * NW * 1024 == L::kPart, "loads shared evenly");
@@ -76,25 +78,24 @@ __global__ __launch_bounds__(NW * KG * kWave, 2) void k_attend(AttendArgs a) {
 
   // Workgroups go round-robin over the eight XCDs: each takes a run of heads, whose keys its L2 then serves, the tiles of several heads
   // side by side; the last tiles, which see the most keys, first.
-  const long long total = (long long)a.heads * a.tiles, per = (total + 7) / 8;
-  const long long id = (long long)(blockIdx.x % 8) * per + blockIdx.x / 8;
+  const unsigned total = (unsigned)a.heads * (unsigned)a.tiles, per = (total + 7) / 8;  // (a launch has less than 2^32 threads)
+  const unsigned id = blockIdx.x % 8 * per + blockIdx.x / 8;
   if (blockIdx.x / 8 >= per || id >= total) return;
-  const int band = a.heads % 8 == 0 ? a.heads / 8 : 1;
-  const long long in_band = id % ((long long)band * a.tiles);
-  const int head = (int)(id / ((long long)band * a.tiles)) * band + (int)(in_band % band);
-  const long long tile = a.tiles - 1 - in_band / band;
+  const unsigned band = a.heads % 8 == 0 ? a.heads / 8 : 1, in_band = id % (band * a.tiles);
+  const int head = (int)(id / (band * a.tiles) * band + in_band % band), tile = a.tiles - 1 - (int)(in_band / band);
   const int b = last_not_above(a.B, [&](int i) { return first_tile(a.offsets, i, a.T, 1, kRows) <= tile; });
-  const int row0 = row_at(a.offsets, b, a.T), n = row_at(a.offsets, b + 1, a.T) - row0;  // (n may be negative: no rows)
+  const int row0 = __builtin_amdgcn_readfirstlane(row_at(a.offsets, b, a.T));
+  const int n = __builtin_amdgcn_readfirstlane(row_at(a.offsets, b + 1, a.T)) - row0;  // (may be negative: no rows)
   const long long q_first = (tile - first_tile(a.offsets, b, a.T, 1, kRows)) * kRows;
   if (q_first < 0 || q_first >= n) return;
-  const int q0 = (int)q_first, qw = q0 + wave * 32, qr = qw + r32;  // the tile's first row in its sequence, the wave's, the lane's
+  const int q0 = __builtin_amdgcn_readfirstlane((int)q_first), qw = q0 + wave * 32, qr = qw + r32;  // the tile's first row in its sequence, the wave's, the lane's
   const int end = a.causal ? min(n, q0 + kRows) : n, steps = (end + KK - 1) / KK, rounds = (steps + KG - 1) / KG;
   const uint8_t* const keep = a.keep ? a.keep + row0 : nullptr;
   // rounds whose keys are all there, and seen by all queries of the tile
   const int whole_steps = keep ? 0 : (a.causal ? min(n, q0 + 1) : n) / KK, whole = whole_steps / KG;
 
   // the wave's queries, for good: lane = query, sixteen-byte pieces 2 s + half
-  constexpr int kPieces = L::kChunks / 2, kPer = 16 / kEb;
+  constexpr int kPieces = DC * kEb / 32, kPer = 16 / kEb;
   tok_u4 qf[kPieces];
   {
     const __amdgpu_buffer_rsrc_t rq = bytes_of(reinterpret_cast<const ET*>(a.q) + (row0 + (long long)q0) * a.ldq + head * a.D,
@@ -141,28 +142,30 @@ __global__ __launch_bounds__(NW * KG * kWave, 2) void k_attend(AttendArgs a) {
     vk[i] = ck < a.D ? (unsigned)(row * a.ldk + ck) * kEb : kOutside;
     vv[i] = cv < a.D ? (unsigned)(row * a.ldv + cv) * kEb : kOutside;
   }
-  const unsigned stage0 = group * L::kGroup;
-  auto request = [&](int stage_of, int step, bool all) {
-    const unsigned stage = __builtin_amdgcn_readfirstlane(stage0 + stage_of * L::kStage + wave * 1024);
-    const __amdgpu_buffer_rsrc_t rk = bytes_of(scalar_pointer(kp + (long long)step * KK * a.ldk), 0x7fffffff);
-    const __amdgpu_buffer_rsrc_t rv = bytes_of(scalar_pointer(vp + (long long)step * KK * a.ldv), 0x7fffffff);
+  const unsigned keys0 = group * L::kGroup, values0 = keys0 + 2 * L::kPart;  // the group's stages
+  auto request = [&](const ET* from, int64_t ld, const unsigned (&off)[kOffsets], unsigned to, bool all, unsigned long long there) {
+    const unsigned stage = __builtin_amdgcn_readfirstlane(to + wave * 1024);
+    const __amdgpu_buffer_rsrc_t r = bytes_of(scalar_pointer(from), 0x7fffffff);
     if (all) {
 #pragma unroll
-      for (int i = 0; i < kLoads; ++i) {
-        const unsigned skip = kSame ? (unsigned)i * NW * kRowsLoad * kEb : 0u;
-        dma16(rk, vk[kSame ? 0 : i], skip * (unsigned)a.ldk, stage + i * NW * 1024);
-        dma16(rv, vv[kSame ? 0 : i], skip * (unsigned)a.ldv, stage + L::kPart + i * NW * 1024);
-      }
+      for (int i = 0; i < kLoads; ++i)
+        dma16(r, off[kSame ? 0 : i], kSame ? (unsigned)(i * NW * kRowsLoad * kEb) * (unsigned)ld : 0u, stage + i * NW * 1024);
     } else {  // rows that are not there come as zeros (their weights are 0, and so are not 0 * NaN)
-      const unsigned long long there = rows_there(step);
 #pragma unroll
       for (int i = 0; i < kLoads; ++i) {
-        const unsigned skip = kSame ? (unsigned)i * NW * kRowsLoad * kEb : 0u, ok = vk[kSame ? 0 : i], ov = vv[kSame ? 0 : i];
+        const unsigned skip = kSame ? (unsigned)(i * NW * kRowsLoad * kEb) * (unsigned)ld : 0u, o = off[kSame ? 0 : i];
         const bool in = (unsigned)(there >> (i * NW + wave) * kRowsLoad) >> lane / kLanesRow & 1;
-        dma16(rk, in && ok != kOutside ? ok + skip * (unsigned)a.ldk : kOutside, 0, stage + i * NW * 1024);
-        dma16(rv, in && ov != kOutside ? ov + skip * (unsigned)a.ldv : kOutside, 0, stage + L::kPart + i * NW * 1024);
+        dma16(r, in && o != kOutside ? o + skip : kOutside, 0, stage + i * NW * 1024);
       }
     }
+  };
+  auto ask_keys = [&](int round) {
+    const int step = round * KG + group;
+    request(kp + (long long)step * KK * a.ldk, a.ldk, vk, keys0 + (round & 1) * L::kPart, round < whole, round < whole ? 0 : rows_there(step));
+  };
+  auto ask_values = [&](int round) {
+    const int step = round * KG + group;
+    request(vp + (long long)step * KK * a.ldv, a.ldv, vv, values0 + (round & 1) * L::kPart, round < whole, round < whole ? 0 : rows_there(step));
   };
 
   f32x16 acc[kDt];
@@ -179,48 +182,48 @@ __global__ __launch_bounds__(NW * KG * kWave, 2) void k_attend(AttendArgs a) {
     const int last = qr - k0;
     return last < 0 ? 0 : last >= 63 ? here : here & ((2ull << last) - 1);
   };
-  auto multiply = [&](auto some, int stage_of, int k0, unsigned long long here, bool asks) {
-    constexpr bool kSome = decltype(some)::value;  // some keys are not there, or not seen by every query
-    const unsigned char *ks = lds + stage0 + stage_of * L::kStage, *vs = ks + L::kPart;
-    // scores: key 32 u + 8 * (e / 4) + 4 * half + e % 4 with the lane's query
-    f32x16 s[kBlocks];
+  const int i16 = lane % 16, low = (lane / 16) % 2 * 2 + i16 % 4 / 2;
+  // keys 32 u + 8 * (e / 4) + 4 * half + e % 4 of a step with the lane's query
+  auto scores_part = [&](f32x16 (&s)[kBlocks], const unsigned char* ks, int i) {
+#pragma unroll
+    for (int u = 0; u < kBlocks; ++u) {
+      const tok_u4 kf = *reinterpret_cast<const tok_u4*>(ks + (u * 32 + r32) * L::kRow + (((2 * i + half) ^ L::key_swizzle(r32)) << 4));
+      if constexpr (kHalf) {
+        s[u] = mma32(kf, qf[i], s[u]);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s[u] = mma32(__uint_as_float(kf[j]), __uint_as_float(qf[i][j]), s[u]);
+      }
+    }
+  };
+  auto clear = [&](f32x16 (&s)[kBlocks]) {
 #pragma unroll
     for (int u = 0; u < kBlocks; ++u)
 #pragma unroll
       for (int e = 0; e < 16; ++e) s[u][e] = 0.f;
-    const unsigned char* const row = ks + r32 * L::kRow;
-    __builtin_amdgcn_s_setprio(1);
+  };
+  auto hide = [&](f32x16 (&s)[kBlocks], unsigned long long seen) {  // what the lane's query does not see
+    seen >>= 4 * half;
 #pragma unroll
-    for (int i = 0; i < kPieces; ++i)
+    for (int u = 0; u < kBlocks; ++u) {
+      const unsigned bits = (unsigned)(seen >> (32 * u));
 #pragma unroll
-      for (int u = 0; u < kBlocks; ++u) {
-        const tok_u4 kf = *reinterpret_cast<const tok_u4*>(row + u * 32 * L::kRow + (((2 * i + half) ^ L::key_swizzle(r32)) << 4));
-        if constexpr (kHalf) {
-          s[u] = mma32(kf, qf[i], s[u]);
-        } else {
-#pragma unroll
-          for (int j = 0; j < 4; ++j) s[u] = mma32(__uint_as_float(kf[j]), __uint_as_float(qf[i][j]), s[u]);
-        }
-      }
-    __builtin_amdgcn_s_setprio(0);
-    if constexpr (kSome) {
-      const unsigned long long seen = seen_of(k0, here, asks) >> (4 * half);
-#pragma unroll
-      for (int u = 0; u < kBlocks; ++u) {
-        const unsigned bits = (unsigned)(seen >> (32 * u));
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const unsigned m = (unsigned)((int)(bits << (31 - 8 * (e / 4) - e % 4)) >> 31);  // all bits, or none
-          s[u][e] = __uint_as_float((__float_as_uint(s[u][e]) & m) | (__float_as_uint(kNoScore) & ~m));
-        }
+      for (int e = 0; e < 16; ++e) {
+        const unsigned m = (unsigned)((int)(bits << (31 - 8 * (e / 4) - e % 4)) >> 31);  // all bits, or none
+        s[u][e] = __uint_as_float((__float_as_uint(s[u][e]) & m) | (__float_as_uint(kNoScore) & ~m));
       }
     }
-    float most = s[0][0];
+  };
+  // whether a score has grown past the maximum that the sums are relative to
+  auto most_of = [&](const f32x16 (&s)[kBlocks]) {
+    float most[2] = {s[0][0], s[0][1]};
 #pragma unroll
     for (int u = 0; u < kBlocks; ++u)
 #pragma unroll
-      for (int e = 0; e < 16; ++e) most = fmaxf(most, s[u][e]);
-    most = other_half_max(most) * a.c;
+      for (int e = 0; e < 16; ++e) most[e % 2] = fmaxf(most[e % 2], s[u][e]);
+    return other_half_max(fmaxf(most[0], most[1])) * a.c;
+  };
+  auto raise = [&](float most) {
     if (__ballot(most > top + kSlack)) {  // (the first score: more than -infinity)
       most = fmaxf(top, most);
       const float shrink = exp2_fast(top - shift_of(most));
@@ -231,48 +234,13 @@ __global__ __launch_bounds__(NW * KG * kWave, 2) void k_attend(AttendArgs a) {
         for (int e = 0; e < 16; ++e) acc[t][e] *= shrink;
       top = most;
     }
-    const float shift = shift_of(top);
-#pragma unroll
-    for (int u = 0; u < kBlocks; ++u)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        s[u][e] = exp2_fast(fmaf(s[u][e], a.c, -shift));
-        sum += s[u][e];
-      }
-
-    // out^T += values^T * weights
-    __builtin_amdgcn_s_setprio(1);
-    if constexpr (kHalf) {
-      tok_u4 w[kBlocks * 2];
-#pragma unroll
-      for (int t = 0; t < kBlocks * 2; ++t)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) w[t][j] = pack_bf16(s[t / 2][8 * (t % 2) + 2 * j], s[t / 2][8 * (t % 2) + 2 * j + 1]);
-      const int i16 = lane % 16, low = (lane / 16) % 2 * 2 + i16 % 4 / 2;
-      const unsigned char* const from = vs + (4 * half + i16 / 4) * L::kRow + i16 % 2 * 8;
-#pragma unroll
-      for (int t = 0; t < kBlocks * 2; ++t)
-#pragma unroll
-        for (int dt = 0; dt < kDt; ++dt) {
-          const unsigned char* const at = from + 16 * t * L::kRow + (((4 * dt + low) ^ L::value_swizzle(i16 / 4)) << 4);
-          const tok_u2 lo = read_transposed(at), hi = read_transposed(at + 8 * L::kRow);
-          acc[dt] = mma32(tok_u4{lo[0], lo[1], hi[0], hi[1]}, w[t], acc[dt]);
-        }
-    } else {
-      const float* const from = reinterpret_cast<const float*>(vs) + 4 * half * DP + r32;
-#pragma unroll
-      for (int e = 0; e < 16; ++e)
-#pragma unroll
-        for (int dt = 0; dt < kDt; ++dt) acc[dt] = mma32(from[(8 * (e / 4) + e % 4) * DP + 32 * dt], s[0][e], acc[dt]);
-    }
-    __builtin_amdgcn_s_setprio(0);
   };
 
   // 0 * NaN is NaN, so where some queries of a tile do not see all of a step's keys, values that are not finite must not meet the matrix
   // instructions.  They become zeros in LDS, and are added to the queries that see them one by one, from memory.
   int* const found = reinterpret_cast<int*>(lds + L::with_masks(NW, KG));  // [2][KG]
-  auto take_out = [&](int stage_of, int turn) {
-    tok_u4* const vs = reinterpret_cast<tok_u4*>(lds + stage0 + stage_of * L::kStage + L::kPart);
+  auto take_out = [&](int turn) {
+    tok_u4* const vs = reinterpret_cast<tok_u4*>(lds + values0 + turn * L::kPart);
     bool bad = false;
 #pragma unroll
     for (int i = 0; i < L::kPart / 16 / (NW * kWave); ++i) {
@@ -317,59 +285,98 @@ __global__ __launch_bounds__(NW * KG * kWave, 2) void k_attend(AttendArgs a) {
     }
   };
 
-  // Rounds of whole steps, then those of which some keys are not there or not seen.  Loads are asked for NS - 1 rounds ahead; behind the
-  // last round they fetch nothing, so that what is under way is always as much.
-  int now = 0, fill = NS - 1;  // stages of this round and of the one asked for
-  auto ask = [&](int round, int stage_of) {
-    const int step = round * KG + group;
-    request(stage_of, step, round < whole);
-  };
+  // A round's scores are made while the round before becomes weights: matrix and vector instructions of one wave side by side.  Keys are
+  // asked for two rounds ahead, values one.
+  const bool asks = qr < n && (!keep || keep[min(qr, n - 1)] != 0);
   if (keep) {
     fill_window(0);
     fill_window(1);
-    __syncthreads();
   }
+  if (a.causal && threadIdx.x < 2 * KG) found[threadIdx.x] = 0;
+  if (keep) __syncthreads();
+  ask_keys(0);
+  ask_values(0);
+  ask_keys(1);
+  auto key_of = [&](int round) { return (round * KG + group) * KK; };
+  auto hidden = [&](f32x16 (&s)[kBlocks], int round) {
+    if (round >= whole) hide(s, seen_of(key_of(round), rows_there(round * KG + group), asks));
+  };
+  f32x16 s0[kBlocks], s1[kBlocks];
+  vm_wait<2 * kLoads>();
+  __syncthreads();
+  clear(s0);
 #pragma unroll
-  for (int r = 0; r < NS - 1; ++r) ask(r, r);
-  int round = 0;
-  auto begin = [&] {  // the round's rows are there, and nobody reads the stage of the one before any more
-    vm_wait<(NS - 2) * 2 * kLoads>();
-    __syncthreads();
-    ask(round + NS - 1, fill);
-  };
-  auto next = [&] {
-    fill = now;
-    now = now + 1 < NS ? now + 1 : 0;
-  };
-  for (; round < whole; ++round, next()) {
-    begin();
-    multiply(std::false_type(), now, 0, 0, true);
-  }
-  if (round < rounds) {
-    const bool asks = qr < n && (!keep || keep[min(qr, n - 1)] != 0);
-    if (threadIdx.x < 2 * KG) found[threadIdx.x] = 0;
-    for (; round < rounds; ++round, next()) {
-      const int k0 = (round * KG + group) * KK, turn = round & 1;
-      begin();
-      if (keep && round > 0 && k0 / 4096 * 4096 == k0 - group * KK) fill_window(k0 / 4096 + 1);  // (in the place of the window before)
-      if (a.causal) {
-        take_out(now, turn);
-        __syncthreads();
-        if (threadIdx.x < KG) found[(turn ^ 1) * KG + threadIdx.x] = 0;  // (the next round's, whose last reader has passed this barrier)
-      }
-      if (k0 >= end || (a.causal && k0 > qw + 31)) continue;  // (no keys, or none that the wave's queries see)
-      const unsigned long long here = rows_there(k0 / KK);
-      multiply(std::true_type(), now, k0, here, asks);
-      if (a.causal && found[turn * KG + group]) add_back(k0, here, asks);
+  for (int i = 0; i < kPieces; ++i) scores_part(s0, lds + keys0, i);
+  hidden(s0, 0);
+  raise(most_of(s0));
+  auto body = [&](int round, f32x16 (&s)[kBlocks], f32x16 (&next)[kBlocks]) {
+    const int k0 = key_of(round), turn = round & 1;
+    vm_wait<0>();
+    __syncthreads();  // the next keys and the values are there, and nobody reads the stages that are filled now any more
+    if (keep && round > 0 && k0 / 4096 * 4096 == k0 - group * KK) fill_window(k0 / 4096 + 1);  // (in the place of the window before)
+    ask_keys(round + 2);
+    ask_values(round + 1);
+    const bool partly = a.causal && round >= whole;
+    if (partly) {
+      take_out(turn);
+      __syncthreads();
+      if (threadIdx.x < KG) found[(turn ^ 1) * KG + threadIdx.x] = 0;  // (the next round's, whose last reader has passed this barrier)
     }
+    if (k0 >= end || (a.causal && k0 > qw + 31)) return;  // (no keys, or none that the wave's queries see, from here on)
+    const unsigned char *ks = lds + keys0 + (turn ^ 1) * L::kPart, *vs = lds + values0 + turn * L::kPart;
+    clear(next);
+    const float shift = shift_of(top);
+    float part[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) {
+      scores_part(next, ks, i);
+#pragma unroll
+      for (int e = i * 16 * kBlocks / kPieces; e < (i + 1) * 16 * kBlocks / kPieces; ++e) {
+        s[e / 16][e % 16] = exp2_fast(fmaf(s[e / 16][e % 16], a.c, -shift));
+        part[e % 4] += s[e / 16][e % 16];
+      }
+    }
+    sum += (part[0] + part[1]) + (part[2] + part[3]);
+    // out^T += values^T * weights
+    if constexpr (kHalf) {
+      tok_u4 w[kBlocks * 2];
+#pragma unroll
+      for (int t = 0; t < kBlocks * 2; ++t)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[t][j] = pack_bf16(s[t / 2][8 * (t % 2) + 2 * j], s[t / 2][8 * (t % 2) + 2 * j + 1]);
+      const unsigned char* const from = vs + (4 * half + i16 / 4) * L::kRow + i16 % 2 * 8;
+#pragma unroll
+      for (int t = 0; t < kBlocks * 2; ++t)
+#pragma unroll
+        for (int dt = 0; dt < kDt; ++dt) {
+          const unsigned char* const at = from + 16 * t * L::kRow + (((4 * dt + low) ^ L::value_swizzle(i16 / 4)) << 4);
+          const tok_u2 lo = read_transposed(at), hi = read_transposed(at + 8 * L::kRow);
+          acc[dt] = mma32(tok_u4{lo[0], lo[1], hi[0], hi[1]}, w[t], acc[dt]);
+        }
+    } else {
+      const float* const from = reinterpret_cast<const float*>(vs) + 4 * half * DP + r32;
+#pragma unroll
+      for (int e = 0; e < 16; ++e)
+#pragma unroll
+        for (int dt = 0; dt < kDt; ++dt) acc[dt] = mma32(from[(8 * (e / 4) + e % 4) * DP + 32 * dt], s[0][e], acc[dt]);
+    }
+    hidden(next, round + 1);
+    const float most = most_of(next);
+    if (partly && found[turn * KG + group]) add_back(k0, rows_there(k0 / KK), asks);
+    raise(most);
+  };
+  for (int round = 0; round < rounds;) {
+    body(round++, s0, s1);
+    if (round >= rounds) break;
+    body(round++, s1, s0);
   }
+  vm_wait<0>();  // (no load into LDS is left behind)
   sum = other_half_sum(sum);
 
   if constexpr (KG > 1) {  // the other groups' sums through LDS to the first, in their order
     constexpr int kSums = L::kSums;
     f32x4* const sums = reinterpret_cast<f32x4*>(lds);
     float* const stats = reinterpret_cast<float*>(lds + (KG - 1) * NW * kSums * 16);
-    vm_wait<0>();  // (no load into LDS is left behind)
     __syncthreads();
     if (group != 0) {
       const int at = (group - 1) * NW + wave;
@@ -439,30 +446,37 @@ __global__ __launch_bounds__(NW * KG * kWave, 2) void k_attend(AttendArgs a) {
   }
 }
 
-template <typename ET, int DP, int NW, int KG, int KK, int NS>
+template <typename ET, int DC, int NW, int KG, int KK>
 int ask_tile_lds() {
-  return hipFuncSetAttribute(reinterpret_cast<const void*>(&k_attend<ET, DP, NW, KG, KK, NS>), hipFuncAttributeMaxDynamicSharedMemorySize,
-                             (Tile<ET, DP, KK, NS>::all_bytes(NW, KG))) == hipSuccess ? LAUD_OK : LAUD_ERR_HIP;
+  return hipFuncSetAttribute(reinterpret_cast<const void*>(&k_attend<ET, DC, NW, KG, KK>), hipFuncAttributeMaxDynamicSharedMemorySize,
+                             (Tile<ET, DC, KK>::all_bytes(NW, KG))) == hipSuccess ? LAUD_OK : LAUD_ERR_HIP;
 }
-template <typename ET, int DP, int NW, int KG, int KK, int NS>
+template <typename ET, int DC, int NW, int KG, int KK>
 int launch_tiles(AttendArgs a, hipStream_t st) {
   const long long tiles = tiles_of(a.T, a.B, 1, NW * 32), groups = (tiles * a.heads + 7) / 8 * 8;
   if (!launchable((double)groups, NW * KG * kWave)) return LAUD_ERR_UNSUPPORTED;
   a.tiles = (int)tiles;
-  constexpr int lds = Tile<ET, DP, KK, NS>::all_bytes(NW, KG);
-  if (lds > 65536 && ask_tile_lds<ET, DP, NW, KG, KK, NS>() != LAUD_OK) return LAUD_ERR_HIP;
-  hipLaunchKernelGGL((k_attend<ET, DP, NW, KG, KK, NS>), dim3((unsigned)groups), dim3(NW * KG * kWave), lds, st, a);
+  constexpr int lds = Tile<ET, DC, KK>::all_bytes(NW, KG);
+  if (lds > 65536 && ask_tile_lds<ET, DC, NW, KG, KK>() != LAUD_OK) return LAUD_ERR_HIP;
+  hipLaunchKernelGGL((k_attend<ET, DC, NW, KG, KK>), dim3((unsigned)groups), dim3(NW * KG * kWave), lds, st, a);
   return check_launch();
 }
 
-template <typename ET, int DP>
+template <typename ET, int DC>
 int launch_attend(const AttendArgs& a, hipStream_t st) {
   constexpr bool kHalf = sizeof(ET) == 2;
 #ifdef LAUD_TILE
-  return launch_tiles<ET, DP, LAUD_TILE>(a, st);
+  return launch_tiles<ET, DC, LAUD_TILE>(a, st);
 #endif
-  if constexpr (kHalf) return launch_tiles<ET, DP, 4, 1, 64, 2>(a, st);
-  else return launch_tiles<ET, DP, 4, 1, 32, 2>(a, st);
+  if constexpr (kHalf) return launch_tiles<ET, DC, 4, 1, 64>(a, st);
+  else return launch_tiles<ET, DC, 4, 1, 32>(a, st);
+}
+template <typename ET>
+int launch_width(const AttendArgs& a, hipStream_t st) {
+  if (a.D <= 32) return launch_attend<ET, 32>(a, st);
+  if (a.D <= 64) return launch_attend<ET, 64>(a, st);
+  if (a.D <= 96) return launch_attend<ET, 96>(a, st);
+  return launch_attend<ET, 128>(a, st);
 }
 
 }  // namespace
@@ -493,6 +507,5 @@ extern "C" int laud_attention(const laud_heads* p, int B, const int32_t* offsets
   a.ldq = ldq; a.ldk = ldk; a.ldv = ldv; a.ldo = ldo;
   clear_stale_error();
   hipStream_t st = (hipStream_t)stream;
-  if (p->dtype == LAUD_BF16) return p->D <= 64 ? launch_attend<bf16_t, 64>(a, st) : launch_attend<bf16_t, 128>(a, st);
-  return p->D <= 64 ? launch_attend<float, 64>(a, st) : launch_attend<float, 128>(a, st);
+  return p->dtype == LAUD_BF16 ? launch_width<bf16_t>(a, st) : launch_width<float>(a, st);
 }
