@@ -507,5 +507,11 @@ extern "C" int laud_attention(const laud_heads* p, int B, const int32_t* offsets
   a.ldq = ldq; a.ldk = ldk; a.ldv = ldv; a.ldo = ldo;
   clear_stale_error();
   hipStream_t st = (hipStream_t)stream;
+  // Few rows leave these tiles without enough workgroups; 16 rows a workgroup with its waves sharing the keys fill the card sooner, but
+  // fetch the keys more often.  Both, in us (sequences x heads x tokens, widths of 64 float32 and 128 bf16):
+  //   1 x 8 x 64   10,  5    4 x 16 x 128  16, 10    8 x 16 x 200  40, 27    1 x 16 x 1024  82, 55    1 x 16 x 2048  159, 183    4 x 32 x 512  87, 111
+  //   1 x 8 x 64    7,  6    1 x 16 x 256  11,  8    4 x 16 x 128   8,  8    16 x 16 x 64    8, 12    1 x 32 x 512    15,  28
+  if ((int64_t)p->heads * T <= (p->dtype == LAUD_F32 ? 28000 : 8192))
+    return attend_few(*p, B, offsets, T, q, ldq, k, ldk, v, ldv, keep, out, ldo, st);
   return p->dtype == LAUD_BF16 ? launch_width<bf16_t>(a, st) : launch_width<float>(a, st);
 }

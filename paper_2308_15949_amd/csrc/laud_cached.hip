@@ -11,7 +11,11 @@ struct CachedArgs {
   int tiles, splits, prefix_tiles, prefix_splits;
   unsigned prefix_groups;
   int by_xcd, prefix_by_xcd;
+  // rows of this call in place of a cache: how far apart, and which the masker kept
+  int64_t ldk, ldv;
+  const uint8_t* keep;
   float c;                // scale * log2(e)
+  unsigned group_by, group_shift;  // x / group = x * group_by >> group_shift (x below 2^31)
   const int32_t *offsets, *lens, *table, *prefix;
   const uint8_t *k, *v;
   const float *ks, *vs;
@@ -49,17 +53,17 @@ struct Operands<bf16_t, DP, GROUPS> {
   static constexpr int kBytes = 2;
   tok_u4 k[kGroups][kPieces];
   unsigned v[kGroups][4][kEach / 2];
-  __device__ __forceinline__ void load_keys(int u, __amdgpu_buffer_rsrc_t rk, int D, int r16, int quarter) {
+  __device__ __forceinline__ void load_keys(int u, __amdgpu_buffer_rsrc_t rk, int D, unsigned pitch, unsigned there, int r16, int quarter) {
 #pragma unroll
     for (int s = 0; s < kPieces; ++s) {
       const int d = 32 * s + 8 * quarter;
-      k[u][s] = load16(rk, d < D ? (unsigned)(r16 * D + d) * 2u : kOutside);
+      k[u][s] = load16(rk, d < D && (there >> r16 & 1) ? (r16 * pitch + d) * 2u : kOutside);
     }
   }
-  __device__ __forceinline__ void load_values(int u, __amdgpu_buffer_rsrc_t rv, int D, int r16, int quarter) {
+  __device__ __forceinline__ void load_values(int u, __amdgpu_buffer_rsrc_t rv, int D, unsigned pitch, unsigned there, int r16, int quarter) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const unsigned at = r16 * kEach < D ? (unsigned)((4 * quarter + j) * D + r16 * kEach) * 2u : kOutside;
+      const unsigned at = r16 * kEach < D && (there >> (4 * quarter + j) & 1) ? ((4 * quarter + j) * pitch + r16 * kEach) * 2u : kOutside;
       if constexpr (kEach == 8) {
         const tok_u4 w = load16(rv, at);
 #pragma unroll
@@ -100,17 +104,17 @@ struct Operands<uint8_t, DP, GROUPS> {
   static constexpr int kBytes = 1;
   tok_u4 k[kGroups][kPieces];
   unsigned v[kGroups][4][kEach / 4];
-  __device__ __forceinline__ void load_keys(int u, __amdgpu_buffer_rsrc_t rk, int D, int r16, int quarter) {
+  __device__ __forceinline__ void load_keys(int u, __amdgpu_buffer_rsrc_t rk, int D, unsigned pitch, unsigned there, int r16, int quarter) {
 #pragma unroll
     for (int s = 0; s < kPieces; ++s) {
       const int d = 64 * s + 16 * quarter;
-      k[u][s] = load16(rk, d < D ? (unsigned)(r16 * D + d) : kOutside);
+      k[u][s] = load16(rk, d < D && (there >> r16 & 1) ? r16 * pitch + d : kOutside);
     }
   }
-  __device__ __forceinline__ void load_values(int u, __amdgpu_buffer_rsrc_t rv, int D, int r16, int quarter) {
+  __device__ __forceinline__ void load_values(int u, __amdgpu_buffer_rsrc_t rv, int D, unsigned pitch, unsigned there, int r16, int quarter) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const unsigned at = r16 * kEach < D ? (unsigned)((4 * quarter + j) * D + r16 * kEach) : kOutside;
+      const unsigned at = r16 * kEach < D && (there >> (4 * quarter + j) & 1) ? (4 * quarter + j) * pitch + r16 * kEach : kOutside;
       if constexpr (kEach == 8) {
         const tok_u2 w = load8(rv, at);
         v[u][j][0] = w[0];
@@ -153,19 +157,19 @@ struct Operands<float, DP, GROUPS> {
   static constexpr int kBytes = 4;
   tok_u4 k[kGroups][kPieces];
   float v[kGroups][4][kEach];
-  __device__ __forceinline__ void load_keys(int u, __amdgpu_buffer_rsrc_t rk, int D, int r16, int quarter) {
+  __device__ __forceinline__ void load_keys(int u, __amdgpu_buffer_rsrc_t rk, int D, unsigned pitch, unsigned there, int r16, int quarter) {
 #pragma unroll
     for (int s = 0; s < kPieces; ++s) {
       const int d = 16 * s + 4 * quarter;
-      k[u][s] = load16(rk, d < D ? (unsigned)(r16 * D + d) * 4u : kOutside);
+      k[u][s] = load16(rk, d < D && (there >> r16 & 1) ? (r16 * pitch + d) * 4u : kOutside);
     }
   }
-  __device__ __forceinline__ void load_values(int u, __amdgpu_buffer_rsrc_t rv, int D, int r16, int quarter) {
+  __device__ __forceinline__ void load_values(int u, __amdgpu_buffer_rsrc_t rv, int D, unsigned pitch, unsigned there, int r16, int quarter) {
 #pragma unroll
     for (int j = 0; j < 4; ++j)
 #pragma unroll
       for (int h = 0; h < kEach / 4; ++h) {
-        const tok_u4 w = load16(rv, r16 * kEach < D ? (unsigned)((4 * quarter + j) * D + r16 * kEach + 4 * h) * 4u : kOutside);
+        const tok_u4 w = load16(rv, r16 * kEach < D && (there >> (4 * quarter + j) & 1) ? ((4 * quarter + j) * pitch + r16 * kEach + 4 * h) * 4u : kOutside);
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[u][j][4 * h + e] = __uint_as_float(w[e]);
       }
@@ -191,7 +195,7 @@ __device__ __forceinline__ f32x4 of_four(float v) { return f32x4{dpp_movf<0x00>(
 
 // Sixteen query rows a row tile (RT of them a workgroup): the tokens of a sequence times the query heads of a key head, so that a key is
 // fetched once for all of them.  Four waves share a part's keys, each takes every fourth step of 16 or 32 keys; their sums are joined through LDS.
-template <typename ET, typename CT, int DP, int RT>
+template <typename ET, typename CT, int DP, int RT, bool ROWS>
 __global__ __launch_bounds__(kWaves * kWave, 2) void k_cached(CachedArgs a) {
   typedef Operands<CT, DP, (sizeof(CT) == 4 ? 1 : 2)> O;
   constexpr bool kWide = sizeof(CT) == 4;  // float32 instructions
@@ -226,7 +230,7 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void k_cached(CachedArgs a) {
     n = row_at(a.offsets, b + 1, a.T) - row0;
     if ((long long)tile < first_tile(a.offsets, b, a.T, a.group, kRows)) return;
     tile -= (int)first_tile(a.offsets, b, a.T, a.group, kRows);
-    len = cached_tokens(a, b);
+    len = ROWS ? max(n, 0) : cached_tokens(a, b);
     table = a.table + (long long)b * a.table_ld;
   }
   if (n <= 0) return;
@@ -235,14 +239,16 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void k_cached(CachedArgs a) {
   const int there = (int)min((unsigned)kRows, rows - first_row);  // rows of this tile
   const int each = part_keys(len, splits);
   if (split > 0 && (long long)split * each >= len) return;
-  const long long past = (long long)(shared ? len : a.lens[b]) - n;  // position of the first token
+  const long long past = (long long)(shared || ROWS ? len : a.lens[b]) - n;  // position of the first token
   const bool causal = a.causal && !shared;
+  auto token_of = [&](unsigned row) { return (unsigned)((unsigned long long)row * a.group_by >> a.group_shift); };
   auto limit_of = [&](unsigned row) -> int {  // keys that a row sees
-    return causal ? (int)min(max(past + row / (unsigned)a.group + 1, 0ll), (long long)len) : len;
+    return causal ? (int)min(max(past + token_of(row) + 1, 0ll), (long long)len) : len;
   };
   const int begin = split * each;
   const int end = __builtin_amdgcn_readfirstlane(min(min(begin + each, len), limit_of(first_row + there - 1)));
-  const int all_see = __builtin_amdgcn_readfirstlane(limit_of(first_row));  // keys that every row sees
+  const uint8_t* const keep = ROWS && a.keep ? a.keep + row0 : nullptr;
+  const int all_see = keep ? 0 : __builtin_amdgcn_readfirstlane(limit_of(first_row));  // keys that every row sees
 
   // Queries: one row tile stays in registers; several lie in LDS, where every wave reads them step by step (in registers as well they
   // would push sums out into memory).
@@ -253,9 +259,9 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void k_cached(CachedArgs a) {
   tok_u4 q[O::kQuery];
 #pragma unroll
   for (int t = 0; t < RT; ++t) {
-    const unsigned row = first_row + t * 16 + r16, token = row / (unsigned)a.group;
+    const unsigned row = first_row + t * 16 + r16, token = token_of(row);
     const bool in = t * 16 + r16 < there;
-    limit[t] = in ? limit_of(row) : 0;
+    limit[t] = in && (!keep || keep[token] != 0) ? limit_of(row) : 0;
     if (kQueryLds && t % kWaves != wave) continue;
     const ET* const from = reinterpret_cast<const ET*>(a.q) + (long long)(row0 + token) * a.ldq + (hk * a.group + (row - token * a.group)) * a.D;
 #pragma unroll
@@ -283,27 +289,43 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void k_cached(CachedArgs a) {
   }
 
   // Where a step's keys are: of each sixteen how many (a page that is none has none), and the first one's row of the cache.
+  // Where the keys are rows of this call: which of the sixteen the masker kept.
   struct Place {
     int valid[kGroups];
+    unsigned there[kGroups];
     long long at[kGroups];
   };
   auto place_of = [&](int key) {
     Place s;
 #pragma unroll
     for (int u = 0; u < kGroups; ++u) {
-      const int pos = key + 16 * u, pg = pos < end ? __builtin_amdgcn_readfirstlane(table[pos >> a.page_bits]) : -1;
+      const int pos = key + 16 * u;
+      s.there[u] = 0xffffu;
+      if constexpr (ROWS) {
+        s.valid[u] = min(16, max(end - pos, 0));
+        s.at[u] = row0 + pos;
+        if (keep) s.there[u] = (unsigned)__ballot(r16 < s.valid[u] && keep[min(pos + r16, n - 1)] != 0) & 0xffffu;
+        continue;
+      }
+      const int pg = pos < end ? __builtin_amdgcn_readfirstlane(table[pos >> a.page_bits]) : -1;
       const bool ok = (unsigned)pg < (unsigned)a.pages;
       s.valid[u] = ok ? min(16, end - pos) : 0;
       s.at[u] = ok ? (((long long)pg * a.kv_heads + hk) << a.page_bits) + (pos & ((1 << a.page_bits) - 1)) : 0;
     }
     return s;
   };
+  // bytes from a row to the next, of keys and of values, and to the row that a place begins with
+  const long long pitch_k = ROWS ? a.ldk : a.D, pitch_v = ROWS ? a.ldv : a.D, skip = ROWS ? hk * a.D : 0;
+  auto row_of = [&](const uint8_t* base, long long at, long long pitch) { return base + (at * pitch + skip) * O::kBytes; };
+  auto rows_in = [&](const uint8_t* base, const Place& s, int u, long long pitch) {
+    return bytes_of(scalar_pointer(row_of(base, s.at[u], pitch)), s.valid[u] ? ((s.valid[u] - 1) * pitch + a.D) * O::kBytes : 0);
+  };
   O o;
   float ks[kGroups], vs[kGroups];  // scales: of four lanes in a row each has one of their four keys'
   auto load_keys = [&](const Place& s) {
 #pragma unroll
     for (int u = 0; u < kGroups; ++u) {
-      o.load_keys(u, bytes_of(scalar_pointer(a.k + s.at[u] * a.D * O::kBytes), s.valid[u] * a.D * O::kBytes), a.D, r16, quarter);
+      o.load_keys(u, rows_in(a.k, s, u, pitch_k), a.D, (unsigned)pitch_k, s.there[u], r16, quarter);
       if constexpr (O::kBytes == 1)  // (all of a page's scales are there)
         ks[u] = __uint_as_float(load4(bytes_of(scalar_pointer(a.ks + s.at[u]), s.valid[u] ? 64 : 0), quarter * 16 + r16 % 4 * 4));
     }
@@ -311,7 +333,7 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void k_cached(CachedArgs a) {
   auto load_values = [&](const Place& s) {
 #pragma unroll
     for (int u = 0; u < kGroups; ++u) {
-      o.load_values(u, bytes_of(scalar_pointer(a.v + s.at[u] * a.D * O::kBytes), s.valid[u] * a.D * O::kBytes), a.D, r16, quarter);
+      o.load_values(u, rows_in(a.v, s, u, pitch_v), a.D, (unsigned)pitch_v, s.there[u], r16, quarter);
       if constexpr (O::kBytes == 1)
         vs[u] = __uint_as_float(load4(bytes_of(scalar_pointer(a.vs + s.at[u]), s.valid[u] ? 64 : 0), quarter * 16 + r16 % 4 * 4));
     }
@@ -361,7 +383,7 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void k_cached(CachedArgs a) {
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const int at = 4 * quarter + i;
-            if (!(at < here.valid[u] && key + 16 * u + at < limit[t])) sc[t][u][i] = kNoScore;
+            if (!(at < here.valid[u] && key + 16 * u + at < limit[t] && (here.there[u] >> at & 1))) sc[t][u][i] = kNoScore;
           }
       }
       float most = sc[t][0][0];
@@ -425,7 +447,8 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void k_cached(CachedArgs a) {
       for (int u = 0; u < kGroups; ++u)
 #pragma unroll 1
         for (int j = 0; j < here.valid[u]; ++j) {
-          const uint8_t* const row = a.v + (here.at[u] + j) * a.D * O::kBytes;
+          if (!(here.there[u] >> j & 1)) continue;
+          const uint8_t* const row = row_of(a.v, here.at[u] + j, pitch_v);
 #pragma unroll 1
           for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -478,8 +501,9 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void k_cached(CachedArgs a) {
     }
     if (t * 16 + r >= there) continue;
     const unsigned row = first_row + t * 16 + r;
-    const long long tok = row0 + row / (unsigned)a.group;
-    const int h = hk * a.group + (int)(row % (unsigned)a.group);
+    const unsigned token = token_of(row);
+    const long long tok = row0 + token;
+    const int h = hk * a.group + (int)(row - token * a.group);
     if (a.splits + a.prefix_splits > 1) {
       const long long at = ((long long)(shared ? a.splits + split : split) * a.T + tok) * a.heads + h;
       if (d < a.D)
@@ -551,6 +575,16 @@ __global__ __launch_bounds__(256) void k_join(CachedArgs a) {
   store4(reinterpret_cast<ET*>(a.out) + token * a.ldo + head * a.D + d, f);
 }
 
+// group_by, group_shift: with 2^l the next power of two, the least multiple m / 2^(31 + l) not below 1 / group is off by less than
+// 2^l / 2^(31 + l) / group, which 2^31 rows do not raise to another whole number.
+void set_group(CachedArgs& a, int group) {
+  int l = 0;
+  while ((1 << l) < group) ++l;
+  a.group = group;
+  a.group_shift = 31 + l;
+  a.group_by = (unsigned)(((1ull << (31 + l)) + group - 1) / group);
+}
+
 // ---- plan -------------------------------------------------------------------------------------------------------------------
 struct Plan {
   int rt;                   // row tiles of a workgroup
@@ -588,24 +622,45 @@ Plan plan_of(const laud_heads* p, const laud_cache* c, const laud_batch* b, int 
   return s;
 }
 
-template <typename ET, typename CT, int DP, int RT>
+template <typename ET, typename CT, int DP, int RT, bool ROWS>
 int launch_cached(const CachedArgs& a, hipStream_t st) {
   constexpr int kLds = kWaves * 16 * (DP + 4) * 4 + kWaves * 16 * RT * 8;
   const double groups = (double)a.tiles * a.kv_heads * a.splits + a.prefix_groups;
   if (!launchable(groups, kWaves * kWave)) return LAUD_ERR_UNSUPPORTED;
-  hipLaunchKernelGGL((k_cached<ET, CT, DP, RT>), dim3((unsigned)groups), dim3(kWaves * kWave), kLds, st, a);
+  hipLaunchKernelGGL((k_cached<ET, CT, DP, RT, ROWS>), dim3((unsigned)groups), dim3(kWaves * kWave), kLds, st, a);
   return LAUD_OK;
 }
 template <typename ET, typename CT, int DP>
 int launch_rows(const CachedArgs& a, int rt, hipStream_t st) {
-  if (rt == 1) return launch_cached<ET, CT, DP, 1>(a, st);
-  return launch_cached<ET, CT, DP, 2>(a, st);
+  if (rt == 1) return launch_cached<ET, CT, DP, 1, false>(a, st);
+  return launch_cached<ET, CT, DP, 2, false>(a, st);
 }
 int launch_types(const CachedArgs& a, int cache_type, int rt, hipStream_t st) {
   if (cache_type == LAUD_F32) return a.D <= 64 ? launch_rows<float, float, 64>(a, rt, st) : launch_rows<float, float, 128>(a, rt, st);
   if (cache_type == LAUD_BF16) return a.D <= 64 ? launch_rows<bf16_t, bf16_t, 64>(a, rt, st) : launch_rows<bf16_t, bf16_t, 128>(a, rt, st);
   return a.D <= 64 ? launch_rows<bf16_t, uint8_t, 64>(a, rt, st) : launch_rows<bf16_t, uint8_t, 128>(a, rt, st);
 }
+
+}  // namespace
+
+int attend_few(const laud_heads& p, int B, const int32_t* offsets, int T, const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v,
+               int64_t ldv, const uint8_t* keep, void* out, int64_t ldo, hipStream_t st) {
+  CachedArgs a{};
+  set_group(a, p.heads / p.kv_heads);
+  a.heads = p.heads; a.kv_heads = p.kv_heads; a.D = p.D; a.causal = p.causal; a.B = B; a.T = T;
+  a.splits = 1; a.c = p.scale * kLog2e;
+  a.offsets = offsets; a.k = (const uint8_t*)k; a.v = (const uint8_t*)v; a.ldk = ldk; a.ldv = ldv; a.keep = keep;
+  a.q = q; a.out = out; a.ldq = ldq; a.ldo = ldo;
+  const long long tiles = tiles_of(T, B, a.group, 16);
+  if (!launchable((double)tiles * a.kv_heads, kWaves * kWave)) return LAUD_ERR_UNSUPPORTED;
+  a.tiles = (int)tiles;
+  int status;
+  if (p.dtype == LAUD_F32) status = p.D <= 64 ? launch_cached<float, float, 64, 1, true>(a, st) : launch_cached<float, float, 128, 1, true>(a, st);
+  else status = p.D <= 64 ? launch_cached<bf16_t, bf16_t, 64, 1, true>(a, st) : launch_cached<bf16_t, bf16_t, 128, 1, true>(a, st);
+  return status ? status : check_launch();
+}
+
+namespace {
 
 // The arguments that the host sees, all but the rows and the workspace.
 int check_cached(const laud_heads* p, const laud_cache* c, const laud_batch* b, int T) {
@@ -652,7 +707,8 @@ extern "C" int laud_cache_attention(const laud_heads* p, const laud_cache* c, co
   const double own = (double)s.tiles * p->kv_heads * s.own, shared = (double)s.prefix_tiles * p->kv_heads * s.shared;
   if (!launchable(own + shared, kWaves * kWave) || !launchable((double)T * p->heads, 256)) return LAUD_ERR_UNSUPPORTED;
   CachedArgs a{};
-  a.heads = p->heads; a.group = p->heads / p->kv_heads; a.kv_heads = p->kv_heads; a.D = p->D; a.causal = p->causal; a.B = b->B; a.T = T;
+  set_group(a, p->heads / p->kv_heads);
+  a.heads = p->heads; a.kv_heads = p->kv_heads; a.D = p->D; a.causal = p->causal; a.B = b->B; a.T = T;
   a.pages = c->pages; a.page_bits = page_bits(c); a.table_ld = b->table_ld;
   a.tiles = (int)s.tiles; a.splits = s.own; a.prefix_tiles = (int)s.prefix_tiles; a.prefix_splits = s.shared;
   a.prefix_groups = (unsigned)shared; a.prefix_len = b->prefix_len;

@@ -114,6 +114,9 @@ inline int check_cache(const laud_cache* c, const laud_batch* b) {
   return LAUD_OK;
 }
 inline int page_bits(const laud_cache* c) { return __builtin_ctz((unsigned)c->page); }
+// laud_attention by the kernel of few rows (laud_cached.hip): 16 query rows a workgroup, keys straight into registers
+int attend_few(const laud_heads& p, int B, const int32_t* offsets, int T, const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v,
+               int64_t ldv, const uint8_t* keep, void* out, int64_t ldo, hipStream_t st);
 inline bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 inline bool check_batch(const laud_batch* b) {
   return b->offsets && b->lens && b->table && aligned4(b->offsets) && aligned4(b->lens) && aligned4(b->table);
