@@ -510,12 +510,12 @@ typedef struct {
  */
 typedef struct {
   int32_t B;
-  int32_t table_ld;       /* pages of a row of table, at least 1; table_ld * page below 2^31 */
+  int32_t table_ld;       /* pages of a row of table, at least 1; table_ld * page at most 2^30 */
   const int32_t* offsets; /* [B + 1] */
   const int32_t* lens;    /* [B] */
   const int32_t* table;   /* [B][table_ld] */
   const int32_t* prefix;  /* [ceil(prefix_len / page)] pages of the tokens that come before the first of every sequence, or NULL */
-  int32_t prefix_len;     /* their number (0: none); laud_cache_attention only */
+  int32_t prefix_len;     /* their number (0: none; at most 2^30); laud_cache_attention only */
 } laud_batch;
 
 /*

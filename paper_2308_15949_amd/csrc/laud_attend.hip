@@ -1,7 +1,8 @@
-// Attention over the tokens of packed sequences: one pass over keys and values with the running maximum and sum of each query's softmax.
-#include <type_traits>
+// Attention over the tokens of packed sequences, and of many new tokens over a cache: one pass over keys and values with the running
+// maximum and sum of each query's softmax.
+#include <atomic>
 
-#include "laud_heads.h"
+#include "laud_cached.h"
 
 namespace laud {
 namespace {
@@ -62,8 +63,8 @@ __device__ __forceinline__ f32x16 mma32(float a, float b, const f32x16& c) { ret
 // 2^8 instead of 1, which costs float32 nothing, and most steps are spared the scaling of all sums (64 instructions).
 constexpr float kSlack = 8.f;
 
-template <typename ET, int DC, int NW, int KG, int KK>
-__global__ __launch_bounds__(NW * KG * kWave, 2) void k_attend(AttendArgs a) {
+template <typename ET, int DC, int NW, int KG, int KK, bool PAGED>
+__global__ __launch_bounds__(NW * KG * kWave, 2) void k_attend(AttendArgs a, CachedArgs cache) {
   typedef Tile<ET, DC, KK> L;
   constexpr int DP = L::DP;
   constexpr bool kHalf = L::kHalf;
@@ -76,38 +77,93 @@ __global__ __launch_bounds__(NW * KG * kWave, 2) void k_attend(AttendArgs a) {
   const int group = __builtin_amdgcn_readfirstlane(threadIdx.x / (NW * kWave));
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave) - group * NW;
 
-  // Workgroups go round-robin over the eight XCDs: each takes a run of heads, whose keys its L2 then serves, the tiles of several heads
-  // side by side; the last tiles, which see the most keys, first.
-  const unsigned total = (unsigned)a.heads * (unsigned)a.tiles, per = (total + 7) / 8;  // (a launch has less than 2^32 threads)
-  const unsigned id = blockIdx.x % 8 * per + blockIdx.x / 8;
-  if (blockIdx.x / 8 >= per || id >= total) return;
-  const unsigned band = a.heads % 8 == 0 ? a.heads / 8 : 1, in_band = id % (band * a.tiles);
-  const int head = (int)(id / (band * a.tiles) * band + in_band % band), tile = a.tiles - 1 - (int)(in_band / band);
-  const int b = last_not_above(a.B, [&](int i) { return first_tile(a.offsets, i, a.T, 1, kRows) <= tile; });
-  const int row0 = __builtin_amdgcn_readfirstlane(row_at(a.offsets, b, a.T));
-  const int n = __builtin_amdgcn_readfirstlane(row_at(a.offsets, b + 1, a.T)) - row0;  // (may be negative: no rows)
-  const long long q_first = (tile - first_tile(a.offsets, b, a.T, 1, kRows)) * kRows;
-  if (q_first < 0 || q_first >= n) return;
-  const int q0 = __builtin_amdgcn_readfirstlane((int)q_first), qw = q0 + wave * 32, qr = qw + r32;  // the tile's first row in its sequence, the wave's, the lane's
-  const int end = a.causal ? min(n, q0 + kRows) : n, steps = (end + KK - 1) / KK, rounds = (steps + KG - 1) / KG;
-  const uint8_t* const keep = a.keep ? a.keep + row0 : nullptr;
-  // rounds whose keys are all there, and seen by all queries of the tile
-  const int whole_steps = keep ? 0 : (a.causal ? min(n, q0 + 1) : n) / KK, whole = whole_steps / KG;
+  // The tile's queries and their keys.  Keys are counted from the first that this workgroup looks at: there are `end` of them, a query sees
+  // those below its limit, every query of the tile those below all_see.
+  int head, hk, n, end, all_see, limit = 0;
+  long long my_row;  // the lane's query among all rows
+  bool in;
+  const uint8_t* keep = nullptr;
+  const ET *kp = nullptr, *vp = nullptr;
+  CachedTile part;
+  if constexpr (PAGED) {
+    if (!cached_tile<kRows>(part, cache)) return;
+    const unsigned row = part.first_row + wave * 32 + r32, token = token_of(cache, row);
+    in = row < part.rows;
+    hk = part.hk;
+    head = hk * cache.group + (int)(row - token * cache.group);
+    my_row = (long long)part.row0 + token;
+    n = end = max(part.end - part.begin, 0);
+    all_see = min(max(part.all_see - part.begin, 0), end);
+    if (in) limit = min(max(part.limit_of(cache, row) - part.begin, 0), end);
+  } else {
+    // Workgroups go round-robin over the eight XCDs: each takes a run of heads, whose keys its L2 then serves, the tiles of several heads
+    // side by side; the last tiles, which see the most keys, first.
+    const unsigned total = (unsigned)a.heads * (unsigned)a.tiles, per = (total + 7) / 8;  // (a launch has less than 2^32 threads)
+    const unsigned id = blockIdx.x % 8 * per + blockIdx.x / 8;
+    if (blockIdx.x / 8 >= per || id >= total) return;
+    const unsigned band = a.heads % 8 == 0 ? a.heads / 8 : 1, in_band = id % (band * a.tiles);
+    head = (int)(id / (band * a.tiles) * band + in_band % band);
+    hk = head / a.group;
+    const int tile = a.tiles - 1 - (int)(in_band / band);
+    const int b = last_not_above(a.B, [&](int i) { return first_tile(a.offsets, i, a.T, 1, kRows) <= tile; });
+    const int row0 = __builtin_amdgcn_readfirstlane(row_at(a.offsets, b, a.T));
+    n = __builtin_amdgcn_readfirstlane(row_at(a.offsets, b + 1, a.T)) - row0;  // (may be negative: no rows)
+    const long long q_first = (tile - first_tile(a.offsets, b, a.T, 1, kRows)) * kRows;
+    if (q_first < 0 || q_first >= n) return;
+    const int q0 = __builtin_amdgcn_readfirstlane((int)q_first), qr = q0 + wave * 32 + r32;
+    in = qr < n;
+    my_row = row0 + (long long)qr;
+    keep = a.keep ? a.keep + row0 : nullptr;
+    kp = reinterpret_cast<const ET*>(a.k) + (long long)row0 * a.ldk + hk * a.D;
+    vp = reinterpret_cast<const ET*>(a.v) + (long long)row0 * a.ldv + hk * a.D;
+    end = a.causal ? min(n, q0 + kRows) : n;
+    all_see = a.causal ? min(n, q0 + 1) : n;
+    if (in && (!keep || keep[qr] != 0)) limit = a.causal ? qr + 1 : n;
+  }
+  const int steps = (end + KK - 1) / KK, rounds = (steps + KG - 1) / KG;
+  const int whole = keep ? 0 : all_see / KK / KG;  // rounds whose keys are all there, and seen by all queries of the tile
+  const int wave_sees = __builtin_amdgcn_readfirstlane((int)lanes64_max((unsigned)limit));
 
   // the wave's queries, for good: lane = query, sixteen-byte pieces 2 s + half
   constexpr int kPieces = DC * kEb / 32, kPer = 16 / kEb;
   tok_u4 qf[kPieces];
-  {
-    const __amdgpu_buffer_rsrc_t rq = bytes_of(reinterpret_cast<const ET*>(a.q) + (row0 + (long long)q0) * a.ldq + head * a.D,
-                                               ((long long)(min(kRows, n - q0) - 1) * a.ldq + a.D) * kEb);
 #pragma unroll
-    for (int s = 0; s < kPieces; ++s) {
-      const int d = (2 * s + half) * kPer;
-      qf[s] = load16(rq, qr < n && d < a.D ? (unsigned)((qr - q0) * a.ldq + d) * kEb : kOutside);
-    }
+  for (int s = 0; s < kPieces; ++s) {
+    const int d = (2 * s + half) * kPer;
+    qf[s] = tok_u4{0, 0, 0, 0};
+    if (in && d < a.D) qf[s] = *reinterpret_cast<const tok_u4*>(reinterpret_cast<const ET*>(a.q) + my_row * a.ldq + head * a.D + d);
   }
-  const ET* const kp = reinterpret_cast<const ET*>(a.k) + (long long)row0 * a.ldk + head / a.group * a.D;
-  const ET* const vp = reinterpret_cast<const ET*>(a.v) + (long long)row0 * a.ldv + head / a.group * a.D;
+
+  // Sixteen keys of a cache lie in one page: a step's pages, and which of its keys are there.
+  constexpr int kSixteens = KK / 16;
+  struct Pages {
+    long long at[kSixteens];  // the first one's row of the cache
+    unsigned long long there;
+  };
+  int ahead[kSixteens];  // page numbers of the step that is asked for next
+  auto look_up = [&](int step) {
+    if constexpr (PAGED) {
+#pragma unroll
+      for (int g = 0; g < kSixteens; ++g) {
+        const int key = step * KK + 16 * g;
+        ahead[g] = key < end ? part.table[(part.begin + key) >> cache.page_bits] : -1;
+      }
+    }
+  };
+  auto pages_of = [&](int step) {
+    Pages s{};
+    if constexpr (PAGED) {
+#pragma unroll
+      for (int g = 0; g < kSixteens; ++g) {
+        const int key = step * KK + 16 * g, page = __builtin_amdgcn_readfirstlane(ahead[g]);
+        if ((unsigned)page < (unsigned)cache.pages) {  // (-1 past the end)
+          s.at[g] = (((long long)page * cache.kv_heads + hk) << cache.page_bits) + ((part.begin + key) & ((1 << cache.page_bits) - 1));
+          s.there |= ((1ull << min(16, end - key)) - 1) << (16 * g);
+        }
+      }
+    }
+    return s;
+  };
 
   // Which of a step's keys are there, a bit each: rows of the sequence that the masker kept.  Its bytes become bits, 4096 keys at a time,
   // a window ahead of the keys that are asked for.
@@ -139,8 +195,9 @@ __global__ __launch_bounds__(NW * KG * kWave, 2) void k_attend(AttendArgs a) {
   for (int i = 0; i < kOffsets; ++i) {
     const int row = (i * NW + wave) * kRowsLoad + lane / kLanesRow, pos = lane % kLanesRow;
     const int ck = (pos ^ L::key_swizzle(row)) * kPer, cv = (pos ^ L::value_swizzle(row)) * kPer;
-    vk[i] = ck < a.D ? (unsigned)(row * a.ldk + ck) * kEb : kOutside;
-    vv[i] = cv < a.D ? (unsigned)(row * a.ldv + cv) * kEb : kOutside;
+    const int from = PAGED ? lane / kLanesRow : row;  // (a load of a cache begins with its first row)
+    vk[i] = ck < a.D ? (unsigned)(from * a.ldk + ck) * kEb : kOutside;
+    vv[i] = cv < a.D ? (unsigned)(from * a.ldv + cv) * kEb : kOutside;
   }
   const unsigned keys0 = group * L::kGroup, values0 = keys0 + 2 * L::kPart;  // the group's stages
   auto request = [&](const ET* from, int64_t ld, const unsigned (&off)[kOffsets], unsigned to, bool all, unsigned long long there) {
@@ -159,13 +216,35 @@ __global__ __launch_bounds__(NW * KG * kWave, 2) void k_attend(AttendArgs a) {
       }
     }
   };
+  auto request_pages = [&](const uint8_t* base, const unsigned (&off)[kOffsets], unsigned to, const Pages& s) {
+    const unsigned stage = __builtin_amdgcn_readfirstlane(to + wave * 1024);
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int row = (i * NW + wave) * kRowsLoad, bits = (int)(s.there >> row & ((1u << kRowsLoad) - 1));
+      long long at = 0;
+#pragma unroll
+      for (int g = 0; g < kSixteens; ++g)
+        if (row / 16 == g) at = s.at[g] + row % 16;
+      dma16(bytes_of(scalar_pointer(base + at * a.D * kEb), __popc((unsigned)bits) * a.D * kEb), off[kSame ? 0 : i], 0, stage + i * NW * 1024);
+    }
+  };
+  Pages asked;  // of the keys that were asked for last
   auto ask_keys = [&](int round) {
     const int step = round * KG + group;
-    request(kp + (long long)step * KK * a.ldk, a.ldk, vk, keys0 + (round & 1) * L::kPart, round < whole, round < whole ? 0 : rows_there(step));
+    const unsigned to = keys0 + (round & 1) * L::kPart;
+    if constexpr (PAGED) {
+      asked = pages_of(step);
+      look_up(step + 1);
+      request_pages(cache.k, vk, to, asked);
+    } else {
+      request(kp + (long long)step * KK * a.ldk, a.ldk, vk, to, round < whole, round < whole ? 0 : rows_there(step));
+    }
   };
-  auto ask_values = [&](int round) {
+  auto ask_values = [&](int round) {  // (of a cache: of the keys that were asked for last)
     const int step = round * KG + group;
-    request(vp + (long long)step * KK * a.ldv, a.ldv, vv, values0 + (round & 1) * L::kPart, round < whole, round < whole ? 0 : rows_there(step));
+    const unsigned to = values0 + (round & 1) * L::kPart;
+    if constexpr (PAGED) request_pages(cache.v, vv, to, asked);
+    else request(vp + (long long)step * KK * a.ldv, a.ldv, vv, to, round < whole, round < whole ? 0 : rows_there(step));
   };
 
   f32x16 acc[kDt];
@@ -175,12 +254,10 @@ __global__ __launch_bounds__(NW * KG * kWave, 2) void k_attend(AttendArgs a) {
     for (int e = 0; e < 16; ++e) acc[t][e] = 0.f;
   float top = kNoScore, sum = 0.f;
 
-  // which keys of a step the lane's query sees
-  auto seen_of = [&](int k0, unsigned long long here, bool asks) -> unsigned long long {
-    if (!asks) return 0;
-    if (!a.causal) return here;
-    const int last = qr - k0;
-    return last < 0 ? 0 : last >= 63 ? here : here & ((2ull << last) - 1);
+  // which of the keys that are there the lane's query sees
+  auto seen_of = [&](int k0, unsigned long long here) -> unsigned long long {
+    const int sees = limit - k0;
+    return sees <= 0 ? 0 : sees >= 64 ? here : here & ((1ull << sees) - 1);
   };
   const int i16 = lane % 16, low = (lane / 16) % 2 * 2 + i16 % 4 / 2;
   // keys 32 u + 8 * (e / 4) + 4 * half + e % 4 of a step with the lane's query
@@ -258,12 +335,18 @@ __global__ __launch_bounds__(NW * KG * kWave, 2) void k_attend(AttendArgs a) {
     }
     if (__ballot(bad) && lane == 0) found[turn * KG + group] = 1;
   };
-  auto add_back = [&](int k0, unsigned long long here, bool asks) {
-    const unsigned long long seen = seen_of(k0, here, asks);
+  auto add_back = [&](int k0, unsigned long long here) {
+    const unsigned long long seen = seen_of(k0, here);
 #pragma unroll 1
     for (int j = 0; j < KK; ++j) {
       if (!((here >> j) & 1)) continue;
-      const __amdgpu_buffer_rsrc_t row = bytes_of(vp + (long long)(k0 + j) * a.ldv, a.D * kEb);
+      const uint8_t* from = reinterpret_cast<const uint8_t*>(vp + (long long)(k0 + j) * a.ldv);
+      if constexpr (PAGED) {
+        const int key = part.begin + k0 + j, page = __builtin_amdgcn_readfirstlane(part.table[key >> cache.page_bits]);
+        const long long at = (((long long)page * cache.kv_heads + hk) << cache.page_bits) + (key & ((1 << cache.page_bits) - 1));
+        from = cache.v + at * a.D * kEb;
+      }
+      const __amdgpu_buffer_rsrc_t row = bytes_of(scalar_pointer(from), a.D * kEb);
       const bool sees = (seen >> j) & 1;
 #pragma unroll
       for (int t = 0; t < kDt; ++t)
@@ -287,19 +370,24 @@ __global__ __launch_bounds__(NW * KG * kWave, 2) void k_attend(AttendArgs a) {
 
   // A round's scores are made while the round before becomes weights: matrix and vector instructions of one wave side by side.  Keys are
   // asked for two rounds ahead, values one.
-  const bool asks = qr < n && (!keep || keep[min(qr, n - 1)] != 0);
+  const bool mixed = all_see < end;  // some queries see fewer keys than others
   if (keep) {
     fill_window(0);
     fill_window(1);
   }
-  if (a.causal && threadIdx.x < 2 * KG) found[threadIdx.x] = 0;
+  if (mixed && threadIdx.x < 2 * KG) found[threadIdx.x] = 0;
   if (keep) __syncthreads();
+  look_up(group);
   ask_keys(0);
   ask_values(0);
+  const unsigned long long there_first = PAGED ? asked.there : 0;
   ask_keys(1);
   auto key_of = [&](int round) { return (round * KG + group) * KK; };
-  auto hidden = [&](f32x16 (&s)[kBlocks], int round) {
-    if (round >= whole) hide(s, seen_of(key_of(round), rows_there(round * KG + group), asks));
+  // of a round's keys, those that are there (of a cache: as they were asked for)
+  auto there_of = [&](int round, unsigned long long pages) { return PAGED ? pages : rows_there(round * KG + group); };
+  constexpr unsigned long long kAll = KK == 64 ? ~0ull : 0xffffffffull;
+  auto hidden = [&](f32x16 (&s)[kBlocks], int round, unsigned long long pages) {
+    if (round >= whole || (PAGED && pages != kAll)) hide(s, seen_of(key_of(round), there_of(round, pages)));
   };
   f32x16 s0[kBlocks], s1[kBlocks];
   vm_wait<2 * kLoads>();
@@ -307,22 +395,25 @@ __global__ __launch_bounds__(NW * KG * kWave, 2) void k_attend(AttendArgs a) {
   clear(s0);
 #pragma unroll
   for (int i = 0; i < kPieces; ++i) scores_part(s0, lds + keys0, i);
-  hidden(s0, 0);
+  hidden(s0, 0, there_first);
   raise(most_of(s0));
+  unsigned long long there_now = there_first;
   auto body = [&](int round, f32x16 (&s)[kBlocks], f32x16 (&next)[kBlocks]) {
     const int k0 = key_of(round), turn = round & 1;
     vm_wait<0>();
     __syncthreads();  // the next keys and the values are there, and nobody reads the stages that are filled now any more
     if (keep && round > 0 && k0 / 4096 * 4096 == k0 - group * KK) fill_window(k0 / 4096 + 1);  // (in the place of the window before)
-    ask_keys(round + 2);
     ask_values(round + 1);
-    const bool partly = a.causal && round >= whole;
+    const unsigned long long there_next = PAGED ? asked.there : 0, there = there_now;
+    there_now = there_next;
+    ask_keys(round + 2);
+    const bool partly = mixed && round >= whole;
     if (partly) {
       take_out(turn);
       __syncthreads();
       if (threadIdx.x < KG) found[(turn ^ 1) * KG + threadIdx.x] = 0;  // (the next round's, whose last reader has passed this barrier)
     }
-    if (k0 >= end || (a.causal && k0 > qw + 31)) return;  // (no keys, or none that the wave's queries see, from here on)
+    if (k0 >= wave_sees) return;  // (no keys that the wave's queries see, from here on)
     const unsigned char *ks = lds + keys0 + (turn ^ 1) * L::kPart, *vs = lds + values0 + turn * L::kPart;
     clear(next);
     const float shift = shift_of(top);
@@ -360,9 +451,9 @@ __global__ __launch_bounds__(NW * KG * kWave, 2) void k_attend(AttendArgs a) {
 #pragma unroll
         for (int dt = 0; dt < kDt; ++dt) acc[dt] = mma32(from[(8 * (e / 4) + e % 4) * DP + 32 * dt], s[0][e], acc[dt]);
     }
-    hidden(next, round + 1);
+    hidden(next, round + 1, there_next);
     const float most = most_of(next);
-    if (partly && found[turn * KG + group]) add_back(k0, rows_there(k0 / KK), asks);
+    if (partly && found[turn * KG + group]) add_back(k0, there_of(round, there));
     raise(most);
   };
   for (int round = 0; round < rounds;) {
@@ -415,10 +506,18 @@ __global__ __launch_bounds__(NW * KG * kWave, 2) void k_attend(AttendArgs a) {
     }
   }
 
-  // out: the lane's query, channels 32 t + 16 * half .. + 15
-  const bool none = sum == 0.f;
-  const float inv = 1.f / sum;
-  ET* const out = reinterpret_cast<ET*>(a.out) + (row0 + (long long)qr) * a.ldo + head * a.D;
+  // out: the lane's query, channels 32 t + 16 * half .. + 15; of a part of the keys its sums as they are, maximum and sum of weights beside
+  const bool parts = PAGED && cache.part_out, none = sum == 0.f;
+  const float inv = parts ? 1.f : 1.f / sum;
+  long long at = 0;
+  if constexpr (PAGED) {
+    at = ((long long)(part.shared ? cache.splits + part.split : part.split) * cache.T + my_row) * a.heads + head;
+    if (parts && in && half == 0) {
+      cache.part_stat[2 * at] = top;
+      cache.part_stat[2 * at + 1] = sum;
+    }
+  }
+  ET* const out = reinterpret_cast<ET*>(a.out) + my_row * a.ldo + head * a.D;
 #pragma unroll
   for (int t = 0; t < kDt; ++t) {
     float v[16];
@@ -437,7 +536,12 @@ __global__ __launch_bounds__(NW * KG * kWave, 2) void k_attend(AttendArgs a) {
 #pragma unroll
     for (int g = 0; g < 2; ++g) {
       const int d = 32 * t + 16 * half + 8 * g;
-      if (qr < n && d < a.D) {
+      if (!in || d >= a.D) continue;
+      if (parts) {
+        piece8<float> p;
+        p.put(f[g]);
+        p.store(cache.part_out + at * a.D, d / 8);
+      } else {
         piece8<ET> p;
         p.put(f[g]);
         p.store(out, d / 8);
@@ -446,30 +550,25 @@ __global__ __launch_bounds__(NW * KG * kWave, 2) void k_attend(AttendArgs a) {
   }
 }
 
-template <typename ET, int DC, int NW, int KG, int KK>
+template <typename ET, int DC, int NW, int KG, int KK, bool PAGED>
 int ask_tile_lds() {
-  return hipFuncSetAttribute(reinterpret_cast<const void*>(&k_attend<ET, DC, NW, KG, KK>), hipFuncAttributeMaxDynamicSharedMemorySize,
+  return hipFuncSetAttribute(reinterpret_cast<const void*>(&k_attend<ET, DC, NW, KG, KK, PAGED>), hipFuncAttributeMaxDynamicSharedMemorySize,
                              (Tile<ET, DC, KK>::all_bytes(NW, KG))) == hipSuccess ? LAUD_OK : LAUD_ERR_HIP;
 }
-template <typename ET, int DC, int NW, int KG, int KK>
-int launch_tiles(AttendArgs a, hipStream_t st) {
-  const long long tiles = tiles_of(a.T, a.B, 1, NW * 32), groups = (tiles * a.heads + 7) / 8 * 8;
-  if (!launchable((double)groups, NW * KG * kWave)) return LAUD_ERR_UNSUPPORTED;
-  a.tiles = (int)tiles;
-  constexpr int lds = Tile<ET, DC, KK>::all_bytes(NW, KG);
-  if (lds > 65536 && ask_tile_lds<ET, DC, NW, KG, KK>() != LAUD_OK) return LAUD_ERR_HIP;
-  hipLaunchKernelGGL((k_attend<ET, DC, NW, KG, KK>), dim3((unsigned)groups), dim3(NW * KG * kWave), lds, st, a);
-  return check_launch();
+template <typename ET, int DC, int NW, int KG, int KK, bool PAGED>
+void launch_tiles(const AttendArgs& a, const CachedArgs& cache, unsigned groups, hipStream_t st) {
+  hipLaunchKernelGGL((k_attend<ET, DC, NW, KG, KK, PAGED>), dim3(groups), dim3(NW * KG * kWave), (Tile<ET, DC, KK>::all_bytes(NW, KG)), st, a, cache);
 }
 
 template <typename ET, int DC>
-int launch_attend(const AttendArgs& a, hipStream_t st) {
-  constexpr bool kHalf = sizeof(ET) == 2;
-#ifdef LAUD_TILE
-  return launch_tiles<ET, DC, LAUD_TILE>(a, st);
-#endif
-  if constexpr (kHalf) return launch_tiles<ET, DC, 4, 1, 64>(a, st);
-  else return launch_tiles<ET, DC, 4, 1, 32>(a, st);
+int launch_attend(AttendArgs a, hipStream_t st) {
+  constexpr int kWaves = 4;
+  const long long tiles = tiles_of(a.T, a.B, 1, kWaves * 32), groups = (tiles * a.heads + 7) / 8 * 8;
+  if (!launchable((double)groups, kWaves * kWave)) return LAUD_ERR_UNSUPPORTED;
+  if (attend_init_device() != LAUD_OK) return LAUD_ERR_HIP;
+  a.tiles = (int)tiles;
+  launch_tiles<ET, DC, kWaves, 1, (sizeof(ET) == 2 ? 64 : 32), false>(a, CachedArgs{}, (unsigned)groups, st);
+  return check_launch();
 }
 template <typename ET>
 int launch_width(const AttendArgs& a, hipStream_t st) {
@@ -480,6 +579,32 @@ int launch_width(const AttendArgs& a, hipStream_t st) {
 }
 
 }  // namespace
+
+// LDS of every instance (more than the 64 KB that a launch may take unasked)
+int attend_init_device() {
+  static std::atomic<unsigned> done{0};  // one bit per device ordinal (ordinals >= 32 repeat the request)
+  int dev = 0;
+  if (hipGetDevice(&dev) != hipSuccess) return LAUD_ERR_HIP;
+  const unsigned bit = dev >= 0 && dev < 32 ? 1u << dev : 0u;
+  if (bit && (done.load(std::memory_order_acquire) & bit)) return LAUD_OK;
+  for (int rc : {ask_tile_lds<bf16_t, 32, 4, 1, 64, false>(), ask_tile_lds<bf16_t, 64, 4, 1, 64, false>(), ask_tile_lds<bf16_t, 96, 4, 1, 64, false>(),
+                 ask_tile_lds<bf16_t, 128, 4, 1, 64, false>(), ask_tile_lds<float, 32, 4, 1, 32, false>(), ask_tile_lds<float, 64, 4, 1, 32, false>(),
+                 ask_tile_lds<float, 96, 4, 1, 32, false>(), ask_tile_lds<float, 128, 4, 1, 32, false>(), ask_tile_lds<bf16_t, 64, 4, 1, 64, true>(),
+                 ask_tile_lds<bf16_t, 128, 4, 1, 64, true>()})
+    if (rc != LAUD_OK) return rc;
+  done.fetch_or(bit, std::memory_order_release);
+  return LAUD_OK;
+}
+
+void launch_many_rows(const CachedArgs& c, unsigned groups, hipStream_t st) {
+  AttendArgs a{};
+  a.heads = c.heads; a.group = c.group; a.D = c.D; a.c = c.c;
+  a.q = c.q; a.out = c.out; a.ldq = c.ldq; a.ldo = c.ldo;
+  a.ldk = a.ldv = c.D;
+  if (c.D <= 64) launch_tiles<bf16_t, 64, 4, 1, 64, true>(a, c, groups, st);
+  else launch_tiles<bf16_t, 128, 4, 1, 64, true>(a, c, groups, st);
+}
+
 }  // namespace laud
 
 extern "C" int laud_attention(const laud_heads* p, int B, const int32_t* offsets, int T, const void* q, int64_t ldq, const void* k, int64_t ldk,

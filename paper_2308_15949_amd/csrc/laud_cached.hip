@@ -1,44 +1,10 @@
 // Attention of new tokens over a paged cache: parts of the keys by workgroup, joined where there are several.
-#include "laud_heads.h"
+#include "laud_cached.h"
 
 namespace laud {
 namespace {
 
-struct CachedArgs {
-  int heads, group, kv_heads, D, causal, B, T, pages, page_bits, table_ld, prefix_len;
-  // of the sequences' own keys, and of the prefix, whose workgroups come first: tiles of query rows, and parts that a tile's keys are
-  // shared out over; all parts of a row are joined, its own first
-  int tiles, splits, prefix_tiles, prefix_splits;
-  unsigned prefix_groups;
-  int by_xcd, prefix_by_xcd;
-  // rows of this call in place of a cache: how far apart, and which the masker kept
-  int64_t ldk, ldv;
-  const uint8_t* keep;
-  float c;                // scale * log2(e)
-  unsigned group_by, group_shift;  // x / group = x * group_by >> group_shift (x below 2^31)
-  const int32_t *offsets, *lens, *table, *prefix;
-  const uint8_t *k, *v;
-  const float *ks, *vs;
-  const void* q;
-  void* out;
-  float *part_out, *part_stat;  // [parts][T * heads][D] and [parts][T * heads][2]: maximum and sum
-  int64_t ldq, ldo;
-};
-
-constexpr int kWaves = 4, kMaxParts = 64, kPartStep = 128;
-// Keys of a part: the same for every tile of a sequence, so that whoever joins the parts knows how many there are.
-__device__ __forceinline__ int part_keys(int len, int splits) {
-  const int each = (len + splits - 1) / splits;
-  return max((each + kPartStep - 1) / kPartStep * kPartStep, kPartStep);
-}
-__device__ __forceinline__ int parts_of(int len, int splits) {  // how many of them have keys; one where there are none
-  const int each = part_keys(len, splits);
-  return max((len + each - 1) / each, 1);
-}
-__device__ __forceinline__ int cached_tokens(const CachedArgs& a, int b) {
-  const long long room = (long long)a.table_ld << a.page_bits;
-  return (int)min((long long)max(a.lens[b], 0), room);
-}
+constexpr int kWaves = kCachedWaves;
 
 // ---- operands ---------------------------------------------------------------------------------------------------------------
 // CT: the cache's type.  A step has GROUPS times sixteen keys; lane l holds key l % 16 of each for the scores (keys * queries: a lane's
@@ -241,9 +207,8 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void k_cached(CachedArgs a) {
   if (split > 0 && (long long)split * each >= len) return;
   const long long past = (long long)(shared || ROWS ? len : a.lens[b]) - n;  // position of the first token
   const bool causal = a.causal && !shared;
-  auto token_of = [&](unsigned row) { return (unsigned)((unsigned long long)row * a.group_by >> a.group_shift); };
   auto limit_of = [&](unsigned row) -> int {  // keys that a row sees
-    return causal ? (int)min(max(past + token_of(row) + 1, 0ll), (long long)len) : len;
+    return causal ? (int)min(max(past + token_of(a, row) + 1, 0ll), (long long)len) : len;
   };
   const int begin = split * each;
   const int end = __builtin_amdgcn_readfirstlane(min(min(begin + each, len), limit_of(first_row + there - 1)));
@@ -259,7 +224,7 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void k_cached(CachedArgs a) {
   tok_u4 q[O::kQuery];
 #pragma unroll
   for (int t = 0; t < RT; ++t) {
-    const unsigned row = first_row + t * 16 + r16, token = token_of(row);
+    const unsigned row = first_row + t * 16 + r16, token = token_of(a, row);
     const bool in = t * 16 + r16 < there;
     limit[t] = in && (!keep || keep[token] != 0) ? limit_of(row) : 0;
     if (kQueryLds && t % kWaves != wave) continue;
@@ -347,6 +312,7 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void k_cached(CachedArgs a) {
     load_keys(here);
     load_values(here);
   }
+#pragma unroll 1
   for (; key < end; key += kStride) {
     const Place next = place_of(key + kStride);  // (past the end: no keys)
     bool whole = key + kKeys <= all_see;
@@ -501,7 +467,7 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void k_cached(CachedArgs a) {
     }
     if (t * 16 + r >= there) continue;
     const unsigned row = first_row + t * 16 + r;
-    const unsigned token = token_of(row);
+    const unsigned token = token_of(a, row);
     const long long tok = row0 + token;
     const int h = hk * a.group + (int)(row - token * a.group);
     if (a.splits + a.prefix_splits > 1) {
@@ -587,16 +553,23 @@ void set_group(CachedArgs& a, int group) {
 
 // ---- plan -------------------------------------------------------------------------------------------------------------------
 struct Plan {
-  int rt;                   // row tiles of a workgroup
+  int rt;                   // row tiles of a workgroup; 0: the kernel of many rows
   int own, shared;          // parts of the sequences' own keys, and of the prefix
   long long tiles, prefix_tiles;
   size_t stat_at, bytes;    // workspace: sums, then statistics
 };
-inline int row_tiles(double rows) { return rows <= 16 ? 1 : 2; }
+// Which kernel: a workgroup of sixteen rows, of 32, or of 128 with its keys through LDS.  The last two, in us (sequences x new tokens + cached
+// ones, 32 heads of 128 over 8, bf16): 1 x 512 + 8000 207, 145;  2 x 200 + 4000 105, 94;  8 x 64 + 4000 120, 122;  16 x 12 + 4000 75, 95.  In
+// float32 32 rows are the faster ones (4 x 300 + 2000, 16 heads of 64: 157, 187), and behind a prefix (32 x 1 + 500 behind 16384: 41, 47).
+inline int row_tiles(double rows, double of_a_sequence, int type) {
+  return type == LAUD_BF16 && of_a_sequence >= 512 ? 0 : rows <= 16 ? 1 : 2;
+}
 
-// Parts: as many workgroups as keep the card's 256 compute units busy for a few rounds, none of fewer than 128 keys.
-inline int parts_for(double groups, long long keys, int most) {
-  const double want = 1024.0 / groups;
+// Parts: as many as make so many workgroups, none of fewer than 128 keys.  1024 where a few rows wait for memory, 512 where many rows keep
+// the matrix cores busy; with a prefix 256 each for it and for the sequences' own keys (32 x 1 + 500 behind 16384: 52 us with 1024, 46 with
+// 512, 41 with 256, 59 with 128: whatever is split is joined again).
+inline int parts_for(double workgroups, double groups, long long keys, int most) {
+  const double want = workgroups / groups;
   const long long room = (keys + kPartStep - 1) / kPartStep;
   return (int)max(1ll, min(min((long long)(want + 0.999), room), (long long)most));
 }
@@ -606,13 +579,14 @@ Plan plan_of(const laud_heads* p, const laud_cache* c, const laud_batch* b, int 
   const int group = p->heads / p->kv_heads;
   const bool prefix = b->prefix_len > 0;
   const double rows = (double)T * group;
-  s.rt = row_tiles(prefix ? rows : rows / b->B);
-  s.tiles = tiles_of(T, b->B, group, 16 * s.rt);
-  const double busy = max((double)b->B, rows / (16 * s.rt)) * p->kv_heads;
-  s.own = parts_for(busy, (long long)b->table_ld * c->page, prefix ? kMaxParts / 2 : kMaxParts);
+  s.rt = row_tiles(prefix ? rows : rows / b->B, rows / b->B, c->dtype);
+  const int per = s.rt ? 16 * s.rt : kManyRows;
+  s.tiles = tiles_of(T, b->B, group, per);
+  const double busy = max((double)b->B, rows / per) * p->kv_heads;
+  s.own = parts_for(prefix ? 256 : s.rt ? 1024 : 512, busy, (long long)b->table_ld * c->page, prefix ? kMaxParts / 2 : kMaxParts);
   if (prefix) {
-    s.prefix_tiles = ((long long)T * group - 1) / (16 * s.rt) + 1;
-    s.shared = parts_for((double)s.prefix_tiles * p->kv_heads, b->prefix_len, kMaxParts / 2);
+    s.prefix_tiles = ((long long)T * group - 1) / per + 1;
+    s.shared = parts_for(256, (double)s.prefix_tiles * p->kv_heads, b->prefix_len, kMaxParts / 2);
   }
   if (s.own + s.shared > 1) {
     const size_t all = (size_t)(s.own + s.shared) * T * p->heads;
@@ -623,22 +597,24 @@ Plan plan_of(const laud_heads* p, const laud_cache* c, const laud_batch* b, int 
 }
 
 template <typename ET, typename CT, int DP, int RT, bool ROWS>
-int launch_cached(const CachedArgs& a, hipStream_t st) {
+void launch_cached(const CachedArgs& a, unsigned groups, hipStream_t st) {
   constexpr int kLds = kWaves * 16 * (DP + 4) * 4 + kWaves * 16 * RT * 8;
-  const double groups = (double)a.tiles * a.kv_heads * a.splits + a.prefix_groups;
-  if (!launchable(groups, kWaves * kWave)) return LAUD_ERR_UNSUPPORTED;
-  hipLaunchKernelGGL((k_cached<ET, CT, DP, RT, ROWS>), dim3((unsigned)groups), dim3(kWaves * kWave), kLds, st, a);
-  return LAUD_OK;
+  hipLaunchKernelGGL((k_cached<ET, CT, DP, RT, ROWS>), dim3(groups), dim3(kWaves * kWave), kLds, st, a);
 }
-template <typename ET, typename CT, int DP>
-int launch_rows(const CachedArgs& a, int rt, hipStream_t st) {
-  if (rt == 1) return launch_cached<ET, CT, DP, 1, false>(a, st);
-  return launch_cached<ET, CT, DP, 2, false>(a, st);
+template <typename ET, typename CT>
+void launch_rows(const CachedArgs& a, int rt, unsigned groups, hipStream_t st) {
+  if (a.D <= 64) {
+    if (rt == 1) launch_cached<ET, CT, 64, 1, false>(a, groups, st);
+    else launch_cached<ET, CT, 64, 2, false>(a, groups, st);
+  } else {
+    if (rt == 1) launch_cached<ET, CT, 128, 1, false>(a, groups, st);
+    else launch_cached<ET, CT, 128, 2, false>(a, groups, st);
+  }
 }
-int launch_types(const CachedArgs& a, int cache_type, int rt, hipStream_t st) {
-  if (cache_type == LAUD_F32) return a.D <= 64 ? launch_rows<float, float, 64>(a, rt, st) : launch_rows<float, float, 128>(a, rt, st);
-  if (cache_type == LAUD_BF16) return a.D <= 64 ? launch_rows<bf16_t, bf16_t, 64>(a, rt, st) : launch_rows<bf16_t, bf16_t, 128>(a, rt, st);
-  return a.D <= 64 ? launch_rows<bf16_t, uint8_t, 64>(a, rt, st) : launch_rows<bf16_t, uint8_t, 128>(a, rt, st);
+void launch_types(const CachedArgs& a, int cache_type, int rt, unsigned groups, hipStream_t st) {
+  if (cache_type == LAUD_F32) launch_rows<float, float>(a, rt, groups, st);
+  else if (cache_type == LAUD_BF16) launch_rows<bf16_t, bf16_t>(a, rt, groups, st);
+  else launch_rows<bf16_t, uint8_t>(a, rt, groups, st);
 }
 
 }  // namespace
@@ -654,10 +630,15 @@ int attend_few(const laud_heads& p, int B, const int32_t* offsets, int T, const 
   const long long tiles = tiles_of(T, B, a.group, 16);
   if (!launchable((double)tiles * a.kv_heads, kWaves * kWave)) return LAUD_ERR_UNSUPPORTED;
   a.tiles = (int)tiles;
-  int status;
-  if (p.dtype == LAUD_F32) status = p.D <= 64 ? launch_cached<float, float, 64, 1, true>(a, st) : launch_cached<float, float, 128, 1, true>(a, st);
-  else status = p.D <= 64 ? launch_cached<bf16_t, bf16_t, 64, 1, true>(a, st) : launch_cached<bf16_t, bf16_t, 128, 1, true>(a, st);
-  return status ? status : check_launch();
+  const unsigned groups = (unsigned)(tiles * a.kv_heads);
+  if (p.dtype == LAUD_F32) {
+    if (p.D <= 64) launch_cached<float, float, 64, 1, true>(a, groups, st);
+    else launch_cached<float, float, 128, 1, true>(a, groups, st);
+  } else {
+    if (p.D <= 64) launch_cached<bf16_t, bf16_t, 64, 1, true>(a, groups, st);
+    else launch_cached<bf16_t, bf16_t, 128, 1, true>(a, groups, st);
+  }
+  return check_launch();
 }
 
 namespace {
@@ -667,7 +648,7 @@ int check_cached(const laud_heads* p, const laud_cache* c, const laud_batch* b, 
   int bad = check_heads(p);
   if (!bad) bad = check_cache(c, b);
   if (bad) return bad;
-  if (T < 0 || p->kv_heads != c->kv_heads || p->D != c->D || b->prefix_len < 0 || (b->prefix_len > 0 && (!b->prefix || !aligned4(b->prefix))) ||
+  if (T < 0 || p->kv_heads != c->kv_heads || p->D != c->D || b->prefix_len < 0 || b->prefix_len > 1 << 30 || (b->prefix_len > 0 && (!b->prefix || !aligned4(b->prefix))) ||
       !(c->dtype == p->dtype || (c->dtype == LAUD_E4M3 && p->dtype == LAUD_BF16)))
     return LAUD_ERR_INVALID_ARG;
   if ((int64_t)T * p->heads > INT32_MAX) return LAUD_ERR_UNSUPPORTED;
@@ -704,6 +685,7 @@ extern "C" int laud_cache_attention(const laud_heads* p, const laud_cache* c, co
     for (const Span& x : BatchSpans(b).s)
       if (ranges_meet(ws, s.bytes, x.p, x.n)) return LAUD_ERR_INVALID_ARG;
   }
+  if (s.rt == 0 && attend_init_device() != LAUD_OK) return LAUD_ERR_HIP;
   const double own = (double)s.tiles * p->kv_heads * s.own, shared = (double)s.prefix_tiles * p->kv_heads * s.shared;
   if (!launchable(own + shared, kWaves * kWave) || !launchable((double)T * p->heads, 256)) return LAUD_ERR_UNSUPPORTED;
   CachedArgs a{};
@@ -712,7 +694,7 @@ extern "C" int laud_cache_attention(const laud_heads* p, const laud_cache* c, co
   a.pages = c->pages; a.page_bits = page_bits(c); a.table_ld = b->table_ld;
   a.tiles = (int)s.tiles; a.splits = s.own; a.prefix_tiles = (int)s.prefix_tiles; a.prefix_splits = s.shared;
   a.prefix_groups = (unsigned)shared; a.prefix_len = b->prefix_len;
-  a.by_xcd = s.rt > 1 && (long long)p->kv_heads * s.own % 8 == 0;
+  a.by_xcd = s.rt != 1 && (long long)p->kv_heads * s.own % 8 == 0;
   a.prefix_by_xcd = (long long)p->kv_heads * s.shared % 8 == 0;
   a.c = p->scale * kLog2e;
   a.offsets = b->offsets; a.lens = b->lens; a.table = b->table; a.prefix = b->prefix;
@@ -722,8 +704,8 @@ extern "C" int laud_cache_attention(const laud_heads* p, const laud_cache* c, co
   a.part_stat = s.bytes ? (float*)((char*)ws + s.stat_at) : nullptr;
   clear_stale_error();
   hipStream_t st = (hipStream_t)stream;
-  const int status = launch_types(a, c->dtype, s.rt, st);
-  if (status) return status;
+  if (s.rt == 0) launch_many_rows(a, (unsigned)(own + shared), st);
+  else launch_types(a, c->dtype, s.rt, (unsigned)(own + shared), st);
   if (s.own + s.shared > 1) {
     const dim3 grid((unsigned)T * (unsigned)p->heads);
     if (p->dtype == LAUD_BF16) hipLaunchKernelGGL((k_join<bf16_t>), grid, dim3(256), 0, st, a);

@@ -110,7 +110,7 @@ inline int check_cache(const laud_cache* c, const laud_batch* b) {
   if (!c->k || !c->v || !aligned16(c->k) || !aligned16(c->v) ||
       (c->dtype == LAUD_E4M3 && (!c->k_scale || !c->v_scale || !aligned16(c->k_scale) || !aligned16(c->v_scale))))
     return LAUD_ERR_INVALID_ARG;
-  if (b->B && (b->table_ld <= 0 || (int64_t)b->table_ld * c->page > INT32_MAX)) return LAUD_ERR_INVALID_ARG;
+  if (b->B && (b->table_ld <= 0 || (int64_t)b->table_ld * c->page > 1 << 30)) return LAUD_ERR_INVALID_ARG;
   return LAUD_OK;
 }
 inline int page_bits(const laud_cache* c) { return __builtin_ctz((unsigned)c->page); }
