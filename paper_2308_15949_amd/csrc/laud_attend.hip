@@ -5,7 +5,6 @@
 #include "laud_cached.h"
 
 namespace laud {
-namespace {
 
 struct AttendArgs {
   int heads, group, D, causal, B, T, tiles;  // group: query heads of a key head; tiles: of queries, over all sequences (tiles_of)
@@ -26,7 +25,7 @@ struct AttendArgs {
 // bf16.
 constexpr int kMaskWords = 128;  // 64 keys' bits each: two windows of 4096 keys
 template <typename ET, int DC, int KK>
-struct Tile {
+struct AttendTile {
   static constexpr int DP = DC <= 64 ? 64 : 128;  // channels of a row in LDS; the first DC of them are multiplied
   static constexpr bool kHalf = sizeof(ET) == 2;
   static constexpr int kRow = DP * (int)sizeof(ET);  // bytes of a row in LDS
@@ -65,7 +64,7 @@ constexpr float kSlack = 8.f;
 
 template <typename ET, int DC, int NW, int KG, int KK, bool PAGED>
 __global__ __launch_bounds__(NW * KG * kWave, 2) void k_attend(AttendArgs a, CachedArgs cache) {
-  typedef Tile<ET, DC, KK> L;
+  typedef AttendTile<ET, DC, KK> L;
   constexpr int DP = L::DP;
   constexpr bool kHalf = L::kHalf;
   constexpr int kBlocks = KK / 32, kRows = NW * 32, kDt = DC / 32, kEb = (int)sizeof(ET);
@@ -553,11 +552,11 @@ __global__ __launch_bounds__(NW * KG * kWave, 2) void k_attend(AttendArgs a, Cac
 template <typename ET, int DC, int NW, int KG, int KK, bool PAGED>
 int ask_tile_lds() {
   return hipFuncSetAttribute(reinterpret_cast<const void*>(&k_attend<ET, DC, NW, KG, KK, PAGED>), hipFuncAttributeMaxDynamicSharedMemorySize,
-                             (Tile<ET, DC, KK>::all_bytes(NW, KG))) == hipSuccess ? LAUD_OK : LAUD_ERR_HIP;
+                             (AttendTile<ET, DC, KK>::all_bytes(NW, KG))) == hipSuccess ? LAUD_OK : LAUD_ERR_HIP;
 }
 template <typename ET, int DC, int NW, int KG, int KK, bool PAGED>
 void launch_tiles(const AttendArgs& a, const CachedArgs& cache, unsigned groups, hipStream_t st) {
-  hipLaunchKernelGGL((k_attend<ET, DC, NW, KG, KK, PAGED>), dim3(groups), dim3(NW * KG * kWave), (Tile<ET, DC, KK>::all_bytes(NW, KG)), st, a, cache);
+  hipLaunchKernelGGL((k_attend<ET, DC, NW, KG, KK, PAGED>), dim3(groups), dim3(NW * KG * kWave), (AttendTile<ET, DC, KK>::all_bytes(NW, KG)), st, a, cache);
 }
 
 template <typename ET, int DC>
@@ -577,8 +576,6 @@ int launch_width(const AttendArgs& a, hipStream_t st) {
   if (a.D <= 96) return launch_attend<ET, 96>(a, st);
   return launch_attend<ET, 128>(a, st);
 }
-
-}  // namespace
 
 // LDS of every instance (more than the 64 KB that a launch may take unasked)
 int attend_init_device() {

@@ -2,7 +2,6 @@
 #include "laud_cached.h"
 
 namespace laud {
-namespace {
 
 constexpr int kWaves = kCachedWaves;
 
@@ -11,10 +10,10 @@ constexpr int kWaves = kCachedWaves;
 // results are keys 4 * (l / 16) .. +3 of its query, l % 16), and of the values keys 4 * (l / 16) .. +3, elements kEach * (l % 16) .. of
 // each: all of a row's bytes come in one piece a lane, straight into registers, and with element e of every lane the matrix instruction
 // makes channels kEach * m + e, m = 0 .. 15.  Nothing has to change lanes between the two products.
-template <typename CT, int DP, int GROUPS> struct Operands;
+template <typename CT, int DP, int GROUPS> struct CacheOperands;
 
 template <int DP, int GROUPS>
-struct Operands<bf16_t, DP, GROUPS> {
+struct CacheOperands<bf16_t, DP, GROUPS> {
   static constexpr int kGroups = GROUPS, kEach = DP / 16, kPieces = DP / 32, kQuery = DP / 32;
   static constexpr int kBytes = 2;
   tok_u4 k[kGroups][kPieces];
@@ -65,7 +64,7 @@ struct Operands<bf16_t, DP, GROUPS> {
 };
 
 template <int DP, int GROUPS>
-struct Operands<uint8_t, DP, GROUPS> {
+struct CacheOperands<uint8_t, DP, GROUPS> {
   static constexpr int kGroups = GROUPS, kEach = DP / 16, kPieces = DP / 64, kQuery = DP / 32;
   static constexpr int kBytes = 1;
   tok_u4 k[kGroups][kPieces];
@@ -118,7 +117,7 @@ struct Operands<uint8_t, DP, GROUPS> {
 };
 
 template <int DP, int GROUPS>
-struct Operands<float, DP, GROUPS> {
+struct CacheOperands<float, DP, GROUPS> {
   static constexpr int kGroups = GROUPS, kEach = DP / 16, kPieces = DP / 16, kQuery = DP / 16;
   static constexpr int kBytes = 4;
   tok_u4 k[kGroups][kPieces];
@@ -163,7 +162,7 @@ __device__ __forceinline__ f32x4 of_four(float v) { return f32x4{dpp_movf<0x00>(
 // fetched once for all of them.  Four waves share a part's keys, each takes every fourth step of 16 or 32 keys; their sums are joined through LDS.
 template <typename ET, typename CT, int DP, int RT, bool ROWS>
 __global__ __launch_bounds__(kWaves * kWave, 2) void k_cached(CachedArgs a) {
-  typedef Operands<CT, DP, (sizeof(CT) == 4 ? 1 : 2)> O;
+  typedef CacheOperands<CT, DP, (sizeof(CT) == 4 ? 1 : 2)> O;
   constexpr bool kWide = sizeof(CT) == 4;  // float32 instructions
   constexpr int kGroups = O::kGroups, kKeys = 16 * kGroups, kRows = 16 * RT, kEach = O::kEach, kLdRow = DP + 4;
   extern __shared__ __align__(16) unsigned char lds[];
@@ -540,6 +539,8 @@ __global__ __launch_bounds__(256) void k_join(CachedArgs a) {
   if (total == 0.f) f = f32x4{0.f, 0.f, 0.f, 0.f};
   store4(reinterpret_cast<ET*>(a.out) + token * a.ldo + head * a.D + d, f);
 }
+
+namespace {
 
 // group_by, group_shift: with 2^l the next power of two, the least multiple m / 2^(31 + l) not below 1 / group is off by less than
 // 2^l / 2^(31 + l) / group, which 2^31 rows do not raise to another whole number.

@@ -2,6 +2,8 @@
 workspace between two pages that nobody may touch; sequences of every length from none on, rows behind the last one, pages that are
 none, lengths past the table and below the new tokens, offsets that are out of order."""
 import ctypes as C
+import re
+import subprocess
 
 import numpy as np
 import pytest
@@ -79,11 +81,26 @@ CASES = {
     "attend_f32_40": (attention, [1, 96, 31], 128, 5, 1, 40, F, 0, 0, False, None, True),
     "attend_many": (attention, [2] * 70 + [0] * 70 + [1], 141, 1, 1, 64, H, 1, 0, False),
     "attend_odd_offsets": (attention, [], 150, 2, 1, 64, H, 1, 0, True, [140, 20, -7, 400, 90, 130]),
+    # many rows: every width of a tile in LDS, causal and not, masked, rows further apart, in place
+    "tiles_bf16_8": (attention, [70, 0, 3], 75, 128, 1, 8, H, 1, 8, False),
+    "tiles_bf16_40": (attention, [129, 1], 133, 64, 2, 40, H, 0, 0, True, None, True),
+    "tiles_bf16_72": (attention, [130], 131, 64, 1, 72, H, 1, 24, True),
+    "tiles_bf16_128": (attention, [65, 66], 131, 64, 8, 128, H, 1, 8, False, None, True),
+    "tiles_f32_32": (attention, [100, 33], 140, 216, 1, 32, F, 1, 8, False),
+    "tiles_f32_64": (attention, [131], 132, 216, 2, 64, F, 0, 0, True),
+    "tiles_f32_96": (attention, [70, 64], 134, 216, 1, 96, F, 1, 0, True),
+    "tiles_f32_120": (attention, [33, 98], 131, 216, 4, 120, F, 0, 8, False),
+    "tiles_odd_offsets": (attention, [], 150, 64, 1, 64, H, 1, 0, True, [140, 20, -7, 400, 90, 130]),
     # caches of every type and page, one new token and many, parts and none
     "cached_bf16": (cached, [1, 1, 1], [300, 1, 17], 3, 8, 2, 128, H, H, 16),
     "cached_bf16_tail": (cached, [1, 3, 0, 2], [63, 64, 100, 2], 9, 4, 4, 64, H, H, 32, 8),
     "cached_bf16_rows": (cached, [40, 25], [190, 25], 70, 4, 1, 128, H, H, 64, 8),
     "cached_bf16_many_rows": (cached, [150, 20], [150, 400], 170, 4, 1, 80, H, H, 256, 0),
+    "cached_bf16_tiles": (cached, [70, 60], [260, 60], 133, 16, 1, 128, H, H, 16, 8),
+    "cached_bf16_tiles_64": (cached, [66], [300], 66, 32, 2, 40, H, H, 64, 0, 33),
+    "cached_bf16_tiles_whole": (cached, [66], [90], 66, 16, 1, 64, H, H, 32, 0, 0, 0),
+    "cached_bf16_tiles_bad": (cached, [130], [200], 131, 8, 1, 64, H, H, 16, 0, 0, 1, None, True),
+    "cached_bf16_tiles_short": (cached, [70, 70], [12, -4], 140, 16, 1, 64, H, H, 16),
     "cached_e4m3": (cached, [1, 1], [513, 40], 2, 16, 2, 128, H, E, 128),
     "cached_e4m3_rows": (cached, [30, 9], [200, 9], 39, 3, 1, 48, H, E, 16, 8),
     "cached_e4m3_many_rows": (cached, [90], [700], 90, 5, 1, 128, H, E, 32),
@@ -105,10 +122,25 @@ CASES = {
 }
 
 
+# The kernels that a case is there for: type, channels multiplied, whether keys are a cache's.
+REACHES = {name: f"k_attend<{'unsigned short' if '_bf16_' in name or '_odd_' in name else 'float'}, {w}, 4, 1, {64 if '_bf16_' in name or '_odd_' in name else 32}, {p}>"
+           for name, w, p in (("tiles_bf16_8", 32, "false"), ("tiles_bf16_40", 64, "false"), ("tiles_bf16_72", 96, "false"),
+                              ("tiles_bf16_128", 128, "false"), ("tiles_f32_32", 32, "false"), ("tiles_f32_64", 64, "false"),
+                              ("tiles_f32_96", 96, "false"), ("tiles_f32_120", 128, "false"), ("tiles_odd_offsets", 64, "false"),
+                              ("cached_bf16_tiles", 128, "true"), ("cached_bf16_tiles_64", 64, "true"), ("cached_bf16_tiles_bad", 64, "true"))}
+
+
+def test_every_tile_has_a_case(lib):  # noqa: F811
+    symbols = subprocess.run(["nm", "-C", lib], check=True, capture_output=True, text=True).stdout
+    assert set(re.findall(r"k_attend<[\w, ]+>", symbols)) == set(REACHES.values()) - {""}
+
+
 @pytest.mark.parametrize("front", [0, 1])
 @pytest.mark.parametrize("name", CASES)
 def test_kernels_stay_inside_their_buffers(lib, name, front, capfd):  # noqa: F811
     def body():
         f, *args = CASES[name]
-        f(Call(lib, front), *args)
+        call = Call(lib, front)
+        f(call, *args)
+        assert REACHES.get(name, "") in call.launched(), call.launched()
     in_a_process_of_its_own(body, capfd)

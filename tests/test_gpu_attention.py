@@ -215,6 +215,86 @@ def test_a_long_sequence():
     attention_case([3001], 1, 1, 128, F32, False, 26)
 
 
+# Many rows (heads times tokens above 8192 in bf16, 28000 in float32) go through the tiles in LDS.
+WIDE = {BF16: 64, F32: 192}
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("D", [8, 24, 32, 40, 64, 72, 80, 96, 104, 128])
+def test_many_rows_widths(D, dtype):
+    attention_case([33, 1, 130, 0, 70], WIDE[dtype], 2, D, dtype, True, D, extra=8)
+    attention_case([65, 128, 3], WIDE[dtype], WIDE[dtype] // 2, D, dtype, False, D + 1, joined=True, extra=24)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("n", [129, 160, 191, 192, 193, 255, 256, 257, 383, 385])
+def test_many_rows_lengths(n, dtype):
+    attention_case([n, 31, 1], WIDE[dtype], 4, 64, dtype, True, n)
+    attention_case([n, 64], WIDE[dtype] + 4, 4, 128, dtype, False, n + 1, extra=16)   # (heads that eight do not divide)
+
+
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_many_rows_masks(dtype, causal):
+    g = np.random.default_rng(5)
+    for share in (0.0, 0.02, 0.5, 1.0):
+        attention_case([150, 1, 70, 64], WIDE[dtype], 2, 80, dtype, causal, 8, keep=g.random(285) < share, extra=8)
+    first = np.ones(300)
+    first[:200] = 0
+    attention_case([300], WIDE[dtype], 2, 64, dtype, causal, 10, keep=first)
+    attention_case([300], WIDE[dtype], 2, 128, dtype, causal, 11, keep=1 - first)
+
+
+@pytest.mark.parametrize("dtype,heads", [(BF16, 1), (F32, 4)])
+def test_masks_of_more_than_4096_keys(dtype, heads):
+    """The masker's bytes become bits 4096 keys at a time."""
+    g = np.random.default_rng(6)
+    keep = g.random(8700) < 0.6
+    keep[4000:4200] = 0
+    attention_case([8500, 200], heads, 1, 64, dtype, False, 12, keep=keep)
+    attention_case([8700], heads, 1, 32, dtype, True, 13, keep=keep)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("what", [math.nan, math.inf, -math.inf])
+def test_many_rows_special_values(dtype, what):
+    heads = WIDE[dtype]
+
+    def put(q, k, v):
+        v[70, 0, 3] = what
+        v[100, 0, 17], v[100, 0, 18] = what, -what
+        v[33], v[128] = what, -what
+    attention_case([129, 40], heads, 1, 64, dtype, True, 15, change=put)
+    attention_case([129, 40], heads, 1, 128, dtype, True, 16, change=put)
+    attention_case([140, 30], heads, 1, 80, dtype, True, 17, change=lambda q, k, v: (k[139].fill_(math.nan), v[139].fill_(what)))
+    keep = np.ones(170)
+    keep[[5, 66, 140]] = 0
+
+    def masked(q, k, v):
+        for t in (5, 66, 140):
+            q[t], k[t], v[t] = math.nan, what, what
+    attention_case([140, 30], heads, 1, 96, dtype, False, 18, keep=keep, change=masked)
+    attention_case([140, 30], heads, 1, 24, dtype, True, 19, keep=keep, change=masked)
+    attention_case([140, 30], heads, 1, 64, dtype, True, 20, change=lambda q, k, v: (q[3].fill_(math.nan), k[150].fill_(what)))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_many_rows_in_place_strays_and_scales(dtype):
+    heads = WIDE[dtype]
+    attention_case([130, 60], heads, 2, 64, dtype, True, 21, in_place=True, extra=8)
+    attention_case([129], heads, 2, 40, dtype, True, 22, start=130, behind=130)
+    attention_case(list(np.random.default_rng(3).integers(0, 9, 150)), heads, 2, 64, dtype, True, 23, start=3, behind=70)
+    attention_case([190], heads, 2, 128, dtype, True, 24, scale=3.0)
+    attention_case([190], heads, 2, 64, dtype, False, 25, scale=1e-6)
+    # scores that grow from step to step: the sums are taken anew again and again, or not (less than 2^8)
+    for by in (1.0, 0.02):
+        def grow(q, k, v):
+            q[:] = 1.0
+            k[:] = (by * torch.arange(len(k)))[:, None, None]
+        attention_case([300], heads, 2, 64, dtype, True, 26, scale=0.05, change=grow)
+        attention_case([300], heads, 2, 128, dtype, False, 27, scale=0.05, change=lambda q, k, v: (grow(q, k, v), k.neg_()))
+
+
 # ----- over a cache --------------------------------------------------------------------------------------------------------------
 class Paged:
     """A cache of pages that belong to sequences in no order; places nobody wrote hold NaN."""
@@ -334,6 +414,25 @@ def test_several_new_tokens(new, dtype, cache):
     cached_case([new, 3], [new + 50, 3], 5, 1, 128, dtype, cache, 32, new, causal=False, extra=8)
 
 
+@pytest.mark.parametrize("D", [8, 64, 72, 128])
+@pytest.mark.parametrize("page", [16, 64, 256])
+def test_many_new_tokens(page, D):
+    """512 query rows a sequence or more: keys through LDS."""
+    cached_case([130, 140], [130, 400], 16, 2, D, BF16, BF16, page, D + page, extra=8)
+    cached_case([129], [1500], 8, 1, D, BF16, BF16, page, D + page + 1, causal=False, in_place=True)
+    cached_case([300, 250], [190, 0], 24, 8, D, BF16, BF16, page, D + 2, prefix=page + 9, start=2, behind=5)
+
+
+@pytest.mark.parametrize("what", [math.nan, math.inf, -math.inf])
+def test_many_new_tokens_special_values(what):
+    def put(k, v):
+        v[350, 0, 3], v[351, 0, 9] = what, -what
+        v[399] = what
+        k[398] = math.nan
+    cached_case([140, 130], [400, 500], 16, 1, 64, BF16, BF16, 16, 1, change=put)
+    cached_case([140, 130], [400, 500], 16, 1, 128, BF16, BF16, 32, 2, change=put, prefix=70)
+
+
 @pytest.mark.parametrize("heads,kv", [(1, 1), (16, 16), (16, 1), (32, 8), (15, 5), (40, 1), (24, 2)])
 def test_cached_head_layouts(heads, kv):
     for dtype, cache in TYPES:
@@ -378,20 +477,22 @@ def test_cached_special_values_in_8_bits():
     cached_case([20, 2], [29, 40], 2, 1, 128, BF16, E4M3, 16, 2, change=put)
 
 
-def test_pages_that_are_none_hold_no_keys():
+@pytest.mark.parametrize("new", [[1, 2], [90, 40]])
+def test_pages_that_are_none_hold_no_keys(new):
     for dtype, cache_type in TYPES:
         g = gen(9)
-        lens, new = [100, 50], [1, 2]
+        lens, n_new = [100, 50], sum(new)
         cache = Paged(g, lens, 2, 64, cache_type, 16)
         fill(cache, g, lens, 0, dtype)
         bad = cache.table.clone()
         bad[0, 2], bad[0, 5], bad[1, 0] = -1, cache.k.shape[0], 2 ** 31 - 1
         gone = [[2, 5], [0]]
-        q = rand(g, 3, 256).to(dtype)
-        out = torch.zeros(3, 256, device="cuda", dtype=dtype)
-        p = L.make_heads(4, 2, 64, dtype, True)
+        heads = 4 if n_new < 9 else 20
+        q = rand(g, n_new, heads * 64).to(dtype)
+        out = torch.zeros(n_new, heads * 64, device="cuda", dtype=dtype)
+        p = L.make_heads(heads, 2, 64, dtype, True)
         b = L.make_batch(ints(offsets_of(new)), ints(lens), bad)
-        ws = torch.empty(max(L.cache_attention_workspace(p, cache.desc, b, 3), 1), dtype=torch.uint8, device="cuda")
+        ws = torch.empty(max(L.cache_attention_workspace(p, cache.desc, b, n_new), 1), dtype=torch.uint8, device="cuda")
         L.laud_cache_attention(p, cache.desc, b, q.cuda(), out, ws)
         offs = offsets_of(new)
         for i in range(2):
@@ -401,7 +502,7 @@ def test_pages_that_are_none_hold_no_keys():
             for pg in gone[i]:
                 allowed[:, 16 * pg:16 * pg + 16] = False
             rows = slice(int(offs[i]), int(offs[i + 1]))
-            assert near(out[rows].cpu().view(m, 4, 64), *attend64(q[rows].double().view(m, 4, 64), k, v, p.scale, allowed), n, dtype)
+            assert near(out[rows].cpu().view(m, heads, 64), *attend64(q[rows].double().view(m, heads, 64), k, v, p.scale, allowed), n, dtype)
 
 
 def test_a_long_cache():
