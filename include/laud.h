@@ -472,7 +472,7 @@ int laud_moe(const laud_moe_layer* p, int T, const void* x, int64_t ldx, const u
  *   - Weights are softmax(scale * q k) over the tokens that a query sees, and nothing else of the call has any part in its result
  *     (a NaN or an infinity in a token that it does not see stays there).  A score of -infinity has no weight; a query that sees
  *     nothing, or has no weight, gets zeros.
- *   - Scores, statistics and sums are float32.  With bf16 rows a weight is rounded to bf16 where it meets its value (2^-9 of itself,
+ *   - Scores, statistics and sums are float32.  With bf16 rows a weight is rounded to bf16 where it meets its value (2^-8 of itself,
  *     the instructions' operand); with float32 rows it is not.
  */
 typedef struct {
@@ -530,10 +530,11 @@ int laud_cache_read(const laud_cache* c, const laud_batch* b, int T, void* k, in
 
 /*
  * out = attention of new tokens (one, or some) over the cached tokens of their sequence, themselves among them, and over
- * the prefix: a query sees the whole prefix, and the positions up to its own (all of them where p->causal is 0).  The prefix is read once for all
- * sequences.  p->dtype is the cache's type, or LAUD_BF16 where that is LAUD_E4M3.
+ * the prefix: a query sees the whole prefix, and the positions up to its own (all of them where p->causal is 0).  The prefix is read
+ * once for all sequences.  p->dtype is the cache's type, or LAUD_BF16 where that is LAUD_E4M3.
  *   q, out [T] rows; out may be q
  * Long sequences are shared out over workgroups, by the table's size and the number of rows; their parts are joined in order.
+ * T * heads is below 2^31, and below 2^24 where parts are joined (the workspace is not 0; LAUD_ERR_UNSUPPORTED beyond).
  * Workspace: laud_cache_attention_workspace(p, c, b, T) bytes (0 for shapes that need none, and for arguments that the call refuses).
  */
 size_t laud_cache_attention_workspace(const laud_heads* p, const laud_cache* c, const laud_batch* b, int T);

@@ -69,11 +69,13 @@ class Heads(C.Structure):
 class Cache(C.Structure):
     _fields_ = [("pages", C.c_int32), ("page", C.c_int32), ("kv_heads", C.c_int32), ("D", C.c_int32), ("dtype", C.c_int32),
                 ("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p)]
+    device = None  # of its tensors (make_cache)
 
 
 class Batch(C.Structure):
     _fields_ = [("B", C.c_int32), ("table_ld", C.c_int32), ("offsets", C.c_void_p), ("lens", C.c_void_p), ("table", C.c_void_p),
                 ("prefix", C.c_void_p), ("prefix_len", C.c_int32)]
+    device = None  # of its tensors (make_batch)
 
 
 class LaudError(RuntimeError):
@@ -563,7 +565,7 @@ def make_cache(k, v, k_scale=None, v_scale=None) -> Cache:
     code = _dtype_of(k)
     c = Cache(pages, page, h, d, code, _dense(k, k.shape, code, where), _dense(v, k.shape, code, where),
               _dense(k_scale, (pages, h, page), F32, where), _dense(v_scale, (pages, h, page), F32, where))
-    c.held = (k, v, k_scale, v_scale)
+    c.held, c.device = (k, v, k_scale, v_scale), k.get_device()
     return c
 
 
@@ -586,8 +588,15 @@ def make_batch(offsets, lens, table, prefix=None, prefix_len: int = 0) -> Batch:
     if offsets.shape[0] != n + 1 or table.shape[0] != n or (n and not table.shape[1]) or prefix_len < 0 or (prefix_len and prefix is None):
         _bad(where)
     b = Batch(n, int(table.shape[1]), *v, int(prefix_len))
-    b.held, b.prefix_pages = (offsets, lens, table, prefix), 0 if prefix is None else int(prefix.shape[0])
+    b.held, b.device, b.prefix_pages = (offsets, lens, table, prefix), lens.get_device(), 0 if prefix is None else int(prefix.shape[0])
     return b
+
+
+def _here(c: Cache, b: Batch, t, where: str) -> None:
+    """Refuses descriptors over another device than the rows t (which the call checks against the current one)."""
+    d = t.get_device()
+    if c.device not in (None, d) or b.device not in (None, d):
+        _bad(where)
 
 
 def laud_attention(p: Heads, offsets, q, k, v, keep, out) -> None:
@@ -600,6 +609,7 @@ def laud_attention(p: Heads, offsets, q, k, v, keep, out) -> None:
 
 def laud_cache_write(c: Cache, b: Batch, k, v) -> None:
     """Rows k, v [T][kv_heads * D] to their places in the cache."""
+    _here(c, b, k, "laud_cache_write")
     s = (_calls or _token_calls()).cache_write(c, b, k, v)
     if s:
         raise LaudError(s, "laud_cache_write")
@@ -607,6 +617,7 @@ def laud_cache_write(c: Cache, b: Batch, k, v) -> None:
 
 def laud_cache_read(c: Cache, b: Batch, k, v) -> None:
     """Rows k, v [T][kv_heads * D] from their places in the cache."""
+    _here(c, b, k, "laud_cache_read")
     s = (_calls or _token_calls()).cache_read(c, b, k, v)
     if s:
         raise LaudError(s, "laud_cache_read")
@@ -620,6 +631,7 @@ def laud_cache_attention(p: Heads, c: Cache, b: Batch, q, out, ws=None) -> None:
     """q, out [T][heads * D]: new tokens over the cached ones of their sequences."""
     if b.prefix_len > getattr(b, "prefix_pages", b.prefix_len) * c.page:
         _bad("laud_cache_attention")
+    _here(c, b, q, "laud_cache_attention")
     s = (_calls or _token_calls()).cache_attention(p, c, b, q, out, ws)
     if s:
         raise LaudError(s, "laud_cache_attention")

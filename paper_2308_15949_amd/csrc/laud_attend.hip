@@ -16,31 +16,25 @@ struct AttendArgs {
   int64_t ldq, ldk, ldv, ldo;  // elements
 };
 
-// A workgroup has a tile of NW * 32 queries of one head, 32 a wave, and goes over their keys, KK at a time; KG groups of waves share the
-// steps, each with stages of its own, and join their sums at the end.  Keys and values come by LDS-direct loads into two stages that take
-// turns: one barrier a step, the next step's loads under way while this one is multiplied.  A wave multiplies keys * queries (32 x 32: a
-// lane has 16 keys of its query, the other half wave the other 16), so that a query's maximum and sum are a lane's own business but for
-// one swap, and the weights lie as the second product, values^T * weights, takes them: its order of keys within 16 is the first product's
-// (lane half h: 4 h .. 4 h + 3 and those 8 behind), and the values are read to match - transposed on their way from LDS where they are
-// bf16.
+// A workgroup has a tile of 128 queries of one head, 32 a wave, and goes over their keys, a step of KK at a time.  Keys and values come by
+// LDS-direct loads into two stages that take turns: one barrier a step, the next step's loads under way while this one is multiplied.  A
+// wave multiplies keys * queries (32 x 32: a lane has 16 keys of its query, the other half wave the other 16), so that a query's maximum
+// and sum are a lane's own business but for one swap, and the weights lie as the second product, values^T * weights, takes them: its order
+// of keys within 16 is the first product's (lane half h: 4 h .. 4 h + 3 and those 8 behind), and the values are read to match - transposed
+// on their way from LDS where they are bf16.
+constexpr int kAttendWaves = 4, kAttendRows = kAttendWaves * 32;
+static_assert(kAttendRows == kManyRows, "the rows that a cache's tiles are counted in");
 constexpr int kMaskWords = 128;  // 64 keys' bits each: two windows of 4096 keys
-template <typename ET, int DC, int KK>
+template <typename ET, int DC>
 struct AttendTile {
+  static constexpr int KK = sizeof(ET) == 2 ? 64 : 32;  // keys of a step
   static constexpr int DP = DC <= 64 ? 64 : 128;  // channels of a row in LDS; the first DC of them are multiplied
   static constexpr bool kHalf = sizeof(ET) == 2;
   static constexpr int kRow = DP * (int)sizeof(ET);  // bytes of a row in LDS
   static constexpr int kChunks = kRow / 16;
   static constexpr int kPart = KK * kRow;  // keys, or values, of a stage
-  static constexpr int kGroup = 4 * kPart;  // two stages of keys, two of values
-  static constexpr int kSums = DC / 32 * 4 * kWave;  // of a wave's 32 queries, in f32x4
-  // LDS of a workgroup: the groups' stages, in whose place all groups' but the first's sums, maxima and sums of weights come
-  static constexpr int bytes(int NW, int KG) {
-    const int stages = KG * kGroup, sums = (KG - 1) * NW * (kSums * 16 + 2 * kWave * 4);
-    return stages > sums ? stages : sums;
-  }
-  // behind them the masker's bits, and two flags a group
-  static constexpr int with_masks(int NW, int KG) { return bytes(NW, KG) + kMaskWords * 8; }
-  static constexpr int all_bytes(int NW, int KG) { return with_masks(NW, KG) + 2 * KG * 4; }
+  // LDS of a workgroup: two stages of keys, two of values, the masker's bits, and a flag for each of two rounds
+  static constexpr int kValues = 2 * kPart, kWords = 4 * kPart, kFlags = kWords + kMaskWords * 8, kBytes = kFlags + 2 * 4;
   // A row's 16-byte chunk c lies at position c ^ swizzle: sixteen lanes that read a chunk of sixteen rows, or a transposed read's four
   // rows of four chunks, meet all banks (no bank conflict counted).
   static __device__ __forceinline__ int key_swizzle(int row) { return kChunks == 8 ? (row >> 1) & 7 : row & 15; }
@@ -62,19 +56,18 @@ __device__ __forceinline__ f32x16 mma32(float a, float b, const f32x16& c) { ret
 // 2^8 instead of 1, which costs float32 nothing, and most steps are spared the scaling of all sums (64 instructions).
 constexpr float kSlack = 8.f;
 
-template <typename ET, int DC, int NW, int KG, int KK, bool PAGED>
-__global__ __launch_bounds__(NW * KG * kWave, 2) void k_attend(AttendArgs a, CachedArgs cache) {
-  typedef AttendTile<ET, DC, KK> L;
-  constexpr int DP = L::DP;
+template <typename ET, int DC, bool PAGED>
+__global__ __launch_bounds__(kAttendWaves * kWave, 2) void k_attend(AttendArgs a, CachedArgs cache) {
+  typedef AttendTile<ET, DC> L;
+  constexpr int DP = L::DP, KK = L::KK, NW = kAttendWaves;
   constexpr bool kHalf = L::kHalf;
-  constexpr int kBlocks = KK / 32, kRows = NW * 32, kDt = DC / 32, kEb = (int)sizeof(ET);
+  constexpr int kBlocks = KK / 32, kRows = kAttendRows, kDt = DC / 32, kEb = (int)sizeof(ET);
   constexpr int kLanesRow = L::kChunks, kRowsLoad = kWave / kLanesRow;  // lanes that bring a row, rows of an LDS-direct load
   constexpr int kLoads = L::kPart / 1024 / NW;                          // loads a wave of a step's keys
   static_assert(kLoads * NW * 1024 == L::kPart, "loads shared evenly");
   extern __shared__ __align__(16) unsigned char lds[];
   const int lane = lane_id(), r32 = lane % 32, half = lane / 32;
-  const int group = __builtin_amdgcn_readfirstlane(threadIdx.x / (NW * kWave));
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave) - group * NW;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
 
   // The tile's queries and their keys.  Keys are counted from the first that this workgroup looks at: there are `end` of them, a query sees
   // those below its limit, every query of the tile those below all_see.
@@ -119,8 +112,8 @@ __global__ __launch_bounds__(NW * KG * kWave, 2) void k_attend(AttendArgs a, Cac
     all_see = a.causal ? min(n, q0 + 1) : n;
     if (in && (!keep || keep[qr] != 0)) limit = a.causal ? qr + 1 : n;
   }
-  const int steps = (end + KK - 1) / KK, rounds = (steps + KG - 1) / KG;
-  const int whole = keep ? 0 : all_see / KK / KG;  // rounds whose keys are all there, and seen by all queries of the tile
+  const int steps = (end + KK - 1) / KK;
+  const int whole = keep ? 0 : all_see / KK;  // steps whose keys are all there, and seen by all queries of the tile
   const int wave_sees = __builtin_amdgcn_readfirstlane((int)lanes64_max((unsigned)limit));
 
   // the wave's queries, for good: lane = query, sixteen-byte pieces 2 s + half
@@ -166,10 +159,10 @@ __global__ __launch_bounds__(NW * KG * kWave, 2) void k_attend(AttendArgs a, Cac
 
   // Which of a step's keys are there, a bit each: rows of the sequence that the masker kept.  Its bytes become bits, 4096 keys at a time,
   // a window ahead of the keys that are asked for.
-  unsigned long long* const words = reinterpret_cast<unsigned long long*>(lds + L::bytes(NW, KG));
+  unsigned long long* const words = reinterpret_cast<unsigned long long*>(lds + L::kWords);
   auto fill_window = [&](int w) {
     const int words_there = (int)min((n - (long long)w * 4096 + 63) / 64, 64ll);
-    for (int i = group * NW + wave; i < words_there; i += NW * KG) {
+    for (int i = wave; i < words_there; i += NW) {
       const long long r = ((long long)w * 64 + i) * 64 + lane;
       const unsigned long long m = __ballot(r < n && keep[r] != 0);
       if (lane == 0) words[(w & 1) * 64 + i] = m;
@@ -198,7 +191,6 @@ __global__ __launch_bounds__(NW * KG * kWave, 2) void k_attend(AttendArgs a, Cac
     vk[i] = ck < a.D ? (unsigned)(from * a.ldk + ck) * kEb : kOutside;
     vv[i] = cv < a.D ? (unsigned)(from * a.ldv + cv) * kEb : kOutside;
   }
-  const unsigned keys0 = group * L::kGroup, values0 = keys0 + 2 * L::kPart;  // the group's stages
   auto request = [&](const ET* from, int64_t ld, const unsigned (&off)[kOffsets], unsigned to, bool all, unsigned long long there) {
     const unsigned stage = __builtin_amdgcn_readfirstlane(to + wave * 1024);
     const __amdgpu_buffer_rsrc_t r = bytes_of(scalar_pointer(from), 0x7fffffff);
@@ -228,22 +220,20 @@ __global__ __launch_bounds__(NW * KG * kWave, 2) void k_attend(AttendArgs a, Cac
     }
   };
   Pages asked;  // of the keys that were asked for last
-  auto ask_keys = [&](int round) {
-    const int step = round * KG + group;
-    const unsigned to = keys0 + (round & 1) * L::kPart;
+  auto ask_keys = [&](int step) {
+    const unsigned to = (step & 1) * L::kPart;
     if constexpr (PAGED) {
       asked = pages_of(step);
       look_up(step + 1);
       request_pages(cache.k, vk, to, asked);
     } else {
-      request(kp + (long long)step * KK * a.ldk, a.ldk, vk, to, round < whole, round < whole ? 0 : rows_there(step));
+      request(kp + (long long)step * KK * a.ldk, a.ldk, vk, to, step < whole, step < whole ? 0 : rows_there(step));
     }
   };
-  auto ask_values = [&](int round) {  // (of a cache: of the keys that were asked for last)
-    const int step = round * KG + group;
-    const unsigned to = values0 + (round & 1) * L::kPart;
+  auto ask_values = [&](int step) {  // (of a cache: of the keys that were asked for last)
+    const unsigned to = L::kValues + (step & 1) * L::kPart;
     if constexpr (PAGED) request_pages(cache.v, vv, to, asked);
-    else request(vp + (long long)step * KK * a.ldv, a.ldv, vv, to, round < whole, round < whole ? 0 : rows_there(step));
+    else request(vp + (long long)step * KK * a.ldv, a.ldv, vv, to, step < whole, step < whole ? 0 : rows_there(step));
   };
 
   f32x16 acc[kDt];
@@ -314,9 +304,9 @@ __global__ __launch_bounds__(NW * KG * kWave, 2) void k_attend(AttendArgs a, Cac
 
   // 0 * NaN is NaN, so where some queries of a tile do not see all of a step's keys, values that are not finite must not meet the matrix
   // instructions.  They become zeros in LDS, and are added to the queries that see them one by one, from memory.
-  int* const found = reinterpret_cast<int*>(lds + L::with_masks(NW, KG));  // [2][KG]
+  int* const found = reinterpret_cast<int*>(lds + L::kFlags);  // of two steps in turn
   auto take_out = [&](int turn) {
-    tok_u4* const vs = reinterpret_cast<tok_u4*>(lds + values0 + turn * L::kPart);
+    tok_u4* const vs = reinterpret_cast<tok_u4*>(lds + L::kValues + turn * L::kPart);
     bool bad = false;
 #pragma unroll
     for (int i = 0; i < L::kPart / 16 / (NW * kWave); ++i) {
@@ -332,7 +322,7 @@ __global__ __launch_bounds__(NW * KG * kWave, 2) void k_attend(AttendArgs a, Cac
         bad = true;
       }
     }
-    if (__ballot(bad) && lane == 0) found[turn * KG + group] = 1;
+    if (__ballot(bad) && lane == 0) found[turn] = 1;
   };
   auto add_back = [&](int k0, unsigned long long here) {
     const unsigned long long seen = seen_of(k0, here);
@@ -367,53 +357,52 @@ __global__ __launch_bounds__(NW * KG * kWave, 2) void k_attend(AttendArgs a, Cac
     }
   };
 
-  // A round's scores are made while the round before becomes weights: matrix and vector instructions of one wave side by side.  Keys are
-  // asked for two rounds ahead, values one.
+  // A step's scores are made while the step before becomes weights: matrix and vector instructions of one wave side by side.  Keys are
+  // asked for two steps ahead, values one.
   const bool mixed = all_see < end;  // some queries see fewer keys than others
   if (keep) {
     fill_window(0);
     fill_window(1);
   }
-  if (mixed && threadIdx.x < 2 * KG) found[threadIdx.x] = 0;
+  if (mixed && threadIdx.x < 2) found[threadIdx.x] = 0;
   if (keep) __syncthreads();
-  look_up(group);
+  look_up(0);
   ask_keys(0);
   ask_values(0);
   const unsigned long long there_first = PAGED ? asked.there : 0;
   ask_keys(1);
-  auto key_of = [&](int round) { return (round * KG + group) * KK; };
-  // of a round's keys, those that are there (of a cache: as they were asked for)
-  auto there_of = [&](int round, unsigned long long pages) { return PAGED ? pages : rows_there(round * KG + group); };
+  // of a step's keys, those that are there (of a cache: as they were asked for)
+  auto there_of = [&](int step, unsigned long long pages) { return PAGED ? pages : rows_there(step); };
   constexpr unsigned long long kAll = KK == 64 ? ~0ull : 0xffffffffull;
-  auto hidden = [&](f32x16 (&s)[kBlocks], int round, unsigned long long pages) {
-    if (round >= whole || (PAGED && pages != kAll)) hide(s, seen_of(key_of(round), there_of(round, pages)));
+  auto hidden = [&](f32x16 (&s)[kBlocks], int step, unsigned long long pages) {
+    if (step >= whole || (PAGED && pages != kAll)) hide(s, seen_of(step * KK, there_of(step, pages)));
   };
   f32x16 s0[kBlocks], s1[kBlocks];
   vm_wait<2 * kLoads>();
   __syncthreads();
   clear(s0);
 #pragma unroll
-  for (int i = 0; i < kPieces; ++i) scores_part(s0, lds + keys0, i);
+  for (int i = 0; i < kPieces; ++i) scores_part(s0, lds, i);
   hidden(s0, 0, there_first);
   raise(most_of(s0));
   unsigned long long there_now = there_first;
-  auto body = [&](int round, f32x16 (&s)[kBlocks], f32x16 (&next)[kBlocks]) {
-    const int k0 = key_of(round), turn = round & 1;
+  auto body = [&](int step, f32x16 (&s)[kBlocks], f32x16 (&next)[kBlocks]) {
+    const int k0 = step * KK, turn = step & 1;
     vm_wait<0>();
     __syncthreads();  // the next keys and the values are there, and nobody reads the stages that are filled now any more
-    if (keep && round > 0 && k0 / 4096 * 4096 == k0 - group * KK) fill_window(k0 / 4096 + 1);  // (in the place of the window before)
-    ask_values(round + 1);
+    if (keep && step > 0 && k0 % 4096 == 0) fill_window(k0 / 4096 + 1);  // (in the place of the window before)
+    ask_values(step + 1);
     const unsigned long long there_next = PAGED ? asked.there : 0, there = there_now;
     there_now = there_next;
-    ask_keys(round + 2);
-    const bool partly = mixed && round >= whole;
+    ask_keys(step + 2);
+    const bool partly = mixed && step >= whole;
     if (partly) {
       take_out(turn);
       __syncthreads();
-      if (threadIdx.x < KG) found[(turn ^ 1) * KG + threadIdx.x] = 0;  // (the next round's, whose last reader has passed this barrier)
+      if (threadIdx.x == 0) found[turn ^ 1] = 0;  // (the next step's, whose last reader has passed this barrier)
     }
     if (k0 >= wave_sees) return;  // (no keys that the wave's queries see, from here on)
-    const unsigned char *ks = lds + keys0 + (turn ^ 1) * L::kPart, *vs = lds + values0 + turn * L::kPart;
+    const unsigned char *ks = lds + (turn ^ 1) * L::kPart, *vs = lds + L::kValues + turn * L::kPart;
     clear(next);
     const float shift = shift_of(top);
     float part[4] = {0.f, 0.f, 0.f, 0.f};
@@ -450,60 +439,18 @@ __global__ __launch_bounds__(NW * KG * kWave, 2) void k_attend(AttendArgs a, Cac
 #pragma unroll
         for (int dt = 0; dt < kDt; ++dt) acc[dt] = mma32(from[(8 * (e / 4) + e % 4) * DP + 32 * dt], s[0][e], acc[dt]);
     }
-    hidden(next, round + 1, there_next);
+    hidden(next, step + 1, there_next);
     const float most = most_of(next);
-    if (partly && found[turn * KG + group]) add_back(k0, there_of(round, there));
+    if (partly && found[turn]) add_back(k0, there_of(step, there));
     raise(most);
   };
-  for (int round = 0; round < rounds;) {
-    body(round++, s0, s1);
-    if (round >= rounds) break;
-    body(round++, s1, s0);
+  for (int step = 0; step < steps;) {
+    body(step++, s0, s1);
+    if (step >= steps) break;
+    body(step++, s1, s0);
   }
   vm_wait<0>();  // (no load into LDS is left behind)
   sum = other_half_sum(sum);
-
-  if constexpr (KG > 1) {  // the other groups' sums through LDS to the first, in their order
-    constexpr int kSums = L::kSums;
-    f32x4* const sums = reinterpret_cast<f32x4*>(lds);
-    float* const stats = reinterpret_cast<float*>(lds + (KG - 1) * NW * kSums * 16);
-    __syncthreads();
-    if (group != 0) {
-      const int at = (group - 1) * NW + wave;
-#pragma unroll
-      for (int t = 0; t < kDt; ++t)
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          sums[at * kSums + (t * 4 + e) * kWave + lane] = f32x4{acc[t][4 * e], acc[t][4 * e + 1], acc[t][4 * e + 2], acc[t][4 * e + 3]};
-      stats[(2 * at) * kWave + lane] = top;
-      stats[(2 * at + 1) * kWave + lane] = sum;
-    }
-    __syncthreads();
-    if (group != 0) return;
-    float most = top;
-#pragma unroll
-    for (int g = 0; g < KG - 1; ++g) most = fmaxf(most, stats[2 * (g * NW + wave) * kWave + lane]);
-    const float shift = shift_of(most), mine = exp2_fast(top - shift);
-    sum *= mine;
-#pragma unroll
-    for (int t = 0; t < kDt; ++t)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) acc[t][e] *= mine;
-#pragma unroll
-    for (int g = 0; g < KG - 1; ++g) {
-      const int at = g * NW + wave;
-      const float by = exp2_fast(stats[2 * at * kWave + lane] - shift);
-      sum = fmaf(stats[(2 * at + 1) * kWave + lane], by, sum);
-#pragma unroll
-      for (int t = 0; t < kDt; ++t)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const f32x4 v = sums[at * kSums + (t * 4 + e) * kWave + lane];
-#pragma unroll
-          for (int j = 0; j < 4; ++j) acc[t][4 * e + j] = fmaf(v[j], by, acc[t][4 * e + j]);
-        }
-    }
-  }
 
   // out: the lane's query, channels 32 t + 16 * half .. + 15; of a part of the keys its sums as they are, maximum and sum of weights beside
   const bool parts = PAGED && cache.part_out, none = sum == 0.f;
@@ -549,24 +496,23 @@ __global__ __launch_bounds__(NW * KG * kWave, 2) void k_attend(AttendArgs a, Cac
   }
 }
 
-template <typename ET, int DC, int NW, int KG, int KK, bool PAGED>
+template <typename ET, int DC, bool PAGED>
 int ask_tile_lds() {
-  return hipFuncSetAttribute(reinterpret_cast<const void*>(&k_attend<ET, DC, NW, KG, KK, PAGED>), hipFuncAttributeMaxDynamicSharedMemorySize,
-                             (AttendTile<ET, DC, KK>::all_bytes(NW, KG))) == hipSuccess ? LAUD_OK : LAUD_ERR_HIP;
+  return hipFuncSetAttribute(reinterpret_cast<const void*>(&k_attend<ET, DC, PAGED>), hipFuncAttributeMaxDynamicSharedMemorySize,
+                             (AttendTile<ET, DC>::kBytes)) == hipSuccess ? LAUD_OK : LAUD_ERR_HIP;
 }
-template <typename ET, int DC, int NW, int KG, int KK, bool PAGED>
+template <typename ET, int DC, bool PAGED>
 void launch_tiles(const AttendArgs& a, const CachedArgs& cache, unsigned groups, hipStream_t st) {
-  hipLaunchKernelGGL((k_attend<ET, DC, NW, KG, KK, PAGED>), dim3(groups), dim3(NW * KG * kWave), (AttendTile<ET, DC, KK>::all_bytes(NW, KG)), st, a, cache);
+  hipLaunchKernelGGL((k_attend<ET, DC, PAGED>), dim3(groups), dim3(kAttendWaves * kWave), (AttendTile<ET, DC>::kBytes), st, a, cache);
 }
 
 template <typename ET, int DC>
 int launch_attend(AttendArgs a, hipStream_t st) {
-  constexpr int kWaves = 4;
-  const long long tiles = tiles_of(a.T, a.B, 1, kWaves * 32), groups = (tiles * a.heads + 7) / 8 * 8;
-  if (!launchable((double)groups, kWaves * kWave)) return LAUD_ERR_UNSUPPORTED;
+  const long long tiles = tiles_of(a.T, a.B, 1, kAttendRows), groups = (tiles * a.heads + 7) / 8 * 8;
+  if (!launchable((double)groups, kAttendWaves * kWave)) return LAUD_ERR_UNSUPPORTED;
   if (attend_init_device() != LAUD_OK) return LAUD_ERR_HIP;
   a.tiles = (int)tiles;
-  launch_tiles<ET, DC, kWaves, 1, (sizeof(ET) == 2 ? 64 : 32), false>(a, CachedArgs{}, (unsigned)groups, st);
+  launch_tiles<ET, DC, false>(a, CachedArgs{}, (unsigned)groups, st);
   return check_launch();
 }
 template <typename ET>
@@ -584,10 +530,10 @@ int attend_init_device() {
   if (hipGetDevice(&dev) != hipSuccess) return LAUD_ERR_HIP;
   const unsigned bit = dev >= 0 && dev < 32 ? 1u << dev : 0u;
   if (bit && (done.load(std::memory_order_acquire) & bit)) return LAUD_OK;
-  for (int rc : {ask_tile_lds<bf16_t, 32, 4, 1, 64, false>(), ask_tile_lds<bf16_t, 64, 4, 1, 64, false>(), ask_tile_lds<bf16_t, 96, 4, 1, 64, false>(),
-                 ask_tile_lds<bf16_t, 128, 4, 1, 64, false>(), ask_tile_lds<float, 32, 4, 1, 32, false>(), ask_tile_lds<float, 64, 4, 1, 32, false>(),
-                 ask_tile_lds<float, 96, 4, 1, 32, false>(), ask_tile_lds<float, 128, 4, 1, 32, false>(), ask_tile_lds<bf16_t, 64, 4, 1, 64, true>(),
-                 ask_tile_lds<bf16_t, 128, 4, 1, 64, true>()})
+  for (int rc : {ask_tile_lds<bf16_t, 32, false>(), ask_tile_lds<bf16_t, 64, false>(), ask_tile_lds<bf16_t, 96, false>(),
+                 ask_tile_lds<bf16_t, 128, false>(), ask_tile_lds<float, 32, false>(), ask_tile_lds<float, 64, false>(),
+                 ask_tile_lds<float, 96, false>(), ask_tile_lds<float, 128, false>(), ask_tile_lds<bf16_t, 64, true>(),
+                 ask_tile_lds<bf16_t, 128, true>()})
     if (rc != LAUD_OK) return rc;
   done.fetch_or(bit, std::memory_order_release);
   return LAUD_OK;
@@ -598,8 +544,8 @@ void launch_many_rows(const CachedArgs& c, unsigned groups, hipStream_t st) {
   a.heads = c.heads; a.group = c.group; a.D = c.D; a.c = c.c;
   a.q = c.q; a.out = c.out; a.ldq = c.ldq; a.ldo = c.ldo;
   a.ldk = a.ldv = c.D;
-  if (c.D <= 64) launch_tiles<bf16_t, 64, 4, 1, 64, true>(a, c, groups, st);
-  else launch_tiles<bf16_t, 128, 4, 1, 64, true>(a, c, groups, st);
+  if (c.D <= 64) launch_tiles<bf16_t, 64, true>(a, c, groups, st);
+  else launch_tiles<bf16_t, 128, true>(a, c, groups, st);
 }
 
 }  // namespace laud

@@ -513,11 +513,14 @@ __global__ __launch_bounds__(256) void k_join(CachedArgs a) {
   const int b = last_not_above(a.B, [&](int i) { return row_at(a.offsets, i, a.T) <= token; });
   const int own = parts_of(cached_tokens(a, b), a.splits), shared = a.prefix_splits ? parts_of(a.prefix_len, a.prefix_splits) : 0;
   if (token < row_at(a.offsets, b, a.T) || token >= row_at(a.offsets, b + 1, a.T)) return;  // (all of the workgroup)
-  if (lane < a.splits ? lane >= own : lane - a.splits >= shared) top = kNoScore;  // (a part that there is not: nobody wrote it)
+  if (lane < a.splits ? lane >= own : lane - a.splits >= shared) {  // (a part that there is not: nobody wrote it)
+    top = kNoScore;
+    sum = 0.f;
+  }
   float most = top;
 #pragma unroll
   for (int o = 1; o < kWave; o <<= 1) most = fmaxf(most, __shfl_xor(most, o, kWave));
-  const bool counts = top != kNoScore;
+  const bool counts = sum != 0.f;  // (has a weight; scores that are all NaN leave a NaN for a sum, and no maximum)
   const float by = counts ? exp2_fast(top - most) : 0.f;
   const float total = lanes64_sum(counts ? sum * by : 0.f);
   const unsigned long long mask = __ballot(counts);
@@ -688,7 +691,7 @@ extern "C" int laud_cache_attention(const laud_heads* p, const laud_cache* c, co
   }
   if (s.rt == 0 && attend_init_device() != LAUD_OK) return LAUD_ERR_HIP;
   const double own = (double)s.tiles * p->kv_heads * s.own, shared = (double)s.prefix_tiles * p->kv_heads * s.shared;
-  if (!launchable(own + shared, kWaves * kWave) || !launchable((double)T * p->heads, 256)) return LAUD_ERR_UNSUPPORTED;
+  if (!launchable(own + shared, kWaves * kWave) || (s.bytes && !launchable((double)T * p->heads, 256))) return LAUD_ERR_UNSUPPORTED;
   CachedArgs a{};
   set_group(a, p->heads / p->kv_heads);
   a.heads = p->heads; a.kv_heads = p->kv_heads; a.D = p->D; a.causal = p->causal; a.B = b->B; a.T = T;

@@ -123,7 +123,7 @@ CASES = {
 
 
 # The kernels that a case is there for: type, channels multiplied, whether keys are a cache's.
-REACHES = {name: f"k_attend<{'unsigned short' if '_bf16_' in name or '_odd_' in name else 'float'}, {w}, 4, 1, {64 if '_bf16_' in name or '_odd_' in name else 32}, {p}>"
+REACHES = {name: f"k_attend<{'unsigned short' if '_bf16_' in name or '_odd_' in name else 'float'}, {w}, {p}>"
            for name, w, p in (("tiles_bf16_8", 32, "false"), ("tiles_bf16_40", 64, "false"), ("tiles_bf16_72", 96, "false"),
                               ("tiles_bf16_128", 128, "false"), ("tiles_f32_32", 32, "false"), ("tiles_f32_64", 64, "false"),
                               ("tiles_f32_96", 96, "false"), ("tiles_f32_120", 128, "false"), ("tiles_odd_offsets", 64, "false"),

@@ -469,6 +469,29 @@ def test_cached_special_values_stay_with_who_sees_them(dtype, cache, what):
     cached_case([1, 1], [29, 40], 2, 1, 64, dtype, cache, 16, 3, change=put, prefix=20)
 
 
+@pytest.mark.parametrize("dtype,cache", TYPES)
+@pytest.mark.parametrize("prefix", [0, 300])
+def test_a_query_that_is_nan_over_parts(dtype, cache, prefix):
+    """Scores that are all NaN have no largest one; a join of parts answers NaN for them as one part does."""
+    g = gen(8)
+    lens = [3000, 900, 20]
+    pages = Paged(g, lens, 2, 64, cache, 16, prefix)
+    fill(pages, g, lens, prefix, dtype)
+    p, b = L.make_heads(4, 2, 64, dtype, True), pages.batch([1, 1, 1], lens, prefix)
+    q = rand(g, 3, 256).to(dtype)
+    n = L.cache_attention_workspace(p, pages.desc, b, 3)
+    assert n
+    clean, out = (torch.zeros(3, 256, dtype=dtype, device="cuda") for _ in range(2))
+    L.laud_cache_attention(p, pages.desc, b, q.cuda(), clean, torch.empty(n, dtype=torch.uint8, device="cuda"))
+    q[0, 64:128] = math.nan
+    q[2, 70] = math.nan
+    L.laud_cache_attention(p, pages.desc, b, q.cuda(), out, torch.empty(n, dtype=torch.uint8, device="cuda"))
+    torch.cuda.synchronize()
+    bad = torch.zeros(3, 256, dtype=torch.bool)
+    bad[0, 64:128] = bad[2, 64:128] = True
+    assert bool(out.cpu()[bad].isnan().all()) and torch.equal(out.cpu()[~bad], clean.cpu()[~bad])
+
+
 def test_cached_special_values_in_8_bits():
     def put(k, v):
         v[27], v[28] = math.nan, math.inf
@@ -592,6 +615,92 @@ def test_quantised_rows_of_special_values():
     assert bool(codes[2].isnan().any()) and math.isinf(float(s[2]))
     assert float(s[3]) == 2.0 ** -126 and bool((codes[3] == 0).all())
     assert bool(codes[[0, 4]].isfinite().all())
+
+
+# ----- together -------------------------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype,cache_type", TYPES)
+@pytest.mark.parametrize("prefix", [0, 45])
+def test_prompts_and_then_token_by_token(dtype, cache_type, prefix):
+    """Prompts are attended to and cached, then answers grow by a token a step, captured and replayed: every row against attention over
+    all tokens so far.  Queries, keys and values are columns of one array, as a projection leaves them."""
+    g = gen(11 + prefix)
+    heads, kv, D, prompt, steps = 6, 2, 64, [37, 1, 0, 140], 6
+    widths, B_ = [heads * D, kv * D, kv * D], len(prompt)
+    total = [n + steps for n in prompt]
+    cache = Paged(g, total, kv, D, cache_type, 16, prefix)
+    p = L.make_heads(heads, kv, D, dtype, True)
+
+    def check(got, q, i, seen):
+        k, v = (torch.cat((cache.rows64(x, cache.prefix_pages, prefix), cache.rows64(x, cache.pages[i], total[i])[:seen])) for x in ("k", "v"))
+        m = got.shape[0]
+        allowed = torch.arange(prefix + seen)[None, :] <= (prefix + seen - m + torch.arange(m))[:, None]
+        ref = attend64(q.double().view(m, heads, D), k, v, p.scale, allowed)
+        assert near(got.view(m, heads, D), *ref, prefix + seen, dtype), (i, seen)
+
+    if prefix:  # the common beginning, over itself and into the cache
+        x = rand(g, prefix, sum(widths)).to(dtype)
+        q, k, v = x.cuda().split(widths, 1)
+        out = torch.zeros(prefix, heads * D, dtype=dtype, device="cuda")
+        L.laud_attention(p, ints([0, prefix]), q, k, v, None, out)
+        L.laud_cache_write(cache.desc, L.make_batch(ints([0, prefix]), ints([prefix]), ints([cache.prefix_pages])), k, v)
+        a, b, c = x.double().split(widths, 1)
+        ref = attend64(a.view(-1, heads, D), b.reshape(-1, kv, D), c.reshape(-1, kv, D), p.scale, torch.ones(prefix, prefix).tril().bool())
+        assert near(out.cpu().view(-1, heads, D), *ref, prefix, dtype)
+    lens = ints(prompt)
+    x = rand(g, sum(prompt), sum(widths)).to(dtype)
+    q, k, v = x.cuda().split(widths, 1)
+    out = torch.zeros(sum(prompt), heads * D, dtype=dtype, device="cuda")
+    at = offsets_of(prompt)
+    b = L.make_batch(ints(at), lens, cache.table, ints(cache.prefix_pages) if prefix else None, prefix)
+    n = L.cache_attention_workspace(p, cache.desc, b, sum(prompt))
+    L.laud_cache_write(cache.desc, b, k, v)
+    L.laud_cache_attention(p, cache.desc, b, q, out, torch.empty(n, dtype=torch.uint8, device="cuda") if n else None)
+    torch.cuda.synchronize()
+    for i, n in enumerate(prompt):
+        check(out.cpu()[at[i]:at[i + 1]], q.cpu()[at[i]:at[i + 1]], i, n)
+    if not prefix and cache_type != E4M3:  # the same rows without a cache
+        again = torch.zeros_like(out)
+        L.laud_attention(p, ints(at), q, k, v, None, again)
+        for i, n in enumerate(prompt):
+            check(again.cpu()[at[i]:at[i + 1]], q.cpu()[at[i]:at[i + 1]], i, n)
+
+    new = torch.zeros(B_, sum(widths), dtype=dtype, device="cuda")
+    q, k, v = new.split(widths, 1)
+    out = torch.zeros(B_, heads * D, dtype=dtype, device="cuda")
+    b = L.make_batch(ints(range(B_ + 1)), lens, cache.table, ints(cache.prefix_pages) if prefix else None, prefix)
+    n = L.cache_attention_workspace(p, cache.desc, b, B_)
+    ws = torch.empty(max(n, 1), dtype=torch.uint8, device="cuda")
+
+    def step():
+        lens.add_(1)
+        L.laud_cache_write(cache.desc, b, k, v)
+        L.laud_cache_attention(p, cache.desc, b, q, out, ws)
+    graph = None
+    for j in range(steps):
+        new.copy_(rand(g, B_, sum(widths)).to(dtype))
+        if j == 1:
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph):
+                step()
+        graph.replay() if graph else step()
+        torch.cuda.synchronize()
+        for i in range(B_):
+            check(out.cpu()[i:i + 1], q.cpu()[i:i + 1], i, prompt[i] + j + 1)
+    assert lens.tolist() == total
+
+
+def test_descriptors_of_another_device():
+    cache = Paged(gen(1), [5], 1, 32, BF16, 16)
+    b, rows = cache.batch([1], [5]), torch.zeros(1, 32, dtype=BF16, device="cuda")
+    p = L.make_heads(1, 1, 32, BF16, True)
+    L.laud_cache_write(cache.desc, b, rows, rows)
+    for d in (cache.desc, b):
+        was, d.device = d.device, 1
+        for call in (lambda: L.laud_cache_write(cache.desc, b, rows, rows), lambda: L.laud_cache_read(cache.desc, b, rows, rows.clone()),
+                     lambda: L.laud_cache_attention(p, cache.desc, b, rows, rows)):
+            with pytest.raises(L.LaudError):
+                call()
+        d.device = was
 
 
 # ----- streams and graphs ---------------------------------------------------------------------------------------------------------
