@@ -24,7 +24,10 @@ struct AttendArgs {
 // on their way from LDS where they are bf16.
 constexpr int kAttendWaves = 4, kAttendRows = kAttendWaves * 32;
 static_assert(kAttendRows == kManyRows, "the rows that a cache's tiles are counted in");
-constexpr int kMaskWords = 128;  // 64 keys' bits each: two windows of 4096 keys
+// Where keys come from: the call's rows; those of them that the masker kept, by a list; a cache.
+enum { kRowsAll, kRowsKept, kRowsCached };
+// The list: rows of kept tokens in order, as a ring.  It is filled kScan rows at a time, whenever it ends less than four steps ahead.
+constexpr int kListed = 2048, kScan = 1024;
 template <typename ET, int DC>
 struct AttendTile {
   static constexpr int KK = sizeof(ET) == 2 ? 64 : 32;  // keys of a step
@@ -33,8 +36,9 @@ struct AttendTile {
   static constexpr int kRow = DP * (int)sizeof(ET);  // bytes of a row in LDS
   static constexpr int kChunks = kRow / 16;
   static constexpr int kPart = KK * kRow;  // keys, or values, of a stage
-  // LDS of a workgroup: two stages of keys, two of values, the masker's bits, and a flag for each of two rounds
-  static constexpr int kValues = 2 * kPart, kWords = 4 * kPart, kFlags = kWords + kMaskWords * 8, kBytes = kFlags + 2 * 4;
+  // LDS of a workgroup: two stages of keys, two of values, a flag for each of two steps; of kept rows their list and the tile's queries
+  static constexpr int kValues = 2 * kPart, kFlags = 4 * kPart, kList = kFlags + 2 * 4, kQueries = kList + kListed * 4;
+  static constexpr int bytes(int FROM) { return FROM == kRowsKept ? kQueries + kAttendRows * 4 : kList; }
   // A row's 16-byte chunk c lies at position c ^ swizzle: sixteen lanes that read a chunk of sixteen rows, or a transposed read's four
   // rows of four chunks, meet all banks (no bank conflict counted).
   static __device__ __forceinline__ int key_swizzle(int row) { return kChunks == 8 ? (row >> 1) & 7 : row & 15; }
@@ -56,11 +60,11 @@ __device__ __forceinline__ f32x16 mma32(float a, float b, const f32x16& c) { ret
 // 2^8 instead of 1, which costs float32 nothing, and most steps are spared the scaling of all sums (64 instructions).
 constexpr float kSlack = 8.f;
 
-template <typename ET, int DC, bool PAGED>
+template <typename ET, int DC, int FROM>
 __global__ __launch_bounds__(kAttendWaves * kWave, 2) void k_attend(AttendArgs a, CachedArgs cache) {
   typedef AttendTile<ET, DC> L;
   constexpr int DP = L::DP, KK = L::KK, NW = kAttendWaves;
-  constexpr bool kHalf = L::kHalf;
+  constexpr bool kHalf = L::kHalf, KEPT = FROM == kRowsKept, PAGED = FROM == kRowsCached;
   constexpr int kBlocks = KK / 32, kRows = kAttendRows, kDt = DC / 32, kEb = (int)sizeof(ET);
   constexpr int kLanesRow = L::kChunks, kRowsLoad = kWave / kLanesRow;  // lanes that bring a row, rows of an LDS-direct load
   constexpr int kLoads = L::kPart / 1024 / NW;                          // loads a wave of a step's keys
@@ -69,12 +73,32 @@ __global__ __launch_bounds__(kAttendWaves * kWave, 2) void k_attend(AttendArgs a
   const int lane = lane_id(), r32 = lane % 32, half = lane / 32;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
 
+  // Rows first .. first + kScan - 1 of n, of which the masker kept some: put(number, row) for each, numbers from `number` on; the number
+  // after them.  Every wave looks at all of them, and puts every fourth sixty-four.
+  auto scan = [&](const uint8_t* keep, int n, int first, int number, auto&& put) {
+    bool here[kScan / kWave];
+#pragma unroll
+    for (int j = 0; j < kScan / kWave; ++j) {
+      const int row = first + j * kWave + lane;
+      here[j] = row < n && keep[min(row, n - 1)] != 0;
+    }
+#pragma unroll
+    for (int j = 0; j < kScan / kWave; ++j) {
+      const unsigned long long m = __ballot(here[j]);
+      if (here[j] && j % NW == wave) put(number + __popcll(m & ((1ull << lane) - 1)), first + j * kWave + lane);
+      number += __popcll(m);
+    }
+    return number;
+  };
+
   // The tile's queries and their keys.  Keys are counted from the first that this workgroup looks at: there are `end` of them, a query sees
   // those below its limit, every query of the tile those below all_see.
   int head, hk, n, end, all_see, limit = 0;
   long long my_row;  // the lane's query among all rows
   bool in;
-  const uint8_t* keep = nullptr;
+  const uint8_t* keep = nullptr;  // of the sequence's rows
+  int rows_of_sequence = 0, listed = 0, scanned = 0;  // kept rows in the list, rows that were looked at for them
+  int* const list = reinterpret_cast<int*>(lds + L::kList);
   const ET *kp = nullptr, *vp = nullptr;
   CachedTile part;
   if constexpr (PAGED) {
@@ -99,21 +123,53 @@ __global__ __launch_bounds__(kAttendWaves * kWave, 2) void k_attend(AttendArgs a
     const int tile = a.tiles - 1 - (int)(in_band / band);
     const int b = last_not_above(a.B, [&](int i) { return first_tile(a.offsets, i, a.T, 1, kRows) <= tile; });
     const int row0 = __builtin_amdgcn_readfirstlane(row_at(a.offsets, b, a.T));
-    n = __builtin_amdgcn_readfirstlane(row_at(a.offsets, b + 1, a.T)) - row0;  // (may be negative: no rows)
+    n = rows_of_sequence = __builtin_amdgcn_readfirstlane(row_at(a.offsets, b + 1, a.T)) - row0;  // (may be negative: no rows)
     const long long q_first = (tile - first_tile(a.offsets, b, a.T, 1, kRows)) * kRows;
     if (q_first < 0 || q_first >= n) return;
     const int q0 = __builtin_amdgcn_readfirstlane((int)q_first), qr = q0 + wave * 32 + r32;
-    in = qr < n;
-    my_row = row0 + (long long)qr;
-    keep = a.keep ? a.keep + row0 : nullptr;
     kp = reinterpret_cast<const ET*>(a.k) + (long long)row0 * a.ldk + hk * a.D;
     vp = reinterpret_cast<const ET*>(a.v) + (long long)row0 * a.ldv + hk * a.D;
+    my_row = row0 + (long long)qr;
+    if constexpr (KEPT) {
+      // Kept tokens are numbered in order, and the tile has the queries of numbers q0 .. q0 + 127: what the masker skipped is neither
+      // fetched nor multiplied.  The tile's rows among the skipped ones, q0 .. q0 + 127 as rows, get their zeros first.
+      keep = a.keep + row0;
+      const int skipped = q0 + threadIdx.x / 2;
+      if (skipped < n && keep[skipped] == 0) {
+        piece8<ET> zero;
+        const float f[8] = {};
+        zero.put(f);
+        for (int d = threadIdx.x % 2; d < a.D / 8; d += 2)
+          zero.store(reinterpret_cast<ET*>(a.out) + (row0 + (long long)skipped) * a.ldo + head * a.D, d);
+      }
+      int* const queries = reinterpret_cast<int*>(lds + L::kQueries);
+      int kept = 0;
+      bool open = true;
+      for (int first = 0; first < n && !(a.causal && kept >= q0 + kRows); first += kScan) {
+        open = open && kept <= kListed - kScan;
+        kept = scan(keep, n, first, kept, [&](int number, int row) {
+          if (open) list[number % kListed] = row;
+          if ((unsigned)(number - q0) < (unsigned)kRows) queries[number - q0] = row;
+        });
+        if (open) {
+          listed = kept;
+          scanned = first + kScan;
+        }
+      }
+      n = kept;
+      if (q0 >= n) return;
+      __syncthreads();
+      in = qr < n;
+      if (in) my_row = row0 + (long long)queries[qr - q0];
+    } else {
+      in = qr < n;
+    }
     end = a.causal ? min(n, q0 + kRows) : n;
     all_see = a.causal ? min(n, q0 + 1) : n;
-    if (in && (!keep || keep[qr] != 0)) limit = a.causal ? qr + 1 : n;
+    if (in) limit = a.causal ? qr + 1 : n;
   }
   const int steps = (end + KK - 1) / KK;
-  const int whole = keep ? 0 : all_see / KK;  // steps whose keys are all there, and seen by all queries of the tile
+  const int whole = all_see / KK;  // steps whose keys are all there, and seen by all queries of the tile
   const int wave_sees = __builtin_amdgcn_readfirstlane((int)lanes64_max((unsigned)limit));
 
   // the wave's queries, for good: lane = query, sixteen-byte pieces 2 s + half
@@ -157,26 +213,10 @@ __global__ __launch_bounds__(kAttendWaves * kWave, 2) void k_attend(AttendArgs a
     return s;
   };
 
-  // Which of a step's keys are there, a bit each: rows of the sequence that the masker kept.  Its bytes become bits, 4096 keys at a time,
-  // a window ahead of the keys that are asked for.
-  unsigned long long* const words = reinterpret_cast<unsigned long long*>(lds + L::kWords);
-  auto fill_window = [&](int w) {
-    const int words_there = (int)min((n - (long long)w * 4096 + 63) / 64, 64ll);
-    for (int i = wave; i < words_there; i += NW) {
-      const long long r = ((long long)w * 64 + i) * 64 + lane;
-      const unsigned long long m = __ballot(r < n && keep[r] != 0);
-      if (lane == 0) words[(w & 1) * 64 + i] = m;
-    }
-  };
+  // which of a step's keys are there, a bit each
   auto rows_there = [&](int step) -> unsigned long long {
-    const long long first = (long long)step * KK, rows = n - first;
-    if (rows <= 0) return 0;
-    if (keep) {
-      const unsigned long long m = words[(first / 64) % kMaskWords] >> (first % 64);
-      return (unsigned long long)__builtin_amdgcn_readfirstlane((int)m) & 0xffffffffull |
-             (unsigned long long)(unsigned)__builtin_amdgcn_readfirstlane((int)(m >> 32)) << 32;
-    }
-    return rows >= 64 ? ~0ull : (1ull << rows) - 1;
+    const long long rows = n - (long long)step * KK;
+    return rows >= 64 ? ~0ull : rows <= 0 ? 0 : (1ull << rows) - 1;
   };
   // LDS-direct loads of a step: load i brings rows i * NW * kRowsLoad + wave * kRowsLoad .., of which a lane has one chunk, the same of
   // each where the swizzles' periods (16 rows) allow.
@@ -187,7 +227,7 @@ __global__ __launch_bounds__(kAttendWaves * kWave, 2) void k_attend(AttendArgs a
   for (int i = 0; i < kOffsets; ++i) {
     const int row = (i * NW + wave) * kRowsLoad + lane / kLanesRow, pos = lane % kLanesRow;
     const int ck = (pos ^ L::key_swizzle(row)) * kPer, cv = (pos ^ L::value_swizzle(row)) * kPer;
-    const int from = PAGED ? lane / kLanesRow : row;  // (a load of a cache begins with its first row)
+    const int from = KEPT ? 0 : PAGED ? lane / kLanesRow : row;  // (a load of a cache begins with its first row)
     vk[i] = ck < a.D ? (unsigned)(from * a.ldk + ck) * kEb : kOutside;
     vv[i] = cv < a.D ? (unsigned)(from * a.ldv + cv) * kEb : kOutside;
   }
@@ -219,6 +259,33 @@ __global__ __launch_bounds__(kAttendWaves * kWave, 2) void k_attend(AttendArgs a
       dma16(bytes_of(scalar_pointer(base + at * a.D * kEb), __popc((unsigned)bits) * a.D * kEb), off[kSame ? 0 : i], 0, stage + i * NW * 1024);
     }
   };
+  // Kept rows: by the list, from the step's first row on.  Where that is too far for one descriptor, row by row.
+  auto request_kept = [&](const ET* base, int64_t ld, const unsigned (&off)[kOffsets], unsigned to, int step) {
+    const unsigned stage = __builtin_amdgcn_readfirstlane(to + wave * 1024);
+    const int k0 = step * KK, rows = min(KK, end - k0);  // (none, past the end)
+    const int first = rows > 0 ? __builtin_amdgcn_readfirstlane(list[k0 % kListed]) : 0;
+    const int last = rows > 0 ? __builtin_amdgcn_readfirstlane(list[(k0 + rows - 1) % kListed]) : 0;
+    if (((long long)(last - first) * ld + a.D) * kEb <= 0x7fffffff) {
+      const __amdgpu_buffer_rsrc_t r = bytes_of(scalar_pointer(base + first * ld), 0x7fffffff);
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) {
+        const int at = (i * NW + wave) * kRowsLoad + lane / kLanesRow;
+        const unsigned o = off[kSame ? 0 : i];
+        const int row = at < rows ? list[(k0 + at) % kListed] - first : -1;
+        dma16(r, row >= 0 && o != kOutside ? (unsigned)row * ((unsigned)ld * kEb) + o : kOutside, 0, stage + i * NW * 1024);
+      }
+    } else {
+#pragma unroll 1
+      for (int i = 0; i < kLoads; ++i)
+#pragma unroll 1
+        for (int j = 0; j < kRowsLoad; ++j) {
+          const int at = (i * NW + wave) * kRowsLoad + j;
+          const int row = at < rows ? __builtin_amdgcn_readfirstlane(list[(k0 + at) % kListed]) : 0;
+          const __amdgpu_buffer_rsrc_t r = bytes_of(scalar_pointer(base + row * ld), at < rows ? a.D * kEb : 0);
+          if (lane / kLanesRow == j) dma16(r, off[kSame ? 0 : i], 0, stage + i * NW * 1024);
+        }
+    }
+  };
   Pages asked;  // of the keys that were asked for last
   auto ask_keys = [&](int step) {
     const unsigned to = (step & 1) * L::kPart;
@@ -226,6 +293,8 @@ __global__ __launch_bounds__(kAttendWaves * kWave, 2) void k_attend(AttendArgs a
       asked = pages_of(step);
       look_up(step + 1);
       request_pages(cache.k, vk, to, asked);
+    } else if constexpr (KEPT) {
+      request_kept(kp, a.ldk, vk, to, step);
     } else {
       request(kp + (long long)step * KK * a.ldk, a.ldk, vk, to, step < whole, step < whole ? 0 : rows_there(step));
     }
@@ -233,6 +302,7 @@ __global__ __launch_bounds__(kAttendWaves * kWave, 2) void k_attend(AttendArgs a
   auto ask_values = [&](int step) {  // (of a cache: of the keys that were asked for last)
     const unsigned to = L::kValues + (step & 1) * L::kPart;
     if constexpr (PAGED) request_pages(cache.v, vv, to, asked);
+    else if constexpr (KEPT) request_kept(vp, a.ldv, vv, to, step);
     else request(vp + (long long)step * KK * a.ldv, a.ldv, vv, to, step < whole, step < whole ? 0 : rows_there(step));
   };
 
@@ -329,7 +399,7 @@ __global__ __launch_bounds__(kAttendWaves * kWave, 2) void k_attend(AttendArgs a
 #pragma unroll 1
     for (int j = 0; j < KK; ++j) {
       if (!((here >> j) & 1)) continue;
-      const uint8_t* from = reinterpret_cast<const uint8_t*>(vp + (long long)(k0 + j) * a.ldv);
+      const uint8_t* from = reinterpret_cast<const uint8_t*>(vp + (long long)(KEPT ? list[(k0 + j) % kListed] : k0 + j) * a.ldv);
       if constexpr (PAGED) {
         const int key = part.begin + k0 + j, page = __builtin_amdgcn_readfirstlane(part.table[key >> cache.page_bits]);
         const long long at = (((long long)page * cache.kv_heads + hk) << cache.page_bits) + (key & ((1 << cache.page_bits) - 1));
@@ -360,12 +430,7 @@ __global__ __launch_bounds__(kAttendWaves * kWave, 2) void k_attend(AttendArgs a
   // A step's scores are made while the step before becomes weights: matrix and vector instructions of one wave side by side.  Keys are
   // asked for two steps ahead, values one.
   const bool mixed = all_see < end;  // some queries see fewer keys than others
-  if (keep) {
-    fill_window(0);
-    fill_window(1);
-  }
   if (mixed && threadIdx.x < 2) found[threadIdx.x] = 0;
-  if (keep) __syncthreads();
   look_up(0);
   ask_keys(0);
   ask_values(0);
@@ -390,7 +455,9 @@ __global__ __launch_bounds__(kAttendWaves * kWave, 2) void k_attend(AttendArgs a
     const int k0 = step * KK, turn = step & 1;
     vm_wait<0>();
     __syncthreads();  // the next keys and the values are there, and nobody reads the stages that are filled now any more
-    if (keep && step > 0 && k0 % 4096 == 0) fill_window(k0 / 4096 + 1);  // (in the place of the window before)
+    if constexpr (KEPT)  // (for the next step; in the place of rows that steps before this one had)
+      for (; listed < min(end, k0 + 4 * KK) && scanned < rows_of_sequence; scanned += kScan)
+        listed = scan(keep, rows_of_sequence, scanned, listed, [&](int number, int row) { list[number % kListed] = row; });
     ask_values(step + 1);
     const unsigned long long there_next = PAGED ? asked.there : 0, there = there_now;
     there_now = there_next;
@@ -496,14 +563,21 @@ __global__ __launch_bounds__(kAttendWaves * kWave, 2) void k_attend(AttendArgs a
   }
 }
 
-template <typename ET, int DC, bool PAGED>
+// With 64 channels a row a compute unit has room for four workgroups, and a launch of few is spread unevenly: a workgroup then asks for half
+// of the LDS.  4 x 16 x 1024 tokens of float32 211 -> 154 us, 4 x 32 x 512 114 -> 85, 32 x 16 x 197 94 -> 83, of bf16 and 32 channels 4 x 16 x
+// 1024 29 -> 23; with 1024 tiles (1 x 64 x 2048) it costs 2 to 6 %.
+constexpr int kSpreadBytes = 80 * 1024, kSpreadTiles = 1024;
+template <typename ET, int DC, int FROM>
 int ask_tile_lds() {
-  return hipFuncSetAttribute(reinterpret_cast<const void*>(&k_attend<ET, DC, PAGED>), hipFuncAttributeMaxDynamicSharedMemorySize,
-                             (AttendTile<ET, DC>::kBytes)) == hipSuccess ? LAUD_OK : LAUD_ERR_HIP;
+  return hipFuncSetAttribute(reinterpret_cast<const void*>(&k_attend<ET, DC, FROM>), hipFuncAttributeMaxDynamicSharedMemorySize,
+                             kSpreadBytes) == hipSuccess ? LAUD_OK : LAUD_ERR_HIP;
 }
-template <typename ET, int DC, bool PAGED>
+template <typename ET, int DC, int FROM>
 void launch_tiles(const AttendArgs& a, const CachedArgs& cache, unsigned groups, hipStream_t st) {
-  hipLaunchKernelGGL((k_attend<ET, DC, PAGED>), dim3(groups), dim3(kAttendWaves * kWave), (AttendTile<ET, DC>::kBytes), st, a, cache);
+  constexpr int kBytes = AttendTile<ET, DC>::bytes(FROM);
+  static_assert(kBytes <= kSpreadBytes, "two workgroups a compute unit");
+  hipLaunchKernelGGL((k_attend<ET, DC, FROM>), dim3(groups), dim3(kAttendWaves * kWave),
+                     ((long long)a.T * a.heads / kAttendRows < kSpreadTiles ? kSpreadBytes : kBytes), st, a, cache);
 }
 
 template <typename ET, int DC>
@@ -512,7 +586,8 @@ int launch_attend(AttendArgs a, hipStream_t st) {
   if (!launchable((double)groups, kAttendWaves * kWave)) return LAUD_ERR_UNSUPPORTED;
   if (attend_init_device() != LAUD_OK) return LAUD_ERR_HIP;
   a.tiles = (int)tiles;
-  launch_tiles<ET, DC, false>(a, CachedArgs{}, (unsigned)groups, st);
+  if (a.keep) launch_tiles<ET, DC, kRowsKept>(a, CachedArgs{}, (unsigned)groups, st);
+  else launch_tiles<ET, DC, kRowsAll>(a, CachedArgs{}, (unsigned)groups, st);
   return check_launch();
 }
 template <typename ET>
@@ -524,16 +599,20 @@ int launch_width(const AttendArgs& a, hipStream_t st) {
 }
 
 // LDS of every instance (more than the 64 KB that a launch may take unasked)
+template <typename ET, int DC>
+int ask_lds_of_width() {
+  const int rc = ask_tile_lds<ET, DC, kRowsAll>();
+  return rc != LAUD_OK ? rc : ask_tile_lds<ET, DC, kRowsKept>();
+}
 int attend_init_device() {
   static std::atomic<unsigned> done{0};  // one bit per device ordinal (ordinals >= 32 repeat the request)
   int dev = 0;
   if (hipGetDevice(&dev) != hipSuccess) return LAUD_ERR_HIP;
   const unsigned bit = dev >= 0 && dev < 32 ? 1u << dev : 0u;
   if (bit && (done.load(std::memory_order_acquire) & bit)) return LAUD_OK;
-  for (int rc : {ask_tile_lds<bf16_t, 32, false>(), ask_tile_lds<bf16_t, 64, false>(), ask_tile_lds<bf16_t, 96, false>(),
-                 ask_tile_lds<bf16_t, 128, false>(), ask_tile_lds<float, 32, false>(), ask_tile_lds<float, 64, false>(),
-                 ask_tile_lds<float, 96, false>(), ask_tile_lds<float, 128, false>(), ask_tile_lds<bf16_t, 64, true>(),
-                 ask_tile_lds<bf16_t, 128, true>()})
+  for (int rc : {ask_lds_of_width<bf16_t, 32>(), ask_lds_of_width<bf16_t, 64>(), ask_lds_of_width<bf16_t, 96>(), ask_lds_of_width<bf16_t, 128>(),
+                 ask_lds_of_width<float, 32>(), ask_lds_of_width<float, 64>(), ask_lds_of_width<float, 96>(), ask_lds_of_width<float, 128>(),
+                 ask_tile_lds<bf16_t, 64, kRowsCached>(), ask_tile_lds<bf16_t, 128, kRowsCached>()})
     if (rc != LAUD_OK) return rc;
   done.fetch_or(bit, std::memory_order_release);
   return LAUD_OK;
@@ -541,11 +620,11 @@ int attend_init_device() {
 
 void launch_many_rows(const CachedArgs& c, unsigned groups, hipStream_t st) {
   AttendArgs a{};
-  a.heads = c.heads; a.group = c.group; a.D = c.D; a.c = c.c;
+  a.heads = c.heads; a.group = c.group; a.D = c.D; a.c = c.c; a.T = c.T;
   a.q = c.q; a.out = c.out; a.ldq = c.ldq; a.ldo = c.ldo;
   a.ldk = a.ldv = c.D;
-  if (c.D <= 64) launch_tiles<bf16_t, 64, true>(a, c, groups, st);
-  else launch_tiles<bf16_t, 128, true>(a, c, groups, st);
+  if (c.D <= 64) launch_tiles<bf16_t, 64, kRowsCached>(a, c, groups, st);
+  else launch_tiles<bf16_t, 128, kRowsCached>(a, c, groups, st);
 }
 
 }  // namespace laud

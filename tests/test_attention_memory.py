@@ -83,14 +83,25 @@ CASES = {
     "attend_odd_offsets": (attention, [], 150, 2, 1, 64, H, 1, 0, True, [140, 20, -7, 400, 90, 130]),
     # many rows: every width of a tile in LDS, causal and not, masked, rows further apart, in place
     "tiles_bf16_8": (attention, [70, 0, 3], 75, 128, 1, 8, H, 1, 8, False),
-    "tiles_bf16_40": (attention, [129, 1], 133, 64, 2, 40, H, 0, 0, True, None, True),
-    "tiles_bf16_72": (attention, [130], 131, 64, 1, 72, H, 1, 24, True),
+    "tiles_bf16_8_kept": (attention, [70, 0, 3], 75, 128, 1, 8, H, 0, 8, True),
+    "tiles_bf16_40": (attention, [129, 1], 133, 64, 2, 40, H, 0, 0, False, None, True),
+    "tiles_bf16_40_kept": (attention, [129, 1], 133, 64, 2, 40, H, 0, 0, True, None, True),
+    "tiles_bf16_72": (attention, [130], 131, 64, 1, 72, H, 1, 24, False),
+    "tiles_bf16_72_kept": (attention, [130], 131, 64, 1, 72, H, 1, 24, True),
     "tiles_bf16_128": (attention, [65, 66], 131, 64, 8, 128, H, 1, 8, False, None, True),
+    "tiles_bf16_128_kept": (attention, [65, 166], 235, 64, 8, 128, H, 1, 8, True, None, True),
     "tiles_f32_32": (attention, [100, 33], 140, 216, 1, 32, F, 1, 8, False),
-    "tiles_f32_64": (attention, [131], 132, 216, 2, 64, F, 0, 0, True),
-    "tiles_f32_96": (attention, [70, 64], 134, 216, 1, 96, F, 1, 0, True),
+    "tiles_f32_32_kept": (attention, [100, 33], 140, 216, 1, 32, F, 1, 8, True),
+    "tiles_f32_64": (attention, [131], 132, 216, 2, 64, F, 0, 0, False),
+    "tiles_f32_64_kept": (attention, [131], 132, 216, 2, 64, F, 0, 0, True),
+    "tiles_f32_96": (attention, [70, 64], 134, 216, 1, 96, F, 1, 0, False),
+    "tiles_f32_96_kept": (attention, [70, 64], 134, 216, 1, 96, F, 1, 0, True),
     "tiles_f32_120": (attention, [33, 98], 131, 216, 4, 120, F, 0, 8, False),
-    "tiles_odd_offsets": (attention, [], 150, 64, 1, 64, H, 1, 0, True, [140, 20, -7, 400, 90, 130]),
+    "tiles_f32_120_kept": (attention, [33, 98], 131, 216, 4, 120, F, 0, 8, True),
+    "tiles_bf16_64_odd_offsets": (attention, [], 150, 64, 1, 64, H, 1, 0, False, [140, 20, -7, 400, 90, 130]),
+    "tiles_bf16_64_odd_offsets_kept": (attention, [], 150, 64, 1, 64, H, 1, 0, True, [140, 20, -7, 400, 90, 130]),
+    # a list of kept rows that goes round in its ring
+    "tiles_bf16_64_long_kept": (attention, [4300], 4301, 2, 1, 64, H, 0, 0, True),
     # caches of every type and page, one new token and many, parts and none
     "cached_bf16": (cached, [1, 1, 1], [300, 1, 17], 3, 8, 2, 128, H, H, 16),
     "cached_bf16_tail": (cached, [1, 3, 0, 2], [63, 64, 100, 2], 9, 4, 4, 64, H, H, 32, 8),
@@ -122,12 +133,14 @@ CASES = {
 }
 
 
-# The kernels that a case is there for: type, channels multiplied, whether keys are a cache's.
-REACHES = {name: f"k_attend<{'unsigned short' if '_bf16_' in name or '_odd_' in name else 'float'}, {w}, {p}>"
-           for name, w, p in (("tiles_bf16_8", 32, "false"), ("tiles_bf16_40", 64, "false"), ("tiles_bf16_72", 96, "false"),
-                              ("tiles_bf16_128", 128, "false"), ("tiles_f32_32", 32, "false"), ("tiles_f32_64", 64, "false"),
-                              ("tiles_f32_96", 96, "false"), ("tiles_f32_120", 128, "false"), ("tiles_odd_offsets", 64, "false"),
-                              ("cached_bf16_tiles", 128, "true"), ("cached_bf16_tiles_64", 64, "true"), ("cached_bf16_tiles_bad", 64, "true"))}
+# The kernels that a case is there for: type, channels multiplied, whether keys are all rows, the kept ones or a cache's.
+def reached(name, case):
+    if name.startswith("tiles_"):
+        return f"k_attend<{'unsigned short' if case[6] == H else 'float'}, {-(-case[5] // 32) * 32}, {int(case[9])}>"
+    return f"k_attend<unsigned short, {64 if case[6] <= 64 else 128}, 2>" if name.startswith("cached_bf16_tiles") and "whole" not in name and "short" not in name else ""
+
+
+REACHES = {name: kernel for name, case in CASES.items() if (kernel := reached(name, case))}
 
 
 def test_every_tile_has_a_case(lib):  # noqa: F811

@@ -247,12 +247,39 @@ def test_many_rows_masks(dtype, causal):
 
 @pytest.mark.parametrize("dtype,heads", [(BF16, 1), (F32, 4)])
 def test_masks_of_more_than_4096_keys(dtype, heads):
-    """The masker's bytes become bits 4096 keys at a time."""
+    """The list of kept rows goes round."""
     g = np.random.default_rng(6)
     keep = g.random(8700) < 0.6
     keep[4000:4200] = 0
     attention_case([8500, 200], heads, 1, 64, dtype, False, 12, keep=keep)
     attention_case([8700], heads, 1, 32, dtype, True, 13, keep=keep)
+    keep = g.random(9000) < 0.02
+    keep[2000:5000] = 1
+    attention_case([6500, 2500], heads, 1, 64, dtype, True, 14, keep=keep)
+    attention_case([9000], heads, 1, 96, dtype, False, 15, keep=1 - keep)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("causal", [False, True])
+def test_kept_rows_far_apart(dtype, causal):
+    """Keys of one step more than 2 GiB from each other, and less."""
+    heads, D, n = WIDE[dtype], 64, 420
+    g = gen(30)
+    wide = torch.empty(n, 1 << 22, dtype=dtype, device="cuda")
+    k, v = wide[:, 8:8 + D], wide[:, -D:]
+    q, kh, vh = rand(g, n, heads * D).to(dtype), rand(g, n, D).to(dtype), rand(g, n, D).to(dtype)
+    k.copy_(kh)
+    v.copy_(vh)
+    out = torch.full((n, heads * D), 7.0, dtype=dtype, device="cuda")
+    p = L.make_heads(heads, 1, D, dtype, causal)
+    for share in (0.1, 0.9):
+        kept = torch.rand(n, generator=g) < share
+        L.laud_attention(p, ints([0, n]), q.cuda(), k, v, kept.to(torch.uint8).cuda(), out)
+        torch.cuda.synchronize()
+        allowed = kept[:, None] & kept[None, :]
+        allowed = allowed.tril() if causal else allowed
+        ref = attend64(q.double().view(n, heads, D), kh.double().view(n, 1, D), vh.double().view(n, 1, D), p.scale, allowed)
+        assert near(out.cpu().view(n, heads, D), *ref, n, dtype)
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
