@@ -259,29 +259,36 @@ __global__ __launch_bounds__(kAttendWaves * kWave, 2) void k_attend(AttendArgs a
       dma16(bytes_of(scalar_pointer(base + at * a.D * kEb), __popc((unsigned)bits) * a.D * kEb), off[kSame ? 0 : i], 0, stage + i * NW * 1024);
     }
   };
-  // Kept rows: by the list, from the step's first row on.  Where that is too far for one descriptor, row by row.
+  // Kept rows, by the list: a lane's row of each load, from the wave's first one on.  Where that is too far for one descriptor, row by row.
+  constexpr int kOfList = KEPT ? kLoads : 1;
+  int row_of[kOfList];  // of the keys that were asked for last
+  auto look_at_list = [&](int step) {
+    const int k0 = step * KK, rows = min(KK, end - k0);
+#pragma unroll
+    for (int i = 0; i < kOfList; ++i)
+      row_of[i] = list[(k0 + min((i * NW + wave) * kRowsLoad + lane / kLanesRow, max(rows - 1, 0))) % kListed];
+  };
   auto request_kept = [&](const ET* base, int64_t ld, const unsigned (&off)[kOffsets], unsigned to, int step) {
     const unsigned stage = __builtin_amdgcn_readfirstlane(to + wave * 1024);
-    const int k0 = step * KK, rows = min(KK, end - k0);  // (none, past the end)
-    const int first = rows > 0 ? __builtin_amdgcn_readfirstlane(list[k0 % kListed]) : 0;
-    const int last = rows > 0 ? __builtin_amdgcn_readfirstlane(list[(k0 + rows - 1) % kListed]) : 0;
+    const int rows = min(KK, end - step * KK);  // (none, past the end)
+    const int first = rows > 0 ? __builtin_amdgcn_readlane(row_of[0], 0) : 0;
+    const int last = rows > 0 ? __builtin_amdgcn_readlane(row_of[kOfList - 1], kWave - 1) : 0;
     if (((long long)(last - first) * ld + a.D) * kEb <= 0x7fffffff) {
       const __amdgpu_buffer_rsrc_t r = bytes_of(scalar_pointer(base + first * ld), 0x7fffffff);
 #pragma unroll
-      for (int i = 0; i < kLoads; ++i) {
-        const int at = (i * NW + wave) * kRowsLoad + lane / kLanesRow;
+      for (int i = 0; i < kOfList; ++i) {
+        const bool there = (i * NW + wave) * kRowsLoad + lane / kLanesRow < rows;
         const unsigned o = off[kSame ? 0 : i];
-        const int row = at < rows ? list[(k0 + at) % kListed] - first : -1;
-        dma16(r, row >= 0 && o != kOutside ? (unsigned)row * ((unsigned)ld * kEb) + o : kOutside, 0, stage + i * NW * 1024);
+        dma16(r, there && o != kOutside ? (unsigned)(row_of[i] - first) * ((unsigned)ld * kEb) + o : kOutside, 0, stage + i * NW * 1024);
       }
     } else {
-#pragma unroll 1
-      for (int i = 0; i < kLoads; ++i)
+#pragma unroll
+      for (int i = 0; i < kOfList; ++i)
 #pragma unroll 1
         for (int j = 0; j < kRowsLoad; ++j) {
-          const int at = (i * NW + wave) * kRowsLoad + j;
-          const int row = at < rows ? __builtin_amdgcn_readfirstlane(list[(k0 + at) % kListed]) : 0;
-          const __amdgpu_buffer_rsrc_t r = bytes_of(scalar_pointer(base + row * ld), at < rows ? a.D * kEb : 0);
+          const bool there = (i * NW + wave) * kRowsLoad + j < rows;
+          const int row = there ? __builtin_amdgcn_readlane(row_of[i], j * kLanesRow) : 0;
+          const __amdgpu_buffer_rsrc_t r = bytes_of(scalar_pointer(base + row * ld), there ? a.D * kEb : 0);
           if (lane / kLanesRow == j) dma16(r, off[kSame ? 0 : i], 0, stage + i * NW * 1024);
         }
     }
@@ -294,6 +301,7 @@ __global__ __launch_bounds__(kAttendWaves * kWave, 2) void k_attend(AttendArgs a
       look_up(step + 1);
       request_pages(cache.k, vk, to, asked);
     } else if constexpr (KEPT) {
+      look_at_list(step);
       request_kept(kp, a.ldk, vk, to, step);
     } else {
       request(kp + (long long)step * KK * a.ldk, a.ldk, vk, to, step < whole, step < whole ? 0 : rows_there(step));

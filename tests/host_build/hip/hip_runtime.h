@@ -136,6 +136,7 @@ static inline int lanes_below(unsigned mask, int first) {  // set bits of 32 lan
 #define __builtin_amdgcn_exp2f(x) exp2f(x)
 #define atomicAdd(p, v) __atomic_fetch_add(p, v, __ATOMIC_RELAXED)
 #define __builtin_amdgcn_readfirstlane(x) (x)
+#define __builtin_amdgcn_readlane(v, l) host::shuffle(host::FROM, v, l)
 #define __builtin_amdgcn_sched_barrier(x)
 #define __builtin_amdgcn_s_setprio(x)
 #define __builtin_amdgcn_mbcnt_lo(m, v) ((v) + host::lanes_below(m, 0))
