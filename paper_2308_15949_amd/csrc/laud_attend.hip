@@ -97,8 +97,16 @@ __global__ __launch_bounds__(kAttendWaves * kWave, 2) void k_attend(AttendArgs a
   long long my_row;  // the lane's query among all rows
   bool in;
   const uint8_t* keep = nullptr;  // of the sequence's rows
-  int rows_of_sequence = 0, listed = 0, scanned = 0;  // kept rows in the list, rows that were looked at for them
+  int first_row = 0, first_query = 0, rows_of_sequence = 0, listed = 0, scanned = 0;  // kept rows in the list, rows that were looked at for them
   int* const list = reinterpret_cast<int*>(lds + L::kList);
+  unsigned long long skipped = 0;  // lanes whose row of the output the masker skipped, two a row
+  auto put_zeros = [&](long long row, int head) {
+    if (!(skipped >> lane & 1)) return;
+    piece8<ET> zero;
+    const float f[8] = {};
+    zero.put(f);
+    for (int d = lane % 2; d < a.D / 8; d += 2) zero.store(reinterpret_cast<ET*>(a.out) + row * a.ldo + head * a.D, d);
+  };
   const ET *kp = nullptr, *vp = nullptr;
   CachedTile part;
   if constexpr (PAGED) {
@@ -121,10 +129,10 @@ __global__ __launch_bounds__(kAttendWaves * kWave, 2) void k_attend(AttendArgs a
     head = (int)(id / (band * a.tiles) * band + in_band % band);
     hk = head / a.group;
     const int tile = a.tiles - 1 - (int)(in_band / band);
-    const int b = last_not_above(a.B, [&](int i) { return first_tile(a.offsets, i, a.T, 1, kRows) <= tile; });
-    const int row0 = __builtin_amdgcn_readfirstlane(row_at(a.offsets, b, a.T));
-    n = rows_of_sequence = __builtin_amdgcn_readfirstlane(row_at(a.offsets, b + 1, a.T)) - row0;  // (may be negative: no rows)
-    const long long q_first = (tile - first_tile(a.offsets, b, a.T, 1, kRows)) * kRows;
+    const Sequence s = sequence_at(a.offsets, nullptr, a.B, a.T, [&](int row, int i) { return first_tile(row, i, 1, kRows) <= tile; });
+    const int row0 = s.row0;
+    n = rows_of_sequence = s.next - row0;  // (may be negative: no rows)
+    const long long q_first = (tile - first_tile(row0, s.b, 1, kRows)) * kRows;
     if (q_first < 0 || q_first >= n) return;
     const int q0 = __builtin_amdgcn_readfirstlane((int)q_first), qr = q0 + wave * 32 + r32;
     kp = reinterpret_cast<const ET*>(a.k) + (long long)row0 * a.ldk + hk * a.D;
@@ -132,16 +140,10 @@ __global__ __launch_bounds__(kAttendWaves * kWave, 2) void k_attend(AttendArgs a
     my_row = row0 + (long long)qr;
     if constexpr (KEPT) {
       // Kept tokens are numbered in order, and the tile has the queries of numbers q0 .. q0 + 127: what the masker skipped is neither
-      // fetched nor multiplied.  The tile's rows among the skipped ones, q0 .. q0 + 127 as rows, get their zeros first.
+      // fetched nor multiplied.  Of the skipped rows, those of numbers q0 .. q0 + 127 among all get their zeros here.
       keep = a.keep + row0;
-      const int skipped = q0 + threadIdx.x / 2;
-      if (skipped < n && keep[skipped] == 0) {
-        piece8<ET> zero;
-        const float f[8] = {};
-        zero.put(f);
-        for (int d = threadIdx.x % 2; d < a.D / 8; d += 2)
-          zero.store(reinterpret_cast<ET*>(a.out) + (row0 + (long long)skipped) * a.ldo + head * a.D, d);
-      }
+      const int here = q0 + threadIdx.x / 2;
+      const bool skip = here < n && keep[min(here, n - 1)] == 0;
       int* const queries = reinterpret_cast<int*>(lds + L::kQueries);
       int kept = 0;
       bool open = true;
@@ -157,7 +159,13 @@ __global__ __launch_bounds__(kAttendWaves * kWave, 2) void k_attend(AttendArgs a
         }
       }
       n = kept;
-      if (q0 >= n) return;
+      skipped = __ballot(skip);
+      if (q0 >= n) {
+        put_zeros(row0 + (long long)here, head);
+        return;
+      }
+      first_row = row0;
+      first_query = q0;
       __syncthreads();
       in = qr < n;
       if (in) my_row = row0 + (long long)queries[qr - q0];
@@ -527,6 +535,7 @@ __global__ __launch_bounds__(kAttendWaves * kWave, 2) void k_attend(AttendArgs a
   vm_wait<0>();  // (no load into LDS is left behind)
   sum = other_half_sum(sum);
 
+  if constexpr (KEPT) put_zeros(first_row + (long long)first_query + threadIdx.x / 2, head);
   // out: the lane's query, channels 32 t + 16 * half .. + 15; of a part of the keys its sums as they are, maximum and sum of weights beside
   const bool parts = PAGED && cache.part_out, none = sum == 0.f;
   const float inv = parts ? 1.f : 1.f / sum;

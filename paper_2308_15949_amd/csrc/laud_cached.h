@@ -36,9 +36,9 @@ __device__ __forceinline__ int parts_of(int len, int splits) {  // how many of t
   const int each = part_keys(len, splits);
   return max((len + each - 1) / each, 1);
 }
-__device__ __forceinline__ int cached_tokens(const CachedArgs& a, int b) {
+__device__ __forceinline__ int cached_tokens(const CachedArgs& a, int len) {  // of a sequence's length, those that its table has room for
   const long long room = (long long)a.table_ld << a.page_bits;
-  return (int)min((long long)max(a.lens[b], 0), room);
+  return (int)min((long long)max(len, 0), room);
 }
 
 __device__ __forceinline__ unsigned token_of(const CachedArgs& a, unsigned row) {
@@ -78,18 +78,19 @@ __device__ __forceinline__ bool cached_tile(CachedTile& t, const CachedArgs& a) 
     t.hk = j % a.kv_heads;
     tile = j / a.kv_heads;
   }
-  int b = 0;
-  t.row0 = 0; t.n = a.T; t.len = a.prefix_len;
+  int len = a.prefix_len;
+  t.row0 = 0; t.n = a.T; t.len = len;
   t.table = a.prefix;
   if (!t.shared) {
-    b = last_not_above(a.B, [&](int i) { return first_tile(a.offsets, i, a.T, a.group, ROWS_TILE) <= tile; });
-    t.row0 = __builtin_amdgcn_readfirstlane(row_at(a.offsets, b, a.T));
-    t.n = __builtin_amdgcn_readfirstlane(row_at(a.offsets, b + 1, a.T)) - t.row0;
-    const long long before = first_tile(a.offsets, b, a.T, a.group, ROWS_TILE);
+    const Sequence s = sequence_at(a.offsets, a.lens, a.B, a.T, [&](int row, int i) { return first_tile(row, i, a.group, ROWS_TILE) <= tile; });
+    t.row0 = s.row0;
+    t.n = s.next - s.row0;
+    len = s.len;
+    const long long before = first_tile(s.row0, s.b, a.group, ROWS_TILE);
     if ((long long)tile < before) return false;
     tile = __builtin_amdgcn_readfirstlane(tile - (int)before);
-    t.len = __builtin_amdgcn_readfirstlane(cached_tokens(a, b));
-    t.table = a.table + (long long)b * a.table_ld;
+    t.len = __builtin_amdgcn_readfirstlane(cached_tokens(a, s.len));
+    t.table = a.table + (long long)s.b * a.table_ld;
   }
   if (t.n <= 0) return false;
   t.rows = (unsigned)t.n * (unsigned)a.group;  // (T * heads is below 2^31)
@@ -98,7 +99,7 @@ __device__ __forceinline__ bool cached_tile(CachedTile& t, const CachedArgs& a) 
   t.there = (int)min((unsigned)ROWS_TILE, t.rows - t.first_row);
   const int each = part_keys(t.len, splits);
   if (t.split > 0 && (long long)t.split * each >= t.len) return false;
-  t.past = (long long)(t.shared ? t.len : a.lens[b]) - t.n;
+  t.past = (long long)len - t.n;
   t.causal = a.causal && !t.shared;
   t.begin = __builtin_amdgcn_readfirstlane(t.split * each);
   t.hk = __builtin_amdgcn_readfirstlane(t.hk);

@@ -187,16 +187,18 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void k_cached(CachedArgs a) {
     hk = j % a.kv_heads;
     tile = j / a.kv_heads;
   }
-  int b = 0, row0 = 0, n = a.T, len = a.prefix_len;
+  int row0 = 0, n = a.T, len = a.prefix_len, whole_len = len;
   const int32_t* table = a.prefix;
   if (!shared) {
-    b = last_not_above(a.B, [&](int i) { return first_tile(a.offsets, i, a.T, a.group, kRows) <= tile; });
-    row0 = row_at(a.offsets, b, a.T);
-    n = row_at(a.offsets, b + 1, a.T) - row0;
-    if ((long long)tile < first_tile(a.offsets, b, a.T, a.group, kRows)) return;
-    tile -= (int)first_tile(a.offsets, b, a.T, a.group, kRows);
-    len = ROWS ? max(n, 0) : cached_tokens(a, b);
-    table = a.table + (long long)b * a.table_ld;
+    const Sequence s = sequence_at(a.offsets, ROWS ? nullptr : a.lens, a.B, a.T, [&](int row, int i) { return first_tile(row, i, a.group, kRows) <= tile; });
+    row0 = s.row0;
+    n = s.next - s.row0;
+    whole_len = s.len;
+    const long long before = first_tile(s.row0, s.b, a.group, kRows);
+    if ((long long)tile < before) return;
+    tile -= (int)before;
+    len = ROWS ? max(n, 0) : cached_tokens(a, s.len);
+    table = a.table + (long long)s.b * a.table_ld;
   }
   if (n <= 0) return;
   const unsigned rows = (unsigned)n * (unsigned)a.group, first_row = (unsigned)tile * kRows;  // (T * heads is below 2^31)
@@ -204,7 +206,7 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void k_cached(CachedArgs a) {
   const int there = (int)min((unsigned)kRows, rows - first_row);  // rows of this tile
   const int each = part_keys(len, splits);
   if (split > 0 && (long long)split * each >= len) return;
-  const long long past = (long long)(shared || ROWS ? len : a.lens[b]) - n;  // position of the first token
+  const long long past = (long long)(ROWS ? len : whole_len) - n;  // position of the first token
   const bool causal = a.causal && !shared;
   auto limit_of = [&](unsigned row) -> int {  // keys that a row sees
     return causal ? (int)min(max(past + token_of(a, row) + 1, 0ll), (long long)len) : len;
@@ -510,9 +512,9 @@ __global__ __launch_bounds__(256) void k_join(CachedArgs a) {
     top = s.x;
     sum = s.y;
   }
-  const int b = last_not_above(a.B, [&](int i) { return row_at(a.offsets, i, a.T) <= token; });
-  const int own = parts_of(cached_tokens(a, b), a.splits), shared = a.prefix_splits ? parts_of(a.prefix_len, a.prefix_splits) : 0;
-  if (token < row_at(a.offsets, b, a.T) || token >= row_at(a.offsets, b + 1, a.T)) return;  // (all of the workgroup)
+  const Sequence seq = sequence_at(a.offsets, a.lens, a.B, a.T, [&](int row, int) { return row <= token; });
+  const int own = parts_of(cached_tokens(a, seq.len), a.splits), shared = a.prefix_splits ? parts_of(a.prefix_len, a.prefix_splits) : 0;
+  if (token < seq.row0 || token >= seq.next) return;  // (all of the workgroup)
   if (lane < a.splits ? lane >= own : lane - a.splits >= shared) {  // (a part that there is not: nobody wrote it)
     top = kNoScore;
     sum = 0.f;

@@ -18,21 +18,23 @@ __device__ __forceinline__ int row_at(const int32_t* offsets, int i, int T) { re
 // for all of them whatever the lengths are, so that a launch's size follows from T and B alone and no tile's place from a sum over
 // the sequences before it.
 inline __host__ __device__ long long tiles_of(long long T, int B, int per, int tile) { return T * per / tile + B; }
-__device__ __forceinline__ long long first_tile(const int32_t* offsets, int b, int T, int per, int tile) {
-  return (long long)row_at(offsets, b, T) * per / tile + b;
-}
-// The last b of 0 .. B - 1 with at(b) <= x (0 if there is none); a whole wave asks, 64 places at a time.
+__device__ __forceinline__ long long first_tile(int row, int b, int per, int tile) { return (long long)row * per / tile + b; }
+// The last sequence that begins at or before something (below(its first row, its number); the first one if none does), its rows and, of a
+// batch, its length.  A whole wave asks, 64 sequences at a time, and has all of it after one trip to memory.
+struct Sequence { int b, row0, next, len; };
 template <typename F>
-__device__ __forceinline__ int last_not_above(int B, F&& below) {
+__device__ __forceinline__ Sequence sequence_at(const int32_t* offsets, const int32_t* lens, int B, int T, F&& below) {
   int lo = 0, hi = B;  // the answer lies in [lo, hi)
   while (hi - lo > kWave) {
     const int mid = lo + (hi - lo) / 2;
-    if (below(mid)) lo = mid;
+    if (below(row_at(offsets, mid, T), mid)) lo = mid;
     else hi = mid;
   }
-  const int i = lo + lane_id();
-  const unsigned long long m = __ballot(i < hi && below(i));
-  return __builtin_amdgcn_readfirstlane(lo + max(__popcll(m), 1) - 1);
+  const int i = min(lo + lane_id(), B - 1);
+  const int row = row_at(offsets, i, T), next = row_at(offsets, i + 1, T), len = lens ? lens[i] : 0;
+  const unsigned long long m = __ballot(lo + lane_id() < hi && below(row, i));
+  const int at = __builtin_amdgcn_readfirstlane(max(__popcll(m), 1) - 1);
+  return {lo + at, __builtin_amdgcn_readlane(row, at), __builtin_amdgcn_readlane(next, at), __builtin_amdgcn_readlane(len, at)};
 }
 
 // a pointer that is the same for the wave, in scalar registers (what descriptors are made of)
