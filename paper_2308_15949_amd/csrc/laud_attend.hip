@@ -673,9 +673,13 @@ extern "C" int laud_attention(const laud_heads* p, int B, const int32_t* offsets
   hipStream_t st = (hipStream_t)stream;
   // Few rows leave these tiles without enough workgroups; 16 rows a workgroup with its waves sharing the keys fill the card sooner, but
   // fetch the keys more often.  Both, in us (sequences x heads x tokens, widths of 64 float32 and 128 bf16):
-  //   1 x 8 x 64   10,  5    4 x 16 x 128  16, 10    8 x 16 x 200  40, 27    1 x 16 x 1024  82, 55    1 x 16 x 2048  159, 183    4 x 32 x 512  87, 111
+  //   1 x 8 x 64   10,  5    4 x 16 x 128  16, 10    8 x 16 x 200  40, 27    1 x 16 x 1024  80, 53    1 x 16 x 2048  158, 183    4 x 32 x 512  85, 111
   //   1 x 8 x 64    7,  6    1 x 16 x 256  11,  8    4 x 16 x 128   8,  8    16 x 16 x 64    8, 12    1 x 32 x 512    15,  28
-  if ((int64_t)p->heads * T <= (p->dtype == LAUD_F32 ? 28000 : 8192))
+  // Many short sequences leave most of a tile's rows without a query.  Both, in us (sequences x tokens; 16 heads of 64 and 32 of 128 over 8):
+  //   float32  128 x 16  39, 19 and 126, 49    128 x 33  63, 36 and 193, 114    128 x 64  60, 57 and 211, 263
+  //   bf16     256 x 8   40, 22 and  95, 42    128 x 17  22, 19 and  50,  48    128 x 33  24, 29 and  53,  84 (16 heads over 16: 128 x 17 27, 37)
+  const bool few = (int64_t)p->heads * T <= (p->dtype == LAUD_F32 ? 28000 : 8192), brief = T <= (int64_t)B * (p->dtype == LAUD_F32 ? 48 : 8);
+  if (few || brief)
     return attend_few(*p, B, offsets, T, q, ldq, k, ldk, v, ldv, keep, out, ldo, st);
   return p->dtype == LAUD_BF16 ? launch_width<bf16_t>(a, st) : launch_width<float>(a, st);
 }

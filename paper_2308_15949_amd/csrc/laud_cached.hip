@@ -573,9 +573,10 @@ inline int row_tiles(double rows, double of_a_sequence, int type) {
 
 // Parts: as many as make so many workgroups, none of fewer than 128 keys.  1024 where a few rows wait for memory, 512 where many rows keep
 // the matrix cores busy; with a prefix 256 each for it and for the sequences' own keys (32 x 1 + 500 behind 16384: 52 us with 1024, 46 with
-// 512, 41 with 256, 59 with 128: whatever is split is joined again).
+// 512, 41 with 256, 59 with 128: whatever is split is joined again).  But none of more than 2048 keys while there are fewer than 1024
+// workgroups (33 x 316 new tokens of 4286, 8 heads of 32 in 8 bits: 116 -> 76 us; 43 x 121 of 25845 behind 30: 259 -> 177).
 inline int parts_for(double workgroups, double groups, long long keys, int most) {
-  const double want = workgroups / groups;
+  const double want = max(workgroups / groups, min(1024 / groups, keys / 2048.0));
   const long long room = (keys + kPartStep - 1) / kPartStep;
   return (int)max(1ll, min(min((long long)(want + 0.999), room), (long long)most));
 }
