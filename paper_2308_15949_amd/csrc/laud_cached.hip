@@ -493,52 +493,82 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void k_cached(CachedArgs a) {
   }
 }
 
-// Joins the parts of a row: eight parts at a time, 32 threads each.  Every wave works the row's statistics out; what it reads does not
-// depend on them (parts that do not count are dropped behind their loads), so that the trips to memory overlap.
-template <typename ET>
+// Joins the parts of a row, 32 threads each of which has four channels: SLOTS groups of them a row, each takes every SLOTSth part, eight at
+// most.  What a thread reads of the sums does not depend on the row's statistics (parts that do not count are dropped behind their loads), so
+// that the trips to memory overlap.  One row a workgroup where there are few (8 slots), eight where there are many.
+template <typename ET, int SLOTS>
 __global__ __launch_bounds__(256) void k_join(CachedArgs a) {
-  __shared__ f32x4 part[8][32];
-  const int lane = lane_id(), slot = threadIdx.x / 32, d = threadIdx.x % 32 * 4, parts = a.splits + a.prefix_splits;
-  const unsigned row = blockIdx.x;
+  constexpr int kRows = 8 / SLOTS, kHalf = kWave / 2;
+  __shared__ f32x4 part[8][kHalf];
+  const int lane = lane_id(), r32 = lane % kHalf, slot = threadIdx.x / kHalf % SLOTS, d = r32 * 4, parts = a.splits + a.prefix_splits;
   const long long rows = (long long)a.T * a.heads;
+  const unsigned mine = blockIdx.x * kRows + threadIdx.x / (kHalf * SLOTS);
+  const unsigned row = (unsigned)min((long long)mine, rows - 1);  // (below 2^31)
   const int token = (int)(row / (unsigned)a.heads), head = (int)(row - (unsigned)token * a.heads);
-  f32x4 v[kMaxParts / 8];
+  f32x4 v[8];
 #pragma unroll
-  for (int i = 0; i < kMaxParts / 8; ++i)
-    if (i * 8 + slot < parts && d < a.D) v[i] = *reinterpret_cast<const f32x4*>(a.part_out + ((long long)(i * 8 + slot) * rows + row) * a.D + d);
-  float top = kNoScore, sum = 0.f;
-  if (lane < parts) {
-    const float2 s = *reinterpret_cast<const float2*>(a.part_stat + 2 * ((long long)lane * rows + row));
-    top = s.x;
-    sum = s.y;
+  for (int i = 0; i < 8; ++i)
+    if (i * SLOTS + slot < parts && d < a.D) v[i] = *reinterpret_cast<const f32x4*>(a.part_out + ((long long)(i * SLOTS + slot) * rows + row) * a.D + d);
+  // statistics: a lane has parts r32 and r32 + 32 (more than 32 where a row has all of a workgroup only)
+  float top[2], sum[2];
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    const int p = r32 + j * kHalf;
+    float2 s = {kNoScore, 0.f};
+    if (p < parts) s = *reinterpret_cast<const float2*>(a.part_stat + 2 * ((long long)p * rows + row));
+    top[j] = s.x;
+    sum[j] = s.y;
   }
-  const Sequence seq = sequence_at(a.offsets, a.lens, a.B, a.T, [&](int row, int) { return row <= token; });
+  // the halves of a wave may have rows of two tokens
+  const int first = __builtin_amdgcn_readlane(token, 0), second = __builtin_amdgcn_readlane(token, kHalf);
+  Sequence seq = sequence_at(a.offsets, a.lens, a.B, a.T, [&](int r, int) { return r <= first; });
+  if (SLOTS == 1 && second != first) {
+    const Sequence s = sequence_at(a.offsets, a.lens, a.B, a.T, [&](int r, int) { return r <= second; });
+    if (lane >= kHalf) seq = s;
+  }
   const int own = parts_of(cached_tokens(a, seq.len), a.splits), shared = a.prefix_splits ? parts_of(a.prefix_len, a.prefix_splits) : 0;
-  if (token < seq.row0 || token >= seq.next) return;  // (all of the workgroup)
-  if (lane < a.splits ? lane >= own : lane - a.splits >= shared) {  // (a part that there is not: nobody wrote it)
-    top = kNoScore;
-    sum = 0.f;
-  }
-  float most = top;
+  const bool wanted = mine < rows && token >= seq.row0 && token < seq.next;
+  float most = kNoScore;
 #pragma unroll
-  for (int o = 1; o < kWave; o <<= 1) most = fmaxf(most, __shfl_xor(most, o, kWave));
-  const bool counts = sum != 0.f;  // (has a weight; scores that are all NaN leave a NaN for a sum, and no maximum)
-  const float by = counts ? exp2_fast(top - most) : 0.f;
-  const float total = lanes64_sum(counts ? sum * by : 0.f);
-  const unsigned long long mask = __ballot(counts);
+  for (int j = 0; j < 2; ++j) {
+    const int p = r32 + j * kHalf;
+    if (p < a.splits ? p >= own : p - a.splits >= shared) {  // (a part that there is not: nobody wrote it)
+      top[j] = kNoScore;
+      sum[j] = 0.f;
+    }
+    most = fmaxf(most, top[j]);
+  }
+#pragma unroll
+  for (int o = 1; o < kHalf; o <<= 1) most = fmaxf(most, __shfl_xor(most, o, kWave));
+  float by[2], total = 0.f;
+  unsigned counts[2];
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    const bool c = sum[j] != 0.f;  // (has a weight; scores that are all NaN leave a NaN for a sum, and no maximum)
+    by[j] = c ? exp2_fast(top[j] - most) : 0.f;
+    total += c ? sum[j] * by[j] : 0.f;
+    counts[j] = (unsigned)(__ballot(c) >> (lane / kHalf * kHalf));
+  }
+#pragma unroll
+  for (int o = 1; o < kHalf; o <<= 1) total += __shfl_xor(total, o, kWave);
   f32x4 f = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-  for (int i = 0; i < kMaxParts / 8; ++i) {
-    const float w = __shfl(by, i * 8 + slot, kWave);
-    if ((mask >> (i * 8 + slot)) & 1)
+  for (int i = 0; i < 8; ++i) {
+    const int p = i * SLOTS + slot, j = i * SLOTS / kHalf;
+    const float w = __shfl(by[j], lane / kHalf * kHalf + p % kHalf, kWave);
+    if ((counts[j] >> (p % kHalf)) & 1)
 #pragma unroll
       for (int e = 0; e < 4; ++e) f[e] = fmaf(v[i][e], w, f[e]);
   }
-  part[slot][threadIdx.x % 32] = f;
-  __syncthreads();
-  if (threadIdx.x >= 32 || d >= a.D) return;
+  if constexpr (SLOTS > 1) {
+    if (!wanted) return;  // (all of the workgroup)
+    part[slot][r32] = f;
+    __syncthreads();
+    if (slot != 0) return;
 #pragma unroll
-  for (int i = 1; i < 8; ++i) f += part[i][threadIdx.x];
+    for (int i = 1; i < SLOTS; ++i) f += part[i][r32];
+  }
+  if (!wanted || d >= a.D) return;
   const float inv = 1.f / total;
   f *= inv;
   if (total == 0.f) f = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -575,8 +605,13 @@ inline int row_tiles(double rows, double of_a_sequence, int type) {
 // the matrix cores busy; with a prefix 256 each for it and for the sequences' own keys (32 x 1 + 500 behind 16384: 52 us with 1024, 46 with
 // 512, 41 with 256, 59 with 128: whatever is split is joined again).  But none of more than 2048 keys while there are fewer than 1024
 // workgroups (33 x 316 new tokens of 4286, 8 heads of 32 in 8 bits: 116 -> 76 us; 43 x 121 of 25845 behind 30: 259 -> 177).
-inline int parts_for(double workgroups, double groups, long long keys, int most) {
-  const double want = max(workgroups / groups, min(1024 / groups, keys / 2048.0));
+// A part of the sums costs its way to memory and back, c = rows * D * 8 bytes / 5 TB/s, a key 16 ns of a workgroup's time: p parts 16 ns * keys
+// / p + c * p, least at p = sqrt(16 ns * keys / c); and splitting at all costs another launch, 4 us (9 x 398 new tokens, 8 heads of 80: 43 -> 13 us with one
+// part in place of five; 3 x 115 of 4304 in 8 bits, 32 heads of 128: 31.5 -> 12.5; 33 x 1 of 108, 16 heads of 64: 12.8 -> 5.6).
+inline int parts_for(double workgroups, double groups, long long keys, double sums, bool joined, int most) {
+  const double all = 0.016 * keys, part = sums * 8 / 5e6;  // us
+  if (!joined && all / 2 < 4 + 2 * part) return 1;
+  const double want = min(max(workgroups / groups, min(1024 / groups, keys / 2048.0)), sqrt(all / part));
   const long long room = (keys + kPartStep - 1) / kPartStep;
   return (int)max(1ll, min(min((long long)(want + 0.999), room), (long long)most));
 }
@@ -590,10 +625,11 @@ Plan plan_of(const laud_heads* p, const laud_cache* c, const laud_batch* b, int 
   const int per = s.rt ? 16 * s.rt : kManyRows;
   s.tiles = tiles_of(T, b->B, group, per);
   const double busy = max((double)b->B, rows / per) * p->kv_heads;
-  s.own = parts_for(prefix ? 256 : s.rt ? 1024 : 512, busy, (long long)b->table_ld * c->page, prefix ? kMaxParts / 2 : kMaxParts);
+  const double sums = (double)T * p->heads * p->D;
+  s.own = parts_for(prefix ? 256 : s.rt ? 1024 : 512, busy, (long long)b->table_ld * c->page, sums, prefix, prefix ? kMaxParts / 2 : kMaxParts);
   if (prefix) {
     s.prefix_tiles = ((long long)T * group - 1) / per + 1;
-    s.shared = parts_for(256, (double)s.prefix_tiles * p->kv_heads, b->prefix_len, kMaxParts / 2);
+    s.shared = parts_for(256, (double)s.prefix_tiles * p->kv_heads, b->prefix_len, sums, true, kMaxParts / 2);
   }
   if (s.own + s.shared > 1) {
     const size_t all = (size_t)(s.own + s.shared) * T * p->heads;
@@ -617,6 +653,12 @@ void launch_rows(const CachedArgs& a, int rt, unsigned groups, hipStream_t st) {
     if (rt == 1) launch_cached<ET, CT, 128, 1, false>(a, groups, st);
     else launch_cached<ET, CT, 128, 2, false>(a, groups, st);
   }
+}
+template <typename ET>
+void launch_join(const CachedArgs& a, hipStream_t st) {
+  const unsigned rows = (unsigned)a.T * (unsigned)a.heads;
+  if (rows >= 4096 && a.splits + a.prefix_splits <= 8) hipLaunchKernelGGL((k_join<ET, 1>), dim3((rows + 7) / 8), dim3(256), 0, st, a);
+  else hipLaunchKernelGGL((k_join<ET, 8>), dim3(rows), dim3(256), 0, st, a);
 }
 void launch_types(const CachedArgs& a, int cache_type, int rt, unsigned groups, hipStream_t st) {
   if (cache_type == LAUD_F32) launch_rows<float, float>(a, rt, groups, st);
@@ -707,16 +749,15 @@ extern "C" int laud_cache_attention(const laud_heads* p, const laud_cache* c, co
   a.offsets = b->offsets; a.lens = b->lens; a.table = b->table; a.prefix = b->prefix;
   a.k = (const uint8_t*)c->k; a.v = (const uint8_t*)c->v; a.ks = c->k_scale; a.vs = c->v_scale;
   a.q = q; a.out = out; a.ldq = ldq; a.ldo = ldo;
-  a.part_out = (float*)ws;
+  a.part_out = s.bytes ? (float*)ws : nullptr;
   a.part_stat = s.bytes ? (float*)((char*)ws + s.stat_at) : nullptr;
   clear_stale_error();
   hipStream_t st = (hipStream_t)stream;
   if (s.rt == 0) launch_many_rows(a, (unsigned)(own + shared), st);
   else launch_types(a, c->dtype, s.rt, (unsigned)(own + shared), st);
   if (s.own + s.shared > 1) {
-    const dim3 grid((unsigned)T * (unsigned)p->heads);
-    if (p->dtype == LAUD_BF16) hipLaunchKernelGGL((k_join<bf16_t>), grid, dim3(256), 0, st, a);
-    else hipLaunchKernelGGL((k_join<float>), grid, dim3(256), 0, st, a);
+    if (p->dtype == LAUD_BF16) launch_join<bf16_t>(a, st);
+    else launch_join<float>(a, st);
   }
   return check_launch();
 }

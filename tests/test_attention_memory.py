@@ -62,11 +62,11 @@ def cached(call, new, lens, T, heads, kv_heads, D, dtype, cache, page, extra=0, 
     q, ldq = rows(call, T, heads * D, dtype, extra)
     out, ldo = rows(call, T, heads * D, dtype, 2 * extra)
     n = call.host.laud_cache_attention_workspace(C.byref(p), C.byref(c), C.byref(b), T)
-    ws = call.buf(n) if n else None
-    if n:
-        C.memset(ws, 0x7b, n)
+    ws = call.buf(max(n, 16))  # (one that the call does not need is left alone)
+    C.memset(ws, 0x7b, max(n, 16))
     if dtype == cache or dtype == B.BF16:
-        ok(call.host.laud_cache_attention(C.byref(p), C.byref(c), C.byref(b), T, q, ldq, out, ldo, ws, n, None))
+        ok(call.host.laud_cache_attention(C.byref(p), C.byref(c), C.byref(b), T, q, ldq, out, ldo, ws, max(n, 16), None))
+    assert n or C.string_at(ws, 16) == b"\x7b" * 16
     ok(call.host.laud_cache_read(C.byref(c), C.byref(b), T, k, ldk, v, ldv, dtype, None))
 
 
@@ -112,6 +112,8 @@ CASES = {
     "cached_bf16_tiles_whole": (cached, [66], [90], 66, 16, 1, 64, H, H, 32, 0, 0, 0),
     "cached_bf16_tiles_bad": (cached, [130], [200], 131, 8, 1, 64, H, H, 16, 0, 0, 1, None, True),
     "cached_bf16_tiles_short": (cached, [70, 70], [12, -4], 140, 16, 1, 64, H, H, 16),
+    "cached_bf16_tiles_prefix": (cached, [70, 66], [90, 70], 137, 16, 2, 64, H, H, 16, 8, 300),
+    "cached_joined_by_eights": (cached, [100, 37], [640, 500], 138, 31, 31, 8, F, F, 128),
     "cached_e4m3": (cached, [1, 1], [513, 40], 2, 16, 2, 128, H, E, 128),
     "cached_e4m3_rows": (cached, [30, 9], [200, 9], 39, 3, 1, 48, H, E, 16, 8),
     "cached_e4m3_many_rows": (cached, [90], [700], 90, 5, 1, 128, H, E, 32),

@@ -460,6 +460,23 @@ def test_many_new_tokens_special_values(what):
     cached_case([140, 130], [400, 500], 16, 1, 128, BF16, BF16, 32, 2, change=put, prefix=70)
 
 
+@pytest.mark.parametrize("D", [64, 72, 128])
+def test_few_tokens_of_many_sequences_behind_a_prefix(D):
+    """Many rows over the prefix, few over each sequence's own keys."""
+    g = np.random.default_rng(D)
+    new = list(g.integers(0, 5, 40))
+    cached_case(new, [int(n + x) for n, x in zip(new, g.integers(0, 90, 40))], 16, 2, D, BF16, BF16, 32, D, prefix=700, behind=2)
+    cached_case([3] * 60, [3] * 60, 4, 1, D, BF16, BF16, 16, D + 1, prefix=2100, in_place=True, causal=False)
+
+
+@pytest.mark.parametrize("dtype,cache", TYPES)
+@pytest.mark.parametrize("heads,kv", [(15, 5), (16, 1)])
+def test_parts_of_many_rows(heads, kv, dtype, cache):
+    """Joined eight rows a workgroup, two of them a wave: of one token, or two."""
+    cached_case([150, 0, 140], [1500, 3, 900], heads, kv, 64, dtype, cache, 16, heads, start=1, behind=3)
+    cached_case([150, 140], [1200, 700], heads, kv, 32, dtype, cache, 16, heads, prefix=1000)
+
+
 @pytest.mark.parametrize("heads,kv", [(1, 1), (16, 16), (16, 1), (32, 8), (15, 5), (40, 1), (24, 2)])
 def test_cached_head_layouts(heads, kv):
     for dtype, cache in TYPES:
