@@ -468,12 +468,15 @@ int laud_moe(const laud_moe_layer* p, int T, const void* x, int64_t ldx, const u
  * [token][heads][D], rows of k and v [token][kv_heads][D]: columns of one wider array (a projection's result) will do.
  * Query head h belongs to key head h / (heads / kv_heads).
  *   - Sequences lie one behind the other: offsets [B + 1] int32 (device) names the rows offsets[b] .. offsets[b + 1] - 1 of sequence b,
- *     ascending, within 0 .. T; a sequence may have no row.  Rows outside all sequences are not read, and left as they were.
+ *     ascending, within 0 .. T; a sequence may have no row.  Rows outside all sequences count for nothing, and are left as they were.
  *   - Weights are softmax(scale * q k) over the tokens that a query sees, and nothing else of the call has any part in its result
  *     (a NaN or an infinity in a token that it does not see stays there).  A score of -infinity has no weight; a query that sees
  *     nothing, or has no weight, gets zeros.
  *   - Scores, statistics and sums are float32.  With bf16 rows a weight is rounded to bf16 where it meets its value (2^-8 of itself,
- *     the instructions' operand); with float32 rows it is not.
+ *     the instructions' operand); with float32 rows it is not.  Codes of a cache in 8 bits are widened, a key's scale multiplies its
+ *     scores and a value's scale its weights, before they are rounded.
+ *   - The same call gives the same bits.  Which kernel and how many parts it takes follows from its sizes, so that a token's result
+ *     may differ in its last bits between calls of other sizes.
  */
 typedef struct {
   int32_t heads, kv_heads; /* heads: a multiple of kv_heads */
