@@ -665,7 +665,7 @@ extern "C" int laud_attention(const laud_heads* p, int B, const int32_t* offsets
   if (!offsets || !q || !k || !v || !out || !good_ld(ldq, C, 8) || !good_ld(ldk, Ck, 8) || !good_ld(ldv, Ck, 8) || !good_ld(ldo, C, 8) ||
       !aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out) || (reinterpret_cast<uintptr_t>(offsets) & 3u))
     return LAUD_ERR_INVALID_ARG;
-  if (ldq > kMaxRowDistance || ldk > kMaxRowDistance || ldv > kMaxRowDistance || ldo > kMaxRowDistance) return LAUD_ERR_UNSUPPORTED;
+  if (T > 1 << 30 || ldq > kMaxRowDistance || ldk > kMaxRowDistance || ldv > kMaxRowDistance || ldo > kMaxRowDistance) return LAUD_ERR_UNSUPPORTED;
   // a tile's queries are read by the workgroup that writes their results, keys and values by others
   const size_t eb = elem_bytes(p->dtype);
   if (!same_or_apart(q, ldq, eb, out, ldo, eb, T, C) || rows_overlap(out, ldo, eb, C, k, ldk, eb, Ck, T) ||

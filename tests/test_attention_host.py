@@ -52,6 +52,7 @@ def test_attention_refusals(lib):
         assert attention(lib, **{k: None}) == BAD, k
         assert attention(lib, **{k: AT[k] + 2}) == BAD, k
     assert attention(lib, ldq=248) == BAD and attention(lib, ldk=64) == BAD and attention(lib, ldv=132) == BAD and attention(lib, ldo=-256) == BAD
+    assert attention(lib, T=(1 << 30) + 1, heads=1, kv_heads=1, D=8) == UNSUP
     far = (1 << 22) + 8
     assert attention(lib, ldq=far) == UNSUP and attention(lib, ldk=far) == UNSUP and attention(lib, ldv=far) == UNSUP and attention(lib, ldo=far) == UNSUP
     # results over what the call reads

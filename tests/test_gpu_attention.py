@@ -261,9 +261,10 @@ def test_masks_of_more_than_4096_keys(dtype, heads):
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("causal", [False, True])
-def test_kept_rows_far_apart(dtype, causal):
-    """Keys of one step more than 2 GiB from each other, and less."""
-    heads, D, n = WIDE[dtype], 64, 420
+@pytest.mark.parametrize("few", [False, True])
+def test_rows_far_apart(dtype, causal, few):
+    """Rows beyond 2 GiB of the first; kept ones of one step more than that from each other, and less."""
+    heads, D, n = 4 if few else WIDE[dtype], 64, 420
     g = gen(30)
     wide = torch.empty(n, 1 << 22, dtype=dtype, device="cuda")
     k, v = wide[:, 8:8 + D], wide[:, -D:]
@@ -272,9 +273,9 @@ def test_kept_rows_far_apart(dtype, causal):
     v.copy_(vh)
     out = torch.full((n, heads * D), 7.0, dtype=dtype, device="cuda")
     p = L.make_heads(heads, 1, D, dtype, causal)
-    for share in (0.1, 0.9):
+    for share in (0.1, 0.9, 1.0):
         kept = torch.rand(n, generator=g) < share
-        L.laud_attention(p, ints([0, n]), q.cuda(), k, v, kept.to(torch.uint8).cuda(), out)
+        L.laud_attention(p, ints([0, n]), q.cuda(), k, v, kept.to(torch.uint8).cuda() if share < 1.0 else None, out)
         torch.cuda.synchronize()
         allowed = kept[:, None] & kept[None, :]
         allowed = allowed.tril() if causal else allowed
@@ -310,6 +311,9 @@ def test_many_rows_in_place_strays_and_scales(dtype):
     heads = WIDE[dtype]
     attention_case([130, 60], heads, 2, 64, dtype, True, 21, in_place=True, extra=8)
     attention_case([129], heads, 2, 40, dtype, True, 22, start=130, behind=130)
+    keep = np.random.default_rng(5).random(200) < 0.5
+    attention_case([130, 70], heads, 2, 64, dtype, True, 28, keep=keep, in_place=True, extra=8)
+    attention_case([150, 30], heads, 1, 104, dtype, False, 29, keep=keep, in_place=True, start=13, behind=7)
     attention_case(list(np.random.default_rng(3).integers(0, 9, 150)), heads, 2, 64, dtype, True, 23, start=3, behind=70)
     attention_case([190], heads, 2, 128, dtype, True, 24, scale=3.0)
     attention_case([190], heads, 2, 64, dtype, False, 25, scale=1e-6)
@@ -788,6 +792,44 @@ def test_run_on_another_stream_and_captured():
         step()
         torch.cuda.synchronize()
         assert torch.equal(out, ref[0])
+
+
+@pytest.mark.parametrize("dtype,cache", TYPES)
+@pytest.mark.parametrize("new", [1, 150])
+def test_a_cache_of_more_than_32_bits(new, dtype, cache):
+    """Pages whose first element lies beyond 2^32 elements, and some that do not."""
+    kv, D, page, heads = 8, 128, 256, 32
+    pages = (1 << 32) // (kv * D * page) + 40
+    kc, vc = (torch.empty(pages, kv, page, D, dtype=torch.uint8 if cache == E4M3 else cache, device="cuda") for _ in range(2))
+    scales = [torch.empty(pages, kv, page, device="cuda") for _ in range(2)] if cache == E4M3 else [None, None]
+    if cache == E4M3:
+        kc, vc = kc.view(E4M3), vc.view(E4M3)
+    desc = L.make_cache(kc, vc, *scales)
+    g = gen(new)
+    lens, table = [700, new], [[pages - 1, 3, pages - 17], [pages - 30, -1, -1]]
+    k, v = (rand(g, sum(lens), kv * D).to(dtype) for _ in range(2))
+    every = L.make_batch(ints(offsets_of(lens)), ints(lens), ints(table))
+    L.laud_cache_write(desc, every, k.cuda(), v.cuda())
+    kb, vb = (torch.zeros_like(k, device="cuda") for _ in range(2))
+    L.laud_cache_read(desc, every, kb, vb)
+    b = L.make_batch(ints(offsets_of([new, new])), ints(lens), ints(table))
+    p = L.make_heads(heads, kv, D, dtype, True)
+    q = rand(g, 2 * new, heads * D).to(dtype)
+    out = torch.zeros(2 * new, heads * D, dtype=dtype, device="cuda")
+    n = L.cache_attention_workspace(p, desc, b, 2 * new)
+    L.laud_cache_attention(p, desc, b, q.cuda(), out, torch.empty(max(n, 1), dtype=torch.uint8, device="cuda"))
+    torch.cuda.synchronize()
+    if cache != E4M3:
+        assert torch.equal(kb.cpu(), k) and torch.equal(vb.cpu(), v)
+    for i, (j, m) in enumerate(zip(offsets_of(lens), lens)):
+        rows = []
+        for held, s in zip((kc, vc), scales):
+            x = held.view(torch.uint8)[table[i]].view(cache).float().cpu().double()
+            x = x if s is None else x * s[table[i]].cpu().double()[..., None]
+            rows.append(x.permute(0, 2, 1, 3).reshape(-1, kv, D)[:m])
+        allowed = torch.arange(m)[None, :] <= (m - new + torch.arange(new))[:, None]
+        ref = attend64(q[i * new:(i + 1) * new].double().view(new, heads, D), *rows, p.scale, allowed)
+        assert near(out.cpu()[i * new:(i + 1) * new].view(new, heads, D), *ref, m, dtype)
 
 
 def test_the_same_call_gives_the_same_bits():
