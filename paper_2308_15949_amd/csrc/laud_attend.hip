@@ -26,7 +26,7 @@ struct AttendArgs {
 // Bound by the matrix cores: 16384 causal tokens, 16 heads of 128 in bf16, take 1000 to 1050 us on three machines, 1.05 to 1.1 PFLOP/s of the
 // products that the mask leaves (a library product of 8192^3: 1.20); their cores are busy for 56 % of the clocks, of which the load leaves
 // 1.8 GHz.  64 heads over 4096^2: 597 us, of which the loads take 90, what is read from LDS 39, the exponentials 50, the maxima 9.
-// Short prompts (12 of up to 2000 tokens, 150 to 160 us, 0.6 PFLOP/s) pay some 9 us a workgroup for its start, its queries and its results.
+// Short prompts (12 of up to 2000 tokens, 150 to 160 us, 0.6 PFLOP/s) pay 5 us a workgroup for its start, queries and results, 2 for the next one.
 // Tiles: 256 queries by eight waves 1023 and 180 us, 64 queries 1210 and 196, two groups
 // of waves that share the keys 1203 and 210, all at a time when this tile had 1040 and 161.
 constexpr int kAttendWaves = 4, kAttendRows = kAttendWaves * 32;
