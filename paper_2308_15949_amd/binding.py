@@ -628,7 +628,8 @@ def cache_attention_workspace(p: Heads, c: Cache, b: Batch, t: int) -> int:
 
 
 def laud_cache_attention(p: Heads, c: Cache, b: Batch, q, out, ws=None) -> None:
-    """q, out [T][heads * D]: new tokens over the cached ones of their sequences."""
+    """q, out [T][heads * D]: new tokens over the cached ones of their sequences.  ws: cache_attention_workspace(p, c, b, T) bytes on the
+    device (None where that is 0); calls that run at once need one each."""
     if b.prefix_len > getattr(b, "prefix_pages", b.prefix_len) * c.page:
         _bad("laud_cache_attention")
     _here(c, b, q, "laud_cache_attention")
