@@ -133,7 +133,7 @@ int cache_rows(const laud_cache* c, const laud_batch* b, int T, void* k, int64_t
   a.k = (uint8_t*)c->k; a.v = (uint8_t*)c->v; a.ks = c->k_scale; a.vs = c->v_scale;
   a.rk = (uint8_t*)k; a.rv = (uint8_t*)v; a.ldk = ldk; a.ldv = ldv;
   const long long groups = ((long long)T * c->kv_heads + 15) / 16;
-  const dim3 grid((unsigned)min(groups, 1ll << 20));
+  const dim3 grid((unsigned)std::min(groups, 1ll << 20));
   hipStream_t st = (hipStream_t)stream;
   clear_stale_error();
   const bool c8 = c->dtype == LAUD_E4M3;

@@ -607,19 +607,25 @@ inline int row_tiles(double rows, double of_a_sequence, int type) {
   return type == LAUD_BF16 && of_a_sequence >= 512 ? 0 : rows <= 16 ? 1 : 2;
 }
 
-// Parts: as many as make so many workgroups, none of fewer than 128 keys.  1024 where a few rows wait for memory, 512 where many rows keep
+// Parts: as many as stay within so many workgroups, none of fewer than 128 keys.  1024 where a few rows wait for memory, 512 where many rows keep
 // the matrix cores busy; with a prefix 256 each for it and for the sequences' own keys (32 x 1 + 500 behind 16384: 52 us with 1024, 46 with
-// 512, 41 with 256, 59 with 128: whatever is split is joined again).  But none of more than 2048 keys while there are fewer than 1024
-// workgroups (33 x 316 new tokens of 4286, 8 heads of 32 in 8 bits: 116 -> 76 us; 43 x 121 of 25845 behind 30: 259 -> 177).
+// 512, 41 with 256, 59 with 128: whatever is split is joined again).  But none of more than 2048 keys of a row of the table while that stays within 1024
+// workgroups (33 x 316 new tokens of 4286, 8 heads of 32 in 8 bits: 116 -> 76 us; 43 x 121 of 25845 behind 30: 259 -> 177), or makes 1024 to 1640 of one
+// part (65 x 1 of up to 8192, 32 heads of 128 over 8: 224 -> 182 us, 100 x 1 of 32768 in 8 bits 1423 -> 1295, 127 x 1 1391 -> 1418 and left).
+// Rounded up, a last part of few workgroups waits for nearly as long as the others (1 x 512 new tokens of 8512: 109 us with 4 parts, 145 with 5; 48 x 1 of
+// 32768 1063 -> 1092; 20 x 1 of 500 behind 5000 26 -> 31; but 33 x 1 820 -> 796); sixty drawn caches take as long either way.
 // A part of the sums costs its way to memory and back, c = rows * D * 8 bytes / 5 TB/s, a key 16 ns of a workgroup's time: p parts 16 ns * keys
 // / p + c * p, least at p = sqrt(16 ns * keys / c); and splitting at all costs another launch, 4 us (9 x 398 new tokens, 8 heads of 80: 43 -> 13 us with one
 // part in place of five; 3 x 115 of 4304 in 8 bits, 32 heads of 128: 31.5 -> 12.5; 33 x 1 of 108, 16 heads of 64: 12.8 -> 5.6).
+// All of this takes the sequences for about as long as the table has room for: parts of one long sequence among short ones are as many as theirs.
 inline int parts_for(double workgroups, double groups, long long keys, double sums, bool joined, int most) {
   const double all = 0.016 * keys, part = sums * 8 / 5e6;  // us
   if (!joined && all / 2 < 4 + 2 * part) return 1;
-  const double want = min(max(workgroups / groups, min(1024 / groups, keys / 2048.0)), sqrt(all / part));
+  double filled = 1024 / groups;
+  if (filled >= 1.25 && filled < 2) filled = 2;
+  const double want = std::min(std::max(workgroups / groups, std::min(filled, keys / 2048.0)), std::sqrt(all / part));
   const long long room = (keys + kPartStep - 1) / kPartStep;
-  return (int)max(1ll, min(min((long long)(want + 0.999), room), (long long)most));
+  return (int)std::max(1ll, std::min({(long long)want, room, (long long)most}));
 }
 
 Plan plan_of(const laud_heads* p, const laud_cache* c, const laud_batch* b, int T) {
@@ -630,7 +636,7 @@ Plan plan_of(const laud_heads* p, const laud_cache* c, const laud_batch* b, int 
   s.rt = row_tiles(prefix ? rows : rows / b->B, rows / b->B, c->dtype);
   const int per = s.rt ? 16 * s.rt : kManyRows;
   s.tiles = tiles_of(T, b->B, group, per);
-  const double busy = max((double)b->B, rows / per) * p->kv_heads;
+  const double busy = std::max((double)b->B, rows / per) * p->kv_heads;
   const double sums = (double)T * p->heads * p->D;
   s.own = parts_for(prefix ? 256 : s.rt ? 1024 : 512, busy, (long long)b->table_ld * c->page, sums, prefix, prefix ? kMaxParts / 2 : kMaxParts);
   if (prefix) {

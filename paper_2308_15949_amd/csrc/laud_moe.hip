@@ -553,7 +553,7 @@ template <int W, typename ET>
 void launch_moe(MoeArgs& a, hipStream_t st) {
   const long long entries = (long long)a.T * a.top_k;
   a.by_token = entries <= a.E;
-  const dim3 up(a.Fp / 16, (unsigned)min((long long)a.E, entries));
+  const dim3 up(a.Fp / 16, (unsigned)std::min((long long)a.E, entries));
   if (a.T == 1) {
     hipLaunchKernelGGL((k_moe_logits<ET>), dim3((a.E - 1) / kLogitWaves + 1), dim3(kLogitWaves * kWave), 0, st, a);
     hipLaunchKernelGGL((k_moe_up<W, true>), up, dim3(kSplitOne * kWave), 0, st, a);

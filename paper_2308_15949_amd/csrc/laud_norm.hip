@@ -303,7 +303,7 @@ void launch_quant(const void* x, int64_t ldx, int rows, int cols, int block_rows
   const int kb = scale_blocks(cols);
   if (block_rows == 1) {
     const long long blocks = (long long)rows * kb;
-    hipLaunchKernelGGL((k_quant_rows<ET>), dim3((unsigned)min((blocks + 15) / 16, (long long)kMostGroups)), dim3(256), 0, st, (const ET*)x, ldx,
+    hipLaunchKernelGGL((k_quant_rows<ET>), dim3((unsigned)std::min((blocks + 15) / 16, (long long)kMostGroups)), dim3(256), 0, st, (const ET*)x, ldx,
                        blocks, kb, cols, (uint8_t*)q, ldq, scale);
   } else {
     const int rbs = scale_blocks(rows), per = min(rbs, 32768);

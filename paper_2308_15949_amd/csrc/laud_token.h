@@ -2,6 +2,9 @@
 // elements, 8-bit floating point (e4m3) in blocks of 128.
 #pragma once
 
+#include <algorithm>
+#include <cmath>
+
 #include "laud_tile_util.h"
 
 namespace laud {
@@ -159,7 +162,8 @@ __device__ __forceinline__ void store4(OT* out, const f32x4& v) {
   }
 }
 
-// ---- host side: argument checks the token operators share ------------------------------------------------------------------
+// ---- host side: argument checks the token operators share (in host code the compiler's own min and max are those of int: numbers of other
+// types go through std::min and std::max) ------------------------------------------------------------------
 // whether a launch of so many workgroups has less than 2^32 threads, the most that one takes along a dimension
 inline bool launchable(double groups, int threads) { return groups * threads < 4294967296.0; }
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
