@@ -160,7 +160,9 @@ __device__ __forceinline__ f32x4 of_four(float v) { return f32x4{dpp_movf<0x00>(
 
 // Sixteen query rows a row tile (RT of them a workgroup): the tokens of a sequence times the query heads of a key head, so that a key is
 // fetched once for all of them.  Four waves share a part's keys, each takes every fourth step of 16 or 32 keys; their sums are joined through LDS.
-// The softmax runs along: sums are relative to the largest score so far and scaled when a larger one comes.
+// The softmax runs along: sums are relative to the largest score so far and scaled when a larger one comes.  Weights meet values of 8 or 16 bits in two
+// parts: memory bounds these shapes, and a third product costs little (one token over 32767 32.5 -> 32.8 us, 64 in 8 bits 117.1, 32 behind 16384 42.5 -> 44,
+// 5 x 100 over 6000 in 8 bits 154 -> 171) for results whose error is that of their own rounding.
 //
 // Bound by memory: one token over 32767 (32 heads of 128 over 8, bf16) 22.6 us, 5.9 TB/s, and 4.7 for the join; 64 tokens over up to 8000 in 8 bits
 // 104 us, 4.3 TB/s: half the bytes are in flight with the same registers for what they are widened to.  32 tokens behind 16384 33 us: the prefix is
@@ -399,18 +401,26 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void k_cached(CachedArgs a) {
     } else {
 #pragma unroll
       for (int h = 0; h < kGroups / 2; ++h) {
-        tok_u4 w[RT];
+        tok_u4 w[RT], rest[RT];
 #pragma unroll
         for (int t = 0; t < RT; ++t)
           if (t * 16 < there)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) w[t][j] = pack_bf16(sc[t][2 * h + j / 2][j % 2 * 2], sc[t][2 * h + j / 2][j % 2 * 2 + 1]);
+            for (int j = 0; j < 4; ++j) {
+              unsigned lead, last;
+              two_parts(sc[t][2 * h + j / 2][j % 2 * 2], sc[t][2 * h + j / 2][j % 2 * 2 + 1], lead, last);
+              w[t][j] = lead;
+              rest[t][j] = last;
+            }
 #pragma unroll
         for (int e = 0; e < kEach; ++e) {
           const tok_u4 v = o.value(h, e);
 #pragma unroll
           for (int t = 0; t < RT; ++t)
-            if (t * 16 < there) acc[t][e] = mma_bf16_16(__builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, w[t]), acc[t][e]);
+            if (t * 16 < there) {
+              acc[t][e] = mma_bf16_16(__builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, w[t]), acc[t][e]);
+              acc[t][e] = mma_bf16_16(__builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, rest[t]), acc[t][e]);
+            }
         }
       }
     }

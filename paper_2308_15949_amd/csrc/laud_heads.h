@@ -70,6 +70,16 @@ __device__ __forceinline__ float quarters_sum(float v) {
   return other_half_sum(__uint_as_float(r[0]) + __uint_as_float(r[1]));
 }
 
+// Two weights as bf16 operands in two parts each: the leading eight bits, cut off, and the rest, rounded (2^-15 of the weight).  Nothing is rounded up
+// to an infinity.  The weight is lowered a little before it is cut, so that the rest of one that fits in eight bits is not 0 either: 0 * infinity is NaN,
+// and an infinite value is infinite for every weight that is not 0.
+__device__ __forceinline__ void two_parts(float a, float b, unsigned& lead, unsigned& rest) {
+  constexpr float kLower = 1.f - 0x1p-16f;
+  const unsigned ua = __float_as_uint(a * kLower), ub = __float_as_uint(b * kLower);
+  lead = __builtin_amdgcn_perm(ub, ua, 0x07060302u);
+  rest = pack_bf16(a - __uint_as_float(ua & 0xffff0000u), b - __uint_as_float(ub & 0xffff0000u));
+}
+
 // ---- values that are no numbers ---------------------------------------------------------------------------------------------
 // A matrix instruction multiplies every weight with every value, and 0 * NaN is NaN: where some queries of a tile do not see all of a
 // step's keys, values that are not finite become zeros in front of the product, and are added to the queries that see them one by one,
