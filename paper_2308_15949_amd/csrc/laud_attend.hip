@@ -497,15 +497,23 @@ __global__ __launch_bounds__(kAttendWaves * kWave, 2) void k_attend(AttendArgs a
     }
     if (k0 >= wave_sees) return;  // (no keys that the wave's queries see, from here on)
     const unsigned char *ks = lds + (turn ^ 1) * L::kPart, *vs = lds + L::kValues + turn * L::kPart;
+    float shift = shift_of(top), by = a.c;
+    if (any_large(shift)) {  // (exponents in the place of scores)
+#pragma unroll
+      for (int u = 0; u < kBlocks; ++u)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s[u][e] = rounded_exponent(s[u][e], by, shift);
+      shift = 0.f;
+      by = 1.f;
+    }
     clear(next);
-    const float shift = shift_of(top);
     float part[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < kPieces; ++i) {
       scores_part(next, ks, i);
 #pragma unroll
       for (int e = i * 16 * kBlocks / kPieces; e < (i + 1) * 16 * kBlocks / kPieces; ++e) {
-        s[e / 16][e % 16] = exp2_fast(fmaf(s[e / 16][e % 16], a.c, -shift));
+        s[e / 16][e % 16] = exp2_fast(fmaf(s[e / 16][e % 16], by, -shift));
         part[e % 4] += s[e / 16][e % 16];
       }
     }

@@ -375,16 +375,24 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void k_cached(CachedArgs a) {
         for (int e = 0; e < kEach; ++e) acc[t][e] *= shrink;
         top[t] = most;
       }
+      const bool exponents = any_large(shift);
+      const float c = exponents ? 1.f : a.c, less = exponents ? 0.f : shift;
+      if (exponents) {
+#pragma unroll
+        for (int u = 0; u < kGroups; ++u)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) sc[t][u][i] = rounded_exponent(sc[t][u][i], a.c, shift);
+      }
 #pragma unroll
       for (int u = 0; u < kGroups; ++u) {
-        f32x4 by = {1.f, 1.f, 1.f, 1.f};
-        if constexpr (O::kBytes == 1) by = of_four(vs[u]);  // (all lanes take part)
+        f32x4 scales = {1.f, 1.f, 1.f, 1.f};
+        if constexpr (O::kBytes == 1) scales = of_four(vs[u]);  // (all lanes take part)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const bool none = sc[t][u][i] == kNoScore;  // (what a value's scale holds where there is no key is nobody's business)
-          sc[t][u][i] = exp2_fast(fmaf(sc[t][u][i], a.c, -shift));
+          sc[t][u][i] = exp2_fast(fmaf(sc[t][u][i], c, -less));
           sum[t] += sc[t][u][i];
-          if constexpr (O::kBytes == 1) sc[t][u][i] = none ? 0.f : sc[t][u][i] * by[i];
+          if constexpr (O::kBytes == 1) sc[t][u][i] = none ? 0.f : sc[t][u][i] * scales[i];
         }
       }
     }
