@@ -471,7 +471,9 @@ int laud_moe(const laud_moe_layer* p, int T, const void* x, int64_t ldx, const u
  *     ascending, within 0 .. T; a sequence may have no row.  Rows outside all sequences count for nothing, and are left as they were.
  *   - Weights are softmax(scale * q k) over the tokens that a query sees, and nothing else of the call has any part in its result
  *     (a NaN or an infinity in a token that it does not see stays there).  A score of -infinity has no weight; a query that sees
- *     nothing, or has no weight, gets zeros.
+ *     nothing, or has no weight, gets zeros.  A value that is not finite makes its element of every query that sees it an infinity or NaN,
+ *     whatever its weight, unless the query has none at all.  scale * log2(e) * score beyond float32's range is an infinite score, and sums
+ *     are divided by the weights' at the end: values of more than 2^119 / (tokens that a query sees) may end in an infinity.
  *   - Scores, statistics and sums are float32.  Weights of float32 rows are not rounded.  With bf16 rows (bf16 operands of the instructions) a weight
  *     is rounded where it meets its value, by 2^-15 of itself; by 2^-8 where tiles of 128 query rows keep the matrix cores busy: in
  *     laud_attention with T * heads above 8192 and T above 8 B, over a bf16 cache with T * heads / kv_heads at least 512 B.  Codes of a cache in 8 bits

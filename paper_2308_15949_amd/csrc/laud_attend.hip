@@ -556,7 +556,7 @@ __global__ __launch_bounds__(kAttendWaves * kWave, 2) void k_attend(AttendArgs a
 
   if constexpr (KEPT) put_zeros(first_row + (long long)first_query + threadIdx.x / 2, head);
   // out: the lane's query, channels 32 t + 16 * half .. + 15; of a part of the keys its sums as they are, maximum and sum of weights beside
-  const bool parts = PAGED && cache.splits + cache.prefix_splits > 1, none = sum == 0.f;
+  const bool parts = PAGED && cache.splits + cache.prefix_splits > 1, none = !parts && sum == 0.f;
   const float inv = parts ? 1.f : 1.f / sum;
   long long at = 0;
   if constexpr (PAGED) {

@@ -352,13 +352,17 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void k_cached(CachedArgs a) {
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
       if (t * 16 >= there) break;
+      unsigned unseen = 0;  // keys that the lane's row does not see
       if (!whole) {
 #pragma unroll
         for (int u = 0; u < kGroups; ++u)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const int at = 4 * quarter + i;
-            if (!(at < here.valid[u] && key + 16 * u + at < limit[t] && (here.there[u] >> at & 1))) sc[t][u][i] = kNoScore;
+            if (!(at < here.valid[u] && key + 16 * u + at < limit[t] && (here.there[u] >> at & 1))) {
+              sc[t][u][i] = kNoScore;
+              unseen |= 1u << (4 * u + i);
+            }
           }
       }
       float most = sc[t][0][0];
@@ -386,13 +390,19 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void k_cached(CachedArgs a) {
 #pragma unroll
       for (int u = 0; u < kGroups; ++u) {
         f32x4 scales = {1.f, 1.f, 1.f, 1.f};
-        if constexpr (O::kBytes == 1) scales = of_four(vs[u]);  // (all lanes take part)
+        if constexpr (O::kBytes == 1) {
+          scales = of_four(vs[u]);  // (all lanes take part)
+          if (!whole) {             // what a value's scale holds where there is no key, or an unseen one, is nobody's business
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              if (unseen >> (4 * u + i) & 1) scales[i] = 0.f;
+          }
+        }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const bool none = sc[t][u][i] == kNoScore;  // (what a value's scale holds where there is no key is nobody's business)
           sc[t][u][i] = exp2_fast(fmaf(sc[t][u][i], c, -less));
           sum[t] += sc[t][u][i];
-          if constexpr (O::kBytes == 1) sc[t][u][i] = none ? 0.f : sc[t][u][i] * scales[i];
+          if constexpr (O::kBytes == 1) sc[t][u][i] *= scales[i];
         }
       }
     }
@@ -553,14 +563,12 @@ __global__ __launch_bounds__(256) void k_join(CachedArgs a) {
   const int own = parts_of(cached_tokens(a, seq.len), a.splits), shared = a.prefix_splits ? parts_of(a.prefix_len, a.prefix_splits) : 0;
   const bool wanted = mine < rows && token >= seq.row0 && token < seq.next;
   float most = kNoScore;
+  bool there[2];
 #pragma unroll
   for (int j = 0; j < 2; ++j) {
     const int p = r32 + j * kHalf;
-    if (p < a.splits ? p >= own : p - a.splits >= shared) {  // (a part that there is not: nobody wrote it)
-      top[j] = kNoScore;
-      sum[j] = 0.f;
-    }
-    most = fmaxf(most, top[j]);
+    there[j] = p < a.splits ? p < own : p - a.splits < shared;  // (else nobody wrote the part)
+    if (there[j]) most = fmaxf(most, top[j]);
   }
 #pragma unroll
   for (int o = 1; o < kHalf; o <<= 1) most = fmaxf(most, __shfl_xor(most, o, kWave));
@@ -568,10 +576,10 @@ __global__ __launch_bounds__(256) void k_join(CachedArgs a) {
   unsigned counts[2];
 #pragma unroll
   for (int j = 0; j < 2; ++j) {
-    const bool c = sum[j] != 0.f;  // (has a weight; scores that are all NaN leave a NaN for a sum, and no maximum)
+    const bool c = there[j] && sum[j] != 0.f;  // (has a weight; scores that are all NaN leave a NaN for a sum, and no maximum)
     by[j] = c ? exp2_fast(top[j] - most) : 0.f;
     total += c ? sum[j] * by[j] : 0.f;
-    counts[j] = (unsigned)(__ballot(c) >> (lane / kHalf * kHalf));
+    counts[j] = (unsigned)(__ballot(there[j]) >> (lane / kHalf * kHalf));  // (without a weight: sums of 0, or NaN of values that are no numbers)
   }
 #pragma unroll
   for (int o = 1; o < kHalf; o <<= 1) total += __shfl_xor(total, o, kWave);

@@ -26,8 +26,9 @@ def cases(*left_out):
             if form not in left_out and (f[0] == "cache" or t[0] == t[1])]
 
 
-def attend(form, dtype, cache_type, q, k, v, scale, D=64):
-    """q, k, v [tokens][D]: every query head has the same q.  Result [new][heads][D], the values as they are held [tokens][D]."""
+def attend(form, dtype, cache_type, q, k, v, scale, D=64, value_scales={}):
+    """q, k, v [tokens][D]: every query head has the same q.  Result [new][heads][D], the values as they are held [tokens][D].  value_scales: of
+    tokens whose scale in an 8-bit cache is replaced."""
     kind, heads, new, tokens = FORMS[form]
     rows = q[tokens - new:].to(dtype)[:, None, :].expand(new, heads, D).reshape(new, heads * D)
     qd, kd, vd = spread(rows, 8), k.to(dtype).cuda(), v.to(dtype).cuda()
@@ -40,6 +41,8 @@ def attend(form, dtype, cache_type, q, k, v, scale, D=64):
     else:
         cache = Paged(gen(1), [tokens], 1, D, cache_type, 16)
         L.laud_cache_write(cache.desc, cache.batch([tokens], [tokens]), kd, vd)
+        for t, x in value_scales.items():
+            cache.vs[cache.pages[0][t // 16], 0, t % 16] = x
         b = cache.batch([new], [tokens])
         n = L.cache_attention_workspace(p, cache.desc, b, new)
         assert (n > 0) == form.startswith("joined")
@@ -96,3 +99,68 @@ def test_one_score_far_above_the_others(form, dtype, cache_type):
             x = held[best]
             ref, size = x.mean(0), x.abs().mean(0)
             assert bool(((got[i] - ref).abs() <= HALF[dtype] * ref.abs() + size * (len(best) * 2.0 ** -24 + 2.0 ** -20 + (2.0 ** -15 if cache_type == E4M3 else 0))).all()), (grow, i)
+
+
+def hopeless(form):
+    """Tokens whose score is -infinity: a beginning that fills parts, and some near the end, where queries see different numbers of them."""
+    tokens = FORMS[form][3]
+    return [*range(400 if tokens > 1000 else 40), tokens - 90, tokens - 89, tokens - 40, tokens - 7, tokens - 2]
+
+
+def check_hopeless(form, dtype, cache_type, got, held):
+    """Rows without a weight are zeros, others the mean of the values with one, but for elements of values that are not finite: these are not
+    finite where the query sees them."""
+    _, heads, new, tokens = FORMS[form]
+    weight = torch.ones(tokens, 1, dtype=torch.float64)
+    weight[hopeless(form)] = 0
+    bad = ~held.isfinite()
+    x = torch.where(bad, 0.0, held) * weight
+    first = tokens - new
+    n = weight.cumsum(0)[first:]
+    ref, size = ((y.cumsum(0)[first:] / n.clamp_min(1))[:, None, :].expand(new, heads, 64) for y in (x, x.abs()))
+    spoilt = ((bad.cumsum(0) > 0)[first:] & (n > 0))[:, None, :].expand(new, heads, 64)
+    assert not bool(got[spoilt].isfinite().any())
+    tol = HALF[dtype] * ref.abs() + size * (tokens * 2.0 ** -24 + 2.0 ** -20 + (2.0 ** -15 if cache_type == E4M3 else 0.0))
+    assert bool(((got - ref).abs() <= tol)[~spoilt].all())
+    none = (n == 0)[:, 0]
+    assert bool((got[none] == 0).all()) and bool(none.any()) == (new == tokens)
+
+
+def hopeless_case(form, dtype, cache_type, change, **more):
+    tokens = FORMS[form][3]
+    k, v = torch.zeros(tokens, 64), rand(gen(5), tokens, 64)
+    k[hopeless(form)] = -3.0e38
+    change(v)
+    check_hopeless(form, dtype, cache_type, *attend(form, dtype, cache_type, torch.ones(tokens, 64), k, v, 1.0, **more))
+
+
+@pytest.mark.parametrize("form,dtype,cache_type", cases())
+def test_scores_of_minus_infinity_have_no_weight(form, dtype, cache_type):
+    hopeless_case(form, dtype, cache_type, lambda v: None)
+
+
+@pytest.mark.parametrize("what", [math.nan, math.inf, -math.inf])
+@pytest.mark.parametrize("form,dtype,cache_type", cases())
+def test_values_that_are_not_finite_show_whatever_their_weight(form, dtype, cache_type, what):
+    tokens = FORMS[form][3]
+
+    def put(v):  # (in steps that all queries see, and in such as some do not)
+        v[5, 3] = v[39, 63] = v[tokens - 90, 20] = v[tokens - 40, 21] = what
+        v[tokens - 7, 9], v[tokens - 2, 11] = what, -what
+    hopeless_case(form, dtype, cache_type, put)
+
+    def near_the_end(v):  # (an 8-bit row is NaN as a whole: some queries do not see this one)
+        v[tokens - 2, 30] = what
+    hopeless_case(form, dtype, cache_type, near_the_end)
+
+    def with_a_weight(v):
+        v[tokens - 3, 1], v[tokens - 80, 2] = what, -what
+    hopeless_case(form, dtype, cache_type, with_a_weight)
+
+
+@pytest.mark.parametrize("what", [math.nan, math.inf])
+@pytest.mark.parametrize("where", ["beginning", "end", "weight"])
+@pytest.mark.parametrize("form", [f for f in FORMS if FORMS[f][0] == "cache"])
+def test_scales_that_are_not_finite_show_whatever_their_weight(form, where, what):
+    t = FORMS[form][3] - 2 if where == "end" else FORMS[form][3] - 3 if where == "weight" else 17
+    hopeless_case(form, BF16, E4M3, lambda v: None, value_scales={t: what})
