@@ -450,6 +450,14 @@ def _bad(where: str):
     raise LaudError(ERR_INVALID_ARG, where)
 
 
+def _int32(v, where: str) -> int:
+    """A number that a descriptor holds in 32 bits (ctypes would cut it)."""
+    v = int(v)
+    if not -2 ** 31 <= v < 2 ** 31:
+        _bad(where)
+    return v
+
+
 def _dtype_of(t) -> int:
     """laud_dtype of a tensor, -1 for other types."""
     import torch
@@ -545,7 +553,8 @@ def make_heads(heads: int, kv_heads: int, d: int, dtype, causal: bool, scale: fl
     import torch
     if dtype not in (torch.float32, torch.bfloat16) or d <= 0:
         _bad("make_heads")
-    return Heads(int(heads), int(kv_heads), int(d), BF16 if dtype == torch.bfloat16 else F32, 1 if causal else 0,
+    heads, kv_heads, d = (_int32(n, "make_heads") for n in (heads, kv_heads, d))
+    return Heads(heads, kv_heads, d, BF16 if dtype == torch.bfloat16 else F32, 1 if causal else 0,
                  float(d) ** -0.5 if scale is None else float(scale))
 
 
@@ -582,12 +591,13 @@ def make_batch(offsets, lens, table, prefix=None, prefix_len: int = 0) -> Batch:
     """Descriptor of a batch over int32 device tensors: offsets [B + 1], lens [B], table [B][pages of the longest], and prefix [pages],
     those of the prefix_len tokens that come before every sequence's own.  It holds the tensors; their contents may change between calls."""
     where = "make_batch"
+    prefix_len = _int32(prefix_len, where)
     v = [_indices(t, n, where) for t, n in ((offsets, 1), (lens, 1), (table, 2), (prefix, 1))]
     _of_one_device(where, offsets, lens, table, prefix)
     n = int(lens.shape[0])
     if offsets.shape[0] != n + 1 or table.shape[0] != n or (n and not table.shape[1]) or prefix_len < 0 or (prefix_len and prefix is None):
         _bad(where)
-    b = Batch(n, int(table.shape[1]), *v, int(prefix_len))
+    b = Batch(_int32(n, where), _int32(table.shape[1], where), *v, prefix_len)
     b.held, b.device, b.prefix_pages = (offsets, lens, table, prefix), lens.get_device(), 0 if prefix is None else int(prefix.shape[0])
     return b
 
@@ -624,7 +634,7 @@ def laud_cache_read(c: Cache, b: Batch, k, v) -> None:
 
 
 def cache_attention_workspace(p: Heads, c: Cache, b: Batch, t: int) -> int:
-    return int(load().laud_cache_attention_workspace(C.byref(p), C.byref(c), C.byref(b), int(t)))
+    return int(load().laud_cache_attention_workspace(C.byref(p), C.byref(c), C.byref(b), _int32(t, "cache_attention_workspace")))
 
 
 def laud_cache_attention(p: Heads, c: Cache, b: Batch, q, out, ws=None) -> None:

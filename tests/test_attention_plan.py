@@ -65,3 +65,18 @@ def test_both_builds_share_out_alike(lib, host_lib):  # noqa: F811
         several += n > 0
         assert n == workspace(host, **case), case
     assert several > 500
+
+
+def test_numbers_of_more_than_32_bits_are_refused(lib):
+    """ctypes would cut them: 2^32 + 8 heads were 8."""
+    import torch
+
+    import paper_2308_15949_amd as L
+    h, c, b = B.Heads(32, 8, 128, B.BF16, 1, 0.1), B.Cache(1 << 20, 16, 8, 128, B.BF16, 1 << 44, 1 << 45), B.Batch(1, 2048, 1 << 40, 1 << 41, 1 << 42)
+    many = (1 << 32) + 8
+    assert L.cache_attention_workspace(h, c, b, 8) > 0
+    for call in (lambda: L.make_heads(many, 8, 64, torch.bfloat16, True), lambda: L.make_heads(8, many, 64, torch.bfloat16, True),
+                 lambda: L.make_heads(8, 8, many, torch.bfloat16, True), lambda: L.cache_attention_workspace(h, c, b, many)):
+        with pytest.raises(L.LaudError) as refusal:
+            call()
+        assert refusal.value.status == B.ERR_INVALID_ARG
