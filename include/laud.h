@@ -491,7 +491,8 @@ typedef struct {
 
 /*
  * out = attention of every token over its sequence.
- *   q, out [T] rows, k, v [T] rows; out may be q.  T at most 2^30, rows at most 2^22 elements apart (LAUD_ERR_UNSUPPORTED beyond).
+ *   q, out [T] rows, k, v [T] rows; out may be q.  T at most 2^30, (B + T / 128) * heads at most 2^24 - 8, rows at most 2^22 elements apart
+ *   (LAUD_ERR_UNSUPPORTED beyond).
  *   keep [T] bytes or NULL: a token with 0 (the masker's) is no key, and its row of out is zeros
  */
 int laud_attention(const laud_heads* p, int B, const int32_t* offsets, int T, const void* q, int64_t ldq, const void* k, int64_t ldk,

@@ -698,7 +698,7 @@ extern "C" int laud_attention(const laud_heads* p, int B, const int32_t* offsets
   //   float32  128 x 16  39, 19 and 126, 49    128 x 33  63, 36 and 193, 114    128 x 64  60, 57 and 211, 263
   //   bf16     256 x 8   40, 22 and  95, 42    128 x 17  22, 19 and  50,  48    128 x 33  24, 29 and  53,  84 (16 heads over 16: 128 x 17 27, 37)
   const bool few = (int64_t)p->heads * T <= (p->dtype == LAUD_F32 ? 28000 : 8192), brief = T <= (int64_t)B * (p->dtype == LAUD_F32 ? 48 : 8);
-  if (few || brief)
+  if ((few || brief) && launchable((double)tiles_of(T, B, a.group, 16) * p->kv_heads, kAttendWaves * kWave))
     return attend_few(*p, B, offsets, T, q, ldq, k, ldk, v, ldv, keep, out, ldo, st);
   return p->dtype == LAUD_BF16 ? launch_width<bf16_t>(a, st) : launch_width<float>(a, st);
 }

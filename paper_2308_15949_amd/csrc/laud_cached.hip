@@ -714,8 +714,7 @@ int attend_few(const laud_heads& p, int B, const int32_t* offsets, int T, const 
   a.splits = 1; a.c = p.scale * kLog2e;
   a.offsets = offsets; a.k = (const uint8_t*)k; a.v = (const uint8_t*)v; a.ldk = ldk; a.ldv = ldv; a.keep = keep;
   a.q = q; a.out = out; a.ldq = ldq; a.ldo = ldo;
-  const long long tiles = tiles_of(T, B, a.group, 16);
-  if (!launchable((double)tiles * a.kv_heads, kWaves * kWave)) return LAUD_ERR_UNSUPPORTED;
+  const long long tiles = tiles_of(T, B, a.group, 16);  // (as many as a launch takes: laud_attention has looked)
   a.tiles = (int)tiles;
   const unsigned groups = (unsigned)(tiles * a.kv_heads);
   if (p.dtype == LAUD_F32) {
