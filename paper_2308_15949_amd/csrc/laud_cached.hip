@@ -164,8 +164,8 @@ __device__ __forceinline__ f32x4 of_four(float v) { return f32x4{dpp_movf<0x00>(
 // parts: memory bounds these shapes, and a third product costs little (one token over 32767 32.5 -> 32.8 us, 64 in 8 bits 117.1, 32 behind 16384 42.5 -> 44,
 // 5 x 100 over 6000 in 8 bits 154 -> 171) for results whose error is that of their own rounding.
 //
-// Bound by memory: one token over 32767 (32 heads of 128 over 8, bf16) 22.6 us, 5.9 TB/s, and 4.7 for the join; 64 tokens over up to 8000 in 8 bits
-// 104 us, 4.3 TB/s: half the bytes are in flight with the same registers for what they are widened to.  32 tokens behind 16384 33 us: the prefix is
+// Bound by memory: one token over 32767 (32 heads of 128 over 8, bf16) 22.8 us, 5.9 TB/s, and 4.8 for the join; 64 tokens over up to 8000 in 8 bits
+// 105 us, 4.2 TB/s: half the bytes are in flight with the same registers for what they are widened to.  32 tokens behind 16384 35.5 us: the prefix is
 // multiplied for 32 rows a fetch (64 rows: 86 to 114 us, sums in memory).  ROWS, the keys are rows of this call: 5 x 197 tokens, 16 heads of 64
 // in float32 19 to 21 us, of which 9 pass before the first step and behind the last one (1040 workgroups), then 2.7 a step of 64 keys.
 template <typename ET, typename CT, int DP, int RT, bool ROWS>
@@ -379,14 +379,6 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void k_cached(CachedArgs a) {
         for (int e = 0; e < kEach; ++e) acc[t][e] *= shrink;
         top[t] = most;
       }
-      const bool exponents = any_large(shift);
-      const float c = exponents ? 1.f : a.c, less = exponents ? 0.f : shift;
-      if (exponents) {
-#pragma unroll
-        for (int u = 0; u < kGroups; ++u)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) sc[t][u][i] = rounded_exponent(sc[t][u][i], a.c, shift);
-      }
 #pragma unroll
       for (int u = 0; u < kGroups; ++u) {
         f32x4 scales = {1.f, 1.f, 1.f, 1.f};
@@ -400,7 +392,7 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void k_cached(CachedArgs a) {
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          sc[t][u][i] = exp2_fast(fmaf(sc[t][u][i], c, -less));
+          sc[t][u][i] = exp2_fast(rounded_exponent(sc[t][u][i], a.c, shift));
           sum[t] += sc[t][u][i];
           if constexpr (O::kBytes == 1) sc[t][u][i] *= scales[i];
         }
@@ -627,8 +619,9 @@ struct Plan {
   size_t stat_at, bytes;    // workspace: sums, then statistics
 };
 // Which kernel: a workgroup of sixteen rows, of 32, or of 128 with its keys through LDS.  The last two, in us (sequences x new tokens + cached
-// ones, 32 heads of 128 over 8, bf16): 1 x 512 + 8000 207, 145;  2 x 200 + 4000 105, 94;  8 x 64 + 4000 120, 122;  16 x 12 + 4000 75, 95.  In
-// float32 32 rows are the faster ones (4 x 300 + 2000, 16 heads of 64: 157, 187), and behind a prefix (32 x 1 + 500 behind 16384: 41, 47).
+// ones, 32 heads of 128 over 8, bf16): 1 x 512 + 8000 179, 109;  2 x 200 + 4000 96, 77;  4 x 128 + 4000 105, 71;  8 x 64 + 4000 105, 107;  16 x 12 + 4000
+// 75, 94.  In float32 32 rows are the faster ones (4 x 300 + 2000, 16 heads of 64: 157, 187), and behind a prefix (32 x 1 + 500 behind 16384: 41, 47).
+// The rows of a sequence are the mean of all: many new tokens of one among single ones of the others go by 32 rows.
 inline int row_tiles(double rows, double of_a_sequence, int type) {
   return type == LAUD_BF16 && of_a_sequence >= 512 ? 0 : rows <= 16 ? 1 : 2;
 }

@@ -53,15 +53,16 @@ constexpr float kNoScore = -__builtin_inff();
 // a score yet subtracts 0, and its weights exp2(-inf) are 0.
 __device__ __forceinline__ float shift_of(float top) { return top == kNoScore ? 0.f : top; }
 
-// What is left of a product c * score behind its rounding stays in the exponent (one fused operation): of a largest score whose product is beyond 2^24 it may
-// be any number, and its weight 0 or infinite instead of 1.  There the product is rounded before the difference.
-constexpr float kLargeTop = 0x1p24f;
-__device__ __forceinline__ bool any_large(float shift) { return __ballot(fabsf(shift) > kLargeTop) != 0; }
+// The exponent, its product rounded before the difference: what a fused operation would leave of the rounding is any number where the largest product is
+// beyond 2^24, and the largest score's weight 0 or infinite instead of 1.
 __device__ __forceinline__ float rounded_exponent(float score, float c, float shift) {
 #pragma clang fp contract(off)
   const float product = score * c;
   return product - shift;
 }
+// Whether that may be so for a lane of the wave: tiles of many rows, which feel the second instruction, ask.
+constexpr float kLargeTop = 0x1p24f;
+__device__ __forceinline__ bool any_large(float shift) { return __ballot(fabsf(shift) > kLargeTop) != 0; }
 
 __device__ __forceinline__ float other_half_max(float v) {  // over lanes l and l + 32
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
