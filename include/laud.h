@@ -476,7 +476,7 @@ int laud_moe(const laud_moe_layer* p, int T, const void* x, int64_t ldx, const u
  *     are divided by the weights' at the end: values of more than 2^119 / (tokens that a query sees) may end in an infinity.
  *   - Scores, statistics and sums are float32.  Weights of float32 rows are not rounded.  With bf16 rows (bf16 operands of the instructions) a weight
  *     is rounded where it meets its value, by 2^-15 of itself; by 2^-8 where tiles of 128 query rows keep the matrix cores busy: in
- *     laud_attention with T * heads above 8192 and T above 8 B, over a bf16 cache with T * heads / kv_heads at least 512 B.  Codes of a cache in 8 bits
+ *     laud_attention with T * heads above 8192 and T above 14 B, over a bf16 cache with T * heads / kv_heads at least 512 B.  Codes of a cache in 8 bits
  *     are widened, a key's scale multiplies its scores and a value's scale its weights, before they are rounded.
  *   - The same call gives the same bits.  Which kernel and how many parts it takes follows from its sizes, so that a token's result
  *     may differ in its last bits between calls of other sizes.

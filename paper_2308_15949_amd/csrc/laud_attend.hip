@@ -23,10 +23,11 @@ struct AttendArgs {
 // of keys within 16 is the first product's (lane half h: 4 h .. 4 h + 3 and those 8 behind), and the values are read to match - transposed
 // on their way from LDS where they are bf16.
 //
-// Bound by the matrix cores: 16384 causal tokens, 16 heads of 128 in bf16, take 1000 to 1050 us on three machines, 1.05 to 1.1 PFLOP/s of the
-// products that the mask leaves (a library product of 8192^3: 1.20); their cores are busy for 56 % of the clocks, of which the load leaves
-// 1.8 GHz.  64 heads over 4096^2: 597 us, of which the loads take 90, what is read from LDS 39, the exponentials 50, the maxima 9.
-// Short prompts (12 of up to 2000 tokens, 150 to 160 us, 0.6 PFLOP/s) pay 5 us a workgroup for its start, queries and results, 2 for the next one.
+// Bound by the matrix cores: 16384 causal tokens, 16 heads of 128 in bf16, take 990 to 1050 us on five machines, 1.05 to 1.1 PFLOP/s of the
+// products that the mask leaves (a library product of 8192^3: 1.20); their cores are busy for 55 % of the clocks, of which the load leaves
+// 1.9 GHz.
+// Short prompts (12 of up to 2000 tokens, 145 to 152 us, 0.65 PFLOP/s) pay 5 us a workgroup for its start, queries and results, 2 for the next one.
+// Float32 rows of more than 96 channels under a mask keep 6 registers a lane in memory; the other instances none.
 // A weight is rounded to bf16 where it meets bf16 values: in two parts, as k_cached has it, it would be off by 2^-15 instead of 2^-8 and the result by its
 // own rounding (16384 tokens: 1.5e-3 of its size from 64 bits instead of 2.0e-3), but the third product of every two takes 1025 -> 1382 us,
 // 12 prompts 147 -> 182, 3 x 577 masked tokens 18.4 -> 20.0.
@@ -691,13 +692,18 @@ extern "C" int laud_attention(const laud_heads* p, int B, const int32_t* offsets
   clear_stale_error();
   hipStream_t st = (hipStream_t)stream;
   // Few rows leave these tiles without enough workgroups; 16 rows a workgroup with its waves sharing the keys fill the card sooner, but
-  // fetch the keys more often.  Both, in us (sequences x heads x tokens, widths of 64 float32 and 128 bf16):
-  //   1 x 8 x 64   10,  5    4 x 16 x 128  16, 10    8 x 16 x 200  40, 27    1 x 16 x 1024  80, 53    1 x 16 x 2048  158, 183    4 x 32 x 512  85, 111
-  //   1 x 8 x 64    7,  6    1 x 16 x 256  11,  8    4 x 16 x 128   8,  8    16 x 16 x 64    8, 12    1 x 32 x 512    15,  28
+  // fetch the keys more often.  Both, in us (causal; sequences x heads x tokens, widths of 64 float32 and 128 bf16):
+  //   1 x 8 x 64  10.8, 5.4    4 x 16 x 128  18, 10    8 x 16 x 200  34, 24      1 x 16 x 1024  80, 38       1 x 32 x 512  45, 23     4 x 32 x 512  65, 73
+  //   1 x 8 x 64   7.5, 7.1    4 x 16 x 128  11, 11    1 x 16 x 256  12.6, 9.6   1 x 16 x 512   17.8, 15.8   16 x 16 x 64  11, 17     1 x 32 x 512  18, 25
+  // where every query sees all of its sequence:
+  //   8 x 16 x 200  39, 28     1 x 16 x 1024  79, 53    1 x 16 x 2048  154, 177    4 x 32 x 512  80, 106
+  //   4 x 16 x 128  9.3, 9.4   1 x 16 x 256  10.7, 8.5   1 x 16 x 512  16.2, 17.6   1 x 8 x 1024  24.6, 26.5
   // Many short sequences leave most of a tile's rows without a query.  Both, in us (sequences x tokens; 16 heads of 64 and 32 of 128 over 8):
-  //   float32  128 x 16  39, 19 and 126, 49    128 x 33  63, 36 and 193, 114    128 x 64  60, 57 and 211, 263
-  //   bf16     256 x 8   40, 22 and  95, 42    128 x 17  22, 19 and  50,  48    128 x 33  24, 29 and  53,  84 (16 heads over 16: 128 x 17 27, 37)
-  const bool few = (int64_t)p->heads * T <= (p->dtype == LAUD_F32 ? 28000 : 8192), brief = T <= (int64_t)B * (p->dtype == LAUD_F32 ? 48 : 8);
+  //   float32  128 x 16  42, 23 and 133, 61    128 x 33  67, 40 and 203, 128    128 x 48  70, 54 and 207, 178    128 x 64  65, 60 and 214, 242
+  //   bf16     256 x 8   43, 27 and 109, 54    256 x 14  46, 30 and 112, 101    256 x 16  44, 43 and 113, 105    128 x 33  26, 34 and  63, 111
+  //   bf16, 12 heads of 80 and 16 of 128: 256 x 14  44, 44 and 64, 64    256 x 16  42, 53 and 61, 100
+  // Both rules take the sequences for about as long as each other: a long one among many short ones goes their way.
+  const bool few = (int64_t)p->heads * T <= (p->dtype == LAUD_F32 ? 28000 : 8192), brief = T <= (int64_t)B * (p->dtype == LAUD_F32 ? 48 : 14);
   if ((few || brief) && launchable((double)tiles_of(T, B, a.group, 16) * p->kv_heads, kAttendWaves * kWave))
     return attend_few(*p, B, offsets, T, q, ldq, k, ldk, v, ldv, keep, out, ldo, st);
   return p->dtype == LAUD_BF16 ? launch_width<bf16_t>(a, st) : launch_width<float>(a, st);

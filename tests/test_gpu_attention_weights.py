@@ -17,7 +17,7 @@ def close(got, ref, size, off, n):
 
 @pytest.mark.parametrize("new,heads,kv,D,causal,share", [
     ([300, 5], 8, 2, 64, True, 1.0), ([700], 4, 4, 128, False, 1.0), ([150, 33], 16, 1, 80, True, 0.6), ([8] * 60, 20, 5, 128, False, 1.0),
-    ([5, 8, 1, 0, 7] * 30, 16, 16, 64, True, 0.8)])
+    ([5, 8, 1, 0, 7] * 30, 16, 16, 64, True, 0.8), ([13, 14, 20, 9] * 20, 32, 8, 96, True, 1.0)])
 def test_few_rows_and_short_sequences(new, heads, kv, D, causal, share):
     g = gen(heads + D)
     T = sum(new)
