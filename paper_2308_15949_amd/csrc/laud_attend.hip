@@ -25,7 +25,7 @@ struct AttendArgs {
 //
 // Bound by the matrix cores: 16384 causal tokens, 16 heads of 128 in bf16, take 990 to 1050 us on five machines, 1.05 to 1.1 PFLOP/s of the
 // products that the mask leaves (a library product of 8192^3: 1.20); their cores are busy for 55 % of the clocks, of which the load leaves
-// 1.9 GHz.
+// 1.8 to 1.9 GHz.
 // Short prompts (12 of up to 2000 tokens, 145 to 152 us, 0.65 PFLOP/s) pay 5 us a workgroup for its start, queries and results, 2 for the next one.
 // Float32 rows of more than 96 channels under a mask keep 6 registers a lane in memory; the other instances none.
 // A weight is rounded to bf16 where it meets bf16 values: in two parts, as k_cached has it, it would be off by 2^-15 instead of 2^-8 and the result by its

@@ -164,8 +164,8 @@ __device__ __forceinline__ f32x4 of_four(float v) { return f32x4{dpp_movf<0x00>(
 // parts: memory bounds these shapes, and a third product costs little (one token over 32767 32.5 -> 32.8 us, 64 in 8 bits 117.1, 32 behind 16384 42.5 -> 44,
 // 5 x 100 over 6000 in 8 bits 154 -> 171) for results whose error is that of their own rounding.
 //
-// Bound by memory: one token over 32767 (32 heads of 128 over 8, bf16) 22.8 us, 5.9 TB/s, and 4.8 for the join; 64 tokens over up to 8000 in 8 bits
-// 105 us, 4.2 TB/s: half the bytes are in flight with the same registers for what they are widened to.  32 tokens behind 16384 35.5 us: the prefix is
+// Bound by memory: one token over 32767 (32 heads of 128 over 8, bf16) 22.4 us, 6 TB/s, and 4.6 for the join; 64 tokens over up to 8000 in 8 bits
+// 106 us, 4.2 TB/s: half the bytes are in flight with the same registers for what they are widened to.  32 tokens behind 16384 36 us: the prefix is
 // multiplied for 32 rows a fetch (64 rows: 86 to 114 us, sums in memory).  ROWS, the keys are rows of this call: 5 x 197 tokens, 16 heads of 64
 // in float32 19 to 21 us, of which 9 pass before the first step and behind the last one (1040 workgroups), then 2.7 a step of 64 keys.
 template <typename ET, typename CT, int DP, int RT, bool ROWS>
