@@ -629,8 +629,9 @@ inline int row_tiles(double rows, double of_a_sequence, int type) {
 // Parts: as many as stay within so many workgroups, none of fewer than 128 keys.  1024 where a few rows wait for memory, 512 where many rows keep
 // the matrix cores busy; with a prefix 256 each for it and for the sequences' own keys (32 x 1 + 500 behind 16384: 52 us with 1024, 46 with
 // 512, 41 with 256, 59 with 128: whatever is split is joined again).  But none of more than 2048 keys of a row of the table while that stays within 1024
-// workgroups (33 x 316 new tokens of 4286, 8 heads of 32 in 8 bits: 116 -> 76 us; 43 x 121 of 25845 behind 30: 259 -> 177), or makes 1024 to 1640 of one
-// part (65 x 1 of up to 8192, 32 heads of 128 over 8: 224 -> 182 us, 100 x 1 of 32768 in 8 bits 1423 -> 1295, 127 x 1 1391 -> 1418 and left).
+// workgroups (33 x 316 new tokens of 4286, 8 heads of 32 in 8 bits: 116 -> 76 us; 43 x 121 of 25845 behind 30: 259 -> 177); and two parts of as many
+// keys where one makes 512 to 819 workgroups (65 x 1 of up to 8192, 32 heads of 128 over 8: 224 -> 182 us, 100 x 1 of 32768 in 8 bits 1423 -> 1295; of more
+// workgroups it does not pay: 127 x 1 1391 -> 1418).
 // Rounded up, a last part of few workgroups waits for nearly as long as the others (1 x 512 new tokens of 8512: 109 us with 4 parts, 145 with 5; 48 x 1 of
 // 32768 1063 -> 1092; 20 x 1 of 500 behind 5000 26 -> 31; but 33 x 1 820 -> 796); sixty drawn caches take as long either way.
 // A part of the sums costs its way to memory and back, c = rows * D * 8 bytes / 5 TB/s, a key 16 ns of a workgroup's time: p parts 16 ns * keys
